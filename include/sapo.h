@@ -25,6 +25,12 @@
  *   sapo_lmhead_lse_partial, sapo_policy_loss_from_partials, sapo_policy_loss_bwd_shard
  *                                   the same loss with W_head sharded by vocabulary over ranks
  *   sapo_adam_step                  the optimiser step of Section 4.2 on the LM head
+ *   sapo_preference_loss            a preference loss over the completions of a question (paired log
+ *                                   ratios), from per-token log-probs to gscale
+ *   sapo_preference_loss_fwd_bwd    the same through the LM head, with both gradients
+ *   sapo_norm_fwd, sapo_norm_bwd    the norm in front of the LM head (layer norm, RMS norm)
+ *   sapo_ckpt8_store, sapo_ckpt8_restore, sapo_norm_replay
+ *                                   activations kept in 8 bits between forward and backward
  *   sapo_policy_loss_fwd_static     the forward for callers that may not allocate device memory
  *   sapo_group_advantages_warp, sapo_workspace_bytes[_min], sapo_status_string, sapo_timing_*,
  *   sapo_launch_count, sapo_debug_wait_timeout, sapo_debug_bounds_violations
@@ -87,11 +93,23 @@ extern "C" {
 #define SAPO_DTYPE_BF16 0
 #define SAPO_DTYPE_F32  1  /* converted on the device to split bf16; see sapo_policy_loss_fwd */
 
+/* kinds of norm */
+#define SAPO_NORM_LAYER 0
+#define SAPO_NORM_RMS   1
+
+/* kinds of preference loss, and which pairs of a question enter it */
+#define SAPO_PREF_SIGMOID 0
+#define SAPO_PREF_SQUARED 1
+#define SAPO_PREF_HINGE   2
+#define SAPO_PREF_ALL        0
+#define SAPO_PREF_BEST_WORST 1
+
 /* `which` of sapo_workspace_bytes */
 #define SAPO_WS_FWD 0
 #define SAPO_WS_BWD 1
 #define SAPO_WS_BWD_ACTIVE 2
 #define SAPO_WS_FUSED 3
+#define SAPO_WS_PREFERENCE 4     /* sapo_preference_loss_fwd_bwd */
 #define SAPO_WS_OUT_BF16 0x100   /* OR into `which`: the gradients will be asked for in bf16 */
 #define SAPO_WS_GATHER   0x200   /* OR into `which`: for sapo_policy_loss_fwd_bwd_gather          */
 
@@ -387,6 +405,124 @@ int sapo_select_external(const float* rewards, const int32_t* group_offsets, int
                          int32_t* n_candidates, void* workspace, size_t workspace_bytes, void* stream);
 size_t sapo_select_workspace_bytes(int32_t n_entries);
 
+/* Parameters of the preference loss.  beta > 0; label_smoothing in [0, 0.5), sigmoid kind only;
+ * grad_scale multiplies the gradient (upstream dL); kind SAPO_PREF_SIGMOID / _SQUARED / _HINGE;
+ * pairs SAPO_PREF_ALL / _BEST_WORST; length_norm 1: R_s is the mean over the tokens of s. */
+typedef struct sapo_pref_cfg {
+  float beta;
+  float label_smoothing;
+  float grad_scale;
+  int32_t kind;
+  int32_t pairs;
+  int32_t length_norm;
+} sapo_pref_cfg;
+
+/* A preference loss over the completions of a question (no counterpart in the paper, whose update is
+ * the clipped policy loss above): the rewards only order the completions of a question.
+ *   R_s  = sum_{t in s} (logp[t] - ref_logp[t])       (length_norm: divided by T_s)
+ *   h_ij = beta (R_i - R_j) for every pair of one question with rewards[i] > rewards[j]
+ *          (SAPO_PREF_ALL), or for its best against its worst completion only, the first of each
+ *          in packed order where rewards tie (SAPO_PREF_BEST_WORST)
+ *   l    = (1-e) softplus(-h) + e softplus(h), e = label_smoothing     (SAPO_PREF_SIGMOID)
+ *          (R_i - R_j - 1/(2 beta))^2                                  (SAPO_PREF_SQUARED)
+ *          max(0, 1 - h)                                               (SAPO_PREF_HINGE)
+ *   q_loss[q] = mean of l over the pairs of question q (0 if it has none), loss = (1/Q) sum_q q_loss[q]
+ *   seq_grad[s] = grad_scale dloss/dR_s,  gscale[t] = grad_scale dloss/dlogp[t]
+ *   q_margin[q] = mean of h over the pairs, q_pairs[q] their number (each may be NULL)
+ * gscale is what sapo_policy_loss_bwd takes, so that call turns it into dhidden and dW_head.
+ * cu_seqlens [S+1] and group_offsets [Q+1] (first sequence of each question) as sapo_pack_rollouts
+ * writes them, rewards [S]; all sums in fp32 or wider and in a fixed order (the same inputs give the
+ * same bits).  A completion without tokens, with a reward that is not finite
+ * (SAPO_ST_NONFINITE_REWARD), or whose sum left the fp32 range joins no pair.  A token whose logp or
+ * ref_logp is not finite (SAPO_ST_NONFINITE_INPUT) is left out of its sum and gets gscale 0.  Tokens
+ * and sequences that belong to no question get zeros.  Offsets outside their range or below their
+ * predecessor are clamped (SAPO_ST_BAD_INDEX).  T may be 0; Q, S >= 1. */
+int sapo_preference_loss(const float* logp, const float* ref_logp, int64_t T, const int32_t* cu_seqlens,
+                         int32_t S, const float* rewards, const int32_t* group_offsets, int32_t Q,
+                         const sapo_pref_cfg* h_cfg, float* gscale, float* seq_logratio, float* seq_grad,
+                         float* q_loss, float* q_margin, int32_t* q_pairs, float* loss,
+                         int32_t* status, void* stream);
+
+/* The preference loss through the LM head: log-probs of the chosen tokens under (hidden, W_head) as
+ * in sapo_policy_loss_fwd, the loss above on them, and its gradients dhidden and dW_head as in
+ * sapo_policy_loss_bwd (arguments, alignment, out_dtype and accumulate_dW as there; bf16 operands only,
+ * SAPO_ERR_UNSUPPORTED_SHAPE for fp32: those go through sapo_policy_loss_fwd, sapo_preference_loss and
+ * sapo_policy_loss_bwd).
+ * logp, lse, gscale [T]; a token with an id outside [0, V) gets logp 0 (SAPO_ST_BAD_TOKEN_ID), is left
+ * out of its sequence's sum and gets no gradient.
+ * workspace: sapo_workspace_bytes(SAPO_WS_PREFERENCE, ...), at least sapo_workspace_bytes_min of it. */
+int sapo_preference_loss_fwd_bwd(const void* hidden, const void* W_head, int32_t dtype,
+                                 int64_t T, int32_t H, int32_t V, int64_t ld_hidden, int64_t ld_W,
+                                 const int32_t* ids, const float* ref_logp, const int32_t* cu_seqlens, int32_t S,
+                                 const float* rewards, const int32_t* group_offsets, int32_t Q,
+                                 const sapo_pref_cfg* h_cfg, float* logp, float* lse, float* gscale,
+                                 float* seq_logratio, float* seq_grad, float* q_loss, float* q_margin,
+                                 int32_t* q_pairs, float* loss,
+                                 void* dhidden, void* dW_head, int32_t out_dtype, int32_t accumulate_dW,
+                                 void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* An activation [T, H] kept in 8 bits: data [T, ld], and one fp32 scale per row and group of 128
+ * columns, scale [T, ld_scale] with ld_scale >= ceil(H / 128).  Element (t, c) stands for
+ * data[t, c] * scale[t, c / 128].  Storing takes a = max |x| of the group, scale = a (1/127) and
+ * data = rint(x (127 (1/a))), each product and quotient rounded to fp32, so a value is off by at
+ * most a / 254 and a little rounding; a group with a below 2^-119 is stored as zeros.  A group that holds a NaN or an infinity is stored
+ * with scale NaN (SAPO_ST_NONFINITE_INPUT): all its values read back as NaN. */
+typedef struct sapo_ckpt8 {
+  int8_t* data;
+  float*  scale;
+  int64_t ld, ld_scale;
+} sapo_ckpt8;
+
+/* x [T, ld_x] to a checkpoint and back.  x_dtype: SAPO_DTYPE_BF16 or SAPO_DTYPE_F32.  For these
+ * calls and the norms below H is in [1, 16384] (SAPO_ERR_UNSUPPORTED_SHAPE beyond) and T may be 0.  Any H and any leading
+ * dimension from H up will do; rows that start on 16-byte boundaries (8 for the 8-bit data) are read
+ * and written in vectors, others element by element. */
+int sapo_ckpt8_store(const void* x, int32_t x_dtype, int64_t T, int32_t H, int64_t ld_x,
+                     const sapo_ckpt8* h_out, int32_t* status, void* stream);
+int sapo_ckpt8_restore(const sapo_ckpt8* h_in, int64_t T, int32_t H, void* x, int32_t x_dtype, int64_t ld_x,
+                       void* stream);
+
+/* kind SAPO_NORM_LAYER or SAPO_NORM_RMS; eps >= 0 is added to the variance (mean square); w_dtype:
+ * element type of gamma and beta. */
+typedef struct sapo_norm_cfg {
+  int32_t kind;
+  float   eps;
+  int32_t w_dtype;
+} sapo_norm_cfg;
+
+/* The norm in front of the LM head (no counterpart in the paper; hidden of the loss calls is its
+ * output), row by row over H columns:
+ *   layer: mean = (1/H) sum x, rstd = ((1/H) sum (x - mean)^2 + eps)^-1/2;  rms: mean = 0
+ *   xh = (x - mean) rstd,  y = xh gamma + beta          (gamma NULL: ones, beta NULL: zeros)
+ * x [T, ld_x] and y [T, ld_y] of x_dtype / y_dtype (bf16 or fp32, any mix); statistics in fp32 from
+ * one read of x.  mean (layer) and rstd [T] are what the backward wants; each may be NULL.  h_ckpt
+ * (may be NULL; `status` is then not used): x is also stored as an 8-bit checkpoint, in the same pass.  y may be x. */
+int sapo_norm_fwd(const void* x, int32_t x_dtype, int64_t T, int32_t H, int64_t ld_x,
+                  const void* gamma, const void* beta, const sapo_norm_cfg* h_cfg,
+                  void* y, int32_t y_dtype, int64_t ld_y, float* mean, float* rstd,
+                  const sapo_ckpt8* h_ckpt, int32_t* status, void* stream);
+
+/* y again, from the checkpoint and the statistics that the forward stored (cfg.eps is not used): for
+ * a backward that wants hidden after its memory has been given up. */
+int sapo_norm_replay(const sapo_ckpt8* h_x, int64_t T, int32_t H, const void* gamma, const void* beta,
+                     const sapo_norm_cfg* h_cfg, const float* mean, const float* rstd,
+                     void* y, int32_t y_dtype, int64_t ld_y, void* stream);
+
+/* Gradient of sapo_norm_fwd: with g = dy gamma,
+ *   dx = rstd (g - [layer] mean_c(g) - xh mean_c(g xh)),  dgamma = sum_t dy xh,  dbeta = sum_t dy.
+ * Exactly one of x (the forward's input) and h_ckpt (its 8-bit checkpoint, read in place) is given; mean (layer) and rstd
+ * come from the forward.  dy, x, dx each bf16 or fp32; dx may be dy.  dgamma and dbeta (fp32 [H],
+ * either may be NULL) are overwritten, or added to with accumulate != 0; their sums over the rows are
+ * formed in fp32 in a fixed order.  workspace: sapo_norm_workspace_bytes(T, H), not needed when both
+ * are NULL. */
+int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
+                  const void* x, int32_t x_dtype, int64_t ld_x, const sapo_ckpt8* h_ckpt,
+                  int64_t T, int32_t H, const void* gamma, const sapo_norm_cfg* h_cfg,
+                  const float* mean, const float* rstd, void* dx, int32_t dx_dtype, int64_t ld_dx,
+                  float* dgamma, float* dbeta, int32_t accumulate,
+                  void* workspace, size_t workspace_bytes, void* stream);
+size_t sapo_norm_workspace_bytes(int64_t T, int32_t H);
+
 /* Section 4.2: the policy is updated with Adam (default hyper-parameters, learning rate 0.001).
  * One Adam step (Kingma & Ba, Algorithm 1) on a [rows, cols] weight such as W_head, from the
  * fp32 gradient sapo_policy_loss_bwd wrote:
@@ -399,8 +535,8 @@ int sapo_adam_step(float* master, float* m, float* v, const float* grad, void* w
                    int64_t rows, int32_t cols, int64_t ld_w, int32_t step,
                    float lr, float beta1, float beta2, float eps, void* stream);
 
-/* Bytes of scratch the forward (SAPO_WS_FWD), backward (SAPO_WS_BWD, SAPO_WS_BWD_ACTIVE) or
- * fused (SAPO_WS_FUSED) call wants for these sizes; OR SAPO_WS_OUT_BF16 into `which` for a call
+/* Bytes of scratch the forward (SAPO_WS_FWD), backward (SAPO_WS_BWD, SAPO_WS_BWD_ACTIVE),
+ * fused (SAPO_WS_FUSED) or preference (SAPO_WS_PREFERENCE) call wants for these sizes; OR SAPO_WS_OUT_BF16 into `which` for a call
  * with bf16 gradient outputs.  Returns 0 for invalid arguments. */
 size_t sapo_workspace_bytes(int32_t which, int64_t T, int32_t H, int32_t V, int32_t dtype);
 
@@ -460,7 +596,14 @@ int sapo_policy_loss_fwd_static(const void* hidden, const void* W_head, int32_t 
 #define SAPO_K_TARGET_LOGIT 14
 #define SAPO_K_FWD_EXP   15
 #define SAPO_K_FUSED_TAIL 16
-#define SAPO_K_COUNT      17
+#define SAPO_K_NORM_FWD   17
+#define SAPO_K_NORM_BWD   18
+#define SAPO_K_NORM_REDUCE 19
+#define SAPO_K_CKPT8      20
+#define SAPO_K_PREFERENCE 21
+#define SAPO_K_PREF_FINAL 22
+#define SAPO_K_PREF_SCORE 23
+#define SAPO_K_COUNT      24
 int sapo_timing_enable(int32_t on);
 int sapo_timing_read(float* h_ms, int32_t* h_launches);
 int64_t sapo_launch_count(void);

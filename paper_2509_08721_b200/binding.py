@@ -20,6 +20,7 @@ WS_FWD = 0
 WS_BWD = 1
 WS_BWD_ACTIVE = 2
 WS_FUSED = 3
+WS_PREFERENCE = 4
 WS_OUT_BF16 = 0x100      # OR into the workspace kind: gradients in bf16
 WS_GATHER = 0x200        # OR into the workspace kind: hidden rows read in place (..._gather)
 
@@ -35,11 +36,18 @@ EXPORTS = ("sapo_pack_rollouts", "sapo_group_advantages", "sapo_policy_loss_fwd"
            "sapo_policy_loss_fwd_static", "sapo_policy_loss_bwd_active", "sapo_policy_loss_fwd_bwd",
            "sapo_select_external", "sapo_group_advantages_warp", "sapo_debug_wait_timeout", "sapo_debug_bounds_violations",
            "sapo_policy_loss_fwd_bwd_gather", "sapo_lmhead_lse_partial", "sapo_policy_loss_from_partials", "sapo_policy_loss_bwd_shard",
-           "sapo_select_workspace_bytes", "sapo_adam_step")
+           "sapo_select_workspace_bytes", "sapo_adam_step", "sapo_preference_loss", "sapo_preference_loss_fwd_bwd",
+           "sapo_norm_fwd", "sapo_norm_replay", "sapo_norm_bwd", "sapo_norm_workspace_bytes", "sapo_ckpt8_store",
+           "sapo_ckpt8_restore")
+NORM_KINDS = {"layer": 0, "rms": 1}
+PREF_KINDS = {"sigmoid": 0, "squared": 1, "hinge": 2}
+PREF_PAIRS = {"all": 0, "best_worst": 1}
+Q8_GROUP = 128               # columns of an 8-bit checkpoint that share one scale
 STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 KERNEL_NAMES = ("pack_scan", "pack_copy", "group_adv", "split_bf16", "fwd_gemm", "loss_tail",
                 "loss_final", "bwd_dz", "bwd_dh", "bwd_dw", "streamk_fixup", "compact", "select", "adam",
-                "target_logit", "fwd_exp", "fused_tail")
+                "target_logit", "fwd_exp", "fused_tail", "norm_fwd", "norm_bwd", "norm_reduce", "ckpt8", "preference",
+                "pref_final", "pref_score")
 
 
 class RolloutBufC(C.Structure):
@@ -65,6 +73,19 @@ class LossCfgC(C.Structure):
     _fields_ = [("eps_low", C.c_float), ("eps_high", C.c_float), ("grad_scale", C.c_float),
                 ("loss_agg", C.c_int32), ("kl_beta", C.c_float), ("ref_logp", C.c_void_p),
                 ("entropy", C.c_void_p)]
+
+
+class PrefCfgC(C.Structure):
+    _fields_ = [("beta", C.c_float), ("label_smoothing", C.c_float), ("grad_scale", C.c_float),
+                ("kind", C.c_int32), ("pairs", C.c_int32), ("length_norm", C.c_int32)]
+
+
+class Ckpt8C(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("ld_scale", C.c_int64)]
+
+
+class NormCfgC(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("w_dtype", C.c_int32)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -138,6 +159,27 @@ def load() -> C.CDLL:
     lib.sapo_debug_wait_timeout.argtypes = [i64, vp, vp]
     lib.sapo_debug_bounds_violations.restype = C.c_int64
     lib.sapo_debug_bounds_violations.argtypes = []
+    lib.sapo_preference_loss.restype = C.c_int
+    lib.sapo_preference_loss.argtypes = [vp, vp, i64, vp, i32, vp, vp, i32, C.POINTER(PrefCfgC), vp, vp, vp, vp, vp,
+                                         vp, vp, vp, vp]
+    lib.sapo_preference_loss_fwd_bwd.restype = C.c_int
+    lib.sapo_preference_loss_fwd_bwd.argtypes = [vp, vp, i32, i64, i32, i32, i64, i64, vp, vp, vp, i32, vp, vp, i32,
+                                                 C.POINTER(PrefCfgC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32,
+                                                 i32, vp, sz, vp, vp]
+    lib.sapo_norm_fwd.restype = C.c_int
+    lib.sapo_norm_fwd.argtypes = [vp, i32, i64, i32, i64, vp, vp, C.POINTER(NormCfgC), vp, i32, i64, vp, vp,
+                                  C.POINTER(Ckpt8C), vp, vp]
+    lib.sapo_norm_replay.restype = C.c_int
+    lib.sapo_norm_replay.argtypes = [C.POINTER(Ckpt8C), i64, i32, vp, vp, C.POINTER(NormCfgC), vp, vp, vp, i32, i64, vp]
+    lib.sapo_norm_bwd.restype = C.c_int
+    lib.sapo_norm_bwd.argtypes = [vp, i32, i64, vp, i32, i64, C.POINTER(Ckpt8C), i64, i32, vp, C.POINTER(NormCfgC), vp,
+                                  vp, vp, i32, i64, vp, vp, i32, vp, sz, vp]
+    lib.sapo_norm_workspace_bytes.restype = sz
+    lib.sapo_norm_workspace_bytes.argtypes = [i64, i32]
+    lib.sapo_ckpt8_store.restype = C.c_int
+    lib.sapo_ckpt8_store.argtypes = [vp, i32, i64, i32, i64, C.POINTER(Ckpt8C), vp, vp]
+    lib.sapo_ckpt8_restore.restype = C.c_int
+    lib.sapo_ckpt8_restore.argtypes = [C.POINTER(Ckpt8C), i64, i32, vp, i32, i64, vp]
     lib.sapo_launch_count.restype = C.c_int64
     lib.sapo_launch_count.argtypes = []
     lib.sapo_status_string.restype = C.c_char_p
@@ -496,3 +538,183 @@ def sapo_adam_step(master: torch.Tensor, m: torch.Tensor, v: torch.Tensor, grad:
     rc = load().sapo_adam_step(_p(master), _p(m), _p(v), _p(grad), _p(w_bf16), rows, cols, ld, int(step),
                                lr, beta1, beta2, eps, _stream())
     _check(rc, "sapo_adam_step")
+
+
+# ------------------------------------------------------------------------------------------
+# preference loss
+def _pref_cfg(beta: float, kind: str, pairs: str, label_smoothing: float, length_norm: bool, grad_scale: float) -> PrefCfgC:
+    if kind not in PREF_KINDS or pairs not in PREF_PAIRS:
+        raise SapoError(f"kind is one of {tuple(PREF_KINDS)}, pairs one of {tuple(PREF_PAIRS)}")
+    return PrefCfgC(beta, label_smoothing, grad_scale, PREF_KINDS[kind], PREF_PAIRS[pairs], 1 if length_norm else 0)
+
+
+def alloc_preference_outputs(T: int, S: int, Q: int, device="cuda", scores: bool = False) -> Dict[str, torch.Tensor]:
+    """Outputs of the preference loss; scores=True adds logp and lse (the call through the LM head)."""
+    f = lambda n: torch.empty(n, dtype=torch.float32, device=device)
+    out = {"loss": f(1), "gscale": f(T), "seq_logratio": f(S), "seq_grad": f(S), "q_loss": f(Q), "q_margin": f(Q),
+           "q_pairs": torch.empty(Q, dtype=torch.int32, device=device)}
+    if scores:
+        out["logp"], out["lse"] = f(T), f(T)
+    return out
+
+
+def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens: torch.Tensor, rewards: torch.Tensor,
+                         group_offsets: torch.Tensor, beta: float, out: Dict[str, torch.Tensor],
+                         status: torch.Tensor, kind: str = "sigmoid", pairs: str = "all",
+                         label_smoothing: float = 0.0, length_norm: bool = False, grad_scale: float = 1.0) -> None:
+    """Loss over the preference pairs of every question and its gradient factor per token; `out` comes
+    from alloc_preference_outputs."""
+    _require_cuda()
+    cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
+    rc = load().sapo_preference_loss(
+        _p(logp), _p(ref_logp), int(logp.shape[0]), _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards),
+        _p(group_offsets), int(group_offsets.numel() - 1), C.byref(cfg), _p(out["gscale"]), _p(out["seq_logratio"]),
+        _p(out["seq_grad"]), _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]),
+        _p(status), _stream())
+    _check(rc, "sapo_preference_loss")
+
+
+def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids: torch.Tensor, ref_logp: torch.Tensor,
+                                 cu_seqlens: torch.Tensor, rewards: torch.Tensor, group_offsets: torch.Tensor,
+                                 beta: float, out: Dict[str, torch.Tensor], dhidden: torch.Tensor,
+                                 dW_head: torch.Tensor, accumulate_dW: bool, workspace: torch.Tensor,
+                                 status: torch.Tensor, T: Optional[int] = None, kind: str = "sigmoid",
+                                 pairs: str = "all", label_smoothing: float = 0.0, length_norm: bool = False,
+                                 grad_scale: float = 1.0) -> None:
+    """The preference loss through the LM head with both gradients; `out` comes from
+    alloc_preference_outputs(..., scores=True)."""
+    _require_cuda()
+    T = int(hidden.shape[0]) if T is None else int(T)
+    H, V = int(hidden.shape[1]), int(W_head.shape[0])
+    cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
+    rc = load().sapo_preference_loss_fwd_bwd(
+        _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0), _p(ids), _p(ref_logp),
+        _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards), _p(group_offsets), int(group_offsets.numel() - 1),
+        C.byref(cfg), _p(out["logp"]), _p(out["lse"]), _p(out["gscale"]), _p(out["seq_logratio"]), _p(out["seq_grad"]),
+        _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]), _p(dhidden), _p(dW_head),
+        _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
+        _p(workspace), workspace.numel() * workspace.element_size(), _p(status), _stream())
+    _check(rc, "sapo_preference_loss_fwd_bwd")
+
+
+# ------------------------------------------------------------------------------------------
+# the norm in front of the LM head, and activations kept in 8 bits
+@dataclass
+class Ckpt8:
+    """An activation [T, H] in 8 bits: int8 rows, one fp32 scale per row and 128 columns."""
+    data: torch.Tensor
+    scale: torch.Tensor
+    H: int
+
+    def c(self) -> Ckpt8C:
+        return Ckpt8C(_p(self.data), _p(self.scale), self.data.stride(0), self.scale.stride(0))
+
+
+def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:
+    ld = -(-H // 16) * 16                     # rows start on 16-byte boundaries
+    return Ckpt8(torch.empty(T, ld, dtype=torch.int8, device=device),
+                 torch.empty(T, -(-H // Q8_GROUP), dtype=torch.float32, device=device), H)
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Row pitch of a 2-D tensor whose columns are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise SapoError(f"{what} must be two-dimensional with contiguous columns")
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+def _norm_cfg(kind: str, eps: float, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor]) -> NormCfgC:
+    if kind not in NORM_KINDS:
+        raise SapoError(f"kind is one of {tuple(NORM_KINDS)}")
+    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+        raise SapoError("gamma and beta must have the same element type")
+    w = gamma if gamma is not None else beta
+    return NormCfgC(NORM_KINDS[kind], eps, DTYPE_F32 if w is None else _dtype_code(w))
+
+
+def _check_vectors(n: int, fp32: bool, **vectors: Optional[torch.Tensor]) -> None:
+    for name, v in vectors.items():
+        if v is not None and (v.numel() != n or not v.is_contiguous() or (fp32 and v.dtype != torch.float32)):
+            raise SapoError(f"{name} must be contiguous{' float32' if fp32 else ''} with {n} elements")
+
+
+def sapo_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, kind: str,
+                  y: torch.Tensor, mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor],
+                  ckpt: Optional[Ckpt8] = None, status: Optional[torch.Tensor] = None) -> None:
+    """y = layer / RMS norm of the rows of x; with ckpt, x is stored in 8 bits in the same pass."""
+    _require_cuda()
+    T, H = x.shape
+    _check_vectors(H, False, gamma=gamma, beta=beta)
+    _check_vectors(T, True, mean=mean, rstd=rstd)
+    if y.shape != x.shape or (ckpt is not None and (ckpt.H != H or ckpt.data.shape[0] != T)):
+        raise SapoError("y and the checkpoint must have the shape of x")
+    cfg = _norm_cfg(kind, eps, gamma, beta)
+    cc = ckpt.c() if ckpt is not None else None
+    rc = load().sapo_norm_fwd(_p(x), _dtype_code(x), T, H, _rows(x, "x"), _p(gamma), _p(beta), C.byref(cfg), _p(y),
+                              _dtype_code(y), _rows(y, "y"), _p(mean), _p(rstd),
+                              C.byref(cc) if cc is not None else None, _p(status), _stream())
+    _check(rc, "sapo_norm_fwd")
+
+
+def sapo_norm_replay(ckpt: Ckpt8, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], kind: str,
+                     mean: Optional[torch.Tensor], rstd: torch.Tensor, y: torch.Tensor) -> None:
+    """The norm's output again, from the 8-bit checkpoint of its input and the stored statistics."""
+    _require_cuda()
+    T, H = y.shape
+    _check_vectors(H, False, gamma=gamma, beta=beta)
+    _check_vectors(T, True, mean=mean, rstd=rstd)
+    if ckpt.H != H or ckpt.data.shape[0] != T:
+        raise SapoError("y must have the shape of the checkpoint")
+    cfg, cc = _norm_cfg(kind, 0.0, gamma, beta), ckpt.c()
+    rc = load().sapo_norm_replay(C.byref(cc), T, H, _p(gamma), _p(beta), C.byref(cfg), _p(mean), _p(rstd), _p(y),
+                                 _dtype_code(y), _rows(y, "y"), _stream())
+    _check(rc, "sapo_norm_replay")
+
+
+def sapo_norm_workspace_bytes(T: int, H: int) -> int:
+    return int(load().sapo_norm_workspace_bytes(T, H))
+
+
+def sapo_norm_bwd(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: Optional[torch.Tensor],
+                  rstd: torch.Tensor, kind: str, dx: torch.Tensor, dgamma: Optional[torch.Tensor],
+                  dbeta: Optional[torch.Tensor], workspace: Optional[torch.Tensor], accumulate: bool = False) -> None:
+    """dx, dgamma, dbeta of sapo_norm_fwd; x is the forward's input or its 8-bit checkpoint (a Ckpt8)."""
+    _require_cuda()
+    T, H = dy.shape
+    _check_vectors(H, False, gamma=gamma)
+    _check_vectors(H, True, dgamma=dgamma, dbeta=dbeta)
+    _check_vectors(T, True, mean=mean, rstd=rstd)
+    held = isinstance(x, Ckpt8)
+    if dx.shape != dy.shape or (x.data.shape[0] != T or x.H != H if held else x.shape != dy.shape):
+        raise SapoError("dy, dx and x must have the same shape")
+    cfg = _norm_cfg(kind, 0.0, gamma, None)
+    cc = x.c() if held else None
+    rc = load().sapo_norm_bwd(_p(dy), _dtype_code(dy), _rows(dy, "dy"), None if held else _p(x),
+                              DTYPE_BF16 if held else _dtype_code(x), 0 if held else _rows(x, "x"),
+                              C.byref(cc) if held else None, T, H, _p(gamma), C.byref(cfg), _p(mean), _p(rstd), _p(dx),
+                              _dtype_code(dx), _rows(dx, "dx"), _p(dgamma), _p(dbeta), 1 if accumulate else 0,
+                              _p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                              _stream())
+    _check(rc, "sapo_norm_bwd")
+
+
+def sapo_ckpt8_store(x: torch.Tensor, ckpt: Ckpt8, status: torch.Tensor) -> None:
+    """x [T, H] into an 8-bit checkpoint from alloc_ckpt8."""
+    _require_cuda()
+    T, H = x.shape
+    if ckpt.H != H or ckpt.data.shape[0] != T:
+        raise SapoError("the checkpoint must have the shape of x")
+    cc = ckpt.c()
+    rc = load().sapo_ckpt8_store(_p(x), _dtype_code(x), T, H, _rows(x, "x"), C.byref(cc), _p(status), _stream())
+    _check(rc, "sapo_ckpt8_store")
+
+
+def sapo_ckpt8_restore(ckpt: Ckpt8, x: torch.Tensor) -> None:
+    """The values an 8-bit checkpoint stands for."""
+    _require_cuda()
+    T, H = x.shape
+    if ckpt.H != H or ckpt.data.shape[0] != T:
+        raise SapoError("x must have the shape of the checkpoint")
+    cc = ckpt.c()
+    rc = load().sapo_ckpt8_restore(C.byref(cc), T, H, _p(x), _dtype_code(x), _rows(x, "x"), _stream())
+    _check(rc, "sapo_ckpt8_restore")

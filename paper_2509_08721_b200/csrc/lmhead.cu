@@ -21,6 +21,7 @@
 #include "gemm_epilogues.cuh"
 #include "gemm_kernels.cuh"
 #include "loss_kernels.cuh"
+#include "preference.cuh"
 
 namespace sapo {
 using namespace umma;
@@ -519,6 +520,17 @@ static int fwd_check_args(const void* hidden, const void* W_head, int32_t dtype,
   return SAPO_OK;
 }
 
+// Scratch of the preference call behind its log ratios: the forward's partials, then (after them in
+// time) the backward's panel of `panel_rows` tokens, in the same place.
+static size_t pref_scratch(int64_t T, int32_t H, int32_t V, int32_t dtype, bool out_bf16, int64_t panel_rows) {
+  int sms = sm_count();
+  if (sms <= 0) sms = 148;
+  const size_t fwd = fwd_layout(T, H, V, dtype, sms, 0, /*entropy=*/false).total;
+  const BwdLayout L = bwd_layout(T, H, V, dtype, out_bf16);
+  const size_t bwd = L.fixed + (size_t)panel_rows * L.bytes_per_row;
+  return fwd > bwd ? fwd : bwd;
+}
+
 }  // namespace sapo
 
 // =============================================================================== C ABI
@@ -538,6 +550,9 @@ extern "C" size_t sapo_workspace_bytes(int32_t which, int64_t T, int32_t H, int3
     const FusedLayout L = fused_layout(T, H, V, /*S=*/(int32_t)(T < 0x7fffffff ? T : 0x7fffffff), out_bf16, gather);
     return L.fixed + FUSED_CHUNK_SLACK + (size_t)preferred_panel_rows(T, H, V) * L.bytes_per_row;
   }
+  if (which == SAPO_WS_PREFERENCE)
+    return dtype != SAPO_DTYPE_BF16 ? 0 : round_up<size_t>((size_t)T * sizeof(float), 256) +
+           pref_scratch(T, H, V, dtype, out_bf16, preferred_panel_rows(T, H, V));
   if (which == SAPO_WS_BWD || which == SAPO_WS_BWD_ACTIVE) {
     const BwdLayout L = bwd_layout(T, H, V, dtype, out_bf16);
     const size_t extra = which == SAPO_WS_BWD_ACTIVE ? active_layout(T, H).total : 0;
@@ -551,10 +566,12 @@ extern "C" size_t sapo_workspace_bytes_min(int32_t which, int64_t T, int32_t H, 
   const bool out_bf16 = (which & SAPO_WS_OUT_BF16) != 0;
   const bool gather = (which & SAPO_WS_GATHER) != 0;
   const int32_t flags = SAPO_WS_OUT_BF16 | SAPO_WS_GATHER;
-  if ((which & ~flags) != SAPO_WS_BWD && (which & ~flags) != SAPO_WS_FUSED)
+  if ((which & ~flags) != SAPO_WS_BWD && (which & ~flags) != SAPO_WS_FUSED && (which & ~flags) != SAPO_WS_PREFERENCE)
     return sapo_workspace_bytes(which, T, H, V, dtype);
   which &= ~flags;
   if (!shapes_ok(T, H, V) || (dtype != SAPO_DTYPE_BF16 && dtype != SAPO_DTYPE_F32)) return 0;
+  if (which == SAPO_WS_PREFERENCE)
+    return dtype != SAPO_DTYPE_BF16 ? 0 : round_up<size_t>((size_t)T * sizeof(float), 256) + pref_scratch(T, H, V, dtype, out_bf16, BM);
   if (which == SAPO_WS_FUSED) {
     if (dtype != SAPO_DTYPE_BF16) return 0;
     const FusedLayout L = fused_layout(T, H, V, (int32_t)(T < 0x7fffffff ? T : 0x7fffffff), out_bf16, gather);
@@ -1251,6 +1268,91 @@ extern "C" int sapo_policy_loss_fwd_bwd_gather(const void* local_hidden, int64_t
   return sapo::fused_impl(nullptr, &src, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, old_logp, adv, cu_seqlens, S,
                           h_cfg, logp, lse, ratio, surr, gscale, seq_surr, loss, dhidden, dW_head, out_dtype,
                           accumulate_dW, workspace, workspace_bytes, status, stream);
+}
+
+// ------------------------------------------------------------------------------------------
+// The preference loss through the LM head.
+namespace sapo {
+// Per token, from the partials of the forward: lse, logp, and the log ratio to the reference that the
+// preference loss sums (NaN where the token is masked).
+__global__ void __launch_bounds__(256)
+pref_score_kernel(const float* __restrict__ pm, const float* __restrict__ ps, const float* __restrict__ pz,
+                  int32_t n_splits, int64_t T, const int32_t* __restrict__ ids, int32_t V,
+                  const float* __restrict__ ref_logp, const int32_t* __restrict__ cu, int32_t S,
+                  float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ log_ratio, int32_t* status) {
+  int32_t lo, hi;
+  scored_range(cu, S, T, lo, hi);
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < T; t += (int64_t)gridDim.x * 256) {
+    if (t < lo || t >= hi) { logp[t] = 0.f; lse[t] = 0.f; log_ratio[t] = 0.f; continue; }
+    float M = -INFINITY;
+    for (int i = 0; i < n_splits; ++i) M = fmaxf(M, pm[(int64_t)i * T + t]);
+    float sum = 0.f, zy = 0.f;
+    for (int i = 0; i < n_splits; ++i) {
+      const int64_t o = (int64_t)i * T + t;
+      sum += ps[o] * exp2f(pm[o] - M);
+      zy += pz[o];
+    }
+    const float l = (M + log2f(sum)) * LN2;
+    const int32_t y = ids[t];
+    const bool bad_id = y < 0 || y >= V;
+    const float ref = ref_logp[t];
+    const bool bad_ref = !isfinite(ref);
+    if (bad_id) raise_status(status, SAPO_ST_BAD_TOKEN_ID);
+    if (bad_ref) raise_status(status, SAPO_ST_NONFINITE_INPUT);
+    lse[t] = l;
+    logp[t] = bad_id ? 0.f : zy - l;
+    log_ratio[t] = bad_id || bad_ref ? __int_as_float(0x7fc00000) : zy - l - ref;
+  }
+}
+}  // namespace sapo
+
+extern "C" int sapo_preference_loss_fwd_bwd(const void* hidden, const void* W_head, int32_t dtype,
+                                            int64_t T, int32_t H, int32_t V, int64_t ld_hidden, int64_t ld_W,
+                                            const int32_t* ids, const float* ref_logp, const int32_t* cu_seqlens,
+                                            int32_t S, const float* rewards, const int32_t* group_offsets, int32_t Q,
+                                            const sapo_pref_cfg* h_cfg, float* logp, float* lse, float* gscale,
+                                            float* seq_logratio, float* seq_grad, float* q_loss, float* q_margin,
+                                            int32_t* q_pairs, float* loss,
+                                            void* dhidden, void* dW_head, int32_t out_dtype, int32_t accumulate_dW,
+                                            void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  using namespace sapo;
+  const sapo_loss_cfg no_clip{0.f, 0.f, 1.f, 0, 0.f, nullptr, nullptr};
+  int rc = fwd_check_args(hidden, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, ref_logp, rewards, cu_seqlens, S,
+                          &no_clip, logp, lse, gscale, gscale, gscale, loss, status);
+  if (rc != SAPO_OK) return rc;
+  if ((rc = pref_check_cfg(h_cfg)) != SAPO_OK) return rc;
+  if (dtype != SAPO_DTYPE_BF16) return SAPO_ERR_UNSUPPORTED_SHAPE;   // fp32 operands: use the separate calls
+  if (!group_offsets || Q < 1 || !seq_logratio || !seq_grad || !q_loss || !dhidden || !dW_head || !workspace ||
+      !aligned16(workspace) || !aligned16(dhidden) || !aligned16(dW_head) ||
+      (out_dtype != SAPO_DTYPE_BF16 && out_dtype != SAPO_DTYPE_F32))
+    return SAPO_ERR_INVALID_ARG;
+  const int sms = sm_count();
+  if (sms <= 0) return SAPO_ERR_CUDA;
+  const FwdLayout L = fwd_layout(T, H, V, dtype, sms, 0, /*entropy=*/false);
+  const size_t ratio_bytes = round_up<size_t>((size_t)T * sizeof(float), 256);
+  if (workspace_bytes < ratio_bytes + L.total) return SAPO_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  float* log_ratio = static_cast<float*>(workspace);
+  uint8_t* ws = static_cast<uint8_t*>(workspace) + ratio_bytes;
+  float* pm = reinterpret_cast<float*>(ws + L.partials);
+  float* ps = pm + (size_t)2 * L.n_splits * T;
+  float* pz = ps + (size_t)2 * L.n_splits * T;
+  int n_parts = 0;
+  rc = fwd_project(hidden, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, 0, L, ws, pm, ps, pz, nullptr, status, st, &n_parts);
+  if (rc != SAPO_OK) return rc;
+  {
+    int64_t blocks = ceil_div<int64_t>(T, 256);
+    if (blocks > (int64_t)sms * 8) blocks = (int64_t)sms * 8;
+    KernelScope scope(SAPO_K_PREF_SCORE, st);
+    pref_score_kernel<<<(int)blocks, 256, 0, st>>>(pm, ps, pz, n_parts, T, ids, V, ref_logp, cu_seqlens, S, logp, lse,
+                                                   log_ratio, status);
+  }
+  const PrefArgs pa{log_ratio, nullptr, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
+                    h_cfg->grad_scale, h_cfg->kind, h_cfg->pairs, h_cfg->length_norm, gscale, seq_logratio, seq_grad,
+                    q_loss, q_margin, q_pairs, loss, status};
+  if ((rc = launch_preference(pa, st)) != SAPO_OK) return rc;
+  return bwd_impl(hidden, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, 0, lse, gscale, dhidden, dW_head, out_dtype,
+                  accumulate_dW, ws, workspace_bytes - ratio_bytes, status, stream);
 }
 
 namespace sapo {
