@@ -197,16 +197,28 @@ def _check(rc: int, what: str) -> None:
         raise SapoError(f"{what}: {load().sapo_status_string(rc).decode()} ({rc})")
 
 
+_have_cuda = False
+
+
 def _require_cuda() -> None:
-    if not torch.cuda.is_available():
-        raise SapoError("the SAPO B200 library needs a CUDA device; there is no CPU path")
+    global _have_cuda
+    if not _have_cuda:
+        if not torch.cuda.is_available():
+            raise SapoError("the SAPO B200 library needs a CUDA device; there is no CPU path")
+        _have_cuda = True
 
 
 def _p(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    """The current stream's handle (without building a Stream object, which costs 3 us, where torch allows it)."""
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -618,9 +630,10 @@ def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:
 
 def _rows(t: torch.Tensor, what: str) -> int:
     """Row pitch of a 2-D tensor whose columns are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
         raise SapoError(f"{what} must be two-dimensional with contiguous columns")
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+    return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1])
 
 
 def _norm_cfg(kind: str, eps: float, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor]) -> NormCfgC:

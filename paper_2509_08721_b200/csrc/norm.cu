@@ -18,6 +18,7 @@ constexpr int NORM_MAX_H = 16384;
 constexpr int NORM_THREADS = 256;
 constexpr int NORM_MAX_THREADS = 512;    // one row of NORM_MAX_H columns
 constexpr int NV_MAX = 4;
+constexpr int SMEM_MAX = 220 * 1024;     // shared memory a block may take for its rows
 // A group whose largest magnitude is below this is stored as zeros: 127 (1 / amax) would overflow.
 constexpr float Q8_TINY = 1.5046328e-36f;   // 2^-119
 
@@ -114,10 +115,15 @@ __device__ __forceinline__ void store8(const Mat& m, int64_t row, int col, int n
   if (m.dtype == SAPO_DTYPE_F32) store8<VEC>(static_cast<float*>(m.p) + row * m.ld + col, n, v);
   else store8<VEC>(static_cast<__nv_bfloat16*>(m.p) + row * m.ld + col, n, v);
 }
-// per-column weights: fp32 or bf16, no alignment asked for
-__device__ __forceinline__ void load_weight8(const void* w, int32_t dtype, int col, int n, float (&v)[8]) {
-  if (dtype == SAPO_DTYPE_F32) load8<false>(static_cast<const float*>(w) + col, n, v);
-  else load8<false>(static_cast<const __nv_bfloat16*>(w) + col, n, v);
+// per-column weights, fp32 or bf16; `vec`: the array starts on a 16-byte boundary
+__device__ __forceinline__ void load_weight8(const void* w, int32_t dtype, bool vec, int col, int n, float (&v)[8]) {
+  if (dtype == SAPO_DTYPE_F32) {
+    if (vec) load8<true>(static_cast<const float*>(w) + col, n, v);
+    else load8<false>(static_cast<const float*>(w) + col, n, v);
+  } else {
+    if (vec) load8<true>(static_cast<const __nv_bfloat16*>(w) + col, n, v);
+    else load8<false>(static_cast<const __nv_bfloat16*>(w) + col, n, v);
+  }
 }
 
 struct Q8Mat { int8_t* p; float* scale; int64_t ld, ld_scale; };
@@ -170,7 +176,7 @@ __device__ __forceinline__ void quantise8(const float (&v)[8], int width, int (&
 // x to y (and to an 8-bit checkpoint): mean and variance from the row in registers (two passes
 // there, one over memory).  REPLAY: x comes from a checkpoint and mean / rstd are the stored ones.
 struct NormFwdArgs {
-  Mat x, y; Q8Mat q; const void* gamma; const void* beta; int32_t w_dtype, kind; float eps;
+  Mat x, y; Q8Mat q; const void* gamma; const void* beta; int32_t w_dtype, w_vec, kind; float eps;
   float* mean; float* rstd; int64_t T; int32_t H, tpr; int32_t* status;
 };
 
@@ -243,8 +249,8 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_fwd_kernel(NormFwdArgs 
         float g[8], b[8];
         #pragma unroll
         for (int j = 0; j < 8; ++j) { g[j] = 1.f; b[j] = 0.f; }
-        if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, col, n, g);
-        if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, col, n, b);
+        if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, n, g);
+        if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, a.w_vec, col, n, b);
         #pragma unroll
         for (int j = 0; j < 8; ++j) v[i][j] = fmaf((v[i][j] - mean) * rstd, g[j], b[j]);
         store8<VEC>(a.y, row, col, n, v[i]);
@@ -296,7 +302,7 @@ __global__ void __launch_bounds__(256) ckpt8_kernel(Ckpt8Args a) {
 // registers over all rows of its block; the blocks' sums go to `part` ([blocks][2][H]) and
 // norm_reduce_kernel adds them up in block order, so that the result does not depend on timing.
 struct NormBwdArgs {
-  Mat dy, x, dx; Q8Mat q; const void* gamma; int32_t w_dtype, kind; const float* mean; const float* rstd;
+  Mat dy, x, dx; Q8Mat q; const void* gamma; int32_t w_dtype, w_vec, kind; const float* mean; const float* rstd;
   int64_t T; int32_t H, tpr; float* part; float* dgamma; float* dbeta; int32_t accumulate;
 };
 
@@ -313,7 +319,7 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_kernel(NormBwdArgs 
     const int n = min(8, max(0, a.H - col));
     #pragma unroll
     for (int j = 0; j < 8; ++j) { gam[i][j] = 1.f; dg[i][j] = 0.f; db[i][j] = 0.f; }
-    if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, col, n, gam[i]);
+    if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, n, gam[i]);
   }
   for (int64_t base = (int64_t)blockIdx.x * p.rows_per_block; base < a.T; base += (int64_t)gridDim.x * p.rows_per_block) {
     const int64_t row = base + p.r;
@@ -424,6 +430,344 @@ norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float
   if (lane == 0 && c < H) out[c] = accumulate ? out[c] + t : t;
 }
 
+// ---------------------------------------------------------------------------- rows through shared memory
+// The kernels for rows of more than 128 columns that start on 16-byte boundaries.  A row belongs to
+// the `wpr` warps of a group; warp w of them owns VPL * 256 consecutive columns, lane l of it the
+// vectors of 8 columns (w VPL + v) 32 + l, v < VPL.  Each warp streams its part of the group's
+// next STAGES - 1 rows into shared memory with asynchronous copies while it works on the current one, so
+// the bytes in flight do not depend on registers or on how long a row's sums take.  Only lanes of the
+// same warp read what a lane copied: the wait for a row is one __syncwarp.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int src_bytes) {   // the rest is filled with zeros
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void group_barrier(int id, int n_threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n_threads) : "memory");
+}
+
+// One warp's part of a row of TX in shared memory: VPL * 256 elements.
+template <class TX, int VPL>
+struct WarpRow {
+  static constexpr int BYTES = VPL * 256 * (int)sizeof(TX);
+  // src: the warp's first column of the row; cols: how many of its columns exist
+  __device__ static __forceinline__ void copy(uint32_t dst, const TX* src, int cols, int lane) {
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      if constexpr (sizeof(TX) == 4) {
+        // neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
+        // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
+        #pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int j = h * 32 + lane, left = (cols - v * 256 - j * 4) * 4;
+          // (the second half of a vector that ends in its first is filled with zeros)
+          if (left > 0 || (left > -16 && (j & 1)))
+            copy_async<16>(dst + v * 1024 + (j ^ ((j >> 3) & 1)) * 16, left > 0 ? src + v * 256 + j * 4 : src,
+                           left < 16 ? (left > 0 ? left : 0) : 16);
+        }
+      } else {
+        constexpr int B = 8 * (int)sizeof(TX);
+        const int left = (cols - v * 256 - lane * 8) * (int)sizeof(TX);
+        if (left > 0) copy_async<B>(dst + (v * 32 + lane) * B, src + v * 256 + lane * 8, left < B ? left : B);
+      }
+    }
+  }
+  // the lane's vector v; it has to have a column of the row (the others of the vector read as zero)
+  __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float (&x)[8]) {
+    if constexpr (sizeof(TX) == 4) {
+      const int j = 2 * lane, f = (j >> 3) & 1;
+      const float4 a = *reinterpret_cast<const float4*>(at + v * 1024 + (j ^ f) * 16);
+      const float4 b = *reinterpret_cast<const float4*>(at + v * 1024 + ((j + 1) ^ f) * 16);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+      load8<true>(reinterpret_cast<const TX*>(at) + (v * 32 + lane) * 8, 8, x);
+    }
+  }
+};
+
+// sums of two values over a group of warps; red: [2][warps of the block][2], `turn` alternates
+__device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, int group, float2* red, int turn, int n_warps) {
+  #pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, d);
+    b += __shfl_xor_sync(0xffffffffu, b, d);
+  }
+  if (wpr == 1) return make_float2(a, b);
+  float2* r = red + turn * n_warps + group * wpr;
+  if ((threadIdx.x & 31) == 0) r[w] = make_float2(a, b);
+  group_barrier(1 + group, wpr * 32);
+  float2 t = make_float2(0.f, 0.f);
+  for (int i = 0; i < wpr; ++i) { const float2 o = r[i]; t.x += o.x; t.y += o.y; }
+  return t;
+}
+
+template <class TX, int VPL> struct FwdRing {
+  static constexpr int STAGES = 256 * VPL * 8 * (int)sizeof(TX) <= 16384 ? 4 : 3;
+  static constexpr int SMEM = STAGES * (NORM_THREADS / 32) * WarpRow<TX, VPL>::BYTES;
+};
+
+// TX int8_t: replay from a checkpoint (a.q), statistics given.
+template <class TX, int VPL>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
+  constexpr bool REPLAY = sizeof(TX) == 1;
+  constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float2 red[2 * WARPS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / wpr, w = warp - group * wpr;
+  const int64_t step = (int64_t)gridDim.x * (WARPS / wpr);
+  const int64_t row0 = (int64_t)blockIdx.x * (WARPS / wpr) + group;
+  const int col0 = w * VPL * 256;                       // the warp's first column
+  const int cols = a.H - col0;
+  const TX* src = REPLAY ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p);
+  const int64_t ld = REPLAY ? a.q.ld : a.x.ld;
+  uint8_t* mine = ring + warp * WarpRow<TX, VPL>::BYTES;
+  constexpr int STAGE_BYTES = WARPS * WarpRow<TX, VPL>::BYTES;
+  const float inv_h = 1.f / (float)a.H;
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < a.T && cols > 0) WarpRow<TX, VPL>::copy(smem_addr(mine + stage * STAGE_BYTES), src + row * ld + col0, cols, lane);
+    copy_commit();
+  };
+  #pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(row0 + s * step, s);
+  int stage = 0, turn = 0;
+  for (int64_t row = row0; row < a.T; row += step) {
+    copy_wait<S - 2>();
+    __syncwarp();
+    fetch(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+    const uint8_t* at = mine + stage * STAGE_BYTES;
+    stage = stage + 1 == S ? 0 : stage + 1;
+    float x[VPL][8];
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      if ((v * 32 + lane) * 8 < cols) {
+        WarpRow<TX, VPL>::read(at, v, lane, x[v]);
+        if (REPLAY) {
+          const float s = a.q.scale[row * a.q.ld_scale + (col0 + (v * 32 + lane) * 8) / Q8_GROUP];
+          #pragma unroll
+          for (int j = 0; j < 8; ++j) x[v][j] *= s;
+        }
+      } else {
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) x[v][j] = 0.f;
+      }
+    }
+    float mean = 0.f, rstd;
+    if (REPLAY) {
+      mean = a.kind == KIND_LAYER ? a.mean[row] : 0.f;
+      rstd = a.rstd[row];
+    } else {
+      if (a.kind == KIND_LAYER) {
+        float s = 0.f;
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v)
+          #pragma unroll
+          for (int j = 0; j < 8; ++j) s += x[v][j];
+        mean = group_sum2(s, 0.f, wpr, w, group, red, turn, WARPS).x * inv_h;
+        turn ^= 1;
+      }
+      float s2 = 0.f;
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        const int left = cols - (v * 32 + lane) * 8;
+        if (left >= 8) {
+          #pragma unroll
+          for (int j = 0; j < 8; ++j) { const float d = x[v][j] - mean; s2 = fmaf(d, d, s2); }
+        } else {
+          #pragma unroll
+          for (int j = 0; j < 8; ++j) if (j < left) { const float d = x[v][j] - mean; s2 = fmaf(d, d, s2); }
+        }
+      }
+      rstd = 1.f / sqrtf(group_sum2(s2, 0.f, wpr, w, group, red, turn, WARPS).x * inv_h + a.eps);
+      turn ^= 1;
+      if (w == 0 && lane == 0) {
+        if (a.mean != nullptr && a.kind == KIND_LAYER) a.mean[row] = mean;
+        if (a.rstd != nullptr) a.rstd[row] = rstd;
+      }
+    }
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int col = col0 + (v * 32 + lane) * 8;
+      const int n = min(8, a.H - col);
+      if (!REPLAY && a.q.p != nullptr) {
+        int q[8]; float scale; bool bad;
+        quantise8(x[v], 16, q, scale, bad);
+        if (n > 0) {
+          store8<true>(a.q.p + row * a.q.ld + col, n, q);
+          if (col % Q8_GROUP == 0) {
+            a.q.scale[row * a.q.ld_scale + col / Q8_GROUP] = scale;
+            if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+          }
+        }
+      }
+      if (n > 0) {
+        float g[8], b[8];
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) { g[j] = 1.f; b[j] = 0.f; }
+        if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, n, g);
+        if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, a.w_vec, col, n, b);
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) x[v][j] = fmaf((x[v][j] - mean) * rstd, g[j], b[j]);
+        store8<true>(a.y, row, col, n, x[v]);
+      }
+    }
+  }
+}
+
+// Warps of a row and rows of a block in the backward: the sums of a thread's columns over all rows of its
+// block are 16 registers a vector, so a thread owns few of them and a row is spread over more warps.
+template <class TX, class TDY, int VPL, int MAX_THREADS> struct BwdRing {
+  static constexpr int WARP_BYTES = WarpRow<TX, VPL>::BYTES + WarpRow<TDY, VPL>::BYTES + 64 + (sizeof(TX) == 1 ? VPL * 128 : 0);
+  static constexpr int FULL = MAX_THREADS / 32 * WARP_BYTES;         // one row of the widest block
+  static constexpr int STAGES = 4 * FULL <= SMEM_MAX ? 4 : (3 * FULL <= SMEM_MAX ? 3 : 2);
+  static constexpr bool FITS = STAGES * FULL <= SMEM_MAX;            // else norm_bwd_kernel takes it
+  // whether a row stays in registers between the sums and dx; a thread with many columns reads it again
+  static constexpr bool HOLD = VPL <= 2;
+};
+
+template <class TX, class TDY, int VPL, int MAX_THREADS>
+__global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_bwd_ring_kernel(NormBwdArgs a, int wpr) {
+  constexpr bool FROM_Q8 = sizeof(TX) == 1;
+  using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
+  constexpr int S = Ring::STAGES;
+  constexpr bool HOLD = Ring::HOLD;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float2 red[2 * (MAX_THREADS / 32)];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / wpr;
+  const int group = warp / wpr, w = warp - group * wpr;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  const int64_t row0 = (int64_t)blockIdx.x * groups + group;
+  const int col0 = w * VPL * 256, cols = a.H - col0;
+  uint8_t* mine = ring + warp * Ring::WARP_BYTES;
+  const int stage_bytes = warps * Ring::WARP_BYTES;
+  const TX* xp = FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p);
+  const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
+  const TDY* dyp = static_cast<const TDY*>(a.dy.p);
+  constexpr int DY_AT = WarpRow<TX, VPL>::BYTES, ST_AT = DY_AT + WarpRow<TDY, VPL>::BYTES, SC_AT = ST_AT + 64;
+  const float inv_h = 1.f / (float)a.H;
+  const bool layer = a.kind == KIND_LAYER;
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < a.T) {
+      const uint32_t dst = smem_addr(mine + stage * stage_bytes);
+      WarpRow<TX, VPL>::copy(dst, xp + row * ldx + col0, cols, lane);
+      WarpRow<TDY, VPL>::copy(dst + DY_AT, dyp + row * a.dy.ld + col0, cols, lane);
+      if (lane == 0) copy_async<4>(dst + ST_AT, a.rstd + row, 4);
+      if (lane == 1 && layer) copy_async<4>(dst + ST_AT + 4, a.mean + row, 4);
+      if (FROM_Q8) {
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+          const int col = (v * 32 + lane) * 8;
+          if (col < cols) copy_async<4>(dst + SC_AT + (v * 32 + lane) * 4, a.q.scale + row * a.q.ld_scale + (col0 + col) / Q8_GROUP, 4);
+        }
+      }
+    }
+    copy_commit();
+  };
+  #pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(row0 + s * step, s);
+  float gam[HOLD ? VPL : 1][8], dg[VPL][8], db[VPL][8];
+  auto weights = [&](int v, float (&g)[8]) {
+    const int col = col0 + (v * 32 + lane) * 8;
+    #pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = 1.f;
+    if (a.gamma != nullptr && col < a.H) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, min(8, a.H - col), g);
+  };
+  #pragma unroll
+  for (int v = 0; v < VPL; ++v) {
+    #pragma unroll
+    for (int j = 0; j < 8; ++j) { dg[v][j] = 0.f; db[v][j] = 0.f; }
+    if (HOLD) weights(v, gam[v]);
+  }
+  int stage = 0, turn = 0;
+  for (int64_t row = row0; row < a.T; row += step) {
+    copy_wait<S - 2>();
+    __syncwarp();
+    fetch(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+    const uint8_t* at = mine + stage * stage_bytes;
+    stage = stage + 1 == S ? 0 : stage + 1;
+    const float rstd = *reinterpret_cast<const float*>(at + ST_AT);
+    const float mean = layer ? *reinterpret_cast<const float*>(at + ST_AT + 4) : 0.f;
+    float xh[HOLD ? VPL : 1][8], g[HOLD ? VPL : 1][8];
+    // vector v of the row: xh, dy and, in place of dy, g = dy gamma
+    auto take = [&](int v, float (&x)[8], float (&d)[8]) {
+      WarpRow<TX, VPL>::read(at, v, lane, x);
+      WarpRow<TDY, VPL>::read(at + DY_AT, v, lane, d);
+      float s = 1.f;
+      if (FROM_Q8) s = *reinterpret_cast<const float*>(at + SC_AT + (v * 32 + lane) * 4);
+      #pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = ((FROM_Q8 ? x[j] * s : x[j]) - mean) * rstd;
+    };
+    float s1 = 0.f, s2 = 0.f;
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      if ((v * 32 + lane) * 8 >= cols) continue;
+      const int k = HOLD ? v : 0;
+      take(v, xh[k], g[k]);
+      if (!HOLD) weights(v, gam[0]);
+      // (columns past H of the last vector are zero in dy: they add nothing)
+      #pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dg[v][j] = fmaf(g[k][j], xh[k][j], dg[v][j]);
+        db[v][j] += g[k][j];
+        g[k][j] *= gam[k][j];
+        s1 += g[k][j];
+        s2 = fmaf(g[k][j], xh[k][j], s2);
+      }
+    }
+    const float2 sums = group_sum2(s1, s2, wpr, w, group, red, turn, warps);
+    turn ^= 1;
+    const float c1 = layer ? sums.x * inv_h : 0.f, c2 = sums.y * inv_h;
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int col = col0 + (v * 32 + lane) * 8;
+      const int n = min(8, a.H - col);
+      if (n <= 0) continue;
+      const int k = HOLD ? v : 0;
+      if (!HOLD) {
+        take(v, xh[0], g[0]);
+        weights(v, gam[0]);
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) g[0][j] *= gam[0][j];
+      }
+      #pragma unroll
+      for (int j = 0; j < 8; ++j) g[k][j] = rstd * (g[k][j] - c1 - xh[k][j] * c2);
+      store8<true>(a.dx, row, col, n, g[k]);
+    }
+  }
+  if (a.dgamma == nullptr && a.dbeta == nullptr) return;
+  // the groups' sums one after the other, through the ring (no copy is in flight any more)
+  copy_wait<0>();
+  __syncthreads();
+  float* acc = reinterpret_cast<float*>(ring);           // [2][H]
+  for (int k = 0; k < groups; ++k) {
+    if (k == group) {
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v)
+        #pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int col = col0 + (v * 32 + lane) * 8 + j;
+          if (col >= a.H) continue;
+          float g = dg[v][j], b = db[v][j];
+          if (k > 0) { g += acc[col]; b += acc[a.H + col]; }
+          if (k + 1 < groups) { acc[col] = g; acc[a.H + col] = b; continue; }
+          if (gridDim.x > 1) {
+            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H;
+            out[col] = g; out[a.H + col] = b;
+          } else {
+            if (a.dgamma != nullptr) a.dgamma[col] = a.accumulate ? a.dgamma[col] + g : g;
+            if (a.dbeta != nullptr) a.dbeta[col] = a.accumulate ? a.dbeta[col] + b : b;
+          }
+        }
+    }
+    __syncthreads();
+  }
+}
+
 // ---------------------------------------------------------------------------- host side
 struct RowPlan { int tpr, nv, threads; };
 static RowPlan row_plan(int32_t H) {
@@ -437,9 +781,31 @@ static RowPlan row_plan(int32_t H) {
   p.threads = tpr > NORM_THREADS ? tpr : NORM_THREADS;
   return p;
 }
-static int64_t bwd_blocks(int64_t T, const RowPlan& p, int sms) {
-  const int64_t want = ceil_div<int64_t>(T, p.threads / p.tpr);
-  const int64_t most = (int64_t)sms * 2;
+// Rows through shared memory: columns of more than one 16-thread group, rows on 16-byte boundaries.
+static bool ring_ok(int32_t H, bool vec) { return vec && H > Q8_GROUP; }
+struct RingPlan { int wpr, vpl, threads, rows_per_block; };
+static RingPlan fwd_ring_plan(int32_t H) {
+  const int nvec = ceil_div(H, 8);
+  RingPlan p;
+  p.wpr = 1;
+  while (p.wpr * 256 < nvec) p.wpr <<= 1;
+  p.vpl = ceil_div(nvec, p.wpr * 32);
+  p.threads = NORM_THREADS;
+  p.rows_per_block = NORM_THREADS / 32 / p.wpr;
+  return p;
+}
+static RingPlan bwd_ring_plan(int32_t H) {
+  const int nvec = ceil_div(H, 8);
+  RingPlan p;
+  p.vpl = nvec <= 32 ? 1 : (H <= 8192 ? 2 : 4);
+  p.wpr = ceil_div(nvec, p.vpl * 32);
+  p.rows_per_block = p.wpr >= 5 ? 1 : 8 / p.wpr;
+  p.threads = p.wpr * p.rows_per_block * 32;
+  return p;
+}
+static int64_t bwd_blocks(int64_t T, int rows_per_block, int per_sm, int sms) {
+  const int64_t want = ceil_div<int64_t>(T, rows_per_block);
+  const int64_t most = (int64_t)sms * per_sm;
   return want < most ? want : most;
 }
 
@@ -471,6 +837,81 @@ static int cfg_check(const sapo_norm_cfg* c, const void* gamma, const void* beta
 }
 static Q8Mat q8_of(const sapo_ckpt8* c) { return c ? Q8Mat{c->data, c->scale, c->ld, c->ld_scale} : Q8Mat{nullptr, nullptr, 0, 0}; }
 
+// Blocks of a kernel that an SM holds, looked up once per kernel and device; opts in to the shared memory.
+template <class Kernel>
+static int resident_blocks(Kernel kernel, int threads, size_t smem, int* cache) {
+  const int dev = current_device();
+  if (dev < 0) return 0;
+  if (cache[dev] == 0) {
+    int n = 0;
+    if (smem > 48 * 1024 &&
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX) != cudaSuccess) return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) return 0;
+    cache[dev] = n;
+  }
+  return cache[dev];
+}
+
+template <class TX, int VPL>
+static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
+  static int cache[MAX_DEVICES] = {0};
+  auto kernel = norm_fwd_ring_kernel<TX, VPL>;
+  const size_t smem = FwdRing<TX, VPL>::SMEM;
+  const int per_sm = resident_blocks(kernel, p.threads, smem, cache);
+  if (per_sm == 0) return SAPO_ERR_CUDA;
+  int64_t blocks = ceil_div<int64_t>(a.T, p.rows_per_block);
+  if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
+  KernelScope scope(SAPO_K_NORM_FWD, st);
+  kernel<<<(int)blocks, p.threads, smem, st>>>(a, p.wpr);
+  return check_launch();
+}
+template <class TX>
+static int launch_fwd_ring(const NormFwdArgs& a, int sms, cudaStream_t st) {
+  const RingPlan p = fwd_ring_plan(a.H);
+  switch (p.vpl) {
+    case 1: return launch_fwd_ring_vpl<TX, 1>(a, p, sms, st);
+    case 2: return launch_fwd_ring_vpl<TX, 2>(a, p, sms, st);
+    case 3: return launch_fwd_ring_vpl<TX, 3>(a, p, sms, st);
+    case 4: return launch_fwd_ring_vpl<TX, 4>(a, p, sms, st);
+    case 5: return launch_fwd_ring_vpl<TX, 5>(a, p, sms, st);
+    case 6: return launch_fwd_ring_vpl<TX, 6>(a, p, sms, st);
+    case 7: return launch_fwd_ring_vpl<TX, 7>(a, p, sms, st);
+    default: return launch_fwd_ring_vpl<TX, 8>(a, p, sms, st);
+  }
+}
+
+// launch == false: only how many blocks of the plan an SM holds (0: this form does not exist)
+template <class TX, class TDY, int VPL, int MAX_THREADS>
+static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
+  using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
+  if constexpr (!Ring::FITS) {
+    return launch ? SAPO_ERR_CUDA : 0;
+  } else {
+    static int cache[33][MAX_DEVICES] = {{0}};                       // by warps of the block
+    auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS>;
+    // the ring, or the columns' sums that take its place at the end
+    size_t smem = (size_t)Ring::STAGES * (p.threads / 32) * Ring::WARP_BYTES;
+    if (p.rows_per_block > 1 && smem < (size_t)2 * a.H * sizeof(float)) smem = (size_t)2 * a.H * sizeof(float);
+    if (!launch) return resident_blocks(kernel, p.threads, smem, cache[p.threads / 32]);
+    KernelScope scope(SAPO_K_NORM_BWD, st);
+    kernel<<<blocks, p.threads, smem, st>>>(a, p.wpr);
+    return check_launch();
+  }
+}
+template <class TX, class TDY>
+static int bwd_ring_dy(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
+  if (p.vpl == 1) return bwd_ring_vpl<TX, TDY, 1, 256>(a, p, blocks, launch, st);
+  if (p.vpl == 2 && p.threads <= 256) return bwd_ring_vpl<TX, TDY, 2, 256>(a, p, blocks, launch, st);
+  if (p.vpl == 2) return bwd_ring_vpl<TX, TDY, 2, 512>(a, p, blocks, launch, st);
+  return bwd_ring_vpl<TX, TDY, 4, 512>(a, p, blocks, launch, st);
+}
+static int bwd_ring(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
+  const bool f = a.dy.dtype == SAPO_DTYPE_F32;
+  if (a.q.p != nullptr) return f ? bwd_ring_dy<int8_t, float>(a, p, blocks, launch, st) : bwd_ring_dy<int8_t, __nv_bfloat16>(a, p, blocks, launch, st);
+  if (a.x.dtype == SAPO_DTYPE_F32) return f ? bwd_ring_dy<float, float>(a, p, blocks, launch, st) : bwd_ring_dy<float, __nv_bfloat16>(a, p, blocks, launch, st);
+  return f ? bwd_ring_dy<__nv_bfloat16, float>(a, p, blocks, launch, st) : bwd_ring_dy<__nv_bfloat16, __nv_bfloat16>(a, p, blocks, launch, st);
+}
+
 template <int NV, bool REPLAY>
 static int launch_fwd_nv(const NormFwdArgs& a, bool vec, const RowPlan& p, int sms, cudaStream_t st) {
   auto kernel = vec ? norm_fwd_kernel<NV, true, REPLAY> : norm_fwd_kernel<NV, false, REPLAY>;
@@ -489,6 +930,10 @@ static int launch_fwd(NormFwdArgs a, cudaStream_t st) {
   const RowPlan p = row_plan(a.H);
   a.tpr = p.tpr;
   const bool vec = (REPLAY || vec_ok(a.x)) && vec_ok(a.y) && (a.q.p == nullptr || vec_ok(a.q));
+  if (ring_ok(a.H, vec)) {
+    if (REPLAY) return launch_fwd_ring<int8_t>(a, sms, st);
+    return a.x.dtype == SAPO_DTYPE_F32 ? launch_fwd_ring<float>(a, sms, st) : launch_fwd_ring<__nv_bfloat16>(a, sms, st);
+  }
   switch (p.nv) {
     case 1: return launch_fwd_nv<1, REPLAY>(a, vec, p, sms, st);
     case 2: return launch_fwd_nv<2, REPLAY>(a, vec, p, sms, st);
@@ -546,7 +991,8 @@ extern "C" int sapo_norm_fwd(const void* x, int32_t x_dtype, int64_t T, int32_t 
   const Mat mx{const_cast<void*>(x), ld_x, x_dtype}, my{y, ld_y, y_dtype};
   if ((rc = mat_check(mx, T, H)) != SAPO_OK || (rc = mat_check(my, T, H)) != SAPO_OK) return rc;
   if (h_ckpt && ((rc = ckpt_check(h_ckpt, T, H)) != SAPO_OK || !status)) return SAPO_ERR_INVALID_ARG;
-  return launch_fwd<false>(NormFwdArgs{mx, my, q8_of(h_ckpt), gamma, beta, h_cfg->w_dtype, h_cfg->kind, h_cfg->eps,
+  return launch_fwd<false>(NormFwdArgs{mx, my, q8_of(h_ckpt), gamma, beta, h_cfg->w_dtype,
+                                       aligned16(gamma) && aligned16(beta), h_cfg->kind, h_cfg->eps,
                                        mean, rstd, T, H, 0, status}, static_cast<cudaStream_t>(stream));
 }
 
@@ -561,7 +1007,7 @@ extern "C" int sapo_norm_replay(const sapo_ckpt8* h_x, int64_t T, int32_t H, con
   if ((rc = ckpt_check(h_x, T, H)) != SAPO_OK || (rc = mat_check(my, T, H)) != SAPO_OK) return rc;
   if (T > 0 && (!rstd || (h_cfg->kind == SAPO_NORM_LAYER && !mean))) return SAPO_ERR_INVALID_ARG;
   return launch_fwd<true>(NormFwdArgs{Mat{nullptr, 0, SAPO_DTYPE_BF16}, my, q8_of(h_x), gamma, beta, h_cfg->w_dtype,
-                                      h_cfg->kind, 0.f, const_cast<float*>(mean), const_cast<float*>(rstd), T, H, 0,
+                                      aligned16(gamma) && aligned16(beta), h_cfg->kind, 0.f, const_cast<float*>(mean), const_cast<float*>(rstd), T, H, 0,
                                       nullptr}, static_cast<cudaStream_t>(stream));
 }
 
@@ -570,7 +1016,11 @@ extern "C" size_t sapo_norm_workspace_bytes(int64_t T, int32_t H) {
   if (dims_check(T, H) != SAPO_OK) return 0;
   int sms = sm_count();
   if (sms <= 0) sms = 148;
-  const int64_t blocks = bwd_blocks(T > 0 ? T : 1, row_plan(H), sms);
+  // the larger of what the two forms of the kernel take, whatever the alignment of the rows will be
+  const RowPlan p = row_plan(H);
+  int64_t blocks = bwd_blocks(T > 0 ? T : 1, p.threads / p.tpr, 2, sms);
+  const int64_t ring = bwd_blocks(T > 0 ? T : 1, bwd_ring_plan(H).rows_per_block, 2, sms);
+  if (ring > blocks) blocks = ring;
   return round_up<size_t>((size_t)blocks * 2 * H * sizeof(float), 256);
 }
 
@@ -601,16 +1051,21 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
   }
   const int sms = sm_count();
   if (sms <= 0) return SAPO_ERR_CUDA;
+  const bool vec = vec_ok(mdy) && vec_ok(mdx) && (h_ckpt ? vec_ok(q8_of(h_ckpt)) : vec_ok(mx));
+  NormBwdArgs a{mdy, mx, mdx, q8_of(h_ckpt), gamma, h_cfg->w_dtype, aligned16(gamma), h_cfg->kind, mean, rstd, T, H, 0,
+                static_cast<float*>(workspace), dgamma, dbeta, accumulate};
   const RowPlan p = row_plan(H);
-  const int blocks = (int)bwd_blocks(T, p, sms);
+  const RingPlan rp = bwd_ring_plan(H);
+  const int resident = ring_ok(H, vec) ? bwd_ring(a, rp, 0, false, st) : 0;
+  const bool ring = resident > 0;
+  const int blocks = (int)bwd_blocks(T, ring ? rp.rows_per_block : p.threads / p.tpr, ring && resident < 2 ? resident : 2, sms);
+  a.tpr = p.tpr;
   if (reduce && blocks > 1) {
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3u)) return SAPO_ERR_INVALID_ARG;
     if (workspace_bytes < (size_t)blocks * 2 * H * sizeof(float)) return SAPO_ERR_WORKSPACE_TOO_SMALL;
   }
-  NormBwdArgs a{mdy, mx, mdx, q8_of(h_ckpt), gamma, h_cfg->w_dtype, h_cfg->kind, mean, rstd, T, H, p.tpr,
-                static_cast<float*>(workspace), dgamma, dbeta, accumulate};
-  const bool vec = vec_ok(mdy) && vec_ok(mdx) && (h_ckpt ? vec_ok(a.q) : vec_ok(mx));
-  rc = h_ckpt ? launch_bwd<true>(a, vec, p, blocks, st) : launch_bwd<false>(a, vec, p, blocks, st);
+  if (ring) rc = bwd_ring(a, rp, blocks, true, st);
+  else rc = h_ckpt ? launch_bwd<true>(a, vec, p, blocks, st) : launch_bwd<false>(a, vec, p, blocks, st);
   if (rc != SAPO_OK || !reduce || blocks == 1) return rc;
   KernelScope scope(SAPO_K_NORM_REDUCE, st);
   norm_reduce_kernel<<<dim3(ceil_div(H, 32), 2), 1024, 0, st>>>(a.part, blocks, H, dgamma, dbeta, accumulate);
