@@ -431,19 +431,22 @@ norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float
 }
 
 // ---------------------------------------------------------------------------- rows through shared memory
-// The kernels for rows of more than 128 columns that start on 16-byte boundaries.  A row belongs to
-// the `wpr` warps of a group; warp w of them owns VPL * 256 consecutive columns, lane l of it the
-// vectors of 8 columns (w VPL + v) 32 + l, v < VPL.  Each warp streams its part of the group's
+// The kernels for rows of more than 128 columns, a multiple of 8, that start on 16-byte boundaries.
+// A row belongs to the `wpr` warps of a group; warp w of them owns VPL * 256 consecutive columns, lane l
+// of it the vectors of 8 columns (w VPL + v) 32 + l, v < VPL.  Each warp streams its part of the group's
 // next STAGES - 1 rows into shared memory with asynchronous copies while it works on the current one, so
 // the bytes in flight do not depend on registers or on how long a row's sums take.  Only lanes of the
 // same warp read what a lane copied: the wait for a row is one __syncwarp.
+// What then bounds a row kernel is instruction issue (at the copy bandwidth an SM has to finish 4 to 6
+// columns per clock), so the arithmetic is done in pairs (fma.rn.f32x2 and its kin, each half rounded
+// like the scalar operation) and every vector is whole.
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int src_bytes) {   // the rest is filled with zeros
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
   if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -451,55 +454,149 @@ __device__ __forceinline__ void group_barrier(int id, int n_threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n_threads) : "memory");
 }
 
+#define SAPO_F32X2(name, ptx)                                                                             \
+  __device__ __forceinline__ float2 name(float2 a, float2 b) {                                            \
+    float2 d;                                                                                             \
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t" ptx                 \
+        " d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"                                                          \
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));                                 \
+    return d;                                                                                             \
+  }
+SAPO_F32X2(add2, "add.rn.f32x2")
+SAPO_F32X2(mul2, "mul.rn.f32x2")
+#undef SAPO_F32X2
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+__device__ __forceinline__ void unpack8(uint4 u, float2 (&x)[4]) {       // bf16 to fp32: the upper half of the word
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  #pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+}
+// int8 to fp32: the byte, its sign flipped, as the last bits of 2^23; exact
+__device__ __forceinline__ void unpack8(uint2 u, float2 (&x)[4]) {
+  const uint32_t w[2] = {u.x ^ 0x80808080u, u.y ^ 0x80808080u};
+  const float2 back = both(-8388736.f);                                   // -(2^23 + 128)
+  #pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    x[2 * h] = add2(make_float2(__uint_as_float(__byte_perm(w[h], 0x4b000000u, 0x7440)),
+                                __uint_as_float(__byte_perm(w[h], 0x4b000000u, 0x7441))), back);
+    x[2 * h + 1] = add2(make_float2(__uint_as_float(__byte_perm(w[h], 0x4b000000u, 0x7442)),
+                                    __uint_as_float(__byte_perm(w[h], 0x4b000000u, 0x7443))), back);
+  }
+}
+__device__ __forceinline__ void load8(const float* p, float2 (&x)[4]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float2 (&x)[4]) { unpack8(*reinterpret_cast<const uint4*>(p), x); }
+__device__ __forceinline__ void load8(const int8_t* p, float2 (&x)[4]) { unpack8(*reinterpret_cast<const uint2*>(p), x); }
+__device__ __forceinline__ void load_weight8(const void* w, int32_t dtype, int col, float2 (&x)[4]) {
+  if (dtype == SAPO_DTYPE_F32) load8(static_cast<const float*>(w) + col, x);
+  else load8(static_cast<const __nv_bfloat16*>(w) + col, x);
+}
+__device__ __forceinline__ void store8(const Mat& m, int64_t row, int col, const float2 (&x)[4]) {
+  if (m.dtype == SAPO_DTYPE_F32) {
+    float* p = static_cast<float*>(m.p) + row * m.ld + col;
+    *reinterpret_cast<float4*>(p) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(m.p) + row * m.ld + col) =
+        make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
+  }
+}
+// Whole vectors of a group: as quantise8, the rounding to an integer by adding 1.5 2^23 (round to
+// nearest even, the integer in the last bits).  Scalar operations: the product has to be rounded before
+// the sum, and a pair of them is compiled to one fma.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ uint2 quantise8(const float2 (&x)[4], float& scale, bool& bad) {
+  float a = max_nan(max_nan(max_nan(fabsf(x[0].x), fabsf(x[0].y)), max_nan(fabsf(x[1].x), fabsf(x[1].y))),
+                    max_nan(max_nan(fabsf(x[2].x), fabsf(x[2].y)), max_nan(fabsf(x[3].x), fabsf(x[3].y))));
+  #pragma unroll
+  for (int d = 8; d > 0; d >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, d));
+  bad = !(a < INFINITY);
+  const bool some = a >= Q8_TINY && !bad;
+  const float inv = 127.f * __frcp_rn(a);
+  auto integer = [&](float v) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.f)); };
+  scale = bad ? __int_as_float(0x7fc00000) : (some ? a * (1.f / 127.f) : 0.f);
+  uint32_t w[2];
+  #pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __byte_perm(integer(x[2 * h].x), integer(x[2 * h].y), 0x0040);
+    const uint32_t hi = __byte_perm(integer(x[2 * h + 1].x), integer(x[2 * h + 1].y), 0x0040);
+    w[h] = some ? __byte_perm(lo, hi, 0x5410) : 0u;
+  }
+  return make_uint2(w[0], w[1]);
+}
+
 // One warp's part of a row of TX in shared memory: VPL * 256 elements.
 template <class TX, int VPL>
 struct WarpRow {
   static constexpr int BYTES = VPL * 256 * (int)sizeof(TX);
-  // src: the warp's first column of the row; cols: how many of its columns exist
+  // src: the warp's first column of the row; cols: how many of its columns exist (a multiple of 8)
   __device__ static __forceinline__ void copy(uint32_t dst, const TX* src, int cols, int lane) {
-    #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      if constexpr (sizeof(TX) == 4) {
-        // neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
-        // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
-        #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int j = h * 32 + lane, left = (cols - v * 256 - j * 4) * 4;
-          // (the second half of a vector that ends in its first is filled with zeros)
-          if (left > 0 || (left > -16 && (j & 1)))
-            copy_async<16>(dst + v * 1024 + (j ^ ((j >> 3) & 1)) * 16, left > 0 ? src + v * 256 + j * 4 : src,
-                           left < 16 ? (left > 0 ? left : 0) : 16);
-        }
-      } else {
-        constexpr int B = 8 * (int)sizeof(TX);
-        const int left = (cols - v * 256 - lane * 8) * (int)sizeof(TX);
-        if (left > 0) copy_async<B>(dst + (v * 32 + lane) * B, src + v * 256 + lane * 8, left < B ? left : B);
-      }
+    if constexpr (sizeof(TX) == 4) {
+      // neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
+      // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
+      const int j = lane ^ ((lane >> 3) & 1);
+      #pragma unroll
+      for (int v = 0; v < 2 * VPL; ++v)
+        if (v * 128 + lane * 4 < cols) copy_async<16>(dst + v * 512 + j * 16, src + v * 128 + lane * 4);
+    } else {
+      constexpr int B = 8 * (int)sizeof(TX);
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v)
+        if (v * 256 + lane * 8 < cols) copy_async<B>(dst + (v * 32 + lane) * B, src + v * 256 + lane * 8);
     }
   }
-  // the lane's vector v; it has to have a column of the row (the others of the vector read as zero)
-  __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float (&x)[8]) {
+  // the lane's vector v
+  __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float2 (&x)[4]) {
     if constexpr (sizeof(TX) == 4) {
-      const int j = 2 * lane, f = (j >> 3) & 1;
-      const float4 a = *reinterpret_cast<const float4*>(at + v * 1024 + (j ^ f) * 16);
-      const float4 b = *reinterpret_cast<const float4*>(at + v * 1024 + ((j + 1) ^ f) * 16);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+      const int f = (lane >> 2) & 1;
+      const float4 a = *reinterpret_cast<const float4*>(at + v * 1024 + (2 * lane + f) * 16);
+      const float4 b = *reinterpret_cast<const float4*>(at + v * 1024 + (2 * lane + 1 - f) * 16);
+      x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
     } else {
-      load8<true>(reinterpret_cast<const TX*>(at) + (v * 32 + lane) * 8, 8, x);
+      load8(reinterpret_cast<const TX*>(at) + (v * 32 + lane) * 8, x);
     }
   }
 };
 
-// sums of two values over a group of warps; red: [2][warps of the block][2], `turn` alternates
-__device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, int group, float2* red, int turn, int n_warps) {
+// Sums of one or two values over a group of warps; red: [2][warps of the block], `turn` alternates.
+__device__ __forceinline__ float group_sum(float a, int wpr, int w, int group, float2* red, int turn, int n_warps) {
   #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, d);
-    b += __shfl_xor_sync(0xffffffffu, b, d);
-  }
-  if (wpr == 1) return make_float2(a, b);
+  for (int d = 16; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
+  if (wpr == 1) return a;
   float2* r = red + turn * n_warps + group * wpr;
-  if ((threadIdx.x & 31) == 0) r[w] = make_float2(a, b);
+  if ((threadIdx.x & 31) == 0) r[w].x = a;
+  group_barrier(1 + group, wpr * 32);
+  float t = 0.f;
+  for (int i = 0; i < wpr; ++i) t += r[i].x;
+  return t;
+}
+// (after the first exchange half of the lanes carry one value and half the other: 6 shuffles, not 10)
+__device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, int group, float2* red, int turn, int n_warps) {
+  const bool upper = (threadIdx.x & 16) != 0;
+  const float other = __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
+  float x = (upper ? b : a) + other;
+  #pragma unroll
+  for (int d = 8; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  if (wpr == 1) {
+    const float y = __shfl_xor_sync(0xffffffffu, x, 16);
+    return upper ? make_float2(y, x) : make_float2(x, y);
+  }
+  float2* r = red + turn * n_warps + group * wpr;
+  if ((threadIdx.x & 15) == 0) reinterpret_cast<float*>(r + w)[upper] = x;
   group_barrier(1 + group, wpr * 32);
   float2 t = make_float2(0.f, 0.f);
   for (int i = 0; i < wpr; ++i) { const float2 o = r[i]; t.x += o.x; t.y += o.y; }
@@ -530,7 +627,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   constexpr int STAGE_BYTES = WARPS * WarpRow<TX, VPL>::BYTES;
   const float inv_h = 1.f / (float)a.H;
   auto fetch = [&](int64_t row, int stage) {
-    if (row < a.T && cols > 0) WarpRow<TX, VPL>::copy(smem_addr(mine + stage * STAGE_BYTES), src + row * ld + col0, cols, lane);
+    if (row < a.T) WarpRow<TX, VPL>::copy(smem_addr(mine + stage * STAGE_BYTES), src + row * ld + col0, cols, lane);
     copy_commit();
   };
   #pragma unroll
@@ -542,19 +639,19 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
     fetch(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
     const uint8_t* at = mine + stage * STAGE_BYTES;
     stage = stage + 1 == S ? 0 : stage + 1;
-    float x[VPL][8];
+    float2 x[VPL][4];
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       if ((v * 32 + lane) * 8 < cols) {
         WarpRow<TX, VPL>::read(at, v, lane, x[v]);
         if (REPLAY) {
-          const float s = a.q.scale[row * a.q.ld_scale + (col0 + (v * 32 + lane) * 8) / Q8_GROUP];
+          const float2 s = both(a.q.scale[row * a.q.ld_scale + (col0 + (v * 32 + lane) * 8) / Q8_GROUP]);
           #pragma unroll
-          for (int j = 0; j < 8; ++j) x[v][j] *= s;
+          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], s);
         }
       } else {
         #pragma unroll
-        for (int j = 0; j < 8; ++j) x[v][j] = 0.f;
+        for (int j = 0; j < 4; ++j) x[v][j] = both(0.f);
       }
     }
     float mean = 0.f, rstd;
@@ -563,58 +660,62 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
       rstd = a.rstd[row];
     } else {
       if (a.kind == KIND_LAYER) {
-        float s = 0.f;
+        float2 s = both(0.f), t = both(0.f);
         #pragma unroll
-        for (int v = 0; v < VPL; ++v)
-          #pragma unroll
-          for (int j = 0; j < 8; ++j) s += x[v][j];
-        mean = group_sum2(s, 0.f, wpr, w, group, red, turn, WARPS).x * inv_h;
+        for (int v = 0; v < VPL; ++v) { s = add2(s, add2(x[v][0], x[v][1])); t = add2(t, add2(x[v][2], x[v][3])); }
+        s = add2(s, t);
+        mean = group_sum(s.x + s.y, wpr, w, group, red, turn, WARPS) * inv_h;
         turn ^= 1;
       }
-      float s2 = 0.f;
+      const float2 minus = both(-mean);
+      float2 s2 = both(0.f);
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        const int left = cols - (v * 32 + lane) * 8;
-        if (left >= 8) {
-          #pragma unroll
-          for (int j = 0; j < 8; ++j) { const float d = x[v][j] - mean; s2 = fmaf(d, d, s2); }
-        } else {
-          #pragma unroll
-          for (int j = 0; j < 8; ++j) if (j < left) { const float d = x[v][j] - mean; s2 = fmaf(d, d, s2); }
+        if ((v * 32 + lane) * 8 >= cols) continue;
+        float2 s = both(0.f), t = both(0.f);
+        #pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const float2 d = add2(x[v][j], minus), e = add2(x[v][j + 1], minus);
+          s = fma2(d, d, s);
+          t = fma2(e, e, t);
         }
+        s2 = add2(s2, add2(s, t));
       }
-      rstd = 1.f / sqrtf(group_sum2(s2, 0.f, wpr, w, group, red, turn, WARPS).x * inv_h + a.eps);
+      rstd = 1.f / sqrtf(group_sum(s2.x + s2.y, wpr, w, group, red, turn, WARPS) * inv_h + a.eps);
       turn ^= 1;
       if (w == 0 && lane == 0) {
         if (a.mean != nullptr && a.kind == KIND_LAYER) a.mean[row] = mean;
         if (a.rstd != nullptr) a.rstd[row] = rstd;
       }
     }
+    const float2 minus = both(-mean), r2 = both(rstd);
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       const int col = col0 + (v * 32 + lane) * 8;
-      const int n = min(8, a.H - col);
-      if (!REPLAY && a.q.p != nullptr) {
-        int q[8]; float scale; bool bad;
-        quantise8(x[v], 16, q, scale, bad);
-        if (n > 0) {
-          store8<true>(a.q.p + row * a.q.ld + col, n, q);
-          if (col % Q8_GROUP == 0) {
+      if (!REPLAY && a.q.p != nullptr) {               // whole warps: the groups' threads agree by shuffles
+        float scale; bool bad;
+        const uint2 q = quantise8(x[v], scale, bad);
+        if (col < a.H) {
+          *reinterpret_cast<uint2*>(a.q.p + row * a.q.ld + col) = q;
+          if ((lane & 15) == 0) {
             a.q.scale[row * a.q.ld_scale + col / Q8_GROUP] = scale;
             if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
           }
         }
       }
-      if (n > 0) {
-        float g[8], b[8];
-        #pragma unroll
-        for (int j = 0; j < 8; ++j) { g[j] = 1.f; b[j] = 0.f; }
-        if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, n, g);
-        if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, a.w_vec, col, n, b);
-        #pragma unroll
-        for (int j = 0; j < 8; ++j) x[v][j] = fmaf((x[v][j] - mean) * rstd, g[j], b[j]);
-        store8<true>(a.y, row, col, n, x[v]);
+      if (col >= a.H) continue;
+      #pragma unroll
+      for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
+      float2 g[4], b[4];
+      if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, col, g);
+      if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, col, b);
+      #pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (a.gamma != nullptr && a.beta != nullptr) x[v][j] = fma2(x[v][j], g[j], b[j]);
+        else if (a.gamma != nullptr) x[v][j] = mul2(x[v][j], g[j]);
+        else if (a.beta != nullptr) x[v][j] = add2(x[v][j], b[j]);
       }
+      store8(a.y, row, col, x[v]);
     }
   }
 }
@@ -656,13 +757,13 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
       const uint32_t dst = smem_addr(mine + stage * stage_bytes);
       WarpRow<TX, VPL>::copy(dst, xp + row * ldx + col0, cols, lane);
       WarpRow<TDY, VPL>::copy(dst + DY_AT, dyp + row * a.dy.ld + col0, cols, lane);
-      if (lane == 0) copy_async<4>(dst + ST_AT, a.rstd + row, 4);
-      if (lane == 1 && layer) copy_async<4>(dst + ST_AT + 4, a.mean + row, 4);
+      if (lane == 0) copy_async<4>(dst + ST_AT, a.rstd + row);
+      if (lane == 1 && layer) copy_async<4>(dst + ST_AT + 4, a.mean + row);
       if (FROM_Q8) {
         #pragma unroll
         for (int v = 0; v < VPL; ++v) {
           const int col = (v * 32 + lane) * 8;
-          if (col < cols) copy_async<4>(dst + SC_AT + (v * 32 + lane) * 4, a.q.scale + row * a.q.ld_scale + (col0 + col) / Q8_GROUP, 4);
+          if (col < cols) copy_async<4>(dst + SC_AT + (v * 32 + lane) * 4, a.q.scale + row * a.q.ld_scale + (col0 + col) / Q8_GROUP);
         }
       }
     }
@@ -670,17 +771,17 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   };
   #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(row0 + s * step, s);
-  float gam[HOLD ? VPL : 1][8], dg[VPL][8], db[VPL][8];
-  auto weights = [&](int v, float (&g)[8]) {
+  float2 gam[HOLD ? VPL : 1][4], dg[VPL][4], db[VPL][4];
+  auto weights = [&](int v, float2 (&g)[4]) {
     const int col = col0 + (v * 32 + lane) * 8;
     #pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = 1.f;
-    if (a.gamma != nullptr && col < a.H) load_weight8(a.gamma, a.w_dtype, a.w_vec, col, min(8, a.H - col), g);
+    for (int j = 0; j < 4; ++j) g[j] = both(1.f);
+    if (a.gamma != nullptr && col < a.H) load_weight8(a.gamma, a.w_dtype, col, g);
   };
   #pragma unroll
   for (int v = 0; v < VPL; ++v) {
     #pragma unroll
-    for (int j = 0; j < 8; ++j) { dg[v][j] = 0.f; db[v][j] = 0.f; }
+    for (int j = 0; j < 4; ++j) { dg[v][j] = both(0.f); db[v][j] = both(0.f); }
     if (HOLD) weights(v, gam[v]);
   }
   int stage = 0, turn = 0;
@@ -692,51 +793,49 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     stage = stage + 1 == S ? 0 : stage + 1;
     const float rstd = *reinterpret_cast<const float*>(at + ST_AT);
     const float mean = layer ? *reinterpret_cast<const float*>(at + ST_AT + 4) : 0.f;
-    float xh[HOLD ? VPL : 1][8], g[HOLD ? VPL : 1][8];
-    // vector v of the row: xh, dy and, in place of dy, g = dy gamma
-    auto take = [&](int v, float (&x)[8], float (&d)[8]) {
+    const float2 minus = both(-mean), r2 = both(rstd);
+    float2 xh[HOLD ? VPL : 1][4], g[HOLD ? VPL : 1][4];
+    // vector v of the row: xh and dy
+    auto take = [&](int v, float2 (&x)[4], float2 (&d)[4]) {
       WarpRow<TX, VPL>::read(at, v, lane, x);
       WarpRow<TDY, VPL>::read(at + DY_AT, v, lane, d);
-      float s = 1.f;
-      if (FROM_Q8) s = *reinterpret_cast<const float*>(at + SC_AT + (v * 32 + lane) * 4);
+      const float2 s = both(FROM_Q8 ? *reinterpret_cast<const float*>(at + SC_AT + (v * 32 + lane) * 4) : 1.f);
       #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = ((FROM_Q8 ? x[j] * s : x[j]) - mean) * rstd;
+      for (int j = 0; j < 4; ++j) x[j] = mul2(add2(FROM_Q8 ? mul2(x[j], s) : x[j], minus), r2);
     };
-    float s1 = 0.f, s2 = 0.f;
+    float2 s1 = both(0.f), s2 = both(0.f);
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       if ((v * 32 + lane) * 8 >= cols) continue;
       const int k = HOLD ? v : 0;
       take(v, xh[k], g[k]);
       if (!HOLD) weights(v, gam[0]);
-      // (columns past H of the last vector are zero in dy: they add nothing)
       #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dg[v][j] = fmaf(g[k][j], xh[k][j], dg[v][j]);
-        db[v][j] += g[k][j];
-        g[k][j] *= gam[k][j];
-        s1 += g[k][j];
-        s2 = fmaf(g[k][j], xh[k][j], s2);
+      for (int j = 0; j < 4; ++j) {
+        dg[v][j] = fma2(g[k][j], xh[k][j], dg[v][j]);
+        db[v][j] = add2(db[v][j], g[k][j]);
+        g[k][j] = mul2(g[k][j], gam[k][j]);          // dy becomes g = dy gamma
+        s1 = add2(s1, g[k][j]);
+        s2 = fma2(g[k][j], xh[k][j], s2);
       }
     }
-    const float2 sums = group_sum2(s1, s2, wpr, w, group, red, turn, warps);
+    const float2 sums = group_sum2(s1.x + s1.y, s2.x + s2.y, wpr, w, group, red, turn, warps);
     turn ^= 1;
-    const float c1 = layer ? sums.x * inv_h : 0.f, c2 = sums.y * inv_h;
+    const float2 c1 = both(layer ? -sums.x * inv_h : 0.f), c2 = both(-sums.y * inv_h);
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
       const int col = col0 + (v * 32 + lane) * 8;
-      const int n = min(8, a.H - col);
-      if (n <= 0) continue;
+      if (col >= a.H) continue;
       const int k = HOLD ? v : 0;
       if (!HOLD) {
         take(v, xh[0], g[0]);
         weights(v, gam[0]);
         #pragma unroll
-        for (int j = 0; j < 8; ++j) g[0][j] *= gam[0][j];
+        for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], gam[0][j]);
       }
       #pragma unroll
-      for (int j = 0; j < 8; ++j) g[k][j] = rstd * (g[k][j] - c1 - xh[k][j] * c2);
-      store8<true>(a.dx, row, col, n, g[k]);
+      for (int j = 0; j < 4; ++j) g[k][j] = mul2(r2, fma2(xh[k][j], c2, add2(g[k][j], c1)));
+      store8(a.dx, row, col, g[k]);
     }
   }
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
@@ -747,22 +846,32 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   for (int k = 0; k < groups; ++k) {
     if (k == group) {
       #pragma unroll
-      for (int v = 0; v < VPL; ++v)
+      for (int v = 0; v < VPL; ++v) {
+        const int col = col0 + (v * 32 + lane) * 8;
+        if (col >= a.H) continue;
         #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int col = col0 + (v * 32 + lane) * 8 + j;
-          if (col >= a.H) continue;
-          float g = dg[v][j], b = db[v][j];
-          if (k > 0) { g += acc[col]; b += acc[a.H + col]; }
-          if (k + 1 < groups) { acc[col] = g; acc[a.H + col] = b; continue; }
+        for (int j = 0; j < 4; ++j) {
+          float2* pg = reinterpret_cast<float2*>(acc + col + 2 * j);
+          float2* pb = reinterpret_cast<float2*>(acc + a.H + col + 2 * j);
+          if (k > 0) { dg[v][j] = add2(dg[v][j], *pg); db[v][j] = add2(db[v][j], *pb); }
+          if (k + 1 < groups) { *pg = dg[v][j]; *pb = db[v][j]; continue; }
           if (gridDim.x > 1) {
-            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H;
-            out[col] = g; out[a.H + col] = b;
+            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H + col + 2 * j;
+            *reinterpret_cast<float2*>(out) = dg[v][j];
+            *reinterpret_cast<float2*>(out + a.H) = db[v][j];
           } else {
-            if (a.dgamma != nullptr) a.dgamma[col] = a.accumulate ? a.dgamma[col] + g : g;
-            if (a.dbeta != nullptr) a.dbeta[col] = a.accumulate ? a.dbeta[col] + b : b;
+            const int c = col + 2 * j;
+            if (a.dgamma != nullptr) {
+              a.dgamma[c] = a.accumulate ? a.dgamma[c] + dg[v][j].x : dg[v][j].x;
+              a.dgamma[c + 1] = a.accumulate ? a.dgamma[c + 1] + dg[v][j].y : dg[v][j].y;
+            }
+            if (a.dbeta != nullptr) {
+              a.dbeta[c] = a.accumulate ? a.dbeta[c] + db[v][j].x : db[v][j].x;
+              a.dbeta[c + 1] = a.accumulate ? a.dbeta[c + 1] + db[v][j].y : db[v][j].y;
+            }
           }
         }
+      }
     }
     __syncthreads();
   }
@@ -781,8 +890,9 @@ static RowPlan row_plan(int32_t H) {
   p.threads = tpr > NORM_THREADS ? tpr : NORM_THREADS;
   return p;
 }
-// Rows through shared memory: columns of more than one 16-thread group, rows on 16-byte boundaries.
-static bool ring_ok(int32_t H, bool vec) { return vec && H > Q8_GROUP; }
+// Rows through shared memory: whole vectors of 8 columns, more of them than one 16-thread group has, rows
+// (and weights) on 16-byte boundaries.
+static bool ring_ok(int32_t H, bool vec, bool w_vec) { return vec && w_vec && H > Q8_GROUP && H % 8 == 0; }
 struct RingPlan { int wpr, vpl, threads, rows_per_block; };
 static RingPlan fwd_ring_plan(int32_t H) {
   const int nvec = ceil_div(H, 8);
@@ -930,7 +1040,7 @@ static int launch_fwd(NormFwdArgs a, cudaStream_t st) {
   const RowPlan p = row_plan(a.H);
   a.tpr = p.tpr;
   const bool vec = (REPLAY || vec_ok(a.x)) && vec_ok(a.y) && (a.q.p == nullptr || vec_ok(a.q));
-  if (ring_ok(a.H, vec)) {
+  if (ring_ok(a.H, vec, a.w_vec != 0)) {
     if (REPLAY) return launch_fwd_ring<int8_t>(a, sms, st);
     return a.x.dtype == SAPO_DTYPE_F32 ? launch_fwd_ring<float>(a, sms, st) : launch_fwd_ring<__nv_bfloat16>(a, sms, st);
   }
@@ -1056,12 +1166,12 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
                 static_cast<float*>(workspace), dgamma, dbeta, accumulate};
   const RowPlan p = row_plan(H);
   const RingPlan rp = bwd_ring_plan(H);
-  const int resident = ring_ok(H, vec) ? bwd_ring(a, rp, 0, false, st) : 0;
+  const int resident = ring_ok(H, vec, aligned16(gamma)) ? bwd_ring(a, rp, 0, false, st) : 0;
   const bool ring = resident > 0;
   const int blocks = (int)bwd_blocks(T, ring ? rp.rows_per_block : p.threads / p.tpr, ring && resident < 2 ? resident : 2, sms);
   a.tpr = p.tpr;
   if (reduce && blocks > 1) {
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3u)) return SAPO_ERR_INVALID_ARG;
+    if (!workspace || !aligned16(workspace)) return SAPO_ERR_INVALID_ARG;
     if (workspace_bytes < (size_t)blocks * 2 * H * sizeof(float)) return SAPO_ERR_WORKSPACE_TOO_SMALL;
   }
   if (ring) rc = bwd_ring(a, rp, blocks, true, st);
