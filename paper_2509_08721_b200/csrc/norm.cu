@@ -9,6 +9,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace sapo {
@@ -441,12 +443,15 @@ norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float
 // columns per clock), so the arithmetic is done in pairs (fma.rn.f32x2 and its kin, each half rounded
 // like the scalar operation) and every vector is whole.
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+// (predicated, not branched around: a lane whose columns do not exist copies nothing)
 template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool exists) {
   if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
+                 ::"r"(dst), "l"(src), "r"((uint32_t)exists) : "memory");
   else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}"
+                 ::"r"(dst), "l"(src), "r"((uint32_t)exists), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -501,16 +506,6 @@ __device__ __forceinline__ void load_weight8(const void* w, int32_t dtype, int c
   if (dtype == SAPO_DTYPE_F32) load8(static_cast<const float*>(w) + col, x);
   else load8(static_cast<const __nv_bfloat16*>(w) + col, x);
 }
-__device__ __forceinline__ void store8(const Mat& m, int64_t row, int col, const float2 (&x)[4]) {
-  if (m.dtype == SAPO_DTYPE_F32) {
-    float* p = static_cast<float*>(m.p) + row * m.ld + col;
-    *reinterpret_cast<float4*>(p) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
-  } else {
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(m.p) + row * m.ld + col) =
-        make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
-  }
-}
 // Whole vectors of a group: as quantise8, the rounding to an integer by adding 1.5 2^23 (round to
 // nearest even, the integer in the last bits).  Scalar operations: the product has to be rounded before
 // the sum, and a pair of them is compiled to one fma.
@@ -543,21 +538,19 @@ __device__ __forceinline__ uint2 quantise8(const float2 (&x)[4], float& scale, b
 template <class TX, int VPL>
 struct WarpRow {
   static constexpr int BYTES = VPL * 256 * (int)sizeof(TX);
-  // src: the warp's first column of the row; cols: how many of its columns exist (a multiple of 8)
+  // Where lane `lane` of the warp copies from in the warp's part of a row, and to.
+  static constexpr int LANE = sizeof(TX) == 4 ? 4 : 8, PER_V = sizeof(TX) == 4 ? 2 : 1;
+  __device__ static __forceinline__ int lane_dst(int lane) {
+    return sizeof(TX) == 4 ? (lane ^ ((lane >> 3) & 1)) * 16 : lane * 8 * (int)sizeof(TX);
+  }
+  // dst, src: with the lane's offsets; cols: how many of the warp's columns exist (a multiple of 8)
   __device__ static __forceinline__ void copy(uint32_t dst, const TX* src, int cols, int lane) {
-    if constexpr (sizeof(TX) == 4) {
-      // neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
-      // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
-      const int j = lane ^ ((lane >> 3) & 1);
-      #pragma unroll
-      for (int v = 0; v < 2 * VPL; ++v)
-        if (v * 128 + lane * 4 < cols) copy_async<16>(dst + v * 512 + j * 16, src + v * 128 + lane * 4);
-    } else {
-      constexpr int B = 8 * (int)sizeof(TX);
-      #pragma unroll
-      for (int v = 0; v < VPL; ++v)
-        if (v * 256 + lane * 8 < cols) copy_async<B>(dst + (v * 32 + lane) * B, src + v * 256 + lane * 8);
-    }
+    // fp32: neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
+    // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
+    constexpr int B = LANE * (int)sizeof(TX);
+    #pragma unroll
+    for (int v = 0; v < PER_V * VPL; ++v)
+      copy_async<B>(dst + v * 32 * B, src + v * 32 * LANE, v * 32 * LANE + lane * LANE < cols);
   }
   // the lane's vector v
   __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float2 (&x)[4]) {
@@ -608,50 +601,73 @@ template <class TX, int VPL> struct FwdRing {
   static constexpr int SMEM = STAGES * (NORM_THREADS / 32) * WarpRow<TX, VPL>::BYTES;
 };
 
+// Zeros where the warp's columns do not exist: nothing is ever copied there, and zeros add nothing to sums.
+__device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stages, int stage_bytes, int lane) {
+  for (int s = 0; s < stages; ++s)
+    for (int i = lane * 16; i < bytes; i += 512) *reinterpret_cast<uint4*>(mine + s * stage_bytes + i) = make_uint4(0u, 0u, 0u, 0u);
+  __syncwarp();
+}
+// 8 columns to p (fp32 or bf16 as YF says)
+template <bool YF>
+__device__ __forceinline__ void put8(void* p, int at, const float2 (&x)[4]) {
+  if (YF) {
+    float* f = static_cast<float*>(p) + at;
+    *reinterpret_cast<float4*>(f) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+    *reinterpret_cast<float4*>(f + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at) =
+        make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
+  }
+}
+
 // TX int8_t: replay from a checkpoint (a.q), statistics given.
 template <class TX, int VPL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
   constexpr bool REPLAY = sizeof(TX) == 1;
   constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
+  using Row = WarpRow<TX, VPL>;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float2 red[2 * WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = warp / wpr, w = warp - group * wpr;
   const int64_t step = (int64_t)gridDim.x * (WARPS / wpr);
   const int64_t row0 = (int64_t)blockIdx.x * (WARPS / wpr) + group;
-  const int col0 = w * VPL * 256;                       // the warp's first column
-  const int cols = a.H - col0;
-  const TX* src = REPLAY ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p);
+  const int col0 = w * VPL * 256 + lane * 8;            // the lane's first column, and
+  const int left = a.H - col0;                          // what is left of the row there: vector v exists if 256 v < left
+  const int cols = a.H - w * VPL * 256;
   const int64_t ld = REPLAY ? a.q.ld : a.x.ld;
-  uint8_t* mine = ring + warp * WarpRow<TX, VPL>::BYTES;
-  constexpr int STAGE_BYTES = WARPS * WarpRow<TX, VPL>::BYTES;
+  const TX* src = (REPLAY ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) +
+                  row0 * ld + w * VPL * 256 + lane * Row::LANE;
+  constexpr int STAGE_BYTES = WARPS * Row::BYTES;
+  uint8_t* mine = ring + warp * Row::BYTES;
+  if (cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
+  const uint32_t dst = smem_addr(mine) + Row::lane_dst(lane);
   const float inv_h = 1.f / (float)a.H;
-  auto fetch = [&](int64_t row, int stage) {
-    if (row < a.T) WarpRow<TX, VPL>::copy(smem_addr(mine + stage * STAGE_BYTES), src + row * ld + col0, cols, lane);
+  const int ysz = a.y.dtype == SAPO_DTYPE_F32 ? 4 : 2;
+  int64_t ahead = row0;                                 // the next row to fetch, `src` its address
+  auto fetch = [&](int stage) {
+    if (ahead < a.T) Row::copy(dst + stage * STAGE_BYTES, src, cols, lane);
     copy_commit();
+    ahead += step;
+    src += step * ld;
   };
   #pragma unroll
-  for (int s = 0; s < S - 1; ++s) fetch(row0 + s * step, s);
+  for (int s = 0; s < S - 1; ++s) fetch(s);
   int stage = 0, turn = 0;
   for (int64_t row = row0; row < a.T; row += step) {
     copy_wait<S - 2>();
     __syncwarp();
-    fetch(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+    fetch(stage == 0 ? S - 1 : stage - 1);
     const uint8_t* at = mine + stage * STAGE_BYTES;
     stage = stage + 1 == S ? 0 : stage + 1;
     float2 x[VPL][4];
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      if ((v * 32 + lane) * 8 < cols) {
-        WarpRow<TX, VPL>::read(at, v, lane, x[v]);
-        if (REPLAY) {
-          const float2 s = both(a.q.scale[row * a.q.ld_scale + (col0 + (v * 32 + lane) * 8) / Q8_GROUP]);
-          #pragma unroll
-          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], s);
-        }
-      } else {
+      Row::read(at, v, lane, x[v]);
+      if (REPLAY) {
+        const float2 s = both(256 * v < left ? a.q.scale[row * a.q.ld_scale + (col0 + 256 * v) / Q8_GROUP] : 0.f);
         #pragma unroll
-        for (int j = 0; j < 4; ++j) x[v][j] = both(0.f);
+        for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], s);
       }
     }
     float mean = 0.f, rstd;
@@ -667,55 +683,69 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
         mean = group_sum(s.x + s.y, wpr, w, group, red, turn, WARPS) * inv_h;
         turn ^= 1;
       }
-      const float2 minus = both(-mean);
-      float2 s2 = both(0.f);
+      float2 s2 = both(0.f), t2 = both(0.f);
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        if ((v * 32 + lane) * 8 >= cols) continue;
-        float2 s = both(0.f), t = both(0.f);
+        const float2 minus = both(256 * v < left ? -mean : 0.f);
         #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           const float2 d = add2(x[v][j], minus), e = add2(x[v][j + 1], minus);
-          s = fma2(d, d, s);
-          t = fma2(e, e, t);
+          s2 = fma2(d, d, s2);
+          t2 = fma2(e, e, t2);
         }
-        s2 = add2(s2, add2(s, t));
       }
+      s2 = add2(s2, t2);
       rstd = 1.f / sqrtf(group_sum(s2.x + s2.y, wpr, w, group, red, turn, WARPS) * inv_h + a.eps);
       turn ^= 1;
       if (w == 0 && lane == 0) {
         if (a.mean != nullptr && a.kind == KIND_LAYER) a.mean[row] = mean;
         if (a.rstd != nullptr) a.rstd[row] = rstd;
       }
-    }
-    const float2 minus = both(-mean), r2 = both(rstd);
-    #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int col = col0 + (v * 32 + lane) * 8;
-      if (!REPLAY && a.q.p != nullptr) {               // whole warps: the groups' threads agree by shuffles
-        float scale; bool bad;
-        const uint2 q = quantise8(x[v], scale, bad);
-        if (col < a.H) {
-          *reinterpret_cast<uint2*>(a.q.p + row * a.q.ld + col) = q;
-          if ((lane & 15) == 0) {
-            a.q.scale[row * a.q.ld_scale + col / Q8_GROUP] = scale;
+      if (a.q.p != nullptr) {
+        int8_t* q_row = a.q.p + row * a.q.ld + col0;
+        float* scale_row = a.q.scale + row * a.q.ld_scale + col0 / Q8_GROUP;
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v) {                // whole warps: a group's threads agree by shuffles
+          float scale; bool bad;
+          const uint2 q = quantise8(x[v], scale, bad);
+          if (256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = q;
+          if (256 * v < left && (lane & 15) == 0) {
+            scale_row[2 * v] = scale;
             if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
           }
         }
       }
-      if (col >= a.H) continue;
+    }
+    const float2 minus = both(-mean), r2 = both(rstd);
+    void* y_row = static_cast<char*>(a.y.p) + (row * a.y.ld + col0) * ysz;
+    auto finish = [&](auto wf, auto yf) {
+      constexpr bool WF = decltype(wf)::value, YF = decltype(yf)::value;
+      using TW = typename std::conditional<WF, float, __nv_bfloat16>::type;
+      const TW* gp = static_cast<const TW*>(a.gamma) + col0;
+      const TW* bp = static_cast<const TW*>(a.beta) + col0;
       #pragma unroll
-      for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
-      float2 g[4], b[4];
-      if (a.gamma != nullptr) load_weight8(a.gamma, a.w_dtype, col, g);
-      if (a.beta != nullptr) load_weight8(a.beta, a.w_dtype, col, b);
-      #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (a.gamma != nullptr && a.beta != nullptr) x[v][j] = fma2(x[v][j], g[j], b[j]);
-        else if (a.gamma != nullptr) x[v][j] = mul2(x[v][j], g[j]);
-        else if (a.beta != nullptr) x[v][j] = add2(x[v][j], b[j]);
+      for (int v = 0; v < VPL; ++v) {
+        if (256 * v >= left) break;
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
+        float2 g[4];
+        if (a.gamma != nullptr) {
+          load8(gp + 256 * v, g);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], g[j]);
+        }
+        if (a.beta != nullptr) {
+          load8(bp + 256 * v, g);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) x[v][j] = add2(x[v][j], g[j]);
+        }
+        put8<YF>(y_row, 256 * v, x[v]);
       }
-      store8(a.y, row, col, x[v]);
+    };
+    if (a.w_dtype == SAPO_DTYPE_F32) {
+      if (a.y.dtype == SAPO_DTYPE_F32) finish(std::true_type{}, std::true_type{}); else finish(std::true_type{}, std::false_type{});
+    } else {
+      if (a.y.dtype == SAPO_DTYPE_F32) finish(std::false_type{}, std::true_type{}); else finish(std::false_type{}, std::false_type{});
     }
   }
 }
@@ -739,44 +769,54 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   constexpr bool HOLD = Ring::HOLD;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float2 red[2 * (MAX_THREADS / 32)];
+  using RowX = WarpRow<TX, VPL>;
+  using RowD = WarpRow<TDY, VPL>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / wpr;
   const int group = warp / wpr, w = warp - group * wpr;
   const int64_t step = (int64_t)gridDim.x * groups;
   const int64_t row0 = (int64_t)blockIdx.x * groups + group;
-  const int col0 = w * VPL * 256, cols = a.H - col0;
+  const int warp_col = w * VPL * 256, cols = a.H - warp_col;
+  const int col0 = warp_col + lane * 8, left = a.H - col0;          // vector v of the lane exists if 256 v < left
   uint8_t* mine = ring + warp * Ring::WARP_BYTES;
   const int stage_bytes = warps * Ring::WARP_BYTES;
-  const TX* xp = FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p);
+  if (cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
   const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
-  const TDY* dyp = static_cast<const TDY*>(a.dy.p);
-  constexpr int DY_AT = WarpRow<TX, VPL>::BYTES, ST_AT = DY_AT + WarpRow<TDY, VPL>::BYTES, SC_AT = ST_AT + 64;
+  const TX* xp = (FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) + row0 * ldx + warp_col + lane * RowX::LANE;
+  const TDY* dyp = static_cast<const TDY*>(a.dy.p) + row0 * a.dy.ld + warp_col + lane * RowD::LANE;
+  const float* sp = FROM_Q8 ? a.q.scale + row0 * a.q.ld_scale + col0 / Q8_GROUP : nullptr;
+  constexpr int DY_AT = RowX::BYTES, ST_AT = DY_AT + RowD::BYTES, SC_AT = ST_AT + 64;
   const float inv_h = 1.f / (float)a.H;
   const bool layer = a.kind == KIND_LAYER;
-  auto fetch = [&](int64_t row, int stage) {
-    if (row < a.T) {
-      const uint32_t dst = smem_addr(mine + stage * stage_bytes);
-      WarpRow<TX, VPL>::copy(dst, xp + row * ldx + col0, cols, lane);
-      WarpRow<TDY, VPL>::copy(dst + DY_AT, dyp + row * a.dy.ld + col0, cols, lane);
-      if (lane == 0) copy_async<4>(dst + ST_AT, a.rstd + row);
-      if (lane == 1 && layer) copy_async<4>(dst + ST_AT + 4, a.mean + row);
+  const uint32_t base = smem_addr(mine);
+  const uint32_t dst_x = base + RowX::lane_dst(lane), dst_d = base + DY_AT + RowD::lane_dst(lane);
+  // lane 0 copies rstd, lane 1 the mean
+  const float* stat = lane == 0 ? a.rstd : a.mean;
+  const bool copies_stat = lane == 0 || (lane == 1 && layer);
+  int64_t ahead = row0;
+  auto fetch = [&](int stage) {
+    if (ahead < a.T) {
+      const uint32_t off = stage * stage_bytes;
+      RowX::copy(dst_x + off, xp, cols, lane);
+      RowD::copy(dst_d + off, dyp, cols, lane);
+      copy_async<4>(base + off + ST_AT + lane * 4, stat + ahead, copies_stat);
       if (FROM_Q8) {
         #pragma unroll
-        for (int v = 0; v < VPL; ++v) {
-          const int col = (v * 32 + lane) * 8;
-          if (col < cols) copy_async<4>(dst + SC_AT + (v * 32 + lane) * 4, a.q.scale + row * a.q.ld_scale + (col0 + col) / Q8_GROUP);
-        }
+        for (int v = 0; v < VPL; ++v) copy_async<4>(base + off + SC_AT + (v * 32 + lane) * 4, sp + 2 * v, 256 * v < left);
       }
     }
     copy_commit();
+    ahead += step;
+    xp += step * ldx;
+    dyp += step * a.dy.ld;
+    if (FROM_Q8) sp += step * a.q.ld_scale;
   };
   #pragma unroll
-  for (int s = 0; s < S - 1; ++s) fetch(row0 + s * step, s);
+  for (int s = 0; s < S - 1; ++s) fetch(s);
   float2 gam[HOLD ? VPL : 1][4], dg[VPL][4], db[VPL][4];
   auto weights = [&](int v, float2 (&g)[4]) {
-    const int col = col0 + (v * 32 + lane) * 8;
     #pragma unroll
     for (int j = 0; j < 4; ++j) g[j] = both(1.f);
-    if (a.gamma != nullptr && col < a.H) load_weight8(a.gamma, a.w_dtype, col, g);
+    if (a.gamma != nullptr && 256 * v < left) load_weight8(a.gamma, a.w_dtype, col0 + 256 * v, g);
   };
   #pragma unroll
   for (int v = 0; v < VPL; ++v) {
@@ -784,11 +824,12 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     for (int j = 0; j < 4; ++j) { dg[v][j] = both(0.f); db[v][j] = both(0.f); }
     if (HOLD) weights(v, gam[v]);
   }
+  const int dxsz = a.dx.dtype == SAPO_DTYPE_F32 ? 4 : 2;
   int stage = 0, turn = 0;
   for (int64_t row = row0; row < a.T; row += step) {
     copy_wait<S - 2>();
     __syncwarp();
-    fetch(row + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+    fetch(stage == 0 ? S - 1 : stage - 1);
     const uint8_t* at = mine + stage * stage_bytes;
     stage = stage + 1 == S ? 0 : stage + 1;
     const float rstd = *reinterpret_cast<const float*>(at + ST_AT);
@@ -797,16 +838,16 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     float2 xh[HOLD ? VPL : 1][4], g[HOLD ? VPL : 1][4];
     // vector v of the row: xh and dy
     auto take = [&](int v, float2 (&x)[4], float2 (&d)[4]) {
-      WarpRow<TX, VPL>::read(at, v, lane, x);
-      WarpRow<TDY, VPL>::read(at + DY_AT, v, lane, d);
+      RowX::read(at, v, lane, x);
+      RowD::read(at + DY_AT, v, lane, d);
       const float2 s = both(FROM_Q8 ? *reinterpret_cast<const float*>(at + SC_AT + (v * 32 + lane) * 4) : 1.f);
       #pragma unroll
       for (int j = 0; j < 4; ++j) x[j] = mul2(add2(FROM_Q8 ? mul2(x[j], s) : x[j], minus), r2);
     };
+    // (where a vector does not exist dy is zero: it adds nothing to the sums)
     float2 s1 = both(0.f), s2 = both(0.f);
     #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-      if ((v * 32 + lane) * 8 >= cols) continue;
       const int k = HOLD ? v : 0;
       take(v, xh[k], g[k]);
       if (!HOLD) weights(v, gam[0]);
@@ -822,21 +863,23 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     const float2 sums = group_sum2(s1.x + s1.y, s2.x + s2.y, wpr, w, group, red, turn, warps);
     turn ^= 1;
     const float2 c1 = both(layer ? -sums.x * inv_h : 0.f), c2 = both(-sums.y * inv_h);
-    #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-      const int col = col0 + (v * 32 + lane) * 8;
-      if (col >= a.H) continue;
-      const int k = HOLD ? v : 0;
-      if (!HOLD) {
-        take(v, xh[0], g[0]);
-        weights(v, gam[0]);
-        #pragma unroll
-        for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], gam[0][j]);
-      }
+    void* dx_row = static_cast<char*>(a.dx.p) + (row * a.dx.ld + col0) * dxsz;
+    auto finish = [&](auto f) {
       #pragma unroll
-      for (int j = 0; j < 4; ++j) g[k][j] = mul2(r2, fma2(xh[k][j], c2, add2(g[k][j], c1)));
-      store8(a.dx, row, col, g[k]);
-    }
+      for (int v = 0; v < VPL; ++v) {
+        const int k = HOLD ? v : 0;
+        if (!HOLD) {
+          take(v, xh[0], g[0]);
+          weights(v, gam[0]);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], gam[0][j]);
+        }
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) g[k][j] = mul2(r2, fma2(xh[k][j], c2, add2(g[k][j], c1)));
+        if (256 * v < left) put8<decltype(f)::value>(dx_row, 256 * v, g[k]);
+      }
+    };
+    if (a.dx.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
   }
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the groups' sums one after the other, through the ring (no copy is in flight any more)
@@ -847,7 +890,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     if (k == group) {
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        const int col = col0 + (v * 32 + lane) * 8;
+        const int col = col0 + 256 * v;
         if (col >= a.H) continue;
         #pragma unroll
         for (int j = 0; j < 4; ++j) {
