@@ -565,20 +565,27 @@ struct WarpRow {
   }
 };
 
-// Sums of one or two values over a group of warps; red: [2][warps of the block], `turn` alternates.
-__device__ __forceinline__ float group_sum(float a, int wpr, int w, int group, float2* red, int turn, int n_warps) {
+// Sums of one or two values over a group of warps.  Each group has SLOTS places for its warps' sums, zeros in
+// those that have no warp, twice: `turn` alternates, so that one barrier a sum is enough.
+template <int SLOTS>
+__device__ __forceinline__ float group_sum(float a, int wpr, int w, int group, float* red, int turn) {
   #pragma unroll
   for (int d = 16; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
   if (wpr == 1) return a;
-  float2* r = red + turn * n_warps + group * wpr;
-  if ((threadIdx.x & 31) == 0) r[w].x = a;
+  float* r = red + (2 * group + turn) * SLOTS;
+  if ((threadIdx.x & 31) == 0) r[w] = a;
   group_barrier(1 + group, wpr * 32);
   float t = 0.f;
-  for (int i = 0; i < wpr; ++i) t += r[i].x;
+  #pragma unroll
+  for (int i = 0; i < SLOTS; i += 4) {
+    const float4 o = *reinterpret_cast<const float4*>(r + i);
+    t += (o.x + o.y) + (o.z + o.w);
+  }
   return t;
 }
 // (after the first exchange half of the lanes carry one value and half the other: 6 shuffles, not 10)
-__device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, int group, float2* red, int turn, int n_warps) {
+template <int SLOTS>
+__device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, int group, float2* red, int turn) {
   const bool upper = (threadIdx.x & 16) != 0;
   const float other = __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
   float x = (upper ? b : a) + other;
@@ -588,17 +595,22 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, i
     const float y = __shfl_xor_sync(0xffffffffu, x, 16);
     return upper ? make_float2(y, x) : make_float2(x, y);
   }
-  float2* r = red + turn * n_warps + group * wpr;
+  float2* r = red + (2 * group + turn) * SLOTS;
   if ((threadIdx.x & 15) == 0) reinterpret_cast<float*>(r + w)[upper] = x;
   group_barrier(1 + group, wpr * 32);
   float2 t = make_float2(0.f, 0.f);
-  for (int i = 0; i < wpr; ++i) { const float2 o = r[i]; t.x += o.x; t.y += o.y; }
+  #pragma unroll
+  for (int i = 0; i < SLOTS; i += 2) {
+    const float4 o = *reinterpret_cast<const float4*>(r + i);
+    t = add2(t, add2(make_float2(o.x, o.y), make_float2(o.z, o.w)));
+  }
   return t;
 }
 
 template <class TX, int VPL> struct FwdRing {
-  static constexpr int STAGES = 256 * VPL * 8 * (int)sizeof(TX) <= 16384 ? 4 : 3;
-  static constexpr int SMEM = STAGES * (NORM_THREADS / 32) * WarpRow<TX, VPL>::BYTES;
+  static constexpr int STAGE_BYTES = NORM_THREADS / 32 * WarpRow<TX, VPL>::BYTES;
+  static constexpr int STAGES = STAGE_BYTES <= 16384 ? 4 : (STAGE_BYTES <= 26624 ? 3 : 2);
+  static int smem(int H) { return STAGES * STAGE_BYTES + 2 * H * (int)sizeof(float); }   // and the weights
 };
 
 // Zeros where the warp's columns do not exist: nothing is ever copied there, and zeros add nothing to sums.
@@ -627,7 +639,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
   using Row = WarpRow<TX, VPL>;
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float2 red[2 * WARPS];
+  __shared__ __align__(16) float red[2 * WARPS * WARPS];   // [group][turn][slots]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = warp / wpr, w = warp - group * wpr;
   const int64_t step = (int64_t)gridDim.x * (WARPS / wpr);
@@ -640,6 +652,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
                   row0 * ld + w * VPL * 256 + lane * Row::LANE;
   constexpr int STAGE_BYTES = WARPS * Row::BYTES;
   uint8_t* mine = ring + warp * Row::BYTES;
+  for (int i = threadIdx.x; i < 2 * WARPS * WARPS; i += NORM_THREADS) red[i] = 0.f;
   if (cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
   const uint32_t dst = smem_addr(mine) + Row::lane_dst(lane);
   const float inv_h = 1.f / (float)a.H;
@@ -653,6 +666,25 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   };
   #pragma unroll
   for (int s = 0; s < S - 1; ++s) fetch(s);
+  // the weights in fp32, once per block: read from global memory for every row they miss L1 one time in five,
+  // and the wait for them is longer than the rest of the row's work.  In 16-byte pieces in WarpRow's order.
+  float* gs = reinterpret_cast<float*>(ring + S * STAGE_BYTES);
+  float* bs = gs + a.H;
+  for (int i = threadIdx.x * 8; i < a.H; i += NORM_THREADS * 8) {
+    float2 u[4];
+    const int f = (i >> 5) & 1, lo = i + 4 * f, hi = i + 4 - 4 * f;
+    if (a.gamma != nullptr) {
+      load_weight8(a.gamma, a.w_dtype, i, u);
+      *reinterpret_cast<float4*>(gs + lo) = make_float4(u[0].x, u[0].y, u[1].x, u[1].y);
+      *reinterpret_cast<float4*>(gs + hi) = make_float4(u[2].x, u[2].y, u[3].x, u[3].y);
+    }
+    if (a.beta != nullptr) {
+      load_weight8(a.beta, a.w_dtype, i, u);
+      *reinterpret_cast<float4*>(bs + lo) = make_float4(u[0].x, u[0].y, u[1].x, u[1].y);
+      *reinterpret_cast<float4*>(bs + hi) = make_float4(u[2].x, u[2].y, u[3].x, u[3].y);
+    }
+  }
+  __syncthreads();
   int stage = 0, turn = 0;
   for (int64_t row = row0; row < a.T; row += step) {
     copy_wait<S - 2>();
@@ -680,7 +712,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
         #pragma unroll
         for (int v = 0; v < VPL; ++v) { s = add2(s, add2(x[v][0], x[v][1])); t = add2(t, add2(x[v][2], x[v][3])); }
         s = add2(s, t);
-        mean = group_sum(s.x + s.y, wpr, w, group, red, turn, WARPS) * inv_h;
+        mean = group_sum<WARPS>(s.x + s.y, wpr, w, group, red, turn) * inv_h;
         turn ^= 1;
       }
       float2 s2 = both(0.f), t2 = both(0.f);
@@ -695,7 +727,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
         }
       }
       s2 = add2(s2, t2);
-      rstd = 1.f / sqrtf(group_sum(s2.x + s2.y, wpr, w, group, red, turn, WARPS) * inv_h + a.eps);
+      rstd = 1.f / sqrtf(group_sum<WARPS>(s2.x + s2.y, wpr, w, group, red, turn) * inv_h + a.eps);
       turn ^= 1;
       if (w == 0 && lane == 0) {
         if (a.mean != nullptr && a.kind == KIND_LAYER) a.mean[row] = mean;
@@ -718,35 +750,27 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
     }
     const float2 minus = both(-mean), r2 = both(rstd);
     void* y_row = static_cast<char*>(a.y.p) + (row * a.y.ld + col0) * ysz;
-    auto finish = [&](auto wf, auto yf) {
-      constexpr bool WF = decltype(wf)::value, YF = decltype(yf)::value;
-      using TW = typename std::conditional<WF, float, __nv_bfloat16>::type;
-      const TW* gp = static_cast<const TW*>(a.gamma) + col0;
-      const TW* bp = static_cast<const TW*>(a.beta) + col0;
+    auto finish = [&](auto f) {
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
         if (256 * v >= left) break;
         #pragma unroll
         for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
-        float2 g[4];
+        float2 u[4];
         if (a.gamma != nullptr) {
-          load8(gp + 256 * v, g);
+          WarpRow<float, VPL>::read(reinterpret_cast<const uint8_t*>(gs + w * VPL * 256), v, lane, u);
           #pragma unroll
-          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], g[j]);
+          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], u[j]);
         }
         if (a.beta != nullptr) {
-          load8(bp + 256 * v, g);
+          WarpRow<float, VPL>::read(reinterpret_cast<const uint8_t*>(bs + w * VPL * 256), v, lane, u);
           #pragma unroll
-          for (int j = 0; j < 4; ++j) x[v][j] = add2(x[v][j], g[j]);
+          for (int j = 0; j < 4; ++j) x[v][j] = add2(x[v][j], u[j]);
         }
-        put8<YF>(y_row, 256 * v, x[v]);
+        put8<decltype(f)::value>(y_row, 256 * v, x[v]);
       }
     };
-    if (a.w_dtype == SAPO_DTYPE_F32) {
-      if (a.y.dtype == SAPO_DTYPE_F32) finish(std::true_type{}, std::true_type{}); else finish(std::true_type{}, std::false_type{});
-    } else {
-      if (a.y.dtype == SAPO_DTYPE_F32) finish(std::false_type{}, std::true_type{}); else finish(std::false_type{}, std::false_type{});
-    }
+    if (a.y.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
   }
 }
 
@@ -768,7 +792,9 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   constexpr int S = Ring::STAGES;
   constexpr bool HOLD = Ring::HOLD;
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float2 red[2 * (MAX_THREADS / 32)];
+  // [group][turn][slots]: up to 8 groups of up to 4 warps, 2 of up to 8, or 1 of up to 16
+  constexpr int SLOTS = MAX_THREADS / 32;
+  __shared__ __align__(16) float2 red[2 * SLOTS * SLOTS];
   using RowX = WarpRow<TX, VPL>;
   using RowD = WarpRow<TDY, VPL>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / wpr;
@@ -779,6 +805,8 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   const int col0 = warp_col + lane * 8, left = a.H - col0;          // vector v of the lane exists if 256 v < left
   uint8_t* mine = ring + warp * Ring::WARP_BYTES;
   const int stage_bytes = warps * Ring::WARP_BYTES;
+  for (int i = threadIdx.x; i < 2 * SLOTS * SLOTS; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
+  __syncthreads();
   if (cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
   const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
   const TX* xp = (FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) + row0 * ldx + warp_col + lane * RowX::LANE;
@@ -860,7 +888,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
         s2 = fma2(g[k][j], xh[k][j], s2);
       }
     }
-    const float2 sums = group_sum2(s1.x + s1.y, s2.x + s2.y, wpr, w, group, red, turn, warps);
+    const float2 sums = group_sum2<SLOTS>(s1.x + s1.y, s2.x + s2.y, wpr, w, group, red, turn);
     turn ^= 1;
     const float2 c1 = both(layer ? -sums.x * inv_h : 0.f), c2 = both(-sums.y * inv_h);
     void* dx_row = static_cast<char*>(a.dx.p) + (row * a.dx.ld + col0) * dxsz;
@@ -997,7 +1025,7 @@ static int resident_blocks(Kernel kernel, int threads, size_t smem, int* cache) 
   if (dev < 0) return 0;
   if (cache[dev] == 0) {
     int n = 0;
-    if (smem > 48 * 1024 &&
+    if (smem > 40 * 1024 &&
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX) != cudaSuccess) return 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) return 0;
     cache[dev] = n;
@@ -1005,12 +1033,16 @@ static int resident_blocks(Kernel kernel, int threads, size_t smem, int* cache) 
   return cache[dev];
 }
 
+constexpr int RING_TOO_WIDE = 1;         // rows and weights do not fit: norm_fwd_kernel takes them
 template <class TX, int VPL>
 static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
-  static int cache[MAX_DEVICES] = {0};
+  // (by the width of the row in 256 columns, which the weights' share of shared memory follows)
+  static int cache[NORM_MAX_H / 256 + 1][MAX_DEVICES] = {{0}};
   auto kernel = norm_fwd_ring_kernel<TX, VPL>;
-  const size_t smem = FwdRing<TX, VPL>::SMEM;
-  const int per_sm = resident_blocks(kernel, p.threads, smem, cache);
+  const int steps = ceil_div(a.H, 256);
+  const size_t smem = FwdRing<TX, VPL>::smem(steps * 256);
+  if (smem > SMEM_MAX) return RING_TOO_WIDE;
+  const int per_sm = resident_blocks(kernel, p.threads, smem, cache[steps]);
   if (per_sm == 0) return SAPO_ERR_CUDA;
   int64_t blocks = ceil_div<int64_t>(a.T, p.rows_per_block);
   if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
@@ -1084,8 +1116,9 @@ static int launch_fwd(NormFwdArgs a, cudaStream_t st) {
   a.tpr = p.tpr;
   const bool vec = (REPLAY || vec_ok(a.x)) && vec_ok(a.y) && (a.q.p == nullptr || vec_ok(a.q));
   if (ring_ok(a.H, vec, a.w_vec != 0)) {
-    if (REPLAY) return launch_fwd_ring<int8_t>(a, sms, st);
-    return a.x.dtype == SAPO_DTYPE_F32 ? launch_fwd_ring<float>(a, sms, st) : launch_fwd_ring<__nv_bfloat16>(a, sms, st);
+    const int rc = REPLAY ? launch_fwd_ring<int8_t>(a, sms, st)
+                          : (a.x.dtype == SAPO_DTYPE_F32 ? launch_fwd_ring<float>(a, sms, st) : launch_fwd_ring<__nv_bfloat16>(a, sms, st));
+    if (rc != RING_TOO_WIDE) return rc;
   }
   switch (p.nv) {
     case 1: return launch_fwd_nv<1, REPLAY>(a, vec, p, sms, st);
