@@ -3,7 +3,7 @@
 //   R_s = sum over the tokens of s of (logp - ref_logp)   (divided by T_s with length_norm)
 //   pairs (i, j) of one question, i preferred to j (reward_i > reward_j);  h = beta (R_i - R_j)
 //   loss = 1/Q sum_q 1/n_q sum_pairs l(h)
-// A question's completions are neighbours in the packed batch, so a question is one block's work:
+// A question's completions are neighbours in the packed batch, so a question is one cluster's work:
 // the sums of its sequences, its pairs, and one factor per sequence written to all its tokens.
 // Reads 8 bytes and writes 4 per token.
 #include <math.h>
@@ -12,7 +12,10 @@
 
 namespace sapo {
 
-constexpr int PREF_THREADS = 256;
+constexpr int PREF_THREADS = 512;
+constexpr int PREF_WARPS = PREF_THREADS / 32;
+constexpr int PREF_MAX_CLUSTER = 16;
+constexpr int PREF_SEQS = 1024;          // completions of a question whose sums are kept in shared memory
 
 __device__ __forceinline__ int32_t clamp_to(int32_t x, int32_t hi, bool& bad) {
   const int32_t c = x < 0 ? 0 : (x > hi ? hi : x);
@@ -27,15 +30,24 @@ __device__ __forceinline__ void offset_range(const int32_t* offsets, int32_t i, 
   if (b < a) { b = a; bad = true; }
 }
 
-__device__ __forceinline__ double block_sum(double x, double* sh) {
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+// all threads of the cluster; orders their shared and global memory accesses
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// *p = x in the shared memory of the cluster's first block
+__device__ __forceinline__ void store_to_first(float* p, float x) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
+}
+
+template <class T>
+__device__ __forceinline__ T warp_sum(T x) {
   #pragma unroll
   for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double t = 0.0;
-  for (int i = 0; i < PREF_THREADS / 32; ++i) t += sh[i];
-  return t;
+  return x;
 }
 
 // value and derivative (by h) of one pair's loss
@@ -58,118 +70,222 @@ __device__ __forceinline__ void pair_loss(const PrefArgs& a, float h, float& l, 
   }
 }
 
+// log ratio of token t, NaN or infinite where the token is masked
+__device__ __forceinline__ float token_ratio(const PrefArgs& a, int32_t t) {
+  return a.ref_logp != nullptr ? a.logp[t] - a.ref_logp[t] : a.logp[t];
+}
+
+// A cluster of blocks per question.  The question's tokens are one range, cut into equal pieces for the
+// cluster's warps whatever its sequences' lengths are, so that few long sequences keep as many SMs
+// busy as many short ones:
+//   1. every warp sums the pieces of sequences in its range.  The piece with which the range begins goes
+//      to `head` of the first block; any other piece holds its sequence's first token, and goes to
+//      seq_logratio[s]
+//   2. the first block adds up each sequence's pieces (in order), then the pairs: a warp per completion,
+//      lanes over the others
+//   3. every warp writes the factors of its tokens
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
-  __shared__ double sh[PREF_THREADS / 32];
+  __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
+  __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS];
+  __shared__ double sums[3][PREF_WARPS];
+  __shared__ float scale_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t Tc = (int32_t)a.T;
-  for (int32_t q = blockIdx.x; q < a.Q; q += gridDim.x) {
-    bool bad_offset = false, bad_value = false, bad_reward = false;
+  const int rank = (int)cluster_rank(), size = (int)cluster_size();
+  const int gw = rank * PREF_WARPS + warp, n_warps = size * PREF_WARPS;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  bool bad_offset = false, bad_value = false, bad_reward = false;
+  {
+    // what no question covers: sequences before the first and after the last one, and their tokens
+    bool ignore = false;
+    const int32_t s_lo = clamp_to(a.group_offsets[0], a.S, ignore);
+    int32_t s_hi = clamp_to(a.group_offsets[a.Q], a.S, ignore);
+    if (s_hi < s_lo) s_hi = s_lo;
+    const int32_t t_lo = clamp_to(a.cu[s_lo], Tc, ignore);
+    int32_t t_hi = clamp_to(a.cu[s_hi], Tc, ignore);
+    if (t_hi < t_lo) t_hi = t_lo;
+    const int64_t first = (int64_t)blockIdx.x * PREF_THREADS + threadIdx.x, step = (int64_t)gridDim.x * PREF_THREADS;
+    for (int64_t i = first; i < (int64_t)t_lo + (Tc - t_hi); i += step) a.gscale[i < t_lo ? i : t_hi + (i - t_lo)] = 0.f;
+    for (int64_t i = first; i < (int64_t)s_lo + (a.S - s_hi); i += step) {
+      const int64_t s = i < s_lo ? i : s_hi + (i - s_lo);
+      a.seq_logratio[s] = 0.f;
+      a.seq_grad[s] = 0.f;
+    }
+  }
+  for (int32_t q = blockIdx.x / size; q < a.Q; q += gridDim.x / size) {
     int32_t s0, s1;
     offset_range(a.group_offsets, q, a.S, s0, s1, bad_offset);
-    // sums of the sequences
-    for (int32_t s = s0 + warp; s < s1; s += PREF_THREADS / 32) {
-      int32_t t0, t1;
-      offset_range(a.cu, s, Tc, t0, t1, bad_offset);
-      float sum = 0.f;
-      for (int32_t t = t0 + lane; t < t1; t += 32) {
-        const float d = a.ref_logp != nullptr ? a.logp[t] - a.ref_logp[t] : a.logp[t];
-        if (isfinite(d)) sum += d; else bad_value = true;
-      }
-      #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (lane == 0) a.seq_logratio[s] = a.length_norm && t1 > t0 ? sum / (float)(t1 - t0) : sum;
+    const int32_t ta = clamp_to(a.cu[s0], Tc, bad_offset);
+    int32_t tb = clamp_to(a.cu[s1], Tc, bad_offset);
+    if (tb < ta) tb = ta;
+    // tokens per warp: whole steps of 32
+    const int32_t piece = (int32_t)round_up<int64_t>(ceil_div<int64_t>((int64_t)tb - ta, n_warps), 32) + (tb == ta ? 32 : 0);
+    const int64_t begin64 = (int64_t)ta + (int64_t)gw * piece;
+    const int32_t begin = begin64 < tb ? (int32_t)begin64 : tb;
+    const int32_t end = begin64 + piece < tb ? (int32_t)(begin64 + piece) : tb;
+    // the sequence of the range's first token: the first one that ends behind it
+    int32_t s_first = s0;
+    if (begin < end) {
+      int32_t lo = s0, hi = s1;
+      while (lo < hi) { const int32_t mid = lo + ((hi - lo) >> 1); if (a.cu[mid + 1] > begin) hi = mid; else lo = mid + 1; }
+      s_first = lo;
     }
-    __syncthreads();
-    // which completions take part: at least one token, a finite reward and a finite sum
-    auto takes_part = [&](int32_t s) {
-      bool ignore = false;
-      int32_t t0, t1;
-      offset_range(a.cu, s, Tc, t0, t1, ignore);
-      return t1 > t0 && isfinite(a.rewards[s]) && isfinite(a.seq_logratio[s]);
-    };
-    int32_t best = -1, worst = -1;
-    if (a.pairs == SAPO_PREF_BEST_WORST) {
-      for (int32_t s = s0; s < s1; ++s) {
-        if (!takes_part(s)) continue;
-        if (best < 0 || a.rewards[s] > a.rewards[best]) best = s;
-        if (worst < 0 || a.rewards[s] < a.rewards[worst]) worst = s;
+    bool masked = false;                       // a token of this lane's in the range is masked
+    // 1.
+    if (begin < end) {
+      for (int32_t s = s_first; s < s1; ++s) {
+        int32_t t0, t1;
+        offset_range(a.cu, s, Tc, t0, t1, bad_offset);
+        if (t0 >= end) break;
+        const int32_t from = t0 > begin ? t0 : begin, to = t1 < end ? t1 : end;
+        if (from >= to) continue;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};
+        int32_t t = from + lane;
+        for (; t + 96 < to; t += 128) {
+          float d[4];
+          #pragma unroll
+          for (int k = 0; k < 4; ++k) d[k] = token_ratio(a, t + 32 * k);
+          #pragma unroll
+          for (int k = 0; k < 4; ++k) { if (isfinite(d[k])) part[k] += d[k]; else masked = true; }
+        }
+        for (; t < to; t += 32) {
+          const float d = token_ratio(a, t);
+          if (isfinite(d)) part[0] += d; else masked = true;
+        }
+        const float sum = warp_sum((part[0] + part[1]) + (part[2] + part[3]));
+        if (lane == 0) {
+          if (t0 > begin) a.seq_logratio[s] = sum;
+          else store_to_first(&head[gw], sum);
+        }
       }
     }
-    // thread per completion: its pairs as the preferred one count towards the loss, both sides
-    // towards its factor
-    double loss = 0.0, margin = 0.0, count = 0.0;
-    for (int32_t i = s0 + threadIdx.x; i < s1; i += PREF_THREADS) {
-      const float r = a.rewards[i], R = a.seq_logratio[i];
-      if (!isfinite(r)) bad_reward = true;
-      double f = 0.0;
-      if (takes_part(i)) {
-        for (int32_t j = s0; j < s1; ++j) {
-          const float rj = a.rewards[j];
-          if (rj == r || !takes_part(j)) continue;
-          const bool wins = r > rj;
+    bad_value |= masked;
+    cluster_barrier();
+    // 2.
+    if (rank == 0) {
+      const bool kept = s1 - s0 <= PREF_SEQS;
+      for (int32_t s = s0 + warp; s < s1; s += PREF_WARPS) {
+        int32_t t0, t1;
+        offset_range(a.cu, s, Tc, t0, t1, bad_offset);
+        const int32_t n = t1 - t0;
+        float R = 0.f;
+        if (n > 0) {
+          // its pieces: the first where it begins (in seq_logratio unless it begins a range), then the heads of the
+          // ranges that it runs into.  (Malformed offsets, reported above, could point outside the ranges.)
+          const int32_t w0 = t0 < ta ? 0 : (t0 - ta) / piece;
+          int32_t w1 = t1 <= ta ? 0 : (t1 - 1 - ta) / piece;
+          if (w1 >= n_warps) w1 = n_warps - 1;
+          const bool inside = t0 - ta > w0 * piece;
+          float x = 0.f;
+          for (int32_t w = w0 + (inside ? 1 : 0) + lane; w <= w1; w += 32) x += head[w];
+          R = warp_sum(x) + (inside ? __ldcg(a.seq_logratio + s) : 0.f);
+          if (a.length_norm) R /= (float)n;
+        }
+        if (lane == 0) {
+          const float r = a.rewards[s];
+          if (!isfinite(r)) bad_reward = true;
+          a.seq_logratio[s] = R;
+          // a completion takes part if it has a token, a finite reward and a finite sum
+          if (kept) { R_s[s - s0] = R; r_s[s - s0] = n > 0 && isfinite(r) && isfinite(R) ? r : NAN; }
+        }
+      }
+      __syncthreads();
+      auto reward_of = [&](int32_t s) {          // NaN: takes no part, and compares as neither more nor less
+        if (kept) return r_s[s - s0];
+        bool ignore = false;
+        int32_t t0, t1;
+        offset_range(a.cu, s, Tc, t0, t1, ignore);
+        const float r = a.rewards[s];
+        return t1 > t0 && isfinite(r) && isfinite(__ldcg(a.seq_logratio + s)) ? r : NAN;
+      };
+      auto ratio_of = [&](int32_t s) { return kept ? R_s[s - s0] : __ldcg(a.seq_logratio + s); };
+      int32_t best = -1, worst = -1;
+      if (a.pairs == SAPO_PREF_BEST_WORST) {
+        float hi = -INFINITY, lo = INFINITY;
+        for (int32_t s = s0 + lane; s < s1; s += 32) {       // every warp for itself
+          const float r = reward_of(s);
+          if (r > hi) { hi = r; best = s; }
+          if (r < lo) { lo = r; worst = s; }
+        }
+        #pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {                   // the lower index where rewards tie
+          const float h2 = __shfl_xor_sync(0xffffffffu, hi, d), l2 = __shfl_xor_sync(0xffffffffu, lo, d);
+          const int32_t b2 = __shfl_xor_sync(0xffffffffu, best, d), w2 = __shfl_xor_sync(0xffffffffu, worst, d);
+          if (b2 >= 0 && (best < 0 || h2 > hi || (h2 == hi && b2 < best))) { hi = h2; best = b2; }
+          if (w2 >= 0 && (worst < 0 || l2 < lo || (l2 == lo && w2 < worst))) { lo = l2; worst = w2; }
+        }
+      }
+      double loss = 0.0, margin = 0.0, count = 0.0;
+      for (int32_t i = s0 + warp; i < s1; i += PREF_WARPS) {
+        const float r = reward_of(i), R = ratio_of(i);
+        double f = 0.0;
+        for (int32_t j = s0 + lane; j < s1; j += 32) {
+          const float rj = reward_of(j);
+          const bool wins = r > rj, loses = r < rj;
+          if (!(wins || loses)) continue;
           if (a.pairs == SAPO_PREF_BEST_WORST && !(wins ? (i == best && j == worst) : (j == best && i == worst))) continue;
-          const float h = a.beta * (wins ? R - a.seq_logratio[j] : a.seq_logratio[j] - R);
+          const float Rj = ratio_of(j);
+          const float h = a.beta * (wins ? R - Rj : Rj - R);
           float l, dl;
           pair_loss(a, h, l, dl);
           f += wins ? (double)dl : -(double)dl;
-          if (wins) { loss += (double)l; margin += (double)h; count += 1.0; }
+          if (wins) { loss += (double)l; margin += (double)h; count += 1.0; }     // each pair once
         }
+        f = warp_sum(f);
+        if (lane == 0) a.seq_grad[i] = (float)f;             // scaled below, once the pairs are counted
       }
-      a.seq_grad[i] = (float)f;                      // scaled below, once the pairs are counted
+      loss = warp_sum(loss); margin = warp_sum(margin); count = warp_sum(count);
+      if (lane == 0) { sums[0][warp] = loss; sums[1][warp] = margin; sums[2][warp] = count; }
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        loss = margin = count = 0.0;
+        for (int w = 0; w < PREF_WARPS; ++w) { loss += sums[0][w]; margin += sums[1][w]; count += sums[2][w]; }
+        const double per = count > 0.0 ? 1.0 / count : 0.0;
+        a.q_loss[q] = (float)(loss * per);
+        if (a.q_margin != nullptr) a.q_margin[q] = (float)(margin * per);
+        if (a.q_pairs != nullptr) a.q_pairs[q] = (int32_t)count;
+        scale_s = (float)((double)a.grad_scale * (double)a.beta * per / (double)a.Q);
+      }
+      __syncthreads();
+      for (int32_t i = s0 + threadIdx.x; i < s1; i += PREF_THREADS) a.seq_grad[i] *= scale_s;
     }
-    loss = block_sum(loss, sh);
-    margin = block_sum(margin, sh);
-    count = block_sum(count, sh);
-    const double per = count > 0.0 ? 1.0 / count : 0.0;
-    if (threadIdx.x == 0) {
-      a.q_loss[q] = (float)(loss * per);
-      if (a.q_margin != nullptr) a.q_margin[q] = (float)(margin * per);
-      if (a.q_pairs != nullptr) a.q_pairs[q] = (int32_t)count;
-    }
-    const float scale = (float)((double)a.grad_scale * (double)a.beta * per / (double)a.Q);
-    for (int32_t i = s0 + threadIdx.x; i < s1; i += PREF_THREADS) a.seq_grad[i] *= scale;
-    __syncthreads();
-    for (int32_t s = s0 + warp; s < s1; s += PREF_THREADS / 32) {
-      bool ignore = false;
-      int32_t t0, t1;
-      offset_range(a.cu, s, Tc, t0, t1, ignore);
-      const float g = a.length_norm && t1 > t0 ? a.seq_grad[s] / (float)(t1 - t0) : a.seq_grad[s];
-      for (int32_t t = t0 + lane; t < t1; t += 32) {
-        const float d = a.ref_logp != nullptr ? a.logp[t] - a.ref_logp[t] : a.logp[t];
-        a.gscale[t] = isfinite(d) ? g : 0.f;
+    cluster_barrier();
+    // 3.
+    if (begin < end) {
+      for (int32_t s = s_first; s < s1; ++s) {
+        bool ignore = false;
+        int32_t t0, t1;
+        offset_range(a.cu, s, Tc, t0, t1, ignore);
+        if (t0 >= end) break;
+        const int32_t from = t0 > begin ? t0 : begin, to = t1 < end ? t1 : end;
+        if (from >= to) continue;
+        float g = __ldcg(a.seq_grad + s);
+        if (a.length_norm) g /= (float)(t1 - t0);
+        // the lane that summed a token writes its factor, and knows whether any of its tokens was masked
+        for (int32_t t = from + lane; t < to; t += 32) a.gscale[t] = masked && !isfinite(token_ratio(a, t)) ? 0.f : g;
       }
     }
-    if (bad_offset) raise_status(a.status, SAPO_ST_BAD_INDEX);
-    if (bad_value && a.ref_logp != nullptr) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
-    if (bad_reward) raise_status(a.status, SAPO_ST_NONFINITE_REWARD);
-    __syncthreads();
   }
+  if (bad_offset) raise_status(a.status, SAPO_ST_BAD_INDEX);
+  if (bad_value && a.ref_logp != nullptr) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+  if (bad_reward) raise_status(a.status, SAPO_ST_NONFINITE_REWARD);
+  // the first block's shared memory stays until the others have written to it (the last barrier above)
 }
 
-// What no question covers: sequences before the first and after the last one, and their tokens, get
-// zeros.  One block also adds up the questions' losses.
-__global__ void __launch_bounds__(PREF_THREADS) preference_final_kernel(PrefArgs a) {
-  __shared__ double sh[PREF_THREADS / 32];
-  bool ignore = false;
-  const int32_t Tc = (int32_t)a.T;
-  const int32_t s_lo = clamp_to(a.group_offsets[0], a.S, ignore);
-  int32_t s_hi = clamp_to(a.group_offsets[a.Q], a.S, ignore);
-  if (s_hi < s_lo) s_hi = s_lo;
-  const int32_t t_lo = clamp_to(a.cu[s_lo], Tc, ignore);
-  int32_t t_hi = clamp_to(a.cu[s_hi], Tc, ignore);
-  if (t_hi < t_lo) t_hi = t_lo;
-  const int64_t first = (int64_t)blockIdx.x * PREF_THREADS + threadIdx.x, step = (int64_t)gridDim.x * PREF_THREADS;
-  for (int64_t i = first; i < (int64_t)t_lo + (Tc - t_hi); i += step) a.gscale[i < t_lo ? i : t_hi + (i - t_lo)] = 0.f;
-  for (int64_t i = first; i < (int64_t)s_lo + (a.S - s_hi); i += step) {
-    const int64_t s = i < s_lo ? i : s_hi + (i - s_lo);
-    a.seq_logratio[s] = 0.f;
-    a.seq_grad[s] = 0.f;
-  }
-  if (blockIdx.x != 0) return;
+// loss = the mean of the questions' losses
+__global__ void __launch_bounds__(256) preference_final_kernel(const float* q_loss, int32_t Q, float* loss) {
+  __shared__ double sh[8];
+  asm volatile("griddepcontrol.wait;" ::: "memory");         // launched while preference_kernel still runs
   double x = 0.0;
-  for (int32_t q = threadIdx.x; q < a.Q; q += PREF_THREADS) x += (double)a.q_loss[q];
-  x = block_sum(x, sh);
-  if (threadIdx.x == 0) *a.loss = (float)(x / (double)a.Q);
+  for (int32_t q = threadIdx.x; q < Q; q += 256) x += (double)__ldcg(q_loss + q);
+  x = warp_sum(x);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    x = 0.0;
+    for (int i = 0; i < 8; ++i) x += sh[i];
+    *loss = (float)(x / (double)Q);
+  }
 }
 
 int pref_check_cfg(const sapo_pref_cfg* c) {
@@ -182,20 +298,48 @@ int pref_check_cfg(const sapo_pref_cfg* c) {
   return SAPO_OK;
 }
 
+// Blocks per question: a power of two, enough for one to have about 4096 tokens of an average question
+// (8 a thread), while all questions' blocks together still fit on the device at once.
+static int pref_cluster(int64_t T, int32_t Q, int sms) {
+  int c = 1;
+  while (c < PREF_MAX_CLUSTER && (int64_t)Q * c * 4096 < T && (int64_t)Q * c * 2 <= 2 * (int64_t)sms) c <<= 1;
+  return c;
+}
+
 int launch_preference(const PrefArgs& a, cudaStream_t st) {
   const int sms = sm_count();
-  if (sms <= 0) return SAPO_ERR_CUDA;
-  {
-    const int64_t most = (int64_t)sms * 8;
-    KernelScope scope(SAPO_K_PREFERENCE, st);
-    preference_kernel<<<(int)(a.Q < most ? a.Q : most), PREF_THREADS, 0, st>>>(a);
+  const int dev = current_device();
+  if (sms <= 0 || dev < 0) return SAPO_ERR_CUDA;
+  static bool wide[MAX_DEVICES] = {false};                   // clusters of 16 blocks allowed
+  if (!wide[dev]) {
+    if (cudaFuncSetAttribute(preference_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SAPO_ERR_CUDA;
+    wide[dev] = true;
   }
-  int64_t blocks = ceil_div<int64_t>(a.T, 4096);
-  if (blocks < 1) blocks = 1;
-  if (blocks > sms) blocks = sms;
+  const int cluster = pref_cluster(a.T, a.Q, sms);
+  const int64_t most = (int64_t)sms * 4 / cluster;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.gridDim = dim3((unsigned)((a.Q < most ? a.Q : most) * cluster));
+  cfg.blockDim = dim3(PREF_THREADS);
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  {
+    KernelScope scope(SAPO_K_PREFERENCE, st);
+    if (cudaLaunchKernelEx(&cfg, preference_kernel, a) != cudaSuccess) return SAPO_ERR_CUDA;
+  }
+  cudaLaunchConfig_t fin{};
+  fin.gridDim = dim3(1);
+  fin.blockDim = dim3(256);
+  fin.stream = st;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  fin.attrs = attr;
+  fin.numAttrs = 1;
   KernelScope scope(SAPO_K_PREF_FINAL, st);
-  preference_final_kernel<<<(int)blocks, PREF_THREADS, 0, st>>>(a);
-  return check_launch();
+  return cudaLaunchKernelEx(&fin, preference_final_kernel, (const float*)a.q_loss, a.Q, a.loss) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
 }
 
 }  // namespace sapo
