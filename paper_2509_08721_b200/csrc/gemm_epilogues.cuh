@@ -185,6 +185,7 @@ struct ExpEpiT {
     // can have a gradient; the panel rows of a clear block are not written (its sums still are).
     // blk0 = index of this launch's first block in that array
     const uint32_t* need; int32_t blk0;
+    float z_scale;        // log2(e), or a little more (see preference_impl)
   };
   float c, sum, sz; int32_t tile_row0; int r; bool valid, in_panel, store; int64_t row;
   __device__ __forceinline__ void begin_unit(const Params& p, int mb, int r_) {
@@ -214,7 +215,7 @@ struct ExpEpiT {
     for (int h = 0; h < 2; ++h) {
       #pragma unroll
       for (int j = 16 * h; j < 16 * h + 16; ++j) {
-        const float e = ex2(fmaf(v[j], LOG2E, -c));
+        const float e = ex2(fmaf(v[j], p.z_scale, -c));
         // (columns past the vocabulary hold z = 0 from the zero-filled load: they add nothing)
         if constexpr (ENT) sz = fmaf((col0 + j < p.V) ? e : 0.f, v[j], sz);
         v[j] = e;

@@ -520,15 +520,12 @@ static int fwd_check_args(const void* hidden, const void* W_head, int32_t dtype,
   return SAPO_OK;
 }
 
-// Scratch of the preference call behind its log ratios: the forward's partials, then (after them in
-// time) the backward's panel of `panel_rows` tokens, in the same place.
-static size_t pref_scratch(int64_t T, int32_t H, int32_t V, int32_t dtype, bool out_bf16, int64_t panel_rows) {
-  int sms = sm_count();
-  if (sms <= 0) sms = 148;
-  const size_t fwd = fwd_layout(T, H, V, dtype, sms, 0, /*entropy=*/false).total;
-  const BwdLayout L = bwd_layout(T, H, V, dtype, out_bf16);
-  const size_t bwd = L.fixed + (size_t)panel_rows * L.bytes_per_row;
-  return fwd > bwd ? fwd : bwd;
+// Panel rows the workspace query asks for a preference call: the whole batch up to 40 960 tokens (12.5 GB at a
+// vocabulary of 152 000), because a smaller panel costs a second pass over the logits; beyond that, what the
+// backward asks for.
+constexpr int64_t PREF_ROWS_ONE_PIECE = 40960;
+static int64_t preference_panel_rows(int64_t T, int32_t H, int32_t V) {
+  return T <= PREF_ROWS_ONE_PIECE ? round_up<int64_t>(T, BM) : preferred_panel_rows(T, H, V);
 }
 
 }  // namespace sapo
@@ -550,9 +547,11 @@ extern "C" size_t sapo_workspace_bytes(int32_t which, int64_t T, int32_t H, int3
     const FusedLayout L = fused_layout(T, H, V, /*S=*/(int32_t)(T < 0x7fffffff ? T : 0x7fffffff), out_bf16, gather);
     return L.fixed + FUSED_CHUNK_SLACK + (size_t)preferred_panel_rows(T, H, V) * L.bytes_per_row;
   }
-  if (which == SAPO_WS_PREFERENCE)
-    return dtype != SAPO_DTYPE_BF16 ? 0 : round_up<size_t>((size_t)T * sizeof(float), 256) +
-           pref_scratch(T, H, V, dtype, out_bf16, preferred_panel_rows(T, H, V));
+  if (which == SAPO_WS_PREFERENCE) {
+    if (dtype != SAPO_DTYPE_BF16) return 0;
+    const FusedLayout L = fused_layout(T, H, V, (int32_t)T, out_bf16);
+    return L.fixed + FUSED_CHUNK_SLACK + (size_t)preference_panel_rows(T, H, V) * L.bytes_per_row;
+  }
   if (which == SAPO_WS_BWD || which == SAPO_WS_BWD_ACTIVE) {
     const BwdLayout L = bwd_layout(T, H, V, dtype, out_bf16);
     const size_t extra = which == SAPO_WS_BWD_ACTIVE ? active_layout(T, H).total : 0;
@@ -570,9 +569,7 @@ extern "C" size_t sapo_workspace_bytes_min(int32_t which, int64_t T, int32_t H, 
     return sapo_workspace_bytes(which, T, H, V, dtype);
   which &= ~flags;
   if (!shapes_ok(T, H, V) || (dtype != SAPO_DTYPE_BF16 && dtype != SAPO_DTYPE_F32)) return 0;
-  if (which == SAPO_WS_PREFERENCE)
-    return dtype != SAPO_DTYPE_BF16 ? 0 : round_up<size_t>((size_t)T * sizeof(float), 256) + pref_scratch(T, H, V, dtype, out_bf16, BM);
-  if (which == SAPO_WS_FUSED) {
+  if (which == SAPO_WS_FUSED || which == SAPO_WS_PREFERENCE) {
     if (dtype != SAPO_DTYPE_BF16) return 0;
     const FusedLayout L = fused_layout(T, H, V, (int32_t)(T < 0x7fffffff ? T : 0x7fffffff), out_bf16, gather);
     return L.fixed + FUSED_CHUNK_SLACK + (size_t)BM * L.bytes_per_row;
@@ -1184,11 +1181,11 @@ static int fused_impl(const void* hidden, const HiddenSource* src, const void* W
     {
       int rc;
       if (want_entropy) {
-        ExpEpiT<true>::Params ep{c2 + t0, ps, pe, tc, V, nvt, panel, panel_rows, 2 * FUSED_MAX_SPLITS, need, (int32_t)(t0 / BM)};
+        ExpEpiT<true>::Params ep{c2 + t0, ps, pe, tc, V, nvt, panel, panel_rows, 2 * FUSED_MAX_SPLITS, need, (int32_t)(t0 / BM), LOG2E};
         rc = gather ? launch_gemm<0, false, ExpEpiT<true>, FWD_BK, FWD_STAGES, GatherArgs>(map_h_kmajor, map_w_kmajor, fs, ep, status, st, SAPO_K_FWD_EXP, ga)
                     : launch_gemm<0, false, ExpEpiT<true>, FWD_BK, FWD_STAGES>(map_h_kmajor, map_w_kmajor, fs, ep, status, st, SAPO_K_FWD_EXP);
       } else {
-        ExpEpi::Params ep{c2 + t0, ps, nullptr, tc, V, nvt, panel, panel_rows, 2 * FUSED_MAX_SPLITS, need, (int32_t)(t0 / BM)};
+        ExpEpi::Params ep{c2 + t0, ps, nullptr, tc, V, nvt, panel, panel_rows, 2 * FUSED_MAX_SPLITS, need, (int32_t)(t0 / BM), LOG2E};
         rc = gather ? launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES, GatherArgs>(map_h_kmajor, map_w_kmajor, fs, ep, status, st, SAPO_K_FWD_EXP, ga)
                     : launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES>(map_h_kmajor, map_w_kmajor, fs, ep, status, st, SAPO_K_FWD_EXP);
       }
@@ -1273,36 +1270,204 @@ extern "C" int sapo_policy_loss_fwd_bwd_gather(const void* local_hidden, int64_t
 // ------------------------------------------------------------------------------------------
 // The preference loss through the LM head.
 namespace sapo {
-// Per token, from the partials of the forward: lse, logp, and the log ratio to the reference that the
-// preference loss sums (NaN where the token is masked).
-__global__ void __launch_bounds__(256)
-pref_score_kernel(const float* __restrict__ pm, const float* __restrict__ ps, const float* __restrict__ pz,
-                  int32_t n_splits, int64_t T, const int32_t* __restrict__ ids, int32_t V,
-                  const float* __restrict__ ref_logp, const int32_t* __restrict__ cu, int32_t S,
-                  float* __restrict__ logp, float* __restrict__ lse, float* __restrict__ log_ratio, int32_t* status) {
+// Factor on the logits in the forward's exponentials.  The tensor cores truncate when they add to the
+// accumulator: each of the H / 16 additions of a logit loses half an ulp of the running sum on average, always
+// towards zero, and the running sum is on average half the logit, so a logit comes out short by a part
+// delta = 1.5e-8 H / 16 of itself (measured over H 256 to 3584, logits of standard deviation 0.2 to 2, hidden
+// states with and without an offset: 1.3e-8 to 1.6e-8 per addition).  That is far below a logit's use in a
+// gradient, but it has one sign: the log-sum-exp is short by delta E_p[z], 4e-7 a token at H = 896, and a
+// preference loss adds up hundreds of tokens.
+static float z_compensation(int32_t H) { return 1.f + 1.5e-8f * (float)(H / 16); }
+
+struct PrefTailArgs {
+  const float* ps; int32_t n_parts; int64_t t0, tc;      // partial sums [n_parts][tc] of a token chunk
+  const float* zy; const float* c2; float* sum;          // [T]
+  const int32_t* ids; int32_t V; const float* ref_logp; const int32_t* cu; int32_t S; int64_t T;
+  float* logp; float* lse; float* log_ratio;             // [T]
+  int32_t* status;
+};
+
+// After the forward pass of a chunk, one warp per token:  sum = sum_v exp(z - c) with c = z_y - ref (nearly),
+//   lse = c + log sum,  log ratio = z_y - lse - ref = (z_y - ref - c) - log sum.
+// The bracket is the rounding of c, taken in 64 bits: formed this way the log ratio, which a sequence's
+// hundreds of tokens are summed over, is free of the rounding of lse (1e-6 for an lse around 12).
+// A masked token gets the log ratio NaN.
+__global__ void __launch_bounds__(256) pref_score_kernel(PrefTailArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n_warps = (int64_t)gridDim.x * 8;
   int32_t lo, hi;
-  scored_range(cu, S, T, lo, hi);
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < T; t += (int64_t)gridDim.x * 256) {
-    if (t < lo || t >= hi) { logp[t] = 0.f; lse[t] = 0.f; log_ratio[t] = 0.f; continue; }
-    float M = -INFINITY;
-    for (int i = 0; i < n_splits; ++i) M = fmaxf(M, pm[(int64_t)i * T + t]);
-    float sum = 0.f, zy = 0.f;
-    for (int i = 0; i < n_splits; ++i) {
-      const int64_t o = (int64_t)i * T + t;
-      sum += ps[o] * exp2f(pm[o] - M);
-      zy += pz[o];
-    }
-    const float l = (M + log2f(sum)) * LN2;
-    const int32_t y = ids[t];
-    const bool bad_id = y < 0 || y >= V;
-    const float ref = ref_logp[t];
+  scored_range(a.cu, a.S, a.T, lo, hi);
+  for (int64_t lr = warp; lr < a.tc; lr += n_warps) {
+    const int64_t t = a.t0 + lr;
+    float sum = 0.f;
+    for (int i = lane; i < a.n_parts; i += 32) sum += a.ps[(int64_t)i * a.tc + lr];
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane != 0) continue;
+    const bool in_seq = t >= lo && t < hi;
+    const int32_t y = a.ids[t];
+    const bool bad_id = y < 0 || y >= a.V;
+    const bool bad_range = !(sum < EXP_CAP) || !(sum > 1.f / EXP_CAP);
+    const float ref = a.ref_logp[t], zy = a.zy[t], c2 = a.c2[t];
     const bool bad_ref = !isfinite(ref);
-    if (bad_id) raise_status(status, SAPO_ST_BAD_TOKEN_ID);
-    if (bad_ref) raise_status(status, SAPO_ST_NONFINITE_INPUT);
-    lse[t] = l;
-    logp[t] = bad_id ? 0.f : zy - l;
-    log_ratio[t] = bad_id || bad_ref ? __int_as_float(0x7fc00000) : zy - l - ref;
+    const float lse = in_seq && !bad_range ? (c2 + log2f(sum)) * LN2 : 0.f;
+    const float ratio = (float)((double)zy - (double)ref - (double)c2 * 0.69314718055994530942) - logf(sum);
+    const bool masked = bad_id || bad_range || bad_ref;
+    if (in_seq) {
+      if (bad_id) raise_status(a.status, SAPO_ST_BAD_TOKEN_ID);
+      if (bad_range) raise_status(a.status, SAPO_ST_EXP_RANGE);
+      if (bad_ref) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+    }
+    a.lse[t] = lse;
+    a.logp[t] = !in_seq || bad_id || bad_range ? 0.f : (bad_ref ? zy - lse : ref + ratio);
+    a.log_ratio[t] = !in_seq ? 0.f : (masked ? __int_as_float(0x7fc00000) : ratio);
+    a.sum[t] = sum;
   }
+}
+
+struct PrefScaleArgs {
+  const float* sum; const float* zy; const float* c2; const int32_t* ids; int32_t V; const float* gscale; int64_t T;
+  float* row_scale; __nv_bfloat16* panel; int32_t nvt; int64_t panel_rows;
+  const __nv_bfloat16* hidden; int64_t ld; int32_t H; __nv_bfloat16* hs; uint32_t* active_mask;
+};
+
+// Once the factors g_t are known, one warp per token: what turns the stored exponentials into dz, as in
+// fused_tail_kernel: the row scale a_t = -g_t / sum_t, the chosen token's entry e_y - sum_t, hs = a_t hidden.
+// A token without a gradient only needs a zero scale and row.
+__global__ void __launch_bounds__(256) pref_scale_kernel(PrefScaleArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n_warps = (int64_t)gridDim.x * 8;
+  for (int64_t t = warp; t < a.T; t += n_warps) {
+    const float g = a.gscale[t], sum = a.sum[t];
+    const float scale = g == 0.f ? 0.f : -g / sum;
+    if (lane == 0) {
+      a.row_scale[t] = scale;
+      if (scale != 0.f) {
+        if (a.active_mask != nullptr) atomicOr(&a.active_mask[t >> 12], 1u << ((t >> 7) & 31));
+        const int32_t y = a.ids[t];                       // in [0, V): a masked token has g = 0
+        const float ey = ex2(fmaf(a.zy[t], LOG2E, -a.c2[t]));
+        const int64_t tile = (t >> 7) * a.nvt + (y >> 6);
+        if (SAPO_IN_BOUNDS(y >= 0 && y < a.V && tile * BM + (t & 127) < a.panel_rows))
+          a.panel[(tile * BM + (t & 127)) * 64 + (y & 63)] = __float2bfloat16_rn(ey - sum);
+      }
+    }
+    if (!(sum < EXP_CAP)) {
+      // exponentials that are huge or not finite: zero times them would still spoil dW_head
+      uint32_t* row32 = reinterpret_cast<uint32_t*>(a.panel);
+      for (int vt = 0; vt < a.nvt; ++vt)
+        row32[((((t >> 7) * (int64_t)a.nvt + vt) * BM + (t & 127)) * 64 >> 1) + lane] = 0u;
+    }
+    const uint4* src = reinterpret_cast<const uint4*>(a.hidden + t * a.ld);
+    uint4* dst = reinterpret_cast<uint4*>(a.hs + t * (int64_t)a.H);
+    for (int i = lane; i < a.H / 8; i += 32) {
+      uint4 x = make_uint4(0u, 0u, 0u, 0u);
+      if (scale != 0.f) {
+        x = src[i];
+        __nv_bfloat162* px = reinterpret_cast<__nv_bfloat162*>(&x);
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = __bfloat1622float2(px[j]);
+          px[j] = __floats2bfloat162_rn(scale * f.x, scale * f.y);
+        }
+      }
+      dst[i] = x;
+    }
+  }
+}
+
+// The scratch is the single-pass call's (FusedLayout: `obj` holds the log ratios, `seq` the tokens' sums).
+static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, int64_t T, int32_t H, int32_t V,
+                           int64_t ld_hidden, int64_t ld_W, const int32_t* ids, const float* ref_logp, PrefArgs pa,
+                           float* logp, float* lse, void* dhidden, void* dW_head, int32_t out_dtype,
+                           int32_t accumulate_dW, uint8_t* ws, size_t workspace_bytes, cudaStream_t st) {
+  const int sms = sm_count();
+  if (sms <= 0) return SAPO_ERR_CUDA;
+  const bool out_bf16 = out_dtype == SAPO_DTYPE_BF16;
+  const FusedLayout L = fused_layout(T, H, V, (int32_t)T, out_bf16);
+  if (workspace_bytes < L.fixed + FUSED_CHUNK_SLACK + (size_t)BM * L.bytes_per_row) return SAPO_ERR_WORKSPACE_TOO_SMALL;
+  const size_t room = workspace_bytes - L.fixed - FUSED_CHUNK_SLACK;
+  // A pair's factor is known only after both its sequences have been scored.  If the panel holds the whole
+  // batch, the exponentials wait there (6 T V H flops); if not, the forward keeps sums only, and the
+  // backward recomputes the logits chunk by chunk (8 T V H).
+  const bool one_pass = (int64_t)(room / L.bytes_per_row) / BM * BM >= T;
+  const int64_t score_row_bytes = (int64_t)2 * FUSED_MAX_SPLITS * 4;
+  int64_t chunk = round_up<int64_t>(T, BM);
+  if (!one_pass) {
+    const int64_t fit = (int64_t)(room / score_row_bytes) / BM * BM;
+    const int64_t cap = fit < PANEL_ROWS_TARGET ? fit : PANEL_ROWS_TARGET;
+    if (cap < chunk) chunk = equal_chunk_rows(T, cap);
+  }
+  const FusedChunk CL = fused_chunk(L, chunk, H);
+  float* zy = reinterpret_cast<float*>(ws + L.zy);
+  float* c2 = reinterpret_cast<float*>(ws + L.c2);
+  float* log_ratio = reinterpret_cast<float*>(ws + L.obj);
+  float* sum = reinterpret_cast<float*>(ws + L.seq);
+  uint32_t* need = reinterpret_cast<uint32_t*>(ws + L.need);
+  uint32_t* active_mask = reinterpret_cast<uint32_t*>(ws + L.mask);
+  float* ps = reinterpret_cast<float*>(one_pass ? ws + CL.ps : ws + L.fixed);
+  __nv_bfloat16* hs = reinterpret_cast<__nv_bfloat16*>(ws + CL.hs);
+  __nv_bfloat16* panel = one_pass ? reinterpret_cast<__nv_bfloat16*>(ws + CL.panel) : nullptr;
+  const int64_t Vp = padded_vocab(V);
+  const int32_t nvt = (int32_t)(Vp / 64);
+  auto token_blocks = [&](int64_t n) {          // a warp per token
+    const int64_t b = ceil_div<int64_t>(n, 8);
+    return (int)(b < (int64_t)sms * 8 ? b : (int64_t)sms * 8);
+  };
+
+  // 1. chosen-token logits and the reference of the exponentials
+  {
+    KernelScope scope(SAPO_K_TARGET_LOGIT, st);
+    target_logit_kernel<<<token_blocks(T), 256, 0, st>>>(RowSource{hidden, nullptr, ld_hidden, nullptr, 0, 0}, W, ld_W, ids,
+                                                         ref_logp, T, H, V, zy, c2, nullptr, pa.cu, pa.S, nullptr);
+  }
+  if (!one_pass &&                               // no block's exponentials are kept
+      cudaMemsetAsync(need, 0, (size_t)ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) * 4, st) != cudaSuccess)
+    return SAPO_ERR_CUDA;
+  // 2. exponentials and their sums, then the log ratio of every token
+  CUtensorMap map_w;
+  if (!make_map(&map_w, W, H, V, ld_W, 128)) return SAPO_ERR_CUDA;
+  for (int64_t t0 = 0; t0 < T; t0 += chunk) {
+    const int64_t tc = (T - t0) < chunk ? (T - t0) : chunk;
+    CUtensorMap map_h;
+    if (!make_map(&map_h, hidden + t0 * ld_hidden, H, tc, ld_hidden, BM)) return SAPO_ERR_CUDA;
+    int n_splits = fwd_splits(tc, V, H, sms);
+    if (n_splits > FUSED_MAX_SPLITS) n_splits = FUSED_MAX_SPLITS;
+    Sched fs = make_sched(tc, V, H, n_splits, /*m_fastest=*/true, /*tile_align=*/64, FWD_BK);
+    fs.n_cover = (int32_t)Vp;
+    ExpEpi::Params ep{c2 + t0, ps, nullptr, tc, V, nvt, panel, ceil_div<int64_t>(tc, BM) * nvt * BM, 2 * FUSED_MAX_SPLITS,
+                      one_pass ? nullptr : need, (int32_t)(t0 / BM), LOG2E * z_compensation(H)};
+    const int rc = launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES>(map_h, map_w, fs, ep, pa.status, st, SAPO_K_FWD_EXP);
+    if (rc != SAPO_OK) return rc;
+    KernelScope scope(SAPO_K_PREF_SCORE, st);
+    pref_score_kernel<<<token_blocks(tc), 256, 0, st>>>(PrefTailArgs{ps, 2 * fs.units_per_m, t0, tc, zy, c2, sum, ids, V, ref_logp,
+                                                                     pa.cu, pa.S, T, logp, lse, log_ratio, pa.status});
+  }
+  // 3. the loss and every token's factor
+  pa.logp = log_ratio;
+  pa.ref_logp = nullptr;
+  int rc = launch_preference(pa, st);
+  if (rc != SAPO_OK) return rc;
+  // 4. the gradients
+  if (!one_pass)
+    return bwd_impl(hidden, W, SAPO_DTYPE_BF16, T, H, V, ld_hidden, ld_W, ids, 0, lse, pa.gscale, dhidden, dW_head, out_dtype,
+                    accumulate_dW, ws, workspace_bytes, pa.status, st);
+  const int64_t panel_rows = ceil_div<int64_t>(T, BM) * nvt * BM;
+  float* row_scale = reinterpret_cast<float*>(ws + CL.row_scale);
+  const bool masked = ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) <= MASK_WORDS_MAX;
+  if (masked && cudaMemsetAsync(active_mask, 0, (size_t)MASK_WORDS_MAX * 4, st) != cudaSuccess) return SAPO_ERR_CUDA;
+  {
+    KernelScope scope(SAPO_K_FUSED_TAIL, st);
+    pref_scale_kernel<<<token_blocks(T), 256, 0, st>>>(PrefScaleArgs{sum, zy, c2, ids, V, pa.gscale, T, row_scale, panel, nvt,
+                                                                     panel_rows, hidden, ld_hidden, H, hs,
+                                                                     masked ? active_mask : nullptr});
+  }
+  const bool dw_via_acc = out_bf16 && accumulate_dW;
+  float* dw_acc = reinterpret_cast<float*>(ws + L.dw_acc);
+  rc = launch_grad_gemms(panel, panel_rows, nvt, W, ld_W, hs, H, T, H, V, Vp, dhidden, out_bf16, row_scale,
+                         dw_via_acc ? (void*)dw_acc : dW_head, out_bf16 && !dw_via_acc, dw_via_acc ? 0 : accumulate_dW,
+                         reinterpret_cast<float*>(ws + L.partials), masked ? active_mask : nullptr, pa.status, st);
+  if (rc != SAPO_OK || !dw_via_acc) return rc;
+  return launch_round_to_bf16(dw_acc, dW_head, (int64_t)V * H, 1, st);
 }
 }  // namespace sapo
 
@@ -1326,33 +1491,12 @@ extern "C" int sapo_preference_loss_fwd_bwd(const void* hidden, const void* W_he
       !aligned16(workspace) || !aligned16(dhidden) || !aligned16(dW_head) ||
       (out_dtype != SAPO_DTYPE_BF16 && out_dtype != SAPO_DTYPE_F32))
     return SAPO_ERR_INVALID_ARG;
-  const int sms = sm_count();
-  if (sms <= 0) return SAPO_ERR_CUDA;
-  const FwdLayout L = fwd_layout(T, H, V, dtype, sms, 0, /*entropy=*/false);
-  const size_t ratio_bytes = round_up<size_t>((size_t)T * sizeof(float), 256);
-  if (workspace_bytes < ratio_bytes + L.total) return SAPO_ERR_WORKSPACE_TOO_SMALL;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  float* log_ratio = static_cast<float*>(workspace);
-  uint8_t* ws = static_cast<uint8_t*>(workspace) + ratio_bytes;
-  float* pm = reinterpret_cast<float*>(ws + L.partials);
-  float* ps = pm + (size_t)2 * L.n_splits * T;
-  float* pz = ps + (size_t)2 * L.n_splits * T;
-  int n_parts = 0;
-  rc = fwd_project(hidden, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, 0, L, ws, pm, ps, pz, nullptr, status, st, &n_parts);
-  if (rc != SAPO_OK) return rc;
-  {
-    int64_t blocks = ceil_div<int64_t>(T, 256);
-    if (blocks > (int64_t)sms * 8) blocks = (int64_t)sms * 8;
-    KernelScope scope(SAPO_K_PREF_SCORE, st);
-    pref_score_kernel<<<(int)blocks, 256, 0, st>>>(pm, ps, pz, n_parts, T, ids, V, ref_logp, cu_seqlens, S, logp, lse,
-                                                   log_ratio, status);
-  }
-  const PrefArgs pa{log_ratio, nullptr, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
+  const PrefArgs pa{nullptr, nullptr, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
                     h_cfg->grad_scale, h_cfg->kind, h_cfg->pairs, h_cfg->length_norm, gscale, seq_logratio, seq_grad,
                     q_loss, q_margin, q_pairs, loss, status};
-  if ((rc = launch_preference(pa, st)) != SAPO_OK) return rc;
-  return bwd_impl(hidden, W_head, dtype, T, H, V, ld_hidden, ld_W, ids, 0, lse, gscale, dhidden, dW_head, out_dtype,
-                  accumulate_dW, ws, workspace_bytes - ratio_bytes, status, stream);
+  return preference_impl(static_cast<const __nv_bfloat16*>(hidden), static_cast<const __nv_bfloat16*>(W_head), T, H, V,
+                         ld_hidden, ld_W, ids, ref_logp, pa, logp, lse, dhidden, dW_head, out_dtype, accumulate_dW,
+                         static_cast<uint8_t*>(workspace), workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 namespace sapo {
