@@ -228,6 +228,9 @@ def _out_dtype_code(dhidden: torch.Tensor, dW_head: torch.Tensor) -> int:
     return _dtype_code(dhidden)
 
 
+_DTYPE_CODES = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return DTYPE_BF16
@@ -554,10 +557,20 @@ def sapo_adam_step(master: torch.Tensor, m: torch.Tensor, v: torch.Tensor, grad:
 
 # ------------------------------------------------------------------------------------------
 # preference loss
-def _pref_cfg(beta: float, kind: str, pairs: str, label_smoothing: float, length_norm: bool, grad_scale: float) -> PrefCfgC:
-    if kind not in PREF_KINDS or pairs not in PREF_PAIRS:
-        raise SapoError(f"kind is one of {tuple(PREF_KINDS)}, pairs one of {tuple(PREF_PAIRS)}")
-    return PrefCfgC(beta, label_smoothing, grad_scale, PREF_KINDS[kind], PREF_PAIRS[pairs], 1 if length_norm else 0)
+_pref_cfgs: Dict[tuple, PrefCfgC] = {}
+
+
+def _pref_cfg(*key) -> PrefCfgC:
+    """The parameter block of (beta, kind, pairs, label_smoothing, length_norm, grad_scale); read only, kept."""
+    cfg = _pref_cfgs.get(key)
+    if cfg is None:
+        beta, kind, pairs, label_smoothing, length_norm, grad_scale = key
+        if kind not in PREF_KINDS or pairs not in PREF_PAIRS:
+            raise SapoError(f"kind is one of {tuple(PREF_KINDS)}, pairs one of {tuple(PREF_PAIRS)}")
+        cfg = PrefCfgC(beta, label_smoothing, grad_scale, PREF_KINDS[kind], PREF_PAIRS[pairs], 1 if length_norm else 0)
+        if len(_pref_cfgs) < 64:
+            _pref_cfgs[key] = cfg
+    return cfg
 
 
 def alloc_preference_outputs(T: int, S: int, Q: int, device="cuda", scores: bool = False) -> Dict[str, torch.Tensor]:
@@ -580,7 +593,7 @@ def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens:
     cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
     rc = load().sapo_preference_loss(
         _p(logp), _p(ref_logp), int(logp.shape[0]), _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards),
-        _p(group_offsets), int(group_offsets.numel() - 1), C.byref(cfg), _p(out["gscale"]), _p(out["seq_logratio"]),
+        _p(group_offsets), int(group_offsets.numel() - 1), cfg, _p(out["gscale"]), _p(out["seq_logratio"]),
         _p(out["seq_grad"]), _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]),
         _p(status), _stream())
     _check(rc, "sapo_preference_loss")
@@ -602,7 +615,7 @@ def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids
     rc = load().sapo_preference_loss_fwd_bwd(
         _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0), _p(ids), _p(ref_logp),
         _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards), _p(group_offsets), int(group_offsets.numel() - 1),
-        C.byref(cfg), _p(out["logp"]), _p(out["lse"]), _p(out["gscale"]), _p(out["seq_logratio"]), _p(out["seq_grad"]),
+        cfg, _p(out["logp"]), _p(out["lse"]), _p(out["gscale"]), _p(out["seq_logratio"]), _p(out["seq_grad"]),
         _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]), _p(dhidden), _p(dW_head),
         _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
         _p(workspace), workspace.numel() * workspace.element_size(), _p(status), _stream())
@@ -618,8 +631,15 @@ class Ckpt8:
     scale: torch.Tensor
     H: int
 
-    def c(self) -> Ckpt8C:
-        return Ckpt8C(_p(self.data), _p(self.scale), self.data.stride(0), self.scale.stride(0))
+    def c(self, T: int, H: int) -> Ckpt8C:
+        """The C struct, for a call on [T, H]."""
+        data, scale = self.data, self.scale
+        n = -(-H // Q8_GROUP)
+        if (self.H != H or data.shape[0] != T or data.shape[1] < H or scale.shape[0] != T or scale.shape[1] < n
+                or data.dtype != torch.int8 or scale.dtype != torch.float32 or data.stride(1) != 1
+                or scale.stride(1) != 1):
+            raise SapoError("the checkpoint must have the shape of the activation")
+        return Ckpt8C(data.data_ptr(), scale.data_ptr(), max(data.stride(0), H), max(scale.stride(0), n))
 
 
 def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:
@@ -628,27 +648,52 @@ def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:
                  torch.empty(T, -(-H // Q8_GROUP), dtype=torch.float32, device=device), H)
 
 
-def _rows(t: torch.Tensor, what: str) -> int:
-    """Row pitch of a 2-D tensor whose columns are contiguous."""
+def _rows(t: torch.Tensor, T: int, H: int, what: str):
+    """(device pointer, element type, row pitch) of a [T, H] matrix whose columns are contiguous."""
     stride = t.stride()
-    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
-        raise SapoError(f"{what} must be two-dimensional with contiguous columns")
-    return stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1])
+    if t.shape != (T, H) or (stride[1] != 1 and H > 1):
+        raise SapoError(f"{what} must be [{T}, {H}] with contiguous columns")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise SapoError(f"unsupported element type {t.dtype}")
+    return t.data_ptr(), code, stride[0] if T > 1 else max(stride[0], H)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    """Device pointer of an optional float32 vector of n elements."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise SapoError(f"{what} must be contiguous float32 with {n} elements")
+    return t.data_ptr()
+
+
+def _weight(t: Optional[torch.Tensor], H: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.shape != (H,) or not t.is_contiguous():
+        raise SapoError(f"{what} must be contiguous with {H} elements")
+    return t.data_ptr()
+
+
+_norm_cfgs: Dict[tuple, NormCfgC] = {}
 
 
 def _norm_cfg(kind: str, eps: float, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor]) -> NormCfgC:
-    if kind not in NORM_KINDS:
-        raise SapoError(f"kind is one of {tuple(NORM_KINDS)}")
-    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+    """The parameter block of a norm call; the blocks are read only and few, so they are kept."""
+    w = gamma.dtype if gamma is not None else (beta.dtype if beta is not None else torch.float32)
+    cfg = _norm_cfgs.get((kind, eps, w))
+    if beta is not None and beta.dtype != w:
         raise SapoError("gamma and beta must have the same element type")
-    w = gamma if gamma is not None else beta
-    return NormCfgC(NORM_KINDS[kind], eps, DTYPE_F32 if w is None else _dtype_code(w))
-
-
-def _check_vectors(n: int, fp32: bool, **vectors: Optional[torch.Tensor]) -> None:
-    for name, v in vectors.items():
-        if v is not None and (v.numel() != n or not v.is_contiguous() or (fp32 and v.dtype != torch.float32)):
-            raise SapoError(f"{name} must be contiguous{' float32' if fp32 else ''} with {n} elements")
+    if cfg is None:
+        if kind not in NORM_KINDS:
+            raise SapoError(f"kind is one of {tuple(NORM_KINDS)}")
+        if w not in _DTYPE_CODES:
+            raise SapoError(f"unsupported element type {w}")
+        cfg = NormCfgC(NORM_KINDS[kind], eps, _DTYPE_CODES[w])
+        if len(_norm_cfgs) < 64:
+            _norm_cfgs[(kind, eps, w)] = cfg
+    return cfg
 
 
 def sapo_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, kind: str,
@@ -657,15 +702,11 @@ def sapo_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional
     """y = layer / RMS norm of the rows of x; with ckpt, x is stored in 8 bits in the same pass."""
     _require_cuda()
     T, H = x.shape
-    _check_vectors(H, False, gamma=gamma, beta=beta)
-    _check_vectors(T, True, mean=mean, rstd=rstd)
-    if y.shape != x.shape or (ckpt is not None and (ckpt.H != H or ckpt.data.shape[0] != T)):
-        raise SapoError("y and the checkpoint must have the shape of x")
-    cfg = _norm_cfg(kind, eps, gamma, beta)
-    cc = ckpt.c() if ckpt is not None else None
-    rc = load().sapo_norm_fwd(_p(x), _dtype_code(x), T, H, _rows(x, "x"), _p(gamma), _p(beta), C.byref(cfg), _p(y),
-                              _dtype_code(y), _rows(y, "y"), _p(mean), _p(rstd),
-                              C.byref(cc) if cc is not None else None, _p(status), _stream())
+    px, tx, ldx = _rows(x, T, H, "x")
+    py, ty, ldy = _rows(y, T, H, "y")
+    rc = load().sapo_norm_fwd(px, tx, T, H, ldx, _weight(gamma, H, "gamma"), _weight(beta, H, "beta"),
+                              _norm_cfg(kind, eps, gamma, beta), py, ty, ldy, _vector(mean, T, "mean"),
+                              _vector(rstd, T, "rstd"), None if ckpt is None else ckpt.c(T, H), _p(status), _stream())
     _check(rc, "sapo_norm_fwd")
 
 
@@ -674,13 +715,10 @@ def sapo_norm_replay(ckpt: Ckpt8, gamma: Optional[torch.Tensor], beta: Optional[
     """The norm's output again, from the 8-bit checkpoint of its input and the stored statistics."""
     _require_cuda()
     T, H = y.shape
-    _check_vectors(H, False, gamma=gamma, beta=beta)
-    _check_vectors(T, True, mean=mean, rstd=rstd)
-    if ckpt.H != H or ckpt.data.shape[0] != T:
-        raise SapoError("y must have the shape of the checkpoint")
-    cfg, cc = _norm_cfg(kind, 0.0, gamma, beta), ckpt.c()
-    rc = load().sapo_norm_replay(C.byref(cc), T, H, _p(gamma), _p(beta), C.byref(cfg), _p(mean), _p(rstd), _p(y),
-                                 _dtype_code(y), _rows(y, "y"), _stream())
+    py, ty, ldy = _rows(y, T, H, "y")
+    rc = load().sapo_norm_replay(ckpt.c(T, H), T, H, _weight(gamma, H, "gamma"), _weight(beta, H, "beta"),
+                                 _norm_cfg(kind, 0.0, gamma, beta), _vector(mean, T, "mean"), _vector(rstd, T, "rstd"),
+                                 py, ty, ldy, _stream())
     _check(rc, "sapo_norm_replay")
 
 
@@ -694,19 +732,14 @@ def sapo_norm_bwd(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: Opti
     """dx, dgamma, dbeta of sapo_norm_fwd; x is the forward's input or its 8-bit checkpoint (a Ckpt8)."""
     _require_cuda()
     T, H = dy.shape
-    _check_vectors(H, False, gamma=gamma)
-    _check_vectors(H, True, dgamma=dgamma, dbeta=dbeta)
-    _check_vectors(T, True, mean=mean, rstd=rstd)
     held = isinstance(x, Ckpt8)
-    if dx.shape != dy.shape or (x.data.shape[0] != T or x.H != H if held else x.shape != dy.shape):
-        raise SapoError("dy, dx and x must have the same shape")
-    cfg = _norm_cfg(kind, 0.0, gamma, None)
-    cc = x.c() if held else None
-    rc = load().sapo_norm_bwd(_p(dy), _dtype_code(dy), _rows(dy, "dy"), None if held else _p(x),
-                              DTYPE_BF16 if held else _dtype_code(x), 0 if held else _rows(x, "x"),
-                              C.byref(cc) if held else None, T, H, _p(gamma), C.byref(cfg), _p(mean), _p(rstd), _p(dx),
-                              _dtype_code(dx), _rows(dx, "dx"), _p(dgamma), _p(dbeta), 1 if accumulate else 0,
-                              _p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+    pd, td, ldd = _rows(dy, T, H, "dy")
+    po, to, ldo = _rows(dx, T, H, "dx")
+    px, tx, ldx = (None, DTYPE_BF16, 0) if held else _rows(x, T, H, "x")
+    rc = load().sapo_norm_bwd(pd, td, ldd, px, tx, ldx, x.c(T, H) if held else None, T, H, _weight(gamma, H, "gamma"),
+                              _norm_cfg(kind, 0.0, gamma, None), _vector(mean, T, "mean"), _vector(rstd, T, "rstd"),
+                              po, to, ldo, _vector(dgamma, H, "dgamma"), _vector(dbeta, H, "dbeta"),
+                              1 if accumulate else 0, _p(workspace), 0 if workspace is None else workspace.nbytes,
                               _stream())
     _check(rc, "sapo_norm_bwd")
 
@@ -715,19 +748,13 @@ def sapo_ckpt8_store(x: torch.Tensor, ckpt: Ckpt8, status: torch.Tensor) -> None
     """x [T, H] into an 8-bit checkpoint from alloc_ckpt8."""
     _require_cuda()
     T, H = x.shape
-    if ckpt.H != H or ckpt.data.shape[0] != T:
-        raise SapoError("the checkpoint must have the shape of x")
-    cc = ckpt.c()
-    rc = load().sapo_ckpt8_store(_p(x), _dtype_code(x), T, H, _rows(x, "x"), C.byref(cc), _p(status), _stream())
-    _check(rc, "sapo_ckpt8_store")
+    px, tx, ldx = _rows(x, T, H, "x")
+    _check(load().sapo_ckpt8_store(px, tx, T, H, ldx, ckpt.c(T, H), _p(status), _stream()), "sapo_ckpt8_store")
 
 
 def sapo_ckpt8_restore(ckpt: Ckpt8, x: torch.Tensor) -> None:
     """The values an 8-bit checkpoint stands for."""
     _require_cuda()
     T, H = x.shape
-    if ckpt.H != H or ckpt.data.shape[0] != T:
-        raise SapoError("x must have the shape of the checkpoint")
-    cc = ckpt.c()
-    rc = load().sapo_ckpt8_restore(C.byref(cc), T, H, _p(x), _dtype_code(x), _rows(x, "x"), _stream())
-    _check(rc, "sapo_ckpt8_restore")
+    px, tx, ldx = _rows(x, T, H, "x")
+    _check(load().sapo_ckpt8_restore(ckpt.c(T, H), T, H, px, tx, ldx, _stream()), "sapo_ckpt8_restore")

@@ -370,6 +370,7 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_kernel(NormBwdArgs 
       }
     }
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the rows of a warp, then the warps' rows one after the other
   for (int d = 16; d >= a.tpr; d >>= 1) {
@@ -416,10 +417,11 @@ __global__ void __launch_bounds__(1024)
 norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float* dgamma, float* dbeta, int accumulate) {
   __shared__ float sh[32][33];
   float* out = blockIdx.y == 0 ? dgamma : dbeta;
-  if (out == nullptr) return;
+  if (out == nullptr) { asm volatile("griddepcontrol.wait;" ::: "memory"); return; }
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + lane;
   float s = 0.f;
+  asm volatile("griddepcontrol.wait;" ::: "memory");      // launched while the backward's last blocks still run
   if (col < H)
     for (int b = w; b < n_parts; b += 32) s += part[((int64_t)b * 2 + blockIdx.y) * H + col];
   sh[w][lane] = s;
@@ -534,6 +536,69 @@ __device__ __forceinline__ uint2 quantise8(const float2 (&x)[4], float& scale, b
   return make_uint2(w[0], w[1]);
 }
 
+// 8 columns to p (fp32 or bf16 as YF says)
+template <bool YF>
+__device__ __forceinline__ void put8(void* p, int64_t at, const float2 (&x)[4]) {
+  if (YF) {
+    float* f = static_cast<float*>(p) + at;
+    *reinterpret_cast<float4*>(f) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+    *reinterpret_cast<float4*>(f + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at) =
+        make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
+  }
+}
+
+// Checkpoints alone, whole vectors: half a warp takes a group of 128 columns, CKPT_GROUPS of them with all
+// loads before the first use.  Row and group of a half-warp's next group follow from those of its last one.
+constexpr int CKPT_GROUPS = 4;
+template <class TX, bool RESTORE>
+__global__ void __launch_bounds__(256) ckpt8_vec_kernel(Ckpt8Args a, int64_t step_rows, int32_t step_groups) {
+  const int32_t groups = ceil_div(a.H, Q8_GROUP);
+  const int64_t id = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+  const int col_in = (threadIdx.x & 15) * 8;
+  int64_t row = id / groups;
+  int32_t g = (int32_t)(id - row * groups);
+  auto next = [&] { row += step_rows; g += step_groups; if (g >= groups) { g -= groups; ++row; } };
+  TX* x = static_cast<TX*>(a.x.p);
+  // (both halves of a warp stay as long as one of them has rows: they agree on shuffles)
+  while (__any_sync(0xffffffffu, row < a.T)) {
+    int64_t rows[CKPT_GROUPS]; int32_t cols[CKPT_GROUPS]; bool live[CKPT_GROUPS];
+    float2 v[CKPT_GROUPS][4]; float s[CKPT_GROUPS];
+    #pragma unroll
+    for (int k = 0; k < CKPT_GROUPS; ++k) {
+      rows[k] = row; cols[k] = g * Q8_GROUP + col_in;
+      live[k] = row < a.T && cols[k] < a.H;
+      s[k] = 0.f;
+      #pragma unroll
+      for (int j = 0; j < 4; ++j) v[k][j] = both(0.f);
+      if (live[k]) {
+        if (RESTORE) { load8(a.q.p + row * a.q.ld + cols[k], v[k]); s[k] = a.q.scale[row * a.q.ld_scale + g]; }
+        else load8(x + row * a.x.ld + cols[k], v[k]);
+      }
+      next();
+    }
+    #pragma unroll
+    for (int k = 0; k < CKPT_GROUPS; ++k) {
+      if (RESTORE) {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(s[k]));
+        if (live[k]) put8<sizeof(TX) == 4>(x, rows[k] * a.x.ld + cols[k], v[k]);
+      } else {
+        float scale; bool bad;
+        const uint2 q = quantise8(v[k], scale, bad);
+        if (live[k]) {
+          *reinterpret_cast<uint2*>(a.q.p + rows[k] * a.q.ld + cols[k]) = q;
+          if (col_in == 0) {
+            a.q.scale[rows[k] * a.q.ld_scale + cols[k] / Q8_GROUP] = scale;
+            if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+          }
+        }
+      }
+    }
+  }
+}
+
 // One warp's part of a row of TX in shared memory: VPL * 256 elements.
 template <class TX, int VPL>
 struct WarpRow {
@@ -619,19 +684,6 @@ __device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stage
     for (int i = lane * 16; i < bytes; i += 512) *reinterpret_cast<uint4*>(mine + s * stage_bytes + i) = make_uint4(0u, 0u, 0u, 0u);
   __syncwarp();
 }
-// 8 columns to p (fp32 or bf16 as YF says)
-template <bool YF>
-__device__ __forceinline__ void put8(void* p, int at, const float2 (&x)[4]) {
-  if (YF) {
-    float* f = static_cast<float*>(p) + at;
-    *reinterpret_cast<float4*>(f) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
-    *reinterpret_cast<float4*>(f + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
-  } else {
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at) =
-        make_uint4(pack_bf16x2(x[0].x, x[0].y), pack_bf16x2(x[1].x, x[1].y), pack_bf16x2(x[2].x, x[2].y), pack_bf16x2(x[3].x, x[3].y));
-  }
-}
-
 // TX int8_t: replay from a checkpoint (a.q), statistics given.
 template <class TX, int VPL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
@@ -909,6 +961,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     };
     if (a.dx.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the groups' sums one after the other, through the ring (no copy is in flight any more)
   copy_wait<0>();
@@ -1100,9 +1153,11 @@ static int bwd_ring(const NormBwdArgs& a, const RingPlan& p, int blocks, bool la
 template <int NV, bool REPLAY>
 static int launch_fwd_nv(const NormFwdArgs& a, bool vec, const RowPlan& p, int sms, cudaStream_t st) {
   auto kernel = vec ? norm_fwd_kernel<NV, true, REPLAY> : norm_fwd_kernel<NV, false, REPLAY>;
+  static int cache[2][2][MAX_DEVICES] = {{{0}}};
+  const int per_sm = resident_blocks(kernel, p.threads, 0, cache[vec][p.threads > NORM_THREADS]);
+  if (per_sm == 0) return SAPO_ERR_CUDA;
   int64_t blocks = ceil_div<int64_t>(a.T, p.threads / p.tpr);
-  const int64_t most = (int64_t)sms * resident_blocks_per_sm(kernel, p.threads);
-  if (blocks > most) blocks = most;
+  if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
   KernelScope scope(SAPO_K_NORM_FWD, st);
   kernel<<<(int)blocks, p.threads, 0, st>>>(a);
   return check_launch();
@@ -1146,18 +1201,39 @@ static int launch_bwd(const NormBwdArgs& a, bool vec, const RowPlan& p, int bloc
   }
 }
 
+template <class TX, bool RESTORE>
+static int launch_ckpt8_vec(const Ckpt8Args& a, int sms, cudaStream_t st) {
+  static int cache[MAX_DEVICES] = {0};
+  auto kernel = ckpt8_vec_kernel<TX, RESTORE>;
+  const int per_sm = resident_blocks(kernel, 256, 0, cache);
+  if (per_sm == 0) return SAPO_ERR_CUDA;
+  const int32_t groups = ceil_div(a.H, Q8_GROUP);
+  int64_t blocks = ceil_div<int64_t>(a.T * groups, 16 * CKPT_GROUPS);
+  if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
+  const int64_t halves = blocks * 16;
+  KernelScope scope(SAPO_K_CKPT8, st);
+  kernel<<<(int)blocks, 256, 0, st>>>(a, halves / groups, (int32_t)(halves % groups));
+  return check_launch();
+}
+
 static int launch_ckpt8(const Mat& x, const Q8Mat& q, int64_t T, int32_t H, bool restore, int32_t* status, cudaStream_t st) {
   if (T == 0) return SAPO_OK;
   const int sms = sm_count();
   if (sms <= 0) return SAPO_ERR_CUDA;
   Ckpt8Args a{x, q, T, H, ceil_div(H, 8), 0, status};
-  while ((1 << a.vec_log2) < a.nvec) ++a.vec_log2;
   const bool vec = vec_ok(x) && vec_ok(q);
+  if (vec && H % 8 == 0) {
+    if (x.dtype == SAPO_DTYPE_F32) return restore ? launch_ckpt8_vec<float, true>(a, sms, st) : launch_ckpt8_vec<float, false>(a, sms, st);
+    return restore ? launch_ckpt8_vec<__nv_bfloat16, true>(a, sms, st) : launch_ckpt8_vec<__nv_bfloat16, false>(a, sms, st);
+  }
+  while ((1 << a.vec_log2) < a.nvec) ++a.vec_log2;
+  static int cache[4][MAX_DEVICES] = {{0}};
   auto kernel = restore ? (vec ? ckpt8_kernel<true, true> : ckpt8_kernel<false, true>)
                         : (vec ? ckpt8_kernel<true, false> : ckpt8_kernel<false, false>);
+  const int per_sm = resident_blocks(kernel, 256, 0, cache[2 * restore + vec]);
+  if (per_sm == 0) return SAPO_ERR_CUDA;
   int64_t blocks = ceil_div<int64_t>(T << a.vec_log2, 256);
-  const int64_t most = (int64_t)sms * resident_blocks_per_sm(kernel, 256);
-  if (blocks > most) blocks = most;
+  if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
   KernelScope scope(SAPO_K_CKPT8, st);
   kernel<<<(int)blocks, 256, 0, st>>>(a);
   return check_launch();
@@ -1253,9 +1329,18 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
   if (ring) rc = bwd_ring(a, rp, blocks, true, st);
   else rc = h_ckpt ? launch_bwd<true>(a, vec, p, blocks, st) : launch_bwd<false>(a, vec, p, blocks, st);
   if (rc != SAPO_OK || !reduce || blocks == 1) return rc;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(ceil_div(H, 32), 2);
+  cfg.blockDim = dim3(1024);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
   KernelScope scope(SAPO_K_NORM_REDUCE, st);
-  norm_reduce_kernel<<<dim3(ceil_div(H, 32), 2), 1024, 0, st>>>(a.part, blocks, H, dgamma, dbeta, accumulate);
-  return check_launch();
+  return cudaLaunchKernelEx(&cfg, norm_reduce_kernel, (const float*)a.part, blocks, H, dgamma, dbeta, (int)accumulate) == cudaSuccess
+             ? SAPO_OK : SAPO_ERR_CUDA;
 }
 
 extern "C" int sapo_ckpt8_store(const void* x, int32_t x_dtype, int64_t T, int32_t H, int64_t ld_x,

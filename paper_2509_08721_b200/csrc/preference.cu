@@ -75,6 +75,14 @@ __device__ __forceinline__ float token_ratio(const PrefArgs& a, int32_t t) {
   return a.ref_logp != nullptr ? a.logp[t] - a.ref_logp[t] : a.logp[t];
 }
 
+__device__ __forceinline__ float load_from_first(const float* p) {
+  uint32_t at;
+  float x;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+
 // A cluster of blocks per question.  The question's tokens are one range, cut into equal pieces for the
 // cluster's warps whatever its sequences' lengths are, so that few long sequences keep as many SMs
 // busy as many short ones:
@@ -84,19 +92,25 @@ __device__ __forceinline__ float token_ratio(const PrefArgs& a, int32_t t) {
 //   2. the first block adds up each sequence's pieces (in order), then the pairs: a warp per completion,
 //      lanes over the others
 //   3. every warp writes the factors of its tokens
+// A small batch is a chain of waits for memory (each about half a microsecond), so a question's offsets and
+// rewards are read into shared memory at once, and what passes between the steps stays there, for questions of
+// up to PREF_SEQS completions.
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
-  __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS];
+  __shared__ int32_t cu_s[PREF_SEQS + 1];
+  __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS], g_s[PREF_SEQS];     // sums, rewards, factors
   __shared__ double sums[3][PREF_WARPS];
   __shared__ float scale_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t Tc = (int32_t)a.T;
   const int rank = (int)cluster_rank(), size = (int)cluster_size();
   const int gw = rank * PREF_WARPS + warp, n_warps = size * PREF_WARPS;
+  const int32_t cluster = (int32_t)(blockIdx.x / size);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   bool bad_offset = false, bad_value = false, bad_reward = false;
-  {
-    // what no question covers: sequences before the first and after the last one, and their tokens
+  if (cluster >= a.q_clusters) {
+    // the clusters behind those of the questions: what no question covers, sequences before the first and after the
+    // last one and their tokens, gets zeros
     bool ignore = false;
     const int32_t s_lo = clamp_to(a.group_offsets[0], a.S, ignore);
     int32_t s_hi = clamp_to(a.group_offsets[a.Q], a.S, ignore);
@@ -104,19 +118,32 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     const int32_t t_lo = clamp_to(a.cu[s_lo], Tc, ignore);
     int32_t t_hi = clamp_to(a.cu[s_hi], Tc, ignore);
     if (t_hi < t_lo) t_hi = t_lo;
-    const int64_t first = (int64_t)blockIdx.x * PREF_THREADS + threadIdx.x, step = (int64_t)gridDim.x * PREF_THREADS;
+    const int64_t skip = (int64_t)a.q_clusters * size;
+    const int64_t first = (blockIdx.x - skip) * PREF_THREADS + threadIdx.x, step = (gridDim.x - skip) * PREF_THREADS;
     for (int64_t i = first; i < (int64_t)t_lo + (Tc - t_hi); i += step) a.gscale[i < t_lo ? i : t_hi + (i - t_lo)] = 0.f;
     for (int64_t i = first; i < (int64_t)s_lo + (a.S - s_hi); i += step) {
       const int64_t s = i < s_lo ? i : s_hi + (i - s_lo);
       a.seq_logratio[s] = 0.f;
       a.seq_grad[s] = 0.f;
     }
+    return;
   }
-  for (int32_t q = blockIdx.x / size; q < a.Q; q += gridDim.x / size) {
+  for (int32_t q = cluster; q < a.Q; q += a.q_clusters) {
     int32_t s0, s1;
     offset_range(a.group_offsets, q, a.S, s0, s1, bad_offset);
-    const int32_t ta = clamp_to(a.cu[s0], Tc, bad_offset);
-    int32_t tb = clamp_to(a.cu[s1], Tc, bad_offset);
+    const bool kept = s1 - s0 <= PREF_SEQS;
+    if (kept) {
+      // (the previous question's readers are behind the barrier that ended its step 2, or read their own block's)
+      __syncthreads();
+      for (int32_t i = threadIdx.x; i <= s1 - s0; i += PREF_THREADS) {
+        cu_s[i] = a.cu[s0 + i];
+        if (i < s1 - s0) r_s[i] = a.rewards[s0 + i];
+      }
+      __syncthreads();
+    }
+    const int32_t* cu = kept ? cu_s - s0 : a.cu;             // indexed by sequence
+    const int32_t ta = clamp_to(cu[s0], Tc, bad_offset);
+    int32_t tb = clamp_to(cu[s1], Tc, bad_offset);
     if (tb < ta) tb = ta;
     // tokens per warp: whole steps of 32
     const int32_t piece = (int32_t)round_up<int64_t>(ceil_div<int64_t>((int64_t)tb - ta, n_warps), 32) + (tb == ta ? 32 : 0);
@@ -127,7 +154,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     int32_t s_first = s0;
     if (begin < end) {
       int32_t lo = s0, hi = s1;
-      while (lo < hi) { const int32_t mid = lo + ((hi - lo) >> 1); if (a.cu[mid + 1] > begin) hi = mid; else lo = mid + 1; }
+      while (lo < hi) { const int32_t mid = lo + ((hi - lo) >> 1); if (cu[mid + 1] > begin) hi = mid; else lo = mid + 1; }
       s_first = lo;
     }
     bool masked = false;                       // a token of this lane's in the range is masked
@@ -135,7 +162,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     if (begin < end) {
       for (int32_t s = s_first; s < s1; ++s) {
         int32_t t0, t1;
-        offset_range(a.cu, s, Tc, t0, t1, bad_offset);
+        offset_range(cu, s, Tc, t0, t1, bad_offset);
         if (t0 >= end) break;
         const int32_t from = t0 > begin ? t0 : begin, to = t1 < end ? t1 : end;
         if (from >= to) continue;
@@ -154,8 +181,9 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         }
         const float sum = warp_sum((part[0] + part[1]) + (part[2] + part[3]));
         if (lane == 0) {
-          if (t0 > begin) a.seq_logratio[s] = sum;
-          else store_to_first(&head[gw], sum);
+          if (t0 <= begin) store_to_first(&head[gw], sum);
+          else if (kept) store_to_first(&R_s[s - s0], sum);
+          else a.seq_logratio[s] = sum;
         }
       }
     }
@@ -163,14 +191,13 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     cluster_barrier();
     // 2.
     if (rank == 0) {
-      const bool kept = s1 - s0 <= PREF_SEQS;
       for (int32_t s = s0 + warp; s < s1; s += PREF_WARPS) {
         int32_t t0, t1;
-        offset_range(a.cu, s, Tc, t0, t1, bad_offset);
+        offset_range(cu, s, Tc, t0, t1, bad_offset);
         const int32_t n = t1 - t0;
         float R = 0.f;
         if (n > 0) {
-          // its pieces: the first where it begins (in seq_logratio unless it begins a range), then the heads of the
+          // its pieces: the first where it begins (in R_s unless it begins a range), then the heads of the
           // ranges that it runs into.  (Malformed offsets, reported above, could point outside the ranges.)
           const int32_t w0 = t0 < ta ? 0 : (t0 - ta) / piece;
           int32_t w1 = t1 <= ta ? 0 : (t1 - 1 - ta) / piece;
@@ -178,11 +205,12 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           const bool inside = t0 - ta > w0 * piece;
           float x = 0.f;
           for (int32_t w = w0 + (inside ? 1 : 0) + lane; w <= w1; w += 32) x += head[w];
-          R = warp_sum(x) + (inside ? __ldcg(a.seq_logratio + s) : 0.f);
+          R = warp_sum(x) + (inside ? (kept ? R_s[s - s0] : __ldcg(a.seq_logratio + s)) : 0.f);
           if (a.length_norm) R /= (float)n;
         }
+        __syncwarp();
         if (lane == 0) {
-          const float r = a.rewards[s];
+          const float r = kept ? r_s[s - s0] : a.rewards[s];
           if (!isfinite(r)) bad_reward = true;
           a.seq_logratio[s] = R;
           // a completion takes part if it has a token, a finite reward and a finite sum
@@ -194,7 +222,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         if (kept) return r_s[s - s0];
         bool ignore = false;
         int32_t t0, t1;
-        offset_range(a.cu, s, Tc, t0, t1, ignore);
+        offset_range(cu, s, Tc, t0, t1, ignore);
         const float r = a.rewards[s];
         return t1 > t0 && isfinite(r) && isfinite(__ldcg(a.seq_logratio + s)) ? r : NAN;
       };
@@ -232,22 +260,29 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           if (wins) { loss += (double)l; margin += (double)h; count += 1.0; }     // each pair once
         }
         f = warp_sum(f);
-        if (lane == 0) a.seq_grad[i] = (float)f;             // scaled below, once the pairs are counted
+        if (lane == 0) { if (kept) g_s[i - s0] = (float)f; else a.seq_grad[i] = (float)f; }   // scaled below, once the pairs are counted
       }
       loss = warp_sum(loss); margin = warp_sum(margin); count = warp_sum(count);
       if (lane == 0) { sums[0][warp] = loss; sums[1][warp] = margin; sums[2][warp] = count; }
       __syncthreads();
-      if (threadIdx.x == 0) {
-        loss = margin = count = 0.0;
-        for (int w = 0; w < PREF_WARPS; ++w) { loss += sums[0][w]; margin += sums[1][w]; count += sums[2][w]; }
+      if (warp == 0) {
+        loss = warp_sum(lane < PREF_WARPS ? sums[0][lane] : 0.0);
+        margin = warp_sum(lane < PREF_WARPS ? sums[1][lane] : 0.0);
+        count = warp_sum(lane < PREF_WARPS ? sums[2][lane] : 0.0);
         const double per = count > 0.0 ? 1.0 / count : 0.0;
-        a.q_loss[q] = (float)(loss * per);
-        if (a.q_margin != nullptr) a.q_margin[q] = (float)(margin * per);
-        if (a.q_pairs != nullptr) a.q_pairs[q] = (int32_t)count;
-        scale_s = (float)((double)a.grad_scale * (double)a.beta * per / (double)a.Q);
+        if (lane == 0) {
+          a.q_loss[q] = (float)(loss * per);
+          if (a.q_margin != nullptr) a.q_margin[q] = (float)(margin * per);
+          if (a.q_pairs != nullptr) a.q_pairs[q] = (int32_t)count;
+          scale_s = (float)((double)a.grad_scale * (double)a.beta * per / (double)a.Q);
+        }
       }
       __syncthreads();
-      for (int32_t i = s0 + threadIdx.x; i < s1; i += PREF_THREADS) a.seq_grad[i] *= scale_s;
+      for (int32_t i = s0 + threadIdx.x; i < s1; i += PREF_THREADS) {
+        const float g = (kept ? g_s[i - s0] : a.seq_grad[i]) * scale_s;
+        if (kept) g_s[i - s0] = g;
+        a.seq_grad[i] = g;
+      }
     }
     cluster_barrier();
     // 3.
@@ -255,11 +290,11 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
       for (int32_t s = s_first; s < s1; ++s) {
         bool ignore = false;
         int32_t t0, t1;
-        offset_range(a.cu, s, Tc, t0, t1, ignore);
+        offset_range(cu, s, Tc, t0, t1, ignore);
         if (t0 >= end) break;
         const int32_t from = t0 > begin ? t0 : begin, to = t1 < end ? t1 : end;
         if (from >= to) continue;
-        float g = __ldcg(a.seq_grad + s);
+        float g = kept ? load_from_first(&g_s[s - s0]) : __ldcg(a.seq_grad + s);
         if (a.length_norm) g /= (float)(t1 - t0);
         // the lane that summed a token writes its factor, and knows whether any of its tokens was masked
         for (int32_t t = from + lane; t < to; t += 32) a.gscale[t] = masked && !isfinite(token_ratio(a, t)) ? 0.f : g;
@@ -269,7 +304,8 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   if (bad_offset) raise_status(a.status, SAPO_ST_BAD_INDEX);
   if (bad_value && a.ref_logp != nullptr) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
   if (bad_reward) raise_status(a.status, SAPO_ST_NONFINITE_REWARD);
-  // the first block's shared memory stays until the others have written to it (the last barrier above)
+  // the first block's shared memory stays until the others have read the factors from it
+  cluster_barrier();
 }
 
 // loss = the mean of the questions' losses
@@ -306,7 +342,7 @@ static int pref_cluster(int64_t T, int32_t Q, int sms) {
   return c;
 }
 
-int launch_preference(const PrefArgs& a, cudaStream_t st) {
+int launch_preference(PrefArgs a, cudaStream_t st) {
   const int sms = sm_count();
   const int dev = current_device();
   if (sms <= 0 || dev < 0) return SAPO_ERR_CUDA;
@@ -317,9 +353,13 @@ int launch_preference(const PrefArgs& a, cudaStream_t st) {
   }
   const int cluster = pref_cluster(a.T, a.Q, sms);
   const int64_t most = (int64_t)sms * 4 / cluster;
+  a.q_clusters = (int32_t)(a.Q < most ? a.Q : most);
+  // clusters for what no question covers: a capacity behind the last token can be large
+  int64_t outside = ceil_div<int64_t>(a.T, (int64_t)65536 * cluster);
+  outside = outside < 1 ? 1 : (outside > 32 ? 32 : outside);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[1];
-  cfg.gridDim = dim3((unsigned)((a.Q < most ? a.Q : most) * cluster));
+  cfg.gridDim = dim3((unsigned)((a.q_clusters + outside) * cluster));
   cfg.blockDim = dim3(PREF_THREADS);
   cfg.stream = st;
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -360,6 +400,6 @@ extern "C" int sapo_preference_loss(const float* logp, const float* ref_logp, in
   // an empty batch has no pointers to read through, but the kernel asks which kind of input it has
   PrefArgs a{logp, ref_logp, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
              h_cfg->grad_scale, h_cfg->kind, h_cfg->pairs, h_cfg->length_norm, gscale, seq_logratio, seq_grad,
-             q_loss, q_margin, q_pairs, loss, status};
+             q_loss, q_margin, q_pairs, loss, status, 0};
   return launch_preference(a, static_cast<cudaStream_t>(stream));
 }
