@@ -1339,18 +1339,22 @@ __global__ void __launch_bounds__(256) pref_scale_kernel(PrefScaleArgs a) {
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n_warps = (int64_t)gridDim.x * 8;
   for (int64_t t = warp; t < a.T; t += n_warps) {
     const float g = a.gscale[t], sum = a.sum[t];
-    const float scale = g == 0.f ? 0.f : -g / sum;
-    if (lane == 0) {
-      a.row_scale[t] = scale;
-      if (scale != 0.f) {
+    float scale = g == 0.f ? 0.f : -g / sum;
+    if (scale != 0.f) {
+      // The chosen token's entry outweighs the rest of its row (1 - p_y is the sum of the other probabilities, so
+      // at least their norm): the scale takes up that entry's rounding to bf16, and what was rounding of the largest
+      // entry becomes, at half an ulp, a relative error of the small ones.
+      const int32_t y = a.ids[t];                         // in [0, V): a masked token has g = 0
+      const float entry = ex2(fmaf(a.zy[t], LOG2E, -a.c2[t])) - sum;
+      const __nv_bfloat16 kept = __float2bfloat16_rn(entry);
+      if (__bfloat162float(kept) != 0.f) scale *= entry / __bfloat162float(kept);
+      const int64_t tile = (t >> 7) * a.nvt + (y >> 6);
+      if (lane == 0 && SAPO_IN_BOUNDS(y >= 0 && y < a.V && tile * BM + (t & 127) < a.panel_rows)) {
+        a.panel[(tile * BM + (t & 127)) * 64 + (y & 63)] = kept;
         if (a.active_mask != nullptr) atomicOr(&a.active_mask[t >> 12], 1u << ((t >> 7) & 31));
-        const int32_t y = a.ids[t];                       // in [0, V): a masked token has g = 0
-        const float ey = ex2(fmaf(a.zy[t], LOG2E, -a.c2[t]));
-        const int64_t tile = (t >> 7) * a.nvt + (y >> 6);
-        if (SAPO_IN_BOUNDS(y >= 0 && y < a.V && tile * BM + (t & 127) < a.panel_rows))
-          a.panel[(tile * BM + (t & 127)) * 64 + (y & 63)] = __float2bfloat16_rn(ey - sum);
       }
     }
+    if (lane == 0) a.row_scale[t] = scale;
     if (!(sum < EXP_CAP)) {
       // exponentials that are huge or not finite: zero times them would still spoil dW_head
       uint32_t* row32 = reinterpret_cast<uint32_t*>(a.panel);
