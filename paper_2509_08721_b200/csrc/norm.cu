@@ -508,32 +508,68 @@ __device__ __forceinline__ void load_weight8(const void* w, int32_t dtype, int c
   if (dtype == SAPO_DTYPE_F32) load8(static_cast<const float*>(w) + col, x);
   else load8(static_cast<const __nv_bfloat16*>(w) + col, x);
 }
-// Whole vectors of a group: as quantise8, the rounding to an integer by adding 1.5 2^23 (round to
-// nearest even, the integer in the last bits).  Scalar operations: the product has to be rounded before
-// the sum, and a pair of them is compiled to one fma.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float d;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
-__device__ __forceinline__ uint2 quantise8(const float2 (&x)[4], float& scale, bool& bad) {
-  float a = max_nan(max_nan(max_nan(fabsf(x[0].x), fabsf(x[0].y)), max_nan(fabsf(x[1].x), fabsf(x[1].y))),
-                    max_nan(max_nan(fabsf(x[2].x), fabsf(x[2].y)), max_nan(fabsf(x[3].x), fabsf(x[3].y))));
+// Quantises N groups whose 16 threads (half a warp) hold whole vectors x[v], v < N; called by whole warps.
+// The maxima are reduced together: each exchange halves how many groups a lane still carries, so that at the
+// end lane (v << shift) of the half warp has group v's, computes its scale and reciprocal (once, not once per lane)
+// and hands the reciprocal back.  The rounding to an integer adds 1.5 2^23 (to nearest even, the integer in
+// the last bits); the product before it is rounded by itself, in pairs, and the sum is scalar: a pair of both
+// is compiled to one fma.
+// scale, bad: of group `slot` = (lane & 15) >> shift, in all lanes (a slot may be N or more: then 0 and false).
+template <int N>
+__device__ __forceinline__ void quantise(const float2 (&x)[N][4], uint2 (&q)[N], int& slot, float& scale, bool& bad) {
+  constexpr int P = N == 1 ? 1 : (N == 2 ? 2 : (N <= 4 ? 4 : 8));           // N rounded up to a power of two
+  constexpr int SHIFT = P == 1 ? 4 : (P == 2 ? 3 : (P == 4 ? 2 : 1));
+  static_assert(N <= 8, "a half warp reduces up to 8 groups");
+  const int lane = threadIdx.x & 31;
+  float a[P];
   #pragma unroll
-  for (int d = 8; d > 0; d >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, d));
-  bad = !(a < INFINITY);
-  const bool some = a >= Q8_TINY && !bad;
-  const float inv = 127.f * __frcp_rn(a);
-  auto integer = [&](float v) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.f)); };
-  scale = bad ? __int_as_float(0x7fc00000) : (some ? a * (1.f / 127.f) : 0.f);
-  uint32_t w[2];
+  for (int v = 0; v < P; ++v)
+    a[v] = v >= N ? 0.f
+                  : max_nan(max_nan(max_nan(fabsf(x[v < N ? v : 0][0].x), fabsf(x[v < N ? v : 0][0].y)),
+                                    max_nan(fabsf(x[v < N ? v : 0][1].x), fabsf(x[v < N ? v : 0][1].y))),
+                            max_nan(max_nan(fabsf(x[v < N ? v : 0][2].x), fabsf(x[v < N ? v : 0][2].y)),
+                                    max_nan(fabsf(x[v < N ? v : 0][3].x), fabsf(x[v < N ? v : 0][3].y))));
+  int d = 8;
   #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t lo = __byte_perm(integer(x[2 * h].x), integer(x[2 * h].y), 0x0040);
-    const uint32_t hi = __byte_perm(integer(x[2 * h + 1].x), integer(x[2 * h + 1].y), 0x0040);
-    w[h] = some ? __byte_perm(lo, hi, 0x5410) : 0u;
+  for (int half = P / 2; half >= 1; half >>= 1) {
+    const bool upper = (lane & d) != 0;
+    #pragma unroll
+    for (int k = 0; k < half; ++k) {
+      const float other = __shfl_xor_sync(0xffffffffu, upper ? a[k] : a[k + half], d);
+      a[k] = max_nan(upper ? a[k + half] : a[k], other);
+    }
+    d >>= 1;
   }
-  return make_uint2(w[0], w[1]);
+  for (; d > 0; d >>= 1) a[0] = max_nan(a[0], __shfl_xor_sync(0xffffffffu, a[0], d));
+  slot = (lane & 15) >> SHIFT;
+  bad = !(a[0] < INFINITY);
+  const bool some = a[0] >= Q8_TINY && !bad;
+  const float inv = some ? 127.f * __frcp_rn(a[0]) : 0.f;
+  // a group with a value that is not finite keeps no values: its scale says so wherever it is read
+  scale = bad ? __int_as_float(0x7fc00000) : (some ? a[0] * (1.f / 127.f) : 0.f);
+  #pragma unroll
+  for (int v = 0; v < N; ++v) {
+    const float2 i2 = both(P == 1 ? inv : __shfl_sync(0xffffffffu, inv, (lane & 16) | (v << SHIFT)));
+    uint32_t n[8];
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 p = mul2(x[v][j], i2);
+      n[2 * j] = __float_as_uint(__fadd_rn(p.x, 12582912.f));
+      n[2 * j + 1] = __float_as_uint(__fadd_rn(p.y, 12582912.f));
+    }
+    q[v] = make_uint2(__byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(n[4], n[5], 0x0040), __byte_perm(n[6], n[7], 0x0040), 0x5410));
+  }
+  if (__any_sync(0xffffffffu, bad)) {
+    #pragma unroll
+    for (int v = 0; v < N; ++v)
+      if (__shfl_sync(0xffffffffu, (int)bad, (lane & 16) | (v << SHIFT))) q[v] = make_uint2(0u, 0u);
+  }
 }
 
 // 8 columns to p (fp32 or bf16 as YF says)
@@ -578,21 +614,23 @@ __global__ void __launch_bounds__(256) ckpt8_vec_kernel(Ckpt8Args a, int64_t ste
       }
       next();
     }
-    #pragma unroll
-    for (int k = 0; k < CKPT_GROUPS; ++k) {
-      if (RESTORE) {
+    if (RESTORE) {
+      #pragma unroll
+      for (int k = 0; k < CKPT_GROUPS; ++k) {
         #pragma unroll
         for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(s[k]));
         if (live[k]) put8<sizeof(TX) == 4>(x, rows[k] * a.x.ld + cols[k], v[k]);
-      } else {
-        float scale; bool bad;
-        const uint2 q = quantise8(v[k], scale, bad);
-        if (live[k]) {
-          *reinterpret_cast<uint2*>(a.q.p + rows[k] * a.q.ld + cols[k]) = q;
-          if (col_in == 0) {
-            a.q.scale[rows[k] * a.q.ld_scale + cols[k] / Q8_GROUP] = scale;
-            if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
-          }
+      }
+    } else {
+      uint2 q[CKPT_GROUPS];
+      int slot; float scale; bool bad;
+      quantise<CKPT_GROUPS>(v, q, slot, scale, bad);
+      #pragma unroll
+      for (int k = 0; k < CKPT_GROUPS; ++k) {
+        if (live[k]) *reinterpret_cast<uint2*>(a.q.p + rows[k] * a.q.ld + cols[k]) = q[k];
+        if (slot == k && (threadIdx.x & 3) == 0 && rows[k] < a.T) {     // (that lane's own columns may be past the row)
+          a.q.scale[rows[k] * a.q.ld_scale + cols[k] / Q8_GROUP] = scale;
+          if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
         }
       }
     }
@@ -707,6 +745,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   for (int i = threadIdx.x; i < 2 * WARPS * WARPS; i += NORM_THREADS) red[i] = 0.f;
   if (cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
   const uint32_t dst = smem_addr(mine) + Row::lane_dst(lane);
+  constexpr int LANES_PER_SLOT = VPL == 1 ? 16 : (VPL == 2 ? 8 : (VPL <= 4 ? 4 : 2));
+  const bool first_of_slot = (lane & (LANES_PER_SLOT - 1)) == 0;
   const float inv_h = 1.f / (float)a.H;
   const int ysz = a.y.dtype == SAPO_DTYPE_F32 ? 4 : 2;
   int64_t ahead = row0;                                 // the next row to fetch, `src` its address
@@ -787,16 +827,17 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
       }
       if (a.q.p != nullptr) {
         int8_t* q_row = a.q.p + row * a.q.ld + col0;
-        float* scale_row = a.q.scale + row * a.q.ld_scale + col0 / Q8_GROUP;
+        uint2 q[VPL];
+        int slot; float scale; bool bad;
+        quantise<VPL>(x, q, slot, scale, bad);
         #pragma unroll
-        for (int v = 0; v < VPL; ++v) {                // whole warps: a group's threads agree by shuffles
-          float scale; bool bad;
-          const uint2 q = quantise8(x[v], scale, bad);
-          if (256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = q;
-          if (256 * v < left && (lane & 15) == 0) {
-            scale_row[2 * v] = scale;
-            if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
-          }
+        for (int v = 0; v < VPL; ++v)
+          if (256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = q[v];
+        // one lane per group: half h of the warp has the groups at columns 256 v + 128 h
+        const int scale_col = w * VPL * 256 + 256 * slot + 128 * (lane >> 4);
+        if (first_of_slot && slot < VPL && scale_col < a.H) {
+          a.q.scale[row * a.q.ld_scale + scale_col / Q8_GROUP] = scale;
+          if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
         }
       }
     }
@@ -837,16 +878,16 @@ template <class TX, class TDY, int VPL, int MAX_THREADS> struct BwdRing {
   static constexpr bool HOLD = VPL <= 2;
 };
 
-template <class TX, class TDY, int VPL, int MAX_THREADS>
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
 __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_bwd_ring_kernel(NormBwdArgs a, int wpr) {
   constexpr bool FROM_Q8 = sizeof(TX) == 1;
   using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
   constexpr int S = Ring::STAGES;
   constexpr bool HOLD = Ring::HOLD;
   extern __shared__ __align__(16) uint8_t ring[];
-  // [group][turn][slots]: up to 8 groups of up to 4 warps, 2 of up to 8, or 1 of up to 16
-  constexpr int SLOTS = MAX_THREADS / 32;
-  __shared__ __align__(16) float2 red[2 * SLOTS * SLOTS];
+  // [group][turn][slots]: wpr <= SLOTS, and only groups of two warps and more use them
+  constexpr int RED = MAX_THREADS / 32 / 2 * 2 * SLOTS;
+  __shared__ __align__(16) float2 red[RED];
   using RowX = WarpRow<TX, VPL>;
   using RowD = WarpRow<TDY, VPL>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / wpr;
@@ -857,7 +898,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   const int col0 = warp_col + lane * 8, left = a.H - col0;          // vector v of the lane exists if 256 v < left
   uint8_t* mine = ring + warp * Ring::WARP_BYTES;
   const int stage_bytes = warps * Ring::WARP_BYTES;
-  for (int i = threadIdx.x; i < 2 * SLOTS * SLOTS; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
+  for (int i = threadIdx.x; i < RED; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
   __syncthreads();
   if (cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
   const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
@@ -1028,12 +1069,15 @@ static RingPlan fwd_ring_plan(int32_t H) {
   p.rows_per_block = NORM_THREADS / 32 / p.wpr;
   return p;
 }
+// Two blocks of 8 warps an SM, or one of 16: whichever leaves fewer warps of the 16 unused, 3 and 5 warps a row
+// being those that do not divide 8 well (12 and 10 of 16 warps against 15).
 static RingPlan bwd_ring_plan(int32_t H) {
   const int nvec = ceil_div(H, 8);
   RingPlan p;
   p.vpl = nvec <= 32 ? 1 : (H <= 8192 ? 2 : 4);
   p.wpr = ceil_div(nvec, p.vpl * 32);
-  p.rows_per_block = p.wpr >= 5 ? 1 : 8 / p.wpr;
+  const int two = p.wpr > 8 ? 0 : 2 * (8 / p.wpr) * p.wpr, one = 16 / p.wpr * p.wpr;
+  p.rows_per_block = two >= one ? 8 / p.wpr : 16 / p.wpr;
   p.threads = p.wpr * p.rows_per_block * 32;
   return p;
 }
@@ -1119,14 +1163,14 @@ static int launch_fwd_ring(const NormFwdArgs& a, int sms, cudaStream_t st) {
 }
 
 // launch == false: only how many blocks of the plan an SM holds (0: this form does not exist)
-template <class TX, class TDY, int VPL, int MAX_THREADS>
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
 static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
   using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
   if constexpr (!Ring::FITS) {
     return launch ? SAPO_ERR_CUDA : 0;
   } else {
     static int cache[33][MAX_DEVICES] = {{0}};                       // by warps of the block
-    auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS>;
+    auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS, SLOTS>;
     // the ring, or the columns' sums that take its place at the end
     size_t smem = (size_t)Ring::STAGES * (p.threads / 32) * Ring::WARP_BYTES;
     if (p.rows_per_block > 1 && smem < (size_t)2 * a.H * sizeof(float)) smem = (size_t)2 * a.H * sizeof(float);
@@ -1138,10 +1182,12 @@ static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, boo
 }
 template <class TX, class TDY>
 static int bwd_ring_dy(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
-  if (p.vpl == 1) return bwd_ring_vpl<TX, TDY, 1, 256>(a, p, blocks, launch, st);
-  if (p.vpl == 2 && p.threads <= 256) return bwd_ring_vpl<TX, TDY, 2, 256>(a, p, blocks, launch, st);
-  if (p.vpl == 2) return bwd_ring_vpl<TX, TDY, 2, 512>(a, p, blocks, launch, st);
-  return bwd_ring_vpl<TX, TDY, 4, 512>(a, p, blocks, launch, st);
+  if (p.vpl == 1) return bwd_ring_vpl<TX, TDY, 1, 256, 2>(a, p, blocks, launch, st);
+  if (p.vpl == 2 && p.threads <= 256)
+    return p.wpr <= 4 ? bwd_ring_vpl<TX, TDY, 2, 256, 4>(a, p, blocks, launch, st) : bwd_ring_vpl<TX, TDY, 2, 256, 8>(a, p, blocks, launch, st);
+  if (p.vpl == 2)
+    return p.wpr <= 8 ? bwd_ring_vpl<TX, TDY, 2, 512, 8>(a, p, blocks, launch, st) : bwd_ring_vpl<TX, TDY, 2, 512, 16>(a, p, blocks, launch, st);
+  return bwd_ring_vpl<TX, TDY, 4, 512, 16>(a, p, blocks, launch, st);
 }
 static int bwd_ring(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
   const bool f = a.dy.dtype == SAPO_DTYPE_F32;
