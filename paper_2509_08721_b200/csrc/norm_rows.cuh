@@ -1,0 +1,488 @@
+// Norm forward, replay and backward for rows that can be copied 16 bytes at a time.
+#pragma once
+
+#include "norm_common.cuh"
+
+namespace sapo {
+
+// ---------------------------------------------------------------------------- rows through shared memory
+// The kernels for rows of more than 128 columns, a multiple of 8, that start on 16-byte boundaries.
+// A row belongs to the `wpr` warps of a group; warp w of them owns VPL * 256 consecutive columns, lane l
+// of it the vectors of 8 columns (w VPL + v) 32 + l, v < VPL.  Each warp streams its part of the group's
+// next STAGES - 1 rows into shared memory with asynchronous copies while it works on the current one, so
+// the bytes in flight do not depend on registers or on how long a row's sums take.  Only lanes of the
+// same warp read what a lane copied: the wait for a row is one __syncwarp.
+// What then bounds a row kernel is instruction issue (at the copy bandwidth an SM has to finish 4 to 6
+// columns per clock), so the arithmetic is done in pairs and every vector is whole.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+// (predicated, not branched around: a lane whose columns do not exist copies nothing)
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool exists) {
+  if constexpr (BYTES == 16)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
+                 ::"r"(dst), "l"(src), "r"((uint32_t)exists) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %3;\n\t}"
+                 ::"r"(dst), "l"(src), "r"((uint32_t)exists), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// One warp's part of a row of TX in shared memory: VPL * 256 elements.
+template <class TX, int VPL>
+struct WarpRow {
+  static constexpr int BYTES = VPL * 256 * (int)sizeof(TX);
+  // Where lane `lane` of the warp copies from in the warp's part of a row, and to.
+  static constexpr int LANE = sizeof(TX) == 4 ? 4 : 8, PER_V = sizeof(TX) == 4 ? 2 : 1;
+  __device__ static __forceinline__ int lane_dst(int lane) {
+    return sizeof(TX) == 4 ? (lane ^ ((lane >> 3) & 1)) * 16 : lane * 8 * (int)sizeof(TX);
+  }
+  // dst, src: with the lane's offsets; cols: how many of the warp's columns exist (a multiple of 8)
+  __device__ static __forceinline__ void copy(uint32_t dst, const TX* src, int cols, int lane) {
+    // fp32: neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
+    // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
+    constexpr int B = LANE * (int)sizeof(TX);
+    #pragma unroll
+    for (int v = 0; v < PER_V * VPL; ++v)
+      copy_async<B>(dst + v * 32 * B, src + v * 32 * LANE, v * 32 * LANE + lane * LANE < cols);
+  }
+  // the lane's vector v
+  __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float2 (&x)[4]) {
+    if constexpr (sizeof(TX) == 4) {
+      const int f = (lane >> 2) & 1;
+      const float4 a = *reinterpret_cast<const float4*>(at + v * 1024 + (2 * lane + f) * 16);
+      const float4 b = *reinterpret_cast<const float4*>(at + v * 1024 + (2 * lane + 1 - f) * 16);
+      x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
+    } else {
+      load8(reinterpret_cast<const TX*>(at) + (v * 32 + lane) * 8, x);
+    }
+  }
+};
+
+template <class TX, int VPL> struct FwdRing {
+  static constexpr int STAGE_BYTES = NORM_THREADS / 32 * WarpRow<TX, VPL>::BYTES;
+  static constexpr int STAGES = STAGE_BYTES <= 16384 ? 4 : (STAGE_BYTES <= 26624 ? 3 : 2);
+  static int smem(int H) { return STAGES * STAGE_BYTES + 2 * H * (int)sizeof(float); }   // and the weights
+};
+
+// Zeros where the warp's columns do not exist: nothing is ever copied there, and zeros add nothing to sums.
+__device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stages, int stage_bytes, int lane) {
+  for (int s = 0; s < stages; ++s)
+    for (int i = lane * 16; i < bytes; i += 512) *reinterpret_cast<uint4*>(mine + s * stage_bytes + i) = make_uint4(0u, 0u, 0u, 0u);
+  __syncwarp();
+}
+// TX int8_t: replay from a checkpoint (a.q), statistics given.
+template <class TX, int VPL>
+__global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
+  constexpr bool REPLAY = sizeof(TX) == 1;
+  constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
+  using Row = WarpRow<TX, VPL>;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ __align__(16) float red[2 * WARPS * WARPS];   // [group][turn][slots]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / wpr, w = warp - group * wpr;
+  const int64_t step = (int64_t)gridDim.x * (WARPS / wpr);
+  const int64_t row0 = (int64_t)blockIdx.x * (WARPS / wpr) + group;
+  const int col0 = w * VPL * 256 + lane * 8;            // the lane's first column, and
+  const int left = a.H - col0;                          // what is left of the row there: vector v exists if 256 v < left
+  const int cols = a.H - w * VPL * 256;
+  const int64_t ld = REPLAY ? a.q.ld : a.x.ld;
+  const TX* src = (REPLAY ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) +
+                  row0 * ld + w * VPL * 256 + lane * Row::LANE;
+  constexpr int STAGE_BYTES = WARPS * Row::BYTES;
+  uint8_t* mine = ring + warp * Row::BYTES;
+  for (int i = threadIdx.x; i < 2 * WARPS * WARPS; i += NORM_THREADS) red[i] = 0.f;
+  if (cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
+  const uint32_t dst = smem_addr(mine) + Row::lane_dst(lane);
+  const float inv_h = 1.f / (float)a.H;
+  const int ysz = a.y.dtype == SAPO_DTYPE_F32 ? 4 : 2;
+  char* y_row = static_cast<char*>(a.y.p) + (row0 * a.y.ld + col0) * ysz;
+  const int64_t y_step = step * a.y.ld * ysz;
+  int64_t ahead = row0;                                 // the next row to fetch, `src` its address
+  auto fetch = [&](int stage) {
+    if (ahead < a.T) Row::copy(dst + stage * STAGE_BYTES, src, cols, lane);
+    copy_commit();
+    ahead += step;
+    src += step * ld;
+  };
+  #pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(s);
+  // the weights in fp32, once per block: read from global memory for every row they miss L1 one time in five,
+  // and the wait for them is longer than the rest of the row's work.  In 16-byte pieces in WarpRow's order.
+  float* gs = reinterpret_cast<float*>(ring + S * STAGE_BYTES);
+  float* bs = gs + a.H;
+  for (int i = threadIdx.x * 8; i < a.H; i += NORM_THREADS * 8) {
+    float2 u[4];
+    const int f = (i >> 5) & 1, lo = i + 4 * f, hi = i + 4 - 4 * f;
+    if (a.gamma != nullptr) {
+      load_weight8(a.gamma, a.w_dtype, i, u);
+      *reinterpret_cast<float4*>(gs + lo) = make_float4(u[0].x, u[0].y, u[1].x, u[1].y);
+      *reinterpret_cast<float4*>(gs + hi) = make_float4(u[2].x, u[2].y, u[3].x, u[3].y);
+    }
+    if (a.beta != nullptr) {
+      load_weight8(a.beta, a.w_dtype, i, u);
+      *reinterpret_cast<float4*>(bs + lo) = make_float4(u[0].x, u[0].y, u[1].x, u[1].y);
+      *reinterpret_cast<float4*>(bs + hi) = make_float4(u[2].x, u[2].y, u[3].x, u[3].y);
+    }
+  }
+  __syncthreads();
+  int stage = 0, turn = 0;
+  for (int64_t row = row0; row < a.T; row += step) {
+    copy_wait<S - 2>();
+    __syncwarp();
+    fetch(stage == 0 ? S - 1 : stage - 1);
+    const uint8_t* at = mine + stage * STAGE_BYTES;
+    stage = stage + 1 == S ? 0 : stage + 1;
+    float2 x[VPL][4];
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      Row::read(at, v, lane, x[v]);
+      if (REPLAY) {
+        const float2 s = both(256 * v < left ? a.q.scale[row * a.q.ld_scale + (col0 + 256 * v) / Q8_GROUP] : 0.f);
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], s);
+      }
+    }
+    float mean = 0.f, rstd;
+    if (REPLAY) {
+      mean = a.kind == KIND_LAYER ? a.mean[row] : 0.f;
+      rstd = a.rstd[row];
+    } else {
+      if (a.kind == KIND_LAYER) {
+        float2 s = both(0.f), t = both(0.f);
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v) { s = add2(s, add2(x[v][0], x[v][1])); t = add2(t, add2(x[v][2], x[v][3])); }
+        s = add2(s, t);
+        mean = group_sum<WARPS>(s.x + s.y, wpr, w, group, red, turn) * inv_h;
+        turn ^= 1;
+      }
+      float2 s2 = both(0.f), t2 = both(0.f);
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        const float2 minus = both(256 * v < left ? -mean : 0.f);
+        #pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const float2 d = add2(x[v][j], minus), e = add2(x[v][j + 1], minus);
+          s2 = fma2(d, d, s2);
+          t2 = fma2(e, e, t2);
+        }
+      }
+      s2 = add2(s2, t2);
+      rstd = 1.f / sqrtf(group_sum<WARPS>(s2.x + s2.y, wpr, w, group, red, turn) * inv_h + a.eps);
+      turn ^= 1;
+      if (w == 0 && lane == 0) {
+        if (a.mean != nullptr && a.kind == KIND_LAYER) a.mean[row] = mean;
+        if (a.rstd != nullptr) a.rstd[row] = rstd;
+      }
+      if (a.q.p != nullptr) {
+        int8_t* q_row = a.q.p + row * a.q.ld + col0;
+        uint2 bytes[VPL][4];
+        float scale; bool bad;
+        quantise<VPL, 16, 4>(x, bytes, scale, bad);
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v)
+          if (256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = pack_bytes(bytes[v]);
+        // one lane per group: half h of the warp has the groups at columns 256 v + 128 h
+        using Half = Slots<PowerOfTwo<VPL>::value, 16>;
+        const int scale_col = w * VPL * 256 + 256 * Half::slot() + 128 * (lane >> 4);
+        if (Half::first() && Half::slot() < VPL && scale_col < a.H) {
+          a.q.scale[row * a.q.ld_scale + scale_col / Q8_GROUP] = scale;
+          if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+        }
+      }
+    }
+    const float2 minus = both(-mean), r2 = both(rstd);
+    auto finish = [&](auto f) {
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        if (256 * v >= left) break;
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
+        float2 u[4];
+        if (a.gamma != nullptr) {
+          WarpRow<float, VPL>::read(reinterpret_cast<const uint8_t*>(gs + w * VPL * 256), v, lane, u);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], u[j]);
+        }
+        if (a.beta != nullptr) {
+          WarpRow<float, VPL>::read(reinterpret_cast<const uint8_t*>(bs + w * VPL * 256), v, lane, u);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) x[v][j] = add2(x[v][j], u[j]);
+        }
+        put8<decltype(f)::value>(y_row, 256 * v, x[v]);
+      }
+    };
+    if (a.y.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
+    y_row += y_step;
+  }
+}
+
+// Warps of a row and rows of a block in the backward: the sums of a thread's columns over all rows of its
+// block are 16 registers a vector, so a thread owns few of them and a row is spread over more warps.
+template <class TX, class TDY, int VPL, int MAX_THREADS> struct BwdRing {
+  static constexpr int WARP_BYTES = WarpRow<TX, VPL>::BYTES + WarpRow<TDY, VPL>::BYTES + 64 + (sizeof(TX) == 1 ? VPL * 128 : 0);
+  static constexpr int FULL = MAX_THREADS / 32 * WARP_BYTES;         // one row of the widest block
+  static constexpr int STAGES = 4 * FULL <= SMEM_MAX ? 4 : (3 * FULL <= SMEM_MAX ? 3 : 2);
+  static constexpr bool FITS = STAGES * FULL <= SMEM_MAX;            // else norm_bwd_any_kernel takes it
+  // whether a row stays in registers between the sums and dx; a thread with many columns reads it again
+  static constexpr bool HOLD = VPL <= 2;
+};
+
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
+__global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_bwd_ring_kernel(NormBwdArgs a, int wpr) {
+  constexpr bool FROM_Q8 = sizeof(TX) == 1;
+  using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
+  constexpr int S = Ring::STAGES;
+  constexpr bool HOLD = Ring::HOLD;
+  extern __shared__ __align__(16) uint8_t ring[];
+  // [group][turn][slots]: wpr <= SLOTS, and only groups of two warps and more use them
+  constexpr int RED = MAX_THREADS / 32 / 2 * 2 * SLOTS;
+  __shared__ __align__(16) float2 red[RED];
+  using RowX = WarpRow<TX, VPL>;
+  using RowD = WarpRow<TDY, VPL>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / wpr;
+  const int group = warp / wpr, w = warp - group * wpr;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  const int64_t row0 = (int64_t)blockIdx.x * groups + group;
+  const int warp_col = w * VPL * 256, cols = a.H - warp_col;
+  const int col0 = warp_col + lane * 8, left = a.H - col0;          // vector v of the lane exists if 256 v < left
+  uint8_t* mine = ring + warp * Ring::WARP_BYTES;
+  const int stage_bytes = warps * Ring::WARP_BYTES;
+  for (int i = threadIdx.x; i < RED; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
+  __syncthreads();
+  if (cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
+  const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
+  const TX* xp = (FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) + row0 * ldx + warp_col + lane * RowX::LANE;
+  const TDY* dyp = static_cast<const TDY*>(a.dy.p) + row0 * a.dy.ld + warp_col + lane * RowD::LANE;
+  const float* sp = FROM_Q8 ? a.q.scale + row0 * a.q.ld_scale + col0 / Q8_GROUP : nullptr;
+  constexpr int DY_AT = RowX::BYTES, ST_AT = DY_AT + RowD::BYTES, SC_AT = ST_AT + 64;
+  const float inv_h = 1.f / (float)a.H;
+  const bool layer = a.kind == KIND_LAYER;
+  const uint32_t base = smem_addr(mine);
+  const uint32_t dst_x = base + RowX::lane_dst(lane), dst_d = base + DY_AT + RowD::lane_dst(lane);
+  // lane 0 copies rstd, lane 1 the mean
+  const float* stat = lane == 0 ? a.rstd : a.mean;
+  const bool copies_stat = lane == 0 || (lane == 1 && layer);
+  int64_t ahead = row0;
+  auto fetch = [&](int stage) {
+    if (ahead < a.T) {
+      const uint32_t off = stage * stage_bytes;
+      RowX::copy(dst_x + off, xp, cols, lane);
+      RowD::copy(dst_d + off, dyp, cols, lane);
+      copy_async<4>(base + off + ST_AT + lane * 4, stat + ahead, copies_stat);
+      if (FROM_Q8) {
+        #pragma unroll
+        for (int v = 0; v < VPL; ++v) copy_async<4>(base + off + SC_AT + (v * 32 + lane) * 4, sp + 2 * v, 256 * v < left);
+      }
+    }
+    copy_commit();
+    ahead += step;
+    xp += step * ldx;
+    dyp += step * a.dy.ld;
+    if (FROM_Q8) sp += step * a.q.ld_scale;
+  };
+  #pragma unroll
+  for (int s = 0; s < S - 1; ++s) fetch(s);
+  float2 gam[HOLD ? VPL : 1][4], dg[VPL][4], db[VPL][4];
+  auto weights = [&](int v, float2 (&g)[4]) {
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = both(1.f);
+    if (a.gamma != nullptr && 256 * v < left) load_weight8(a.gamma, a.w_dtype, col0 + 256 * v, g);
+  };
+  #pragma unroll
+  for (int v = 0; v < VPL; ++v) {
+    #pragma unroll
+    for (int j = 0; j < 4; ++j) { dg[v][j] = both(0.f); db[v][j] = both(0.f); }
+    if (HOLD) weights(v, gam[v]);
+  }
+  const int dxsz = a.dx.dtype == SAPO_DTYPE_F32 ? 4 : 2;
+  char* dx_row = static_cast<char*>(a.dx.p) + (row0 * a.dx.ld + col0) * dxsz;
+  const int64_t dx_step = step * a.dx.ld * dxsz;
+  int stage = 0, turn = 0;
+  for (int64_t row = row0; row < a.T; row += step) {
+    copy_wait<S - 2>();
+    __syncwarp();
+    fetch(stage == 0 ? S - 1 : stage - 1);
+    const uint8_t* at = mine + stage * stage_bytes;
+    stage = stage + 1 == S ? 0 : stage + 1;
+    const float rstd = *reinterpret_cast<const float*>(at + ST_AT);
+    const float mean = layer ? *reinterpret_cast<const float*>(at + ST_AT + 4) : 0.f;
+    const float2 minus = both(-mean), r2 = both(rstd), shift = both(-mean * rstd);
+    float2 xh[HOLD ? VPL : 1][4], g[HOLD ? VPL : 1][4];
+    // vector v of the row: xh and dy
+    auto take = [&](int v, float2 (&x)[4], float2 (&d)[4]) {
+      RowX::read(at, v, lane, x);
+      RowD::read(at + DY_AT, v, lane, d);
+      if (FROM_Q8) {       // value and (value - mean) rstd in one rounding: the value itself is off by much more
+        const float2 s = both(*reinterpret_cast<const float*>(at + SC_AT + (v * 32 + lane) * 4) * rstd);
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fma2(x[j], s, shift);
+      } else {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = mul2(add2(x[j], minus), r2);
+      }
+    };
+    // (where a vector does not exist dy is zero: it adds nothing to the sums)
+    float2 s1 = both(0.f), s2 = both(0.f);
+    #pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+      const int k = HOLD ? v : 0;
+      take(v, xh[k], g[k]);
+      if (!HOLD) weights(v, gam[0]);
+      #pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        dg[v][j] = fma2(g[k][j], xh[k][j], dg[v][j]);
+        db[v][j] = add2(db[v][j], g[k][j]);
+        g[k][j] = mul2(g[k][j], gam[k][j]);          // dy becomes g = dy gamma
+        s1 = add2(s1, g[k][j]);
+        s2 = fma2(g[k][j], xh[k][j], s2);
+      }
+    }
+    const float2 sums = group_sum2<SLOTS>(s1.x + s1.y, s2.x + s2.y, wpr, w, group, red, turn);
+    turn ^= 1;
+    const float2 c1 = both(layer ? -sums.x * inv_h * rstd : 0.f), c2 = both(-sums.y * inv_h * rstd);
+    auto finish = [&](auto f) {
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        const int k = HOLD ? v : 0;
+        if (!HOLD) {
+          take(v, xh[0], g[0]);
+          weights(v, gam[0]);
+          #pragma unroll
+          for (int j = 0; j < 4; ++j) g[0][j] = mul2(g[0][j], gam[0][j]);
+        }
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) g[k][j] = fma2(xh[k][j], c2, fma2(g[k][j], r2, c1));
+        if (256 * v < left) put8<decltype(f)::value>(dx_row, 256 * v, g[k]);
+      }
+    };
+    if (a.dx.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
+    dx_row += dx_step;
+  }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (a.dgamma == nullptr && a.dbeta == nullptr) return;
+  // the groups' sums one after the other, through the ring (no copy is in flight any more)
+  copy_wait<0>();
+  __syncthreads();
+  float* acc = reinterpret_cast<float*>(ring);           // [2][H]
+  for (int k = 0; k < groups; ++k) {
+    if (k == group) {
+      #pragma unroll
+      for (int v = 0; v < VPL; ++v) {
+        const int col = col0 + 256 * v;
+        if (col >= a.H) continue;
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float2* pg = reinterpret_cast<float2*>(acc + col + 2 * j);
+          float2* pb = reinterpret_cast<float2*>(acc + a.H + col + 2 * j);
+          if (k > 0) { dg[v][j] = add2(dg[v][j], *pg); db[v][j] = add2(db[v][j], *pb); }
+          if (k + 1 < groups) { *pg = dg[v][j]; *pb = db[v][j]; continue; }
+          if (gridDim.x > 1) {
+            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H + col + 2 * j;
+            *reinterpret_cast<float2*>(out) = dg[v][j];
+            *reinterpret_cast<float2*>(out + a.H) = db[v][j];
+          } else {
+            const int c = col + 2 * j;
+            if (a.dgamma != nullptr) {
+              a.dgamma[c] = a.accumulate ? a.dgamma[c] + dg[v][j].x : dg[v][j].x;
+              a.dgamma[c + 1] = a.accumulate ? a.dgamma[c + 1] + dg[v][j].y : dg[v][j].y;
+            }
+            if (a.dbeta != nullptr) {
+              a.dbeta[c] = a.accumulate ? a.dbeta[c] + db[v][j].x : db[v][j].x;
+              a.dbeta[c + 1] = a.accumulate ? a.dbeta[c + 1] + db[v][j].y : db[v][j].y;
+            }
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// dgamma (blockIdx.y 0) and dbeta (1): the sum over the blocks' parts, 32 columns per block, one warp
+// for every 32nd part.
+__global__ void __launch_bounds__(1024)
+norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float* dgamma, float* dbeta, int accumulate) {
+  __shared__ float sh[32][33];
+  float* out = blockIdx.y == 0 ? dgamma : dbeta;
+  if (out == nullptr) { asm volatile("griddepcontrol.wait;" ::: "memory"); return; }
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int col = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  asm volatile("griddepcontrol.wait;" ::: "memory");      // launched while the backward's last blocks still run
+  if (col < H)
+    for (int b = w; b < n_parts; b += 32) s += part[((int64_t)b * 2 + blockIdx.y) * H + col];
+  sh[w][lane] = s;
+  __syncthreads();
+  // transposed: warp w now holds the 32 sums of column w
+  float t = sh[lane][w];
+  #pragma unroll
+  for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+  const int c = blockIdx.x * 32 + w;
+  if (lane == 0 && c < H) out[c] = accumulate ? out[c] + t : t;
+}
+
+// Checkpoints alone: half a warp takes a group of 128 columns, GROUPS of them with all loads before the first use.
+// A half-warp's next group is a fixed number of rows and groups on; its addresses are stepped, not computed.
+template <class TX, bool RESTORE> struct CkptStep {
+  static constexpr int GROUPS = RESTORE ? 8 : 4;       // 64 bytes of loads a thread either way
+};
+template <class TX, bool RESTORE>
+__global__ void __launch_bounds__(256) ckpt8_vec_kernel(Ckpt8Args a, int64_t step_rows, int32_t step_groups) {
+  constexpr int N = CkptStep<TX, RESTORE>::GROUPS;
+  const int32_t groups = ceil_div(a.H, Q8_GROUP);
+  const int64_t id = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+  const int col_in = (threadIdx.x & 15) * 8;
+  int64_t row = id / groups;
+  int32_t g = (int32_t)(id - row * groups);
+  TX* x = static_cast<TX*>(a.x.p) + row * a.x.ld + g * Q8_GROUP + col_in;
+  int8_t* q = a.q.p + row * a.q.ld + g * Q8_GROUP + col_in;
+  float* s = a.q.scale + row * a.q.ld_scale + g;
+  const int64_t x_step = step_rows * a.x.ld + step_groups * Q8_GROUP, x_wrap = a.x.ld - (int64_t)groups * Q8_GROUP;
+  const int64_t q_step = step_rows * a.q.ld + step_groups * Q8_GROUP, q_wrap = a.q.ld - (int64_t)groups * Q8_GROUP;
+  const int64_t s_step = step_rows * a.q.ld_scale + step_groups, s_wrap = a.q.ld_scale - groups;
+  const int32_t last_cols = a.H - (groups - 1) * Q8_GROUP;     // columns of a row's last group
+  // (both halves of a warp stay as long as one of them has rows: they agree on shuffles)
+  while (__any_sync(0xffffffffu, row < a.T)) {
+    TX* xs[N]; int8_t* qs[N]; float* ss[N];
+    bool live[N], in[N];
+    float2 v[N][4]; float scale_of[N];
+    #pragma unroll
+    for (int k = 0; k < N; ++k) {
+      xs[k] = x; qs[k] = q; ss[k] = s;
+      in[k] = row < a.T;
+      live[k] = in[k] && (g != groups - 1 || col_in < last_cols);
+      scale_of[k] = 0.f;
+      #pragma unroll
+      for (int j = 0; j < 4; ++j) v[k][j] = both(0.f);
+      if (live[k]) {
+        if (RESTORE) { load8(qs[k], v[k]); scale_of[k] = *ss[k]; } else load8(xs[k], v[k]);
+      }
+      row += step_rows; g += step_groups; x += x_step; q += q_step; s += s_step;
+      if (g >= groups) { g -= groups; ++row; x += x_wrap; q += q_wrap; s += s_wrap; }
+    }
+    if constexpr (RESTORE) {
+      #pragma unroll
+      for (int k = 0; k < N; ++k) {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(scale_of[k]));
+        if (live[k]) put8<sizeof(TX) == 4>(xs[k], 0, v[k]);
+      }
+    } else {
+      uint2 bytes[N][4];
+      float scale; bool bad;
+      quantise<N, 16, 4>(v, bytes, scale, bad);
+      using Half = Slots<N, 16>;
+      #pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (live[k]) *reinterpret_cast<uint2*>(qs[k]) = pack_bytes(bytes[k]);
+        if (Half::first() && Half::slot() == k && in[k]) {     // (that lane's own columns may be past the row)
+          *ss[k] = scale;
+          if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+        }
+      }
+    }
+  }
+}
+
+}  // namespace sapo
