@@ -236,28 +236,54 @@ static int launch_bwd_any(const NormBwdArgs& a, const AnyPlan& p, bool pairs, in
   return pairs ? launch_bwd_any_w<TX, 2>(a, p, blocks, st) : launch_bwd_any_w<TX, 1>(a, p, blocks, st);
 }
 
-// One launch of a checkpoint kernel whose `lanes` threads take `n` groups at a time.
-template <class Kernel>
-static int launch_ckpt8_groups(Kernel kernel, const Ckpt8Args& a, int lanes, int n, int* cache, int sms, cudaStream_t st) {
+// One launch of a checkpoint kernel: `units` pieces of work of a warp, `per_row` of them a row (or a set of rows), `n` at a time.
+template <class Launch, class Kernel>
+static int launch_ckpt8_warps(Kernel kernel, int64_t units, int32_t per_row, int n, int* cache, int sms, Launch launch) {
   const int per_sm = resident_blocks(kernel, 256, 0, cache);
   if (per_sm == 0) return SAPO_ERR_CUDA;
-  const int32_t groups = ceil_div(a.H, Q8_GROUP);
-  const int per_block = 256 / lanes;
-  int64_t blocks = ceil_div<int64_t>(a.T * groups, (int64_t)per_block * n);
+  int64_t blocks = ceil_div<int64_t>(units, (int64_t)8 * n);
   if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
-  const int64_t at_once = blocks * per_block;
-  KernelScope scope(SAPO_K_CKPT8, st);
-  kernel<<<(int)blocks, 256, 0, st>>>(a, at_once / groups, (int32_t)(at_once % groups));
+  launch((int)blocks, blocks * 8 / per_row, (int32_t)(blocks * 8 % per_row));
   return check_launch();
+}
+template <class TX, int L, int N, bool RESTORE>
+static int launch_ckpt8_rows(const Ckpt8Args& a, int sms, cudaStream_t st) {
+  static int cache[MAX_DEVICES] = {0};
+  auto kernel = ckpt8_rows_kernel<TX, L, N, RESTORE>;
+  const int32_t segments = L == 32 ? ceil_div(a.H, N * 256) : 1;
+  const int64_t units = ceil_div<int64_t>(a.T, L == 32 ? 1 : N * (32 / L)) * segments;
+  KernelScope scope(SAPO_K_CKPT8, st);
+  return launch_ckpt8_warps(kernel, units, segments, 1, cache, sms, [&](int blocks, int64_t rows, int32_t segs) {
+    kernel<<<blocks, 256, 0, st>>>(a, segments, rows, segs);
+  });
+}
+template <class TX, int W, bool RESTORE>
+static int launch_ckpt8_any(const Ckpt8Args& a, int sms, cudaStream_t st) {
+  static int cache[MAX_DEVICES] = {0};
+  auto kernel = ckpt8_any_kernel<TX, W, RESTORE>;
+  const int32_t groups = ceil_div(a.H, Q8_GROUP);
+  KernelScope scope(SAPO_K_CKPT8, st);
+  return launch_ckpt8_warps(kernel, a.T * groups, groups, CkptAny<RESTORE>::GROUPS, cache, sms, [&](int blocks, int64_t rows, int32_t g) {
+    kernel<<<blocks, 256, 0, st>>>(a, rows, g);
+  });
 }
 template <class TX, bool RESTORE>
 static int launch_ckpt8(const Ckpt8Args& a, int sms, cudaStream_t st) {
-  static int cache[3][MAX_DEVICES] = {{0}};
-  if (a.H % 8 == 0 && vec_ok(a.x) && vec_ok(a.q))
-    return launch_ckpt8_groups(ckpt8_vec_kernel<TX, RESTORE>, a, 16, CkptStep<TX, RESTORE>::GROUPS, cache[0], sms, st);
-  if (a.H % 2 == 0 && pairs_ok(a.x) && pairs_ok(a.q))
-    return launch_ckpt8_groups(ckpt8_any_kernel<TX, 2, RESTORE>, a, 32, CkptAny<RESTORE>::GROUPS, cache[1], sms, st);
-  return launch_ckpt8_groups(ckpt8_any_kernel<TX, 1, RESTORE>, a, 32, CkptAny<RESTORE>::GROUPS, cache[2], sms, st);
+  if (a.H % 8 == 0 && vec_ok(a.x) && vec_ok(a.q)) {
+    if (a.H <= 32) return launch_ckpt8_rows<TX, 4, 4, RESTORE>(a, sms, st);
+    if (a.H <= 64) return launch_ckpt8_rows<TX, 8, 4, RESTORE>(a, sms, st);
+    if (a.H <= 128) return launch_ckpt8_rows<TX, 16, 4, RESTORE>(a, sms, st);
+    // vectors a lane takes of a row: up to 4, as many as leave the fewest of the row's last segment unused
+    const int steps = ceil_div(a.H, 256), segments = ceil_div(steps, 4);
+    switch (ceil_div(steps, segments)) {
+      case 1: return launch_ckpt8_rows<TX, 32, 1, RESTORE>(a, sms, st);
+      case 2: return launch_ckpt8_rows<TX, 32, 2, RESTORE>(a, sms, st);
+      case 3: return launch_ckpt8_rows<TX, 32, 3, RESTORE>(a, sms, st);
+      default: return launch_ckpt8_rows<TX, 32, 4, RESTORE>(a, sms, st);
+    }
+  }
+  if (a.H % 2 == 0 && pairs_ok(a.x) && pairs_ok(a.q)) return launch_ckpt8_any<TX, 2, RESTORE>(a, sms, st);
+  return launch_ckpt8_any<TX, 1, RESTORE>(a, sms, st);
 }
 template <bool RESTORE>
 static int launch_ckpt8_x(const Ckpt8Args& a, cudaStream_t st) {

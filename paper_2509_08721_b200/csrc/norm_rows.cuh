@@ -422,66 +422,68 @@ norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float
   if (lane == 0 && c < H) out[c] = accumulate ? out[c] + t : t;
 }
 
-// Checkpoints alone: half a warp takes a group of 128 columns, GROUPS of them with all loads before the first use.
-// A half-warp's next group is a fixed number of rows and groups on; its addresses are stepped, not computed.
-template <class TX, bool RESTORE> struct CkptStep {
-  static constexpr int GROUPS = RESTORE ? 8 : 4;       // 64 bytes of loads a thread either way
-};
-template <class TX, bool RESTORE>
-__global__ void __launch_bounds__(256) ckpt8_vec_kernel(Ckpt8Args a, int64_t step_rows, int32_t step_groups) {
-  constexpr int N = CkptStep<TX, RESTORE>::GROUPS;
-  const int32_t groups = ceil_div(a.H, Q8_GROUP);
-  const int64_t id = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
-  const int col_in = (threadIdx.x & 15) * 8;
-  int64_t row = id / groups;
-  int32_t g = (int32_t)(id - row * groups);
-  TX* x = static_cast<TX*>(a.x.p) + row * a.x.ld + g * Q8_GROUP + col_in;
-  int8_t* q = a.q.p + row * a.q.ld + g * Q8_GROUP + col_in;
-  float* s = a.q.scale + row * a.q.ld_scale + g;
-  const int64_t x_step = step_rows * a.x.ld + step_groups * Q8_GROUP, x_wrap = a.x.ld - (int64_t)groups * Q8_GROUP;
-  const int64_t q_step = step_rows * a.q.ld + step_groups * Q8_GROUP, q_wrap = a.q.ld - (int64_t)groups * Q8_GROUP;
-  const int64_t s_step = step_rows * a.q.ld_scale + step_groups, s_wrap = a.q.ld_scale - groups;
-  const int32_t last_cols = a.H - (groups - 1) * Q8_GROUP;     // columns of a row's last group
-  // (both halves of a warp stay as long as one of them has rows: they agree on shuffles)
-  while (__any_sync(0xffffffffu, row < a.T)) {
-    TX* xs[N]; int8_t* qs[N]; float* ss[N];
-    bool live[N], in[N];
-    float2 v[N][4]; float scale_of[N];
-    #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      xs[k] = x; qs[k] = q; ss[k] = s;
-      in[k] = row < a.T;
-      live[k] = in[k] && (g != groups - 1 || col_in < last_cols);
-      scale_of[k] = 0.f;
-      #pragma unroll
-      for (int j = 0; j < 4; ++j) v[k][j] = both(0.f);
-      if (live[k]) {
-        if (RESTORE) { load8(qs[k], v[k]); scale_of[k] = *ss[k]; } else load8(xs[k], v[k]);
-      }
-      row += step_rows; g += step_groups; x += x_step; q += q_step; s += s_step;
-      if (g >= groups) { g -= groups; ++row; x += x_wrap; q += q_wrap; s += s_wrap; }
-    }
+// Checkpoints alone, rows on 16-byte boundaries in whole vectors.  L = 32: a warp takes N * 256 neighbouring columns of a
+// row (`segments` of them a row), each lane N vectors 256 columns apart, so that one address serves all of a step.
+// L < 32: rows of up to 8 L columns, 32 / L rows a warp at a time and N of those a lane.
+template <class TX, int L, int N, bool RESTORE>
+__global__ void __launch_bounds__(256) ckpt8_rows_kernel(Ckpt8Args a, int32_t segments, int64_t step_rows, int32_t step_segments) {
+  constexpr int ROWS = L == 32 ? 1 : N * (32 / L), G = L < 16 ? L : 16;       // rows of a warp's step, lanes of a group
+  using S = Slots<PowerOfTwo<N>::value, G>;
+  const int lane = threadIdx.x & 31;
+  const int64_t id = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+  int64_t unit = id / segments;                                               // rows unit * ROWS on
+  int32_t seg = (int32_t)(id - unit * segments);
+  while (unit * ROWS < a.T) {
+    const int64_t row = unit * ROWS + (lane / L) * (L == 32 ? 0 : N);
+    const int col = seg * N * 256 * (L == 32) + (lane & (L - 1)) * 8;
+    TX* x = static_cast<TX*>(a.x.p) + row * a.x.ld + col;
+    int8_t* q = a.q.p + row * a.q.ld + col;
+    const int64_t x_next = L == 32 ? 256 : a.x.ld, q_next = L == 32 ? 256 : a.q.ld;
+    // vector k of the lane: 256 k columns on (L = 32), or k rows on
+    auto exists = [&](int k) { return L == 32 ? col + 256 * k < a.H : row + k < a.T && col < a.H; };
+    float2 v[N][4];
     if constexpr (RESTORE) {
+      float s[N];
+      #pragma unroll
+      for (int k = 0; k < N; ++k) {
+        s[k] = 0.f;
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = both(0.f);
+        if (exists(k)) {
+          load8(q + k * q_next, v[k]);
+          s[k] = a.q.scale[(row + (L == 32 ? 0 : k)) * a.q.ld_scale + (col + (L == 32 ? 256 * k : 0)) / Q8_GROUP];
+        }
+      }
       #pragma unroll
       for (int k = 0; k < N; ++k) {
         #pragma unroll
-        for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(scale_of[k]));
-        if (live[k]) put8<sizeof(TX) == 4>(xs[k], 0, v[k]);
+        for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(s[k]));
+        if (exists(k)) put8<sizeof(TX) == 4>(x + k * x_next, 0, v[k]);
       }
     } else {
-      uint2 bytes[N][4];
-      float scale; bool bad;
-      quantise<N, 16, 4>(v, bytes, scale, bad);
-      using Half = Slots<N, 16>;
       #pragma unroll
       for (int k = 0; k < N; ++k) {
-        if (live[k]) *reinterpret_cast<uint2*>(qs[k]) = pack_bytes(bytes[k]);
-        if (Half::first() && Half::slot() == k && in[k]) {     // (that lane's own columns may be past the row)
-          *ss[k] = scale;
-          if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
-        }
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) v[k][j] = both(0.f);
+        if (exists(k)) load8(x + k * x_next, v[k]);
+      }
+      uint2 bytes[N][4];
+      float scale; bool bad;
+      quantise<N, G, 4>(v, bytes, scale, bad);
+      #pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (exists(k)) *reinterpret_cast<uint2*>(q + k * q_next) = pack_bytes(bytes[k]);
+      // one lane per group: of vector slot() of the lane's half warp, or of its row
+      const int k = S::slot();
+      const int group_col = L == 32 ? seg * N * 256 + 256 * k + 128 * (lane >> 4) : 0;
+      const int64_t group_row = L == 32 ? row : row + k;
+      if (S::first() && k < N && group_col < a.H && group_row < a.T) {
+        a.q.scale[group_row * a.q.ld_scale + group_col / Q8_GROUP] = scale;
+        if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
       }
     }
+    unit += step_rows; seg += step_segments;
+    if (seg >= segments) { seg -= segments; ++unit; }
   }
 }
 
