@@ -270,11 +270,11 @@ static int launch_ckpt8_any(const Ckpt8Args& a, int sms, cudaStream_t st) {
 template <class TX, bool RESTORE>
 static int launch_ckpt8(const Ckpt8Args& a, int sms, cudaStream_t st) {
   if (a.H % 8 == 0 && vec_ok(a.x) && vec_ok(a.q)) {
-    if (a.H <= 32) return launch_ckpt8_rows<TX, 4, 4, RESTORE>(a, sms, st);
-    if (a.H <= 64) return launch_ckpt8_rows<TX, 8, 4, RESTORE>(a, sms, st);
-    if (a.H <= 128) return launch_ckpt8_rows<TX, 16, 4, RESTORE>(a, sms, st);
+    if (a.H <= 32) return launch_ckpt8_rows<TX, 4, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
+    if (a.H <= 64) return launch_ckpt8_rows<TX, 8, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
+    if (a.H <= 128) return launch_ckpt8_rows<TX, 16, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
     // vectors a lane takes of a row: up to 4, as many as leave the fewest of the row's last segment unused
-    const int steps = ceil_div(a.H, 256), segments = ceil_div(steps, 4);
+    const int steps = ceil_div(a.H, 256), segments = ceil_div(steps, RESTORE ? 2 : 4);
     switch (ceil_div(steps, segments)) {
       case 1: return launch_ckpt8_rows<TX, 32, 1, RESTORE>(a, sms, st);
       case 2: return launch_ckpt8_rows<TX, 32, 2, RESTORE>(a, sms, st);
