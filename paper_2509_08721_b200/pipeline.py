@@ -1,6 +1,7 @@
 """One policy-scoring step = pack -> group advantages -> loss forward -> loss backward,
-each a call into the CUDA library.  This module only owns buffers and sequences the calls
-(it is the API a training loop would use); it performs no arithmetic of its own.
+each a call into the CUDA library (PolicyScorer); one preference-training step = pack -> norm ->
+preference loss through the head -> norm's backward (PreferenceScorer).  This module only owns buffers
+and sequences the calls (it is the API a training loop would use); it performs no arithmetic of its own.
 """
 from __future__ import annotations
 
@@ -193,6 +194,88 @@ class PolicyScorer:
             self._start_copy(1 - i)
             self._next_set = 1 - i
         return res
+
+    def check_status(self) -> None:
+        word = int(self.status.item())
+        if word:
+            raise B.SapoError("device status: " + ",".join(B.decode_status(word)))
+
+
+@dataclass
+class PreferenceResult:
+    loss: torch.Tensor
+    out: Dict[str, torch.Tensor]        # outputs of the preference loss (gscale, seq_logratio, q_margin, ...)
+    dx: torch.Tensor                    # gradient at the norm's input, [max_tokens, H]
+    dgamma: Optional[torch.Tensor]
+    dbeta: Optional[torch.Tensor]
+    dW: torch.Tensor
+    packed: Dict[str, torch.Tensor]
+
+
+class PreferenceScorer:
+    """One preference-training step of a policy's last layers: pack -> norm -> LM head with the
+    preference loss -> gradients at the head, the norm's weights and the norm's input.
+
+    The rollout stores hold the rows in front of the norm (the residual stream) in `hidden` and the
+    reference policy's log-probs in `old_logp`; the rewards order a question's completions.
+
+    keep: what of the norm's input is held for its backward pass.  "bits8": an 8-bit checkpoint; the norm
+    then writes its output over its input, so a step holds one [T, H] buffer and a half instead of two.
+    "exact": the input itself."""
+
+    def __init__(self, W_head: torch.Tensor, gamma: torch.Tensor, norm_beta: Optional[torch.Tensor], max_tokens: int,
+                 max_seqs: int, max_questions: int, beta: float = 0.1, norm: str = "rms", eps: float = 1e-6,
+                 kind: str = "sigmoid", pairs: str = "all", label_smoothing: float = 0.0, length_norm: bool = False,
+                 grad_scale: float = 1.0, keep: str = "bits8", grad_dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        if not torch.cuda.is_available():
+            raise B.SapoError("PreferenceScorer needs a CUDA device; there is no CPU path")
+        if keep not in ("bits8", "exact"):
+            raise ValueError(f"unknown way to keep the norm's input {keep!r}")
+        if W_head.dtype != torch.bfloat16:
+            raise B.SapoError("the preference loss through the head takes bf16 operands")
+        self.W, self.gamma, self.norm_beta = W_head, gamma, norm_beta
+        self.V, self.H = int(W_head.shape[0]), int(W_head.shape[1])
+        self.max_tokens, self.max_seqs, self.max_q = int(max_tokens), int(max_seqs), int(max_questions)
+        self.norm, self.eps, self.keep = norm, float(eps), keep
+        self.beta = float(beta)
+        self.options = dict(kind=kind, pairs=pairs, label_smoothing=float(label_smoothing),
+                            length_norm=bool(length_norm), grad_scale=float(grad_scale))
+        T, H = self.max_tokens, self.H
+        new = lambda *n, dt=torch.float32: torch.empty(*n, dtype=dt, device=device)
+        self.packed = B.alloc_packed(T, self.max_seqs, self.max_q, H, torch.bfloat16, device)
+        self.hidden = None if keep == "bits8" else new(T, H, dt=torch.bfloat16)
+        self.ckpt = B.alloc_ckpt8(T, H, device) if keep == "bits8" else None
+        self.mean = new(T) if norm == "layer" else None
+        self.rstd = new(T)
+        self.dhidden, self.dW = new(T, H, dt=grad_dtype), new(self.V, H, dt=grad_dtype)
+        self.dgamma = new(H)
+        self.dbeta = None if norm_beta is None else new(H)
+        self.out = B.alloc_preference_outputs(T, self.max_seqs, self.max_q, device, scores=True)
+        kind_ws = B.WS_PREFERENCE | (B.WS_OUT_BF16 if grad_dtype == torch.bfloat16 else 0)
+        n = max(B.sapo_workspace_bytes(kind_ws, T, H, self.V, B.DTYPE_BF16), B.sapo_norm_workspace_bytes(T, H))
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        self.status = B.new_status(device)
+
+    def step(self, local: B.DeviceRollouts, ext: B.DeviceRollouts, sel: B.DeviceSelection, T: int, S: int) -> PreferenceResult:
+        """T and S are the packed token / sequence counts (known on the host from the selection)."""
+        p = self.packed
+        B.sapo_pack_rollouts(local, ext, sel, p, self.status)
+        Q = int(sel.q_offsets_local.numel() - 1)
+        x = p["hidden"][:T]
+        cut = lambda v, n: None if v is None else v[:n]
+        mean, rstd = cut(self.mean, T), self.rstd[:T]
+        held = x if self.ckpt is None else B.Ckpt8(self.ckpt.data[:T], self.ckpt.scale[:T], self.H)
+        hidden = x if self.hidden is None else self.hidden[:T]
+        B.sapo_norm_fwd(x, self.gamma, self.norm_beta, self.eps, self.norm, hidden, mean, rstd,
+                        held if self.ckpt is not None else None, self.status)
+        out = {k: v[:{"l": 1, "g": T, "s": S, "q": Q}[k[0]]] for k, v in self.out.items() if k not in ("logp", "lse")}
+        out["logp"], out["lse"] = self.out["logp"][:T], self.out["lse"][:T]
+        B.sapo_preference_loss_fwd_bwd(hidden, self.W, p["ids"], p["old_logp"], p["cu_seqlens"][:S + 1], p["rewards"],
+                                       p["group_offsets"][:Q + 1], self.beta, out, self.dhidden[:T], self.dW, False,
+                                       self.workspace, self.status, **self.options)
+        dx = self.dhidden[:T]                      # the norm's gradient takes the place of its output's
+        B.sapo_norm_bwd(dx, held, self.gamma, mean, rstd, self.norm, dx, self.dgamma, self.dbeta, self.workspace)
+        return PreferenceResult(out["loss"], out, dx, self.dgamma, self.dbeta, self.dW, p)
 
     def check_status(self) -> None:
         word = int(self.status.item())
