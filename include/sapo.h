@@ -432,8 +432,8 @@ typedef struct sapo_pref_cfg {
  * gscale is what sapo_policy_loss_bwd takes, so that call turns it into dhidden and dW_head.
  * cu_seqlens [S+1] and group_offsets [Q+1] (first sequence of each question) as sapo_pack_rollouts
  * writes them, rewards [S]; all sums in fp32 or wider and in a fixed order (the same inputs give the
- * same bits).  A completion without tokens, with a reward that is not finite
- * (SAPO_ST_NONFINITE_REWARD), or whose sum left the fp32 range joins no pair.  A token whose logp or
+ * same bits).  A completion without tokens or with a reward that is not finite
+ * (SAPO_ST_NONFINITE_REWARD) joins no pair; a pair whose h left the fp32 range is left out.  A token whose logp or
  * ref_logp is not finite (SAPO_ST_NONFINITE_INPUT) is left out of its sum and gets gscale 0.  Tokens
  * and sequences that belong to no question get zeros.  Offsets outside their range or below their
  * predecessor are clamped (SAPO_ST_BAD_INDEX).  T may be 0; Q, S >= 1. */

@@ -590,12 +590,13 @@ def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens:
     """Loss over the preference pairs of every question and its gradient factor per token; `out` comes
     from alloc_preference_outputs."""
     _require_cuda()
-    cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
+    margin, pairs_out = out.get("q_margin"), out.get("q_pairs")
     rc = load().sapo_preference_loss(
-        _p(logp), _p(ref_logp), int(logp.shape[0]), _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards),
-        _p(group_offsets), int(group_offsets.numel() - 1), cfg, _p(out["gscale"]), _p(out["seq_logratio"]),
-        _p(out["seq_grad"]), _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]),
-        _p(status), _stream())
+        logp.data_ptr(), ref_logp.data_ptr(), logp.shape[0], cu_seqlens.data_ptr(), cu_seqlens.shape[0] - 1,
+        rewards.data_ptr(), group_offsets.data_ptr(), group_offsets.shape[0] - 1,
+        _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale), out["gscale"].data_ptr(),
+        out["seq_logratio"].data_ptr(), out["seq_grad"].data_ptr(), out["q_loss"].data_ptr(), _p(margin), _p(pairs_out),
+        out["loss"].data_ptr(), status.data_ptr(), _stream())
     _check(rc, "sapo_preference_loss")
 
 

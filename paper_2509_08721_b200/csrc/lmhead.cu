@@ -1279,6 +1279,50 @@ namespace sapo {
 // preference loss adds up hundreds of tokens.
 static float z_compensation(int32_t H) { return 1.f + 1.5e-8f * (float)(H / 16); }
 
+// flags[s] = 1 for every sequence that may enter a pair, else 0, one warp per question: a sequence with a token and a
+// finite reward, in a question with two different such rewards; with best against worst, those two.  Also zero
+// for sequences of no question.  (A pair can still drop out for its log ratios; none can come in.)
+__global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __restrict__ flags) {
+  const int lane = threadIdx.x & 31;
+  const int32_t q = blockIdx.x * 8 + (threadIdx.x >> 5);
+  auto clamp = [&](int32_t s) { return s < 0 ? 0 : (s > a.S ? a.S : s); };
+  if (q >= a.Q) {                                          // the warps behind the questions: sequences outside them
+    const int32_t lo = clamp(a.group_offsets[0]);
+    int32_t hi = clamp(a.group_offsets[a.Q]);
+    if (hi < lo) hi = lo;
+    const int32_t warps = gridDim.x * 8 - a.Q;
+    for (int32_t i = (q - a.Q) * 32 + lane; i < lo + a.S - hi; i += warps * 32) flags[i < lo ? i : hi + (i - lo)] = 0.f;
+    return;
+  }
+  const int32_t s0 = clamp(a.group_offsets[q]);
+  int32_t s1 = clamp(a.group_offsets[q + 1]);
+  if (s1 < s0) s1 = s0;
+  auto reward = [&](int32_t s) {
+    int32_t t0, t1;
+    seq_range(a.cu, s, a.T, t0, t1, nullptr);
+    const float r = a.rewards[s];
+    return t1 > t0 && isfinite(r) ? r : NAN;
+  };
+  float hi = -INFINITY, lo = INFINITY;
+  int32_t best = 0x7fffffff, worst = 0x7fffffff;
+  for (int32_t s = s0 + lane; s < s1; s += 32) {
+    const float r = reward(s);
+    if (r > hi) { hi = r; best = s; }
+    if (r < lo) { lo = r; worst = s; }
+  }
+  #pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    const float h2 = __shfl_xor_sync(0xffffffffu, hi, d), l2 = __shfl_xor_sync(0xffffffffu, lo, d);
+    const int32_t b2 = __shfl_xor_sync(0xffffffffu, best, d), w2 = __shfl_xor_sync(0xffffffffu, worst, d);
+    if (h2 > hi || (h2 == hi && b2 < best)) { hi = h2; best = b2; }
+    if (l2 < lo || (l2 == lo && w2 < worst)) { lo = l2; worst = w2; }
+  }
+  for (int32_t s = s0 + lane; s < s1; s += 32) {
+    const float r = reward(s);
+    flags[s] = hi > lo && r == r && (a.pairs == SAPO_PREF_ALL || s == best || s == worst) ? 1.f : 0.f;
+  }
+}
+
 struct PrefTailArgs {
   const float* ps; int32_t n_parts; int64_t t0, tc;      // partial sums [n_parts][tc] of a token chunk
   const float* zy; const float* c2; float* sum;          // [T]
@@ -1418,15 +1462,25 @@ static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, 
     return (int)(b < (int64_t)sms * 8 ? b : (int64_t)sms * 8);
   };
 
+  // Blocks of 128 tokens none of whose sequences enters a pair get log-probs but no gradient: their exponentials are
+  // not kept, and the contractions leave them out (where they do skip by block: wide tiles).  A batch in several
+  // chunks keeps no exponentials at all.
+  const bool by_block = use_wide_tiles(H) && ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) <= MASK_WORDS_MAX;
+  const bool choose = one_pass && by_block;
+  float* flags = pa.seq_grad;                    // until the loss writes it
+  if (choose) {
+    KernelScope scope(SAPO_K_PREF_SCORE, st);
+    pref_flags_kernel<<<ceil_div(pa.Q, 8) + 1, 256, 0, st>>>(pa, flags);
+  }
+  if ((choose || !one_pass) &&
+      cudaMemsetAsync(need, 0, (size_t)ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) * 4, st) != cudaSuccess)
+    return SAPO_ERR_CUDA;
   // 1. chosen-token logits and the reference of the exponentials
   {
     KernelScope scope(SAPO_K_TARGET_LOGIT, st);
     target_logit_kernel<<<token_blocks(T), 256, 0, st>>>(RowSource{hidden, nullptr, ld_hidden, nullptr, 0, 0}, W, ld_W, ids,
-                                                         ref_logp, T, H, V, zy, c2, nullptr, pa.cu, pa.S, nullptr);
+                                                         ref_logp, T, H, V, zy, c2, flags, pa.cu, pa.S, choose ? need : nullptr);
   }
-  if (!one_pass &&                               // no block's exponentials are kept
-      cudaMemsetAsync(need, 0, (size_t)ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) * 4, st) != cudaSuccess)
-    return SAPO_ERR_CUDA;
   // 2. exponentials and their sums, then the log ratio of every token
   CUtensorMap map_w;
   if (!make_map(&map_w, W, H, V, ld_W, 128)) return SAPO_ERR_CUDA;
@@ -1439,7 +1493,7 @@ static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, 
     Sched fs = make_sched(tc, V, H, n_splits, /*m_fastest=*/true, /*tile_align=*/64, FWD_BK);
     fs.n_cover = (int32_t)Vp;
     ExpEpi::Params ep{c2 + t0, ps, nullptr, tc, V, nvt, panel, ceil_div<int64_t>(tc, BM) * nvt * BM, 2 * FUSED_MAX_SPLITS,
-                      one_pass ? nullptr : need, (int32_t)(t0 / BM), LOG2E * z_compensation(H)};
+                      choose || !one_pass ? need : nullptr, (int32_t)(t0 / BM), LOG2E * z_compensation(H)};
     const int rc = launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES>(map_h, map_w, fs, ep, pa.status, st, SAPO_K_FWD_EXP);
     if (rc != SAPO_OK) return rc;
     KernelScope scope(SAPO_K_PREF_SCORE, st);
@@ -1457,19 +1511,18 @@ static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, 
                     accumulate_dW, ws, workspace_bytes, pa.status, st);
   const int64_t panel_rows = ceil_div<int64_t>(T, BM) * nvt * BM;
   float* row_scale = reinterpret_cast<float*>(ws + CL.row_scale);
-  const bool masked = ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) <= MASK_WORDS_MAX;
-  if (masked && cudaMemsetAsync(active_mask, 0, (size_t)MASK_WORDS_MAX * 4, st) != cudaSuccess) return SAPO_ERR_CUDA;
+  if (by_block && cudaMemsetAsync(active_mask, 0, (size_t)MASK_WORDS_MAX * 4, st) != cudaSuccess) return SAPO_ERR_CUDA;
   {
     KernelScope scope(SAPO_K_FUSED_TAIL, st);
     pref_scale_kernel<<<token_blocks(T), 256, 0, st>>>(PrefScaleArgs{sum, zy, c2, ids, V, pa.gscale, T, row_scale, panel, nvt,
                                                                      panel_rows, hidden, ld_hidden, H, hs,
-                                                                     masked ? active_mask : nullptr});
+                                                                     by_block ? active_mask : nullptr});
   }
   const bool dw_via_acc = out_bf16 && accumulate_dW;
   float* dw_acc = reinterpret_cast<float*>(ws + L.dw_acc);
   rc = launch_grad_gemms(panel, panel_rows, nvt, W, ld_W, hs, H, T, H, V, Vp, dhidden, out_bf16, row_scale,
                          dw_via_acc ? (void*)dw_acc : dW_head, out_bf16 && !dw_via_acc, dw_via_acc ? 0 : accumulate_dW,
-                         reinterpret_cast<float*>(ws + L.partials), masked ? active_mask : nullptr, pa.status, st);
+                         reinterpret_cast<float*>(ws + L.partials), by_block ? active_mask : nullptr, pa.status, st);
   if (rc != SAPO_OK || !dw_via_acc) return rc;
   return launch_round_to_bf16(dw_acc, dW_head, (int64_t)V * H, 1, st);
 }

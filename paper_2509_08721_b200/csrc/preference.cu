@@ -95,6 +95,7 @@ __device__ __forceinline__ float load_from_first(const float* p) {
 // A small batch is a chain of waits for memory (each about half a microsecond), so a question's offsets and
 // rewards are read into shared memory at once, and what passes between the steps stays there, for questions of
 // up to PREF_SEQS completions.
+template <bool SOLO>
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
   __shared__ int32_t cu_s[PREF_SEQS + 1];
@@ -103,10 +104,13 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   __shared__ float scale_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t Tc = (int32_t)a.T;
-  const int rank = (int)cluster_rank(), size = (int)cluster_size();
+  // SOLO: the grid is one cluster whose blocks take questions each by itself, and the first adds up the losses
+  const int rank = SOLO ? 0 : (int)cluster_rank(), size = SOLO ? 1 : (int)cluster_size();
   const int gw = rank * PREF_WARPS + warp, n_warps = size * PREF_WARPS;
   const int32_t cluster = (int32_t)(blockIdx.x / size);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto team_barrier = [] { if (SOLO) __syncthreads(); else cluster_barrier(); };
+  auto to_first = [](float* p, float x) { if (SOLO) *p = x; else store_to_first(p, x); };
+  if (!SOLO) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   bool bad_offset = false, bad_value = false, bad_reward = false;
   if (cluster >= a.q_clusters) {
     // the clusters behind those of the questions: what no question covers, sequences before the first and after the
@@ -126,7 +130,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
       a.seq_logratio[s] = 0.f;
       a.seq_grad[s] = 0.f;
     }
-    return;
+    if (!SOLO) return;
   }
   for (int32_t q = cluster; q < a.Q; q += a.q_clusters) {
     int32_t s0, s1;
@@ -181,14 +185,14 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         }
         const float sum = warp_sum((part[0] + part[1]) + (part[2] + part[3]));
         if (lane == 0) {
-          if (t0 <= begin) store_to_first(&head[gw], sum);
-          else if (kept) store_to_first(&R_s[s - s0], sum);
+          if (t0 <= begin) to_first(&head[gw], sum);
+          else if (kept) to_first(&R_s[s - s0], sum);
           else a.seq_logratio[s] = sum;
         }
       }
     }
     bad_value |= masked;
-    cluster_barrier();
+    team_barrier();
     // 2.
     if (rank == 0) {
       for (int32_t s = s0 + warp; s < s1; s += PREF_WARPS) {
@@ -213,8 +217,8 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           const float r = kept ? r_s[s - s0] : a.rewards[s];
           if (!isfinite(r)) bad_reward = true;
           a.seq_logratio[s] = R;
-          // a completion takes part if it has a token, a finite reward and a finite sum
-          if (kept) { R_s[s - s0] = R; r_s[s - s0] = n > 0 && isfinite(r) && isfinite(R) ? r : NAN; }
+          // a completion takes part if it has a token and a finite reward
+          if (kept) { R_s[s - s0] = R; r_s[s - s0] = n > 0 && isfinite(r) ? r : NAN; }
         }
       }
       __syncthreads();
@@ -224,7 +228,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         int32_t t0, t1;
         offset_range(cu, s, Tc, t0, t1, ignore);
         const float r = a.rewards[s];
-        return t1 > t0 && isfinite(r) && isfinite(__ldcg(a.seq_logratio + s)) ? r : NAN;
+        return t1 > t0 && isfinite(r) ? r : NAN;
       };
       auto ratio_of = [&](int32_t s) { return kept ? R_s[s - s0] : __ldcg(a.seq_logratio + s); };
       int32_t best = -1, worst = -1;
@@ -254,6 +258,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           if (a.pairs == SAPO_PREF_BEST_WORST && !(wins ? (i == best && j == worst) : (j == best && i == worst))) continue;
           const float Rj = ratio_of(j);
           const float h = a.beta * (wins ? R - Rj : Rj - R);
+          if (!isfinite(h)) continue;                        // a sum that left the fp32 range
           float l, dl;
           pair_loss(a, h, l, dl);
           f += wins ? (double)dl : -(double)dl;
@@ -284,7 +289,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         a.seq_grad[i] = g;
       }
     }
-    cluster_barrier();
+    team_barrier();
     // 3.
     if (begin < end) {
       for (int32_t s = s_first; s < s1; ++s) {
@@ -294,7 +299,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         if (t0 >= end) break;
         const int32_t from = t0 > begin ? t0 : begin, to = t1 < end ? t1 : end;
         if (from >= to) continue;
-        float g = kept ? load_from_first(&g_s[s - s0]) : __ldcg(a.seq_grad + s);
+        float g = !kept ? __ldcg(a.seq_grad + s) : (SOLO ? g_s[s - s0] : load_from_first(&g_s[s - s0]));
         if (a.length_norm) g /= (float)(t1 - t0);
         // the lane that summed a token writes its factor, and knows whether any of its tokens was masked
         for (int32_t t = from + lane; t < to; t += 32) a.gscale[t] = masked && !isfinite(token_ratio(a, t)) ? 0.f : g;
@@ -306,6 +311,12 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   if (bad_reward) raise_status(a.status, SAPO_ST_NONFINITE_REWARD);
   // the first block's shared memory stays until the others have read the factors from it
   cluster_barrier();
+  if (SOLO && blockIdx.x == 0 && warp == 0) {
+    double x = 0.0;
+    for (int32_t q = lane; q < a.Q; q += 32) x += (double)__ldcg(a.q_loss + q);
+    x = warp_sum(x);
+    if (lane == 0) *a.loss = (float)(x / (double)a.Q);
+  }
 }
 
 // loss = the mean of the questions' losses
@@ -348,27 +359,40 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
   if (sms <= 0 || dev < 0) return SAPO_ERR_CUDA;
   static bool wide[MAX_DEVICES] = {false};                   // clusters of 16 blocks allowed
   if (!wide[dev]) {
-    if (cudaFuncSetAttribute(preference_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return SAPO_ERR_CUDA;
+    if (cudaFuncSetAttribute(preference_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+        cudaFuncSetAttribute(preference_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+      return SAPO_ERR_CUDA;
     wide[dev] = true;
   }
-  const int cluster = pref_cluster(a.T, a.Q, sms);
+  int cluster = pref_cluster(a.T, a.Q, sms);
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[1];
+  cfg.blockDim = dim3(PREF_THREADS);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  // Few questions of few tokens: one cluster has a block for each and one for what they do not cover, and needs no
+  // second kernel for the loss (a call for 4 questions of 256 tokens: 8.2 us with it, 10.2 us with the second kernel).
+  if (cluster == 1 && a.Q < PREF_MAX_CLUSTER && a.T <= 65536) {
+    while (cluster <= a.Q) cluster <<= 1;
+    a.q_clusters = a.Q;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    cfg.gridDim = dim3((unsigned)cluster);
+    KernelScope scope(SAPO_K_PREFERENCE, st);
+    return cudaLaunchKernelEx(&cfg, preference_kernel<true>, a) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
+  }
   const int64_t most = (int64_t)sms * 4 / cluster;
   a.q_clusters = (int32_t)(a.Q < most ? a.Q : most);
   // clusters for what no question covers: a capacity behind the last token can be large
   int64_t outside = ceil_div<int64_t>(a.T, (int64_t)65536 * cluster);
   outside = outside < 1 ? 1 : (outside > 32 ? 32 : outside);
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
+  attr[0].val.clusterDim.x = (unsigned)cluster;
   cfg.gridDim = dim3((unsigned)((a.q_clusters + outside) * cluster));
-  cfg.blockDim = dim3(PREF_THREADS);
-  cfg.stream = st;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   {
     KernelScope scope(SAPO_K_PREFERENCE, st);
-    if (cudaLaunchKernelEx(&cfg, preference_kernel, a) != cudaSuccess) return SAPO_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, preference_kernel<false>, a) != cudaSuccess) return SAPO_ERR_CUDA;
   }
   cudaLaunchConfig_t fin{};
   fin.gridDim = dim3(1);

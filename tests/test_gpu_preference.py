@@ -310,3 +310,15 @@ def test_gscale_feeds_the_policy_backward():
     assert TU.rel_fro(dh.cpu().numpy(), one["dhidden"].cpu().numpy()) <= 1e-2
     assert TU.rel_fro(dW.cpu().numpy(), one["dW"].cpu().numpy()) <= 1e-2
     assert abs(out["loss"].item() - one["loss"].item()) <= 1e-5
+
+
+@pytest.mark.parametrize("pairs", ["all", "best_worst"])
+def test_head_leaves_out_blocks_without_a_pair(pairs):
+    """Wide tiles: runs of more than 128 tokens that enter no pair (ties, single completions, completions between the
+    best and the worst) are left out of the contractions, whose panel rows for them were never written."""
+    c = head_case(512, 1800, [300, 280, 150, 400, 200, 310, 260], [2, 1, 4], seed=16)
+    c["rewards"][:] = [0.5, 0.5, 1.0, 0.5, 0.25, 1.0, 0.5]
+    got = head_run(c, 0.1, pairs=pairs)
+    r = head_check(c, got, 0.1, pairs=pairs)
+    assert list(r["q_pairs"]) == [0, 0, 5 if pairs == "all" else 1]
+    assert not got["dhidden"][:730].any() and torch.isfinite(got["dW"]).all() and got["status"] == 0
