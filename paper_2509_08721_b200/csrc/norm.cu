@@ -85,11 +85,11 @@ static int resident_blocks(Kernel kernel, int threads, size_t smem, int* cache) 
 }
 
 constexpr int RING_TOO_WIDE = 1;         // rows and weights do not fit: norm_fwd_any_kernel takes them
-template <class TX, int VPL>
-static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
+template <class TX, int VPL, bool FULL>
+static int launch_fwd_ring_full(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
   // (by the width of the row in 256 columns, which the weights' share of shared memory follows)
   static int cache[NORM_MAX_H / 256 + 1][MAX_DEVICES] = {{0}};
-  auto kernel = norm_fwd_ring_kernel<TX, VPL>;
+  auto kernel = norm_fwd_ring_kernel<TX, VPL, FULL>;
   const int steps = ceil_div(a.H, 256);
   const size_t smem = FwdRing<TX, VPL>::smem(steps * 256);
   if (smem > SMEM_MAX) return RING_TOO_WIDE;
@@ -100,6 +100,11 @@ static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms,
   KernelScope scope(SAPO_K_NORM_FWD, st);
   kernel<<<(int)blocks, p.threads, smem, st>>>(a, p.wpr);
   return check_launch();
+}
+// FULL: the row's last warp has all its columns too, so that nothing is predicated
+template <class TX, int VPL>
+static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
+  return a.H == p.wpr * VPL * 256 ? launch_fwd_ring_full<TX, VPL, true>(a, p, sms, st) : launch_fwd_ring_full<TX, VPL, false>(a, p, sms, st);
 }
 template <class TX>
 static int launch_fwd_ring(const NormFwdArgs& a, int sms, cudaStream_t st) {
@@ -117,14 +122,14 @@ static int launch_fwd_ring(const NormFwdArgs& a, int sms, cudaStream_t st) {
 }
 
 // launch == false: only how many blocks of the plan an SM holds (0: this form does not exist)
-template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
-static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS, bool FULL>
+static int bwd_ring_full(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
   using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
   if constexpr (!Ring::FITS) {
     return launch ? SAPO_ERR_CUDA : 0;
   } else {
     static int cache[33][MAX_DEVICES] = {{0}};                       // by warps of the block
-    auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS, SLOTS>;
+    auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS, SLOTS, FULL>;
     // the ring, or the columns' sums that take its place at the end
     size_t smem = (size_t)Ring::STAGES * (p.threads / 32) * Ring::WARP_BYTES;
     if (p.rows_per_block > 1 && smem < (size_t)2 * a.H * sizeof(float)) smem = (size_t)2 * a.H * sizeof(float);
@@ -133,6 +138,11 @@ static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, boo
     kernel<<<blocks, p.threads, smem, st>>>(a, p.wpr);
     return check_launch();
   }
+}
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
+static int bwd_ring_vpl(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {
+  return a.H == p.wpr * VPL * 256 ? bwd_ring_full<TX, TDY, VPL, MAX_THREADS, SLOTS, true>(a, p, blocks, launch, st)
+                                  : bwd_ring_full<TX, TDY, VPL, MAX_THREADS, SLOTS, false>(a, p, blocks, launch, st);
 }
 template <class TX, class TDY>
 static int bwd_ring_dy(const NormBwdArgs& a, const RingPlan& p, int blocks, bool launch, cudaStream_t st) {

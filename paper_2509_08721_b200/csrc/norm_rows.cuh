@@ -16,9 +16,13 @@ namespace sapo {
 // columns per clock), so the arithmetic is done in pairs and every vector is whole.
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 // (predicated, not branched around: a lane whose columns do not exist copies nothing)
-template <int BYTES>
+template <int BYTES, bool ALWAYS>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool exists) {
-  if constexpr (BYTES == 16)
+  if constexpr (ALWAYS && BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else if constexpr (ALWAYS)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+  else if constexpr (BYTES == 16)
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}"
                  ::"r"(dst), "l"(src), "r"((uint32_t)exists) : "memory");
   else
@@ -38,13 +42,14 @@ struct WarpRow {
     return sizeof(TX) == 4 ? (lane ^ ((lane >> 3) & 1)) * 16 : lane * 8 * (int)sizeof(TX);
   }
   // dst, src: with the lane's offsets; cols: how many of the warp's columns exist (a multiple of 8)
+  template <bool FULL>
   __device__ static __forceinline__ void copy(uint32_t dst, const TX* src, int cols, int lane) {
     // fp32: neighbouring lanes copy neighbouring 16 bytes; a lane then reads two of them in a row, so pieces
     // are stored with the lowest bit of their index flipped in every other eight: no bank conflicts
     constexpr int B = LANE * (int)sizeof(TX);
     #pragma unroll
     for (int v = 0; v < PER_V * VPL; ++v)
-      copy_async<B>(dst + v * 32 * B, src + v * 32 * LANE, v * 32 * LANE + lane * LANE < cols);
+      copy_async<B, FULL>(dst + v * 32 * B, src + v * 32 * LANE, v * 32 * LANE + lane * LANE < cols);
   }
   // the lane's vector v
   __device__ static __forceinline__ void read(const uint8_t* at, int v, int lane, float2 (&x)[4]) {
@@ -72,7 +77,7 @@ __device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stage
   __syncwarp();
 }
 // TX int8_t: replay from a checkpoint (a.q), statistics given.
-template <class TX, int VPL>
+template <class TX, int VPL, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
   constexpr bool REPLAY = sizeof(TX) == 1;
   constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
@@ -92,17 +97,19 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   constexpr int STAGE_BYTES = WARPS * Row::BYTES;
   uint8_t* mine = ring + warp * Row::BYTES;
   for (int i = threadIdx.x; i < 2 * WARPS * WARPS; i += NORM_THREADS) red[i] = 0.f;
-  if (cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
+  if (!FULL && cols < VPL * 256) clear_stages(mine, Row::BYTES, S, STAGE_BYTES, lane);
   const uint32_t dst = smem_addr(mine) + Row::lane_dst(lane);
   const float inv_h = 1.f / (float)a.H;
   const int ysz = a.y.dtype == SAPO_DTYPE_F32 ? 4 : 2;
   char* y_row = static_cast<char*>(a.y.p) + (row0 * a.y.ld + col0) * ysz;
   const int64_t y_step = step * a.y.ld * ysz;
-  int64_t ahead = row0;                                 // the next row to fetch, `src` its address
+  // rows of this group, and how many of them are still to fetch (`src`: the next one)
+  const int n_rows = row0 < a.T ? (int)((a.T - row0 + step - 1) / step) : 0;
+  int to_fetch = n_rows;
   auto fetch = [&](int stage) {
-    if (ahead < a.T) Row::copy(dst + stage * STAGE_BYTES, src, cols, lane);
+    if (to_fetch > 0) Row::template copy<FULL>(dst + stage * STAGE_BYTES, src, cols, lane);
     copy_commit();
-    ahead += step;
+    --to_fetch;
     src += step * ld;
   };
   #pragma unroll
@@ -127,7 +134,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   }
   __syncthreads();
   int stage = 0, turn = 0;
-  for (int64_t row = row0; row < a.T; row += step) {
+  int64_t row = row0;
+  for (int i = 0; i < n_rows; ++i, row += step) {
     copy_wait<S - 2>();
     __syncwarp();
     fetch(stage == 0 ? S - 1 : stage - 1);
@@ -138,7 +146,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
     for (int v = 0; v < VPL; ++v) {
       Row::read(at, v, lane, x[v]);
       if (REPLAY) {
-        const float2 s = both(256 * v < left ? a.q.scale[row * a.q.ld_scale + (col0 + 256 * v) / Q8_GROUP] : 0.f);
+        const float2 s = both(FULL || 256 * v < left ? a.q.scale[row * a.q.ld_scale + (col0 + 256 * v) / Q8_GROUP] : 0.f);
         #pragma unroll
         for (int j = 0; j < 4; ++j) x[v][j] = mul2(x[v][j], s);
       }
@@ -159,7 +167,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
       float2 s2 = both(0.f), t2 = both(0.f);
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        const float2 minus = both(256 * v < left ? -mean : 0.f);
+        const float2 minus = both(FULL || 256 * v < left ? -mean : 0.f);
         #pragma unroll
         for (int j = 0; j < 4; j += 2) {
           const float2 d = add2(x[v][j], minus), e = add2(x[v][j + 1], minus);
@@ -181,7 +189,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
         quantise<VPL, 16, 4>(x, bytes, scale, bad);
         #pragma unroll
         for (int v = 0; v < VPL; ++v)
-          if (256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = pack_bytes(bytes[v]);
+          if (FULL || 256 * v < left) *reinterpret_cast<uint2*>(q_row + 256 * v) = pack_bytes(bytes[v]);
         // one lane per group: half h of the warp has the groups at columns 256 v + 128 h
         using Half = Slots<PowerOfTwo<VPL>::value, 16>;
         const int scale_col = w * VPL * 256 + 256 * Half::slot() + 128 * (lane >> 4);
@@ -195,7 +203,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
     auto finish = [&](auto f) {
       #pragma unroll
       for (int v = 0; v < VPL; ++v) {
-        if (256 * v >= left) break;
+        if (!FULL && 256 * v >= left) break;
         #pragma unroll
         for (int j = 0; j < 4; ++j) x[v][j] = mul2(add2(x[v][j], minus), r2);
         float2 u[4];
@@ -228,7 +236,7 @@ template <class TX, class TDY, int VPL, int MAX_THREADS> struct BwdRing {
   static constexpr bool HOLD = VPL <= 2;
 };
 
-template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
+template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS, bool FULL>
 __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_bwd_ring_kernel(NormBwdArgs a, int wpr) {
   constexpr bool FROM_Q8 = sizeof(TX) == 1;
   using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
@@ -250,7 +258,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   const int stage_bytes = warps * Ring::WARP_BYTES;
   for (int i = threadIdx.x; i < RED; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
   __syncthreads();
-  if (cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
+  if (!FULL && cols < VPL * 256) clear_stages(mine, Ring::WARP_BYTES, S, stage_bytes, lane);
   const int64_t ldx = FROM_Q8 ? a.q.ld : a.x.ld;
   const TX* xp = (FROM_Q8 ? reinterpret_cast<const TX*>(a.q.p) : static_cast<const TX*>(a.x.p)) + row0 * ldx + warp_col + lane * RowX::LANE;
   const TDY* dyp = static_cast<const TDY*>(a.dy.p) + row0 * a.dy.ld + warp_col + lane * RowD::LANE;
@@ -263,20 +271,23 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   // lane 0 copies rstd, lane 1 the mean
   const float* stat = lane == 0 ? a.rstd : a.mean;
   const bool copies_stat = lane == 0 || (lane == 1 && layer);
-  int64_t ahead = row0;
+  const int n_rows = row0 < a.T ? (int)((a.T - row0 + step - 1) / step) : 0;
+  int to_fetch = n_rows;
+  stat += row0;
   auto fetch = [&](int stage) {
-    if (ahead < a.T) {
+    if (to_fetch > 0) {
       const uint32_t off = stage * stage_bytes;
-      RowX::copy(dst_x + off, xp, cols, lane);
-      RowD::copy(dst_d + off, dyp, cols, lane);
-      copy_async<4>(base + off + ST_AT + lane * 4, stat + ahead, copies_stat);
+      RowX::template copy<FULL>(dst_x + off, xp, cols, lane);
+      RowD::template copy<FULL>(dst_d + off, dyp, cols, lane);
+      copy_async<4, false>(base + off + ST_AT + lane * 4, stat, copies_stat);
       if (FROM_Q8) {
         #pragma unroll
-        for (int v = 0; v < VPL; ++v) copy_async<4>(base + off + SC_AT + (v * 32 + lane) * 4, sp + 2 * v, 256 * v < left);
+        for (int v = 0; v < VPL; ++v) copy_async<4, FULL>(base + off + SC_AT + (v * 32 + lane) * 4, sp + 2 * v, 256 * v < left);
       }
     }
     copy_commit();
-    ahead += step;
+    --to_fetch;
+    stat += step;
     xp += step * ldx;
     dyp += step * a.dy.ld;
     if (FROM_Q8) sp += step * a.q.ld_scale;
@@ -299,7 +310,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   char* dx_row = static_cast<char*>(a.dx.p) + (row0 * a.dx.ld + col0) * dxsz;
   const int64_t dx_step = step * a.dx.ld * dxsz;
   int stage = 0, turn = 0;
-  for (int64_t row = row0; row < a.T; row += step) {
+  for (int i = 0; i < n_rows; ++i) {
     copy_wait<S - 2>();
     __syncwarp();
     fetch(stage == 0 ? S - 1 : stage - 1);
@@ -353,7 +364,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
         }
         #pragma unroll
         for (int j = 0; j < 4; ++j) g[k][j] = fma2(xh[k][j], c2, fma2(g[k][j], r2, c1));
-        if (256 * v < left) put8<decltype(f)::value>(dx_row, 256 * v, g[k]);
+        if (FULL || 256 * v < left) put8<decltype(f)::value>(dx_row, 256 * v, g[k]);
       }
     };
     if (a.dx.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
