@@ -601,9 +601,8 @@ int sapo_policy_loss_fwd_static(const void* hidden, const void* W_head, int32_t 
 #define SAPO_K_NORM_REDUCE 19
 #define SAPO_K_CKPT8      20
 #define SAPO_K_PREFERENCE 21
-#define SAPO_K_PREF_FINAL 22
-#define SAPO_K_PREF_SCORE 23
-#define SAPO_K_COUNT      24
+#define SAPO_K_PREF_SCORE 22
+#define SAPO_K_COUNT      23
 int sapo_timing_enable(int32_t on);
 int sapo_timing_read(float* h_ms, int32_t* h_launches);
 int64_t sapo_launch_count(void);

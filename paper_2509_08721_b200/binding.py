@@ -47,7 +47,7 @@ STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 KERNEL_NAMES = ("pack_scan", "pack_copy", "group_adv", "split_bf16", "fwd_gemm", "loss_tail",
                 "loss_final", "bwd_dz", "bwd_dh", "bwd_dw", "streamk_fixup", "compact", "select", "adam",
                 "target_logit", "fwd_exp", "fused_tail", "norm_fwd", "norm_bwd", "norm_reduce", "ckpt8", "preference",
-                "pref_final", "pref_score")
+                "pref_score")
 
 
 class RolloutBufC(C.Structure):

@@ -1550,7 +1550,7 @@ extern "C" int sapo_preference_loss_fwd_bwd(const void* hidden, const void* W_he
     return SAPO_ERR_INVALID_ARG;
   const PrefArgs pa{nullptr, nullptr, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
                     h_cfg->grad_scale, h_cfg->kind, h_cfg->pairs, h_cfg->length_norm, gscale, seq_logratio, seq_grad,
-                    q_loss, q_margin, q_pairs, loss, status, 0};
+                    q_loss, q_margin, q_pairs, loss, status, 0, nullptr};
   return preference_impl(static_cast<const __nv_bfloat16*>(hidden), static_cast<const __nv_bfloat16*>(W_head), T, H, V,
                          ld_hidden, ld_W, ids, ref_logp, pa, logp, lse, dhidden, dW_head, out_dtype, accumulate_dW,
                          static_cast<uint8_t*>(workspace), workspace_bytes, static_cast<cudaStream_t>(stream));

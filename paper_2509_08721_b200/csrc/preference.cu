@@ -8,6 +8,8 @@
 // Reads 8 bytes and writes 4 per token.
 #include <math.h>
 
+#include <atomic>
+
 #include "preference.cuh"
 
 namespace sapo {
@@ -100,7 +102,8 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
   __shared__ int32_t cu_s[PREF_SEQS + 1];
   __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS], g_s[PREF_SEQS];     // sums, rewards, factors
-  __shared__ double sums[3][PREF_WARPS];
+  __shared__ float sums[2][PREF_WARPS];
+  __shared__ int32_t counts[PREF_WARPS];
   __shared__ float scale_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t Tc = (int32_t)a.T;
@@ -110,7 +113,6 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   const int32_t cluster = (int32_t)(blockIdx.x / size);
   auto team_barrier = [] { if (SOLO) __syncthreads(); else cluster_barrier(); };
   auto to_first = [](float* p, float x) { if (SOLO) *p = x; else store_to_first(p, x); };
-  if (!SOLO) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   bool bad_offset = false, bad_value = false, bad_reward = false;
   if (cluster >= a.q_clusters) {
     // the clusters behind those of the questions: what no question covers, sequences before the first and after the
@@ -247,7 +249,9 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           if (w2 >= 0 && (worst < 0 || l2 < lo || (l2 == lo && w2 < worst))) { lo = l2; worst = w2; }
         }
       }
-      double loss = 0.0, margin = 0.0, count = 0.0;
+      // (a lane adds up its pairs in 64 bits; the few lanes' and warps' sums are joined in 32)
+      double loss = 0.0, margin = 0.0;
+      int32_t count = 0;
       for (int32_t i = s0 + warp; i < s1; i += PREF_WARPS) {
         const float r = reward_of(i), R = ratio_of(i);
         double f = 0.0;
@@ -262,24 +266,24 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           float l, dl;
           pair_loss(a, h, l, dl);
           f += wins ? (double)dl : -(double)dl;
-          if (wins) { loss += (double)l; margin += (double)h; count += 1.0; }     // each pair once
+          if (wins) { loss += (double)l; margin += (double)h; ++count; }          // each pair once
         }
-        f = warp_sum(f);
-        if (lane == 0) { if (kept) g_s[i - s0] = (float)f; else a.seq_grad[i] = (float)f; }   // scaled below, once the pairs are counted
+        const float factor = warp_sum((float)f);
+        if (lane == 0) { if (kept) g_s[i - s0] = factor; else a.seq_grad[i] = factor; }   // scaled below, once the pairs are counted
       }
-      loss = warp_sum(loss); margin = warp_sum(margin); count = warp_sum(count);
-      if (lane == 0) { sums[0][warp] = loss; sums[1][warp] = margin; sums[2][warp] = count; }
+      const float loss_w = warp_sum((float)loss), margin_w = warp_sum((float)margin);
+      count = __reduce_add_sync(0xffffffffu, count);
+      if (lane == 0) { sums[0][warp] = loss_w; sums[1][warp] = margin_w; counts[warp] = count; }
       __syncthreads();
       if (warp == 0) {
-        loss = warp_sum(lane < PREF_WARPS ? sums[0][lane] : 0.0);
-        margin = warp_sum(lane < PREF_WARPS ? sums[1][lane] : 0.0);
-        count = warp_sum(lane < PREF_WARPS ? sums[2][lane] : 0.0);
-        const double per = count > 0.0 ? 1.0 / count : 0.0;
+        const float loss_q = warp_sum(lane < PREF_WARPS ? sums[0][lane] : 0.f), margin_q = warp_sum(lane < PREF_WARPS ? sums[1][lane] : 0.f);
+        count = __reduce_add_sync(0xffffffffu, lane < PREF_WARPS ? counts[lane] : 0);
+        const float per = count > 0 ? 1.f / (float)count : 0.f;
         if (lane == 0) {
-          a.q_loss[q] = (float)(loss * per);
-          if (a.q_margin != nullptr) a.q_margin[q] = (float)(margin * per);
-          if (a.q_pairs != nullptr) a.q_pairs[q] = (int32_t)count;
-          scale_s = (float)((double)a.grad_scale * (double)a.beta * per / (double)a.Q);
+          a.q_loss[q] = loss_q * per;
+          if (a.q_margin != nullptr) a.q_margin[q] = margin_q * per;
+          if (a.q_pairs != nullptr) a.q_pairs[q] = count;
+          scale_s = a.grad_scale * a.beta * per / (float)a.Q;
         }
       }
       __syncthreads();
@@ -311,28 +315,39 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   if (bad_reward) raise_status(a.status, SAPO_ST_NONFINITE_REWARD);
   // the first block's shared memory stays until the others have read the factors from it
   cluster_barrier();
-  if (SOLO && blockIdx.x == 0 && warp == 0) {
-    double x = 0.0;
-    for (int32_t q = lane; q < a.Q; q += 32) x += (double)__ldcg(a.q_loss + q);
-    x = warp_sum(x);
-    if (lane == 0) *a.loss = (float)(x / (double)a.Q);
+  // The loss is the mean of the questions' losses, added up in their order by the block that comes last (SOLO: by the
+  // first, behind the barrier).
+  if (rank != 0 || warp != 0 || (SOLO && blockIdx.x != 0)) return;
+  if (!SOLO) {
+    uint32_t before = 0;
+    if (lane == 0) {
+      __threadfence();                                     // this block's q_loss before its ticket
+      before = atomicAdd(a.ticket, 1u);
+    }
+    if (__shfl_sync(0xffffffffu, before, 0) != (uint32_t)a.q_clusters - 1u) return;
+    __threadfence();
+    if (lane == 0) *a.ticket = 0u;
   }
+  double x = 0.0;
+  for (int32_t q = lane; q < a.Q; q += 32) x += (double)__ldcg(a.q_loss + q);
+  x = warp_sum(x);
+  if (lane == 0) *a.loss = (float)(x / (double)a.Q);
 }
 
-// loss = the mean of the questions' losses
-__global__ void __launch_bounds__(256) preference_final_kernel(const float* q_loss, int32_t Q, float* loss) {
-  __shared__ double sh[8];
-  asm volatile("griddepcontrol.wait;" ::: "memory");         // launched while preference_kernel still runs
-  double x = 0.0;
-  for (int32_t q = threadIdx.x; q < Q; q += 256) x += (double)__ldcg(q_loss + q);
-  x = warp_sum(x);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    x = 0.0;
-    for (int i = 0; i < 8; ++i) x += sh[i];
-    *loss = (float)(x / (double)Q);
+// How many clusters of a launch have finished: one counter per launch, left at zero by it.  Launches take them in turn,
+// so two that run at the same time (other streams, other threads) share one only if 16384 launches were made
+// between them; a captured graph keeps the counters of its capture, which is fine as a graph does not run beside itself.
+constexpr int PREF_TICKETS = 16384;
+static __device__ uint32_t g_pref_tickets[PREF_TICKETS];
+static uint32_t* next_ticket(int dev) {
+  static uint32_t* base[MAX_DEVICES] = {nullptr};
+  static std::atomic<uint32_t> next{0};
+  if (base[dev] == nullptr) {
+    void* p = nullptr;
+    if (cudaGetSymbolAddress(&p, g_pref_tickets) != cudaSuccess) return nullptr;
+    base[dev] = static_cast<uint32_t*>(p);
   }
+  return base[dev] + next.fetch_add(1u) % PREF_TICKETS;
 }
 
 int pref_check_cfg(const sapo_pref_cfg* c) {
@@ -373,8 +388,8 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
   cfg.numAttrs = 1;
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  // Few questions of few tokens: one cluster has a block for each and one for what they do not cover, and needs no
-  // second kernel for the loss (a call for 4 questions of 256 tokens: 8.2 us with it, 10.2 us with the second kernel).
+  // Few questions of few tokens: one cluster has a block for each and one for what they do not cover, and its barrier
+  // takes the place of the count of finished clusters.
   if (cluster == 1 && a.Q < PREF_MAX_CLUSTER && a.T <= 65536) {
     while (cluster <= a.Q) cluster <<= 1;
     a.q_clusters = a.Q;
@@ -390,20 +405,10 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
   outside = outside < 1 ? 1 : (outside > 32 ? 32 : outside);
   attr[0].val.clusterDim.x = (unsigned)cluster;
   cfg.gridDim = dim3((unsigned)((a.q_clusters + outside) * cluster));
-  {
-    KernelScope scope(SAPO_K_PREFERENCE, st);
-    if (cudaLaunchKernelEx(&cfg, preference_kernel<false>, a) != cudaSuccess) return SAPO_ERR_CUDA;
-  }
-  cudaLaunchConfig_t fin{};
-  fin.gridDim = dim3(1);
-  fin.blockDim = dim3(256);
-  fin.stream = st;
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  fin.attrs = attr;
-  fin.numAttrs = 1;
-  KernelScope scope(SAPO_K_PREF_FINAL, st);
-  return cudaLaunchKernelEx(&fin, preference_final_kernel, (const float*)a.q_loss, a.Q, a.loss) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
+  a.ticket = next_ticket(dev);
+  if (a.ticket == nullptr) return SAPO_ERR_CUDA;
+  KernelScope scope(SAPO_K_PREFERENCE, st);
+  return cudaLaunchKernelEx(&cfg, preference_kernel<false>, a) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
 }
 
 }  // namespace sapo
@@ -424,6 +429,6 @@ extern "C" int sapo_preference_loss(const float* logp, const float* ref_logp, in
   // an empty batch has no pointers to read through, but the kernel asks which kind of input it has
   PrefArgs a{logp, ref_logp, T, cu_seqlens, S, rewards, group_offsets, Q, h_cfg->beta, h_cfg->label_smoothing,
              h_cfg->grad_scale, h_cfg->kind, h_cfg->pairs, h_cfg->length_norm, gscale, seq_logratio, seq_grad,
-             q_loss, q_margin, q_pairs, loss, status, 0};
+             q_loss, q_margin, q_pairs, loss, status, 0, nullptr};
   return launch_preference(a, static_cast<cudaStream_t>(stream));
 }

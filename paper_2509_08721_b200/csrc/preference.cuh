@@ -13,7 +13,8 @@ struct PrefArgs {
   float beta, smoothing, grad_scale; int32_t kind, pairs, length_norm;
   float* gscale; float* seq_logratio; float* seq_grad; float* q_loss; float* q_margin; int32_t* q_pairs; float* loss;
   int32_t* status;
-  int32_t q_clusters;      // set by launch_preference: clusters of blocks that take questions
+  // set by launch_preference: clusters of blocks that take questions, and the counter of those that have finished
+  int32_t q_clusters; uint32_t* ticket;
 };
 
 int pref_check_cfg(const sapo_pref_cfg* h_cfg);

@@ -5,8 +5,8 @@ Bounds on the call that takes log-probs.  u = 2^-24.  A sequence's sum adds at m
 in a thread and joins 64 such sums in trees or chains, of differences that are off by u |d| themselves:
   tR_s = (T_s / 32 + 70) u sum |d|      (divided by T_s with length_norm, one more rounding)
   th   = beta (tR_i + tR_j) + 4 u |h|
-l changes by at most |l'| th, l' by at most |l''| th, plus 8 roundings of values of their size; the
-pair sums are kept in 64 bits."""
+l changes by at most |l'| th, l' by at most |l''| th, plus 8 roundings of values of their size (a pair's own and
+those of joining the pairs' sums, which a lane keeps in 64 bits)."""
 import numpy as np
 import pytest
 import torch
@@ -322,3 +322,23 @@ def test_head_leaves_out_blocks_without_a_pair(pairs):
     r = head_check(c, got, 0.1, pairs=pairs)
     assert list(r["q_pairs"]) == [0, 0, 5 if pairs == "all" else 1]
     assert not got["dhidden"][:730].any() and torch.isfinite(got["dW"]).all() and got["status"] == 0
+
+
+def test_many_calls_on_two_streams_repeat_bit_for_bit():
+    """Calls on two streams at once, more of them than the library has counters: every loss is the first one's."""
+    c = case(list(RNG.integers(20, 60, size=80)), [2] * 40, seed=18)
+    d = {k: torch.from_numpy(c[k]).cuda() for k in ("logp", "ref", "cu", "go", "rewards")}
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    n = 9000
+    losses = torch.full((2 * n,), float("nan"), device="cuda")
+    status = B.new_status()
+    outs = [B.alloc_preference_outputs(c["T"], c["S"], c["Q"]) for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(n):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                out = dict(outs[k], loss=losses[2 * i + k:2 * i + k + 1])
+                B.sapo_preference_loss(d["logp"], d["ref"], d["cu"], d["rewards"], d["go"], 0.1, out, status)
+    torch.cuda.synchronize()
+    assert torch.isfinite(losses).all() and (losses == losses[0]).all() and status.item() == 0
+    check(c, dict(run(c, 0.1)), 0.1)
