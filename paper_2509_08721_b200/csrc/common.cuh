@@ -93,6 +93,32 @@ struct KernelScope {
   ~KernelScope() { if (slot >= 0) cudaEventRecord(kernel_timer().stop[slot], st); }
 };
 
+// Programmatic dependent launch.  A kernel launched by launch_overlapped may start while the kernel before it in the
+// stream still runs (once all blocks of that one have called let_next_start, or ended) and waits in wait_for_previous
+// until it is complete and its writes are visible; it has to call that before it touches global memory.  Two plain
+// launches in a row cost more than the second's start: on the B200s measured here, kernels that follow one another in
+// a stream took multiples of 2.05 us each (2.1 us of work 4.1 us, 4.1 us of work 6.15 us), overlapped ones their work
+// and 0.5 us.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// cluster: blocks of a cluster, 0 for a launch without clusters
+template <class... Params, class... Args>
+inline int launch_overlapped(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 0 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
+}
+
 template <typename T>
 __host__ __device__ constexpr T ceil_div(T a, T b) { return (a + b - 1) / b; }
 template <typename T>

@@ -345,6 +345,7 @@ struct StoreEpi {
 // Part order is fixed (by pair index), so the result does not depend on timing.
 __global__ void __launch_bounds__(256)
 streamk_fixup_kernel(const Sched s_arg, const StoreEpi::Params p_arg, int pairs) {
+  wait_for_previous();
   Sched s = s_arg;
   StoreEpi::Params p = p_arg;
   finalize_sched(s, pairs);

@@ -73,6 +73,8 @@ umma_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
   fence_before_sync();
   __syncthreads();
   cluster_sync_all();
+  // overlapped launches (never with a size that is read from memory): no global memory before this line
+  wait_for_previous();
   fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   // cluster addresses of barriers the other CTA signals or that live in the even CTA
@@ -328,6 +330,7 @@ umma_gemm2_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
   uint64_t* drain = bars + 2 * STAGES2 + 3;   // MMA thread only, after a wait ran out (see umma_gemm_kernel)
   uint32_t* mask_s = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(bars) + 256);
   uint8_t* out_staging = reinterpret_cast<uint8_t*>(bars) + GEMM2_TAIL_BYTES;
+  wait_for_previous();      // overlapped launches: no global memory before this line
   // the mask only matters if some block of the chunk is clear: decided once, by every thread alike
   bool has_mask = false;
   if (sched.active_mask != nullptr) {

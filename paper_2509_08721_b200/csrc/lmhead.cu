@@ -136,7 +136,7 @@ constexpr int FWD_BK = BK, FWD_STAGES = STAGES;
 template <int A_KIND, bool B_MN, class Epi, int BKT = BK, int NSTAGE = STAGES, class Gather = NoGather>
 static int launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const Sched& sched,
                        const typename Epi::Params& ep, int32_t* status, cudaStream_t st, int kernel_id,
-                       const Gather& ga = Gather{}) {
+                       const Gather& ga = Gather{}, bool overlap = false) {
   auto kern = umma_gemm_kernel<A_KIND, B_MN, Epi, BKT, NSTAGE, Gather>;
   // CTA pairs the device can hold at once; found, together with the kernel's shared-memory
   // opt-in, on the first use on each device
@@ -147,9 +147,11 @@ static int launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const Sched
   if (sched.num_units <= 0) return SAPO_OK;
   Sched sc = sched;
   sc.stats_id = (kernel_id == SAPO_K_FWD_GEMM || kernel_id == SAPO_K_FWD_EXP) ? 0 : kernel_id - SAPO_K_BWD_DZ + 1;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;    // overlap: see launch_overlapped
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(GEMM_THREADS, 1, 1);
   constexpr size_t smem_bytes = 1024 + (size_t)NSTAGE * (BM + BN / 2) * BKT * 2 + 256 +
@@ -180,6 +182,7 @@ static int launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const Sched
     }
   }
   cfg.gridDim = dim3(2 * pairs, 1, 1);
+  cfg.numAttrs = overlap ? 2 : 1;
   {
     KernelScope scope(kernel_id, st);
     if (cudaLaunchKernelEx(&cfg, kern, ma, mb, sc, ep, status, ga) != cudaSuccess) return SAPO_ERR_CUDA;
@@ -190,6 +193,7 @@ static int launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const Sched
     const int fix_tiles = sc.dyn_dim != 0 ? (sc.k_split_ok ? pairs - 1 : 0) : sc.sk_tiles;
     if (fix_tiles > 0) {
       KernelScope scope(SAPO_K_STREAMK_FIXUP, st);
+      if (overlap) return launch_overlapped(streamk_fixup_kernel, dim3((unsigned)fix_tiles * 32), 256, 0, 0, st, sc, ep, pairs);
       streamk_fixup_kernel<<<fix_tiles * 32, 256, 0, st>>>(sc, ep, pairs);
     }
   }
@@ -216,7 +220,7 @@ static bool use_wide_tiles(int32_t N) { return N >= BN; }
 
 template <int A_KIND>
 static int launch_gemm_wide(const CUtensorMap& ma, const CUtensorMap& mb, const Sched& sched,
-                            const StoreEpi::Params& ep, int32_t* status, cudaStream_t st, int kernel_id) {
+                            const StoreEpi::Params& ep, int32_t* status, cudaStream_t st, int kernel_id, bool overlap) {
   CUtensorMap mc;
   if (!make_map_out(&mc, ep.C, ep.out_bf16 != 0, ep.N, ep.M, ep.ldc)) return SAPO_ERR_CUDA;
   auto kern = umma_gemm2_kernel<A_KIND>;
@@ -227,9 +231,11 @@ static int launch_gemm_wide(const CUtensorMap& ma, const CUtensorMap& mb, const 
   if (sched.num_units <= 0) return SAPO_OK;
   Sched sc = sched;
   sc.stats_id = kernel_id - SAPO_K_BWD_DZ + 1;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;    // overlap: see launch_overlapped
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(GEMM_THREADS, 1, 1);
   cfg.dynamicSmemBytes = GEMM2_SMEM_BYTES;
@@ -253,12 +259,14 @@ static int launch_gemm_wide(const CUtensorMap& ma, const CUtensorMap& mb, const 
   split_last_wave(sc, max_pairs);
   if (sc.sk_tiles > 0) pairs = max_pairs;
   cfg.gridDim = dim3(2 * pairs, 1, 1);
+  cfg.numAttrs = overlap ? 2 : 1;
   {
     KernelScope scope(kernel_id, st);
     if (cudaLaunchKernelEx(&cfg, kern, ma, mb, mc, sc, ep, status) != cudaSuccess) return SAPO_ERR_CUDA;
   }
   if (sc.sk_tiles > 0) {
     KernelScope scope(SAPO_K_STREAMK_FIXUP, st);
+    if (overlap) return launch_overlapped(streamk_fixup_kernel, dim3((unsigned)sc.sk_tiles * 32), 256, 0, 0, st, sc, ep, pairs);
     streamk_fixup_kernel<<<sc.sk_tiles * 32, 256, 0, st>>>(sc, ep, pairs);
   }
   return check_launch();
@@ -272,7 +280,7 @@ static int launch_grad_gemms(const __nv_bfloat16* panel, int64_t panel_rows, int
                              const __nv_bfloat16* W, int64_t ldw, const __nv_bfloat16* X, int64_t ldx,
                              int64_t tc, int32_t H, int32_t V, int64_t Vp, void* dhidden, bool dh_bf16,
                              const float* row_scale, void* dW_head, bool dw_bf16, int accumulate, float* partials,
-                             const uint32_t* active_mask, int32_t* status, cudaStream_t st) {
+                             const uint32_t* active_mask, int32_t* status, cudaStream_t st, bool overlap = false) {
   StoreEpi::Params ep_h{dhidden, H, tc, H, 0, partials, nullptr, row_scale, dh_bf16 ? 1 : 0, tc, MAX_PARTS_SCRATCH};
   StoreEpi::Params ep_w{dW_head, H, V, H, accumulate, partials, nullptr, nullptr, dw_bf16 ? 1 : 0, V, MAX_PARTS_SCRATCH};
   if (use_wide_tiles(H)) {
@@ -287,12 +295,12 @@ static int launch_grad_gemms(const __nv_bfloat16* panel, int64_t panel_rows, int
     Sched sh = make_sched_wide(tc, H, Vp);
     sh.panel_nvt = nvt;
     if (masked) { sh.active_mask = active_mask; sh.mask_words = mask_words; sh.mask_dim = 1; }
-    int rc = launch_gemm_wide<2>(map_p_tile, map_w64, sh, ep_h, status, st, SAPO_K_BWD_DH);
+    int rc = launch_gemm_wide<2>(map_p_tile, map_w64, sh, ep_h, status, st, SAPO_K_BWD_DH, overlap);
     if (rc != SAPO_OK) return rc;
     Sched sw = make_sched_wide(V, H, tc);
     sw.panel_nvt = nvt;
     if (masked) { sw.active_mask = active_mask; sw.mask_words = mask_words; sw.mask_dim = 2; }
-    return launch_gemm_wide<3>(map_p_half, map_x64, sw, ep_w, status, st, SAPO_K_BWD_DW);
+    return launch_gemm_wide<3>(map_p_half, map_x64, sw, ep_w, status, st, SAPO_K_BWD_DW, overlap);
   }
   CUtensorMap map_p_two, map_p_tile, map_w_mn, map_x_mn;
   if (!make_map(&map_p_two, panel, 64, panel_rows, 64, 256) || !make_map(&map_p_tile, panel, 64, panel_rows, 64, BM) ||
@@ -300,11 +308,11 @@ static int launch_grad_gemms(const __nv_bfloat16* panel, int64_t panel_rows, int
     return SAPO_ERR_CUDA;
   Sched sh = make_sched(tc, H, Vp, 0, /*m_fastest=*/false);
   sh.panel_nvt = nvt;
-  int rc = launch_gemm<2, true, StoreEpi>(map_p_two, map_w_mn, sh, ep_h, status, st, SAPO_K_BWD_DH);
+  int rc = launch_gemm<2, true, StoreEpi>(map_p_two, map_w_mn, sh, ep_h, status, st, SAPO_K_BWD_DH, NoGather{}, overlap);
   if (rc != SAPO_OK) return rc;
   Sched sw = make_sched(V, H, tc, 0, /*m_fastest=*/false);
   sw.panel_nvt = nvt;
-  return launch_gemm<3, true, StoreEpi>(map_p_tile, map_x_mn, sw, ep_w, status, st, SAPO_K_BWD_DW);
+  return launch_gemm<3, true, StoreEpi>(map_p_tile, map_x_mn, sw, ep_w, status, st, SAPO_K_BWD_DW, NoGather{}, overlap);
 }
 
 static int launch_split(const float* X, int64_t ld, int64_t R, int32_t H, __nv_bfloat16* out, int mode,
@@ -1281,8 +1289,10 @@ static float z_compensation(int32_t H) { return 1.f + 1.5e-8f * (float)(H / 16);
 
 // flags[s] = 1 for every sequence that may enter a pair, else 0, one warp per question: a sequence with a token and a
 // finite reward, in a question with two different such rewards; with best against worst, those two.  Also zero
-// for sequences of no question.  (A pair can still drop out for its log ratios; none can come in.)
-__global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __restrict__ flags) {
+// for sequences of no question, and the words of `need` that target_logit_kernel sets bits in.  (A pair can still drop out for its log ratios; none can come in.)
+__global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __restrict__ flags, uint32_t* need, int32_t need_words) {
+  wait_for_previous();
+  let_next_start();
   const int lane = threadIdx.x & 31;
   const int32_t q = blockIdx.x * 8 + (threadIdx.x >> 5);
   auto clamp = [&](int32_t s) { return s < 0 ? 0 : (s > a.S ? a.S : s); };
@@ -1292,6 +1302,7 @@ __global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __re
     if (hi < lo) hi = lo;
     const int32_t warps = gridDim.x * 8 - a.Q;
     for (int32_t i = (q - a.Q) * 32 + lane; i < lo + a.S - hi; i += warps * 32) flags[i < lo ? i : hi + (i - lo)] = 0.f;
+    for (int32_t i = (q - a.Q) * 32 + lane; i < need_words; i += warps * 32) need[i] = 0u;
     return;
   }
   const int32_t s0 = clamp(a.group_offsets[q]);
@@ -1329,6 +1340,7 @@ struct PrefTailArgs {
   const int32_t* ids; int32_t V; const float* ref_logp; const int32_t* cu; int32_t S; int64_t T;
   float* logp; float* lse; float* log_ratio;             // [T]
   int32_t* status;
+  uint32_t* active_mask;                                 // cleared here for pref_scale_kernel, or nullptr
 };
 
 // After the forward pass of a chunk, one warp per token:  sum = sum_v exp(z - c) with c = z_y - ref (nearly),
@@ -1337,6 +1349,10 @@ struct PrefTailArgs {
 // hundreds of tokens are summed over, is free of the rounding of lse (1e-6 for an lse around 12).
 // A masked token gets the log ratio NaN.
 __global__ void __launch_bounds__(256) pref_score_kernel(PrefTailArgs a) {
+  wait_for_previous();
+  let_next_start();
+  if (a.active_mask != nullptr && blockIdx.x == 0)
+    for (int i = threadIdx.x; i < MASK_WORDS_MAX; i += 256) a.active_mask[i] = 0u;
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n_warps = (int64_t)gridDim.x * 8;
   int32_t lo, hi;
@@ -1379,6 +1395,8 @@ struct PrefScaleArgs {
 // fused_tail_kernel: the row scale a_t = -g_t / sum_t, the chosen token's entry e_y - sum_t, hs = a_t hidden.
 // A token without a gradient only needs a zero scale and row.
 __global__ void __launch_bounds__(256) pref_scale_kernel(PrefScaleArgs a) {
+  wait_for_previous();
+  let_next_start();
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), n_warps = (int64_t)gridDim.x * 8;
   for (int64_t t = warp; t < a.T; t += n_warps) {
@@ -1467,19 +1485,22 @@ static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, 
   // chunks keeps no exponentials at all.
   const bool by_block = use_wide_tiles(H) && ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) <= MASK_WORDS_MAX;
   const bool choose = one_pass && by_block;
+  const int32_t need_words = (int32_t)ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32);
+  int rc = SAPO_OK;
   float* flags = pa.seq_grad;                    // until the loss writes it
   if (choose) {
     KernelScope scope(SAPO_K_PREF_SCORE, st);
-    pref_flags_kernel<<<ceil_div(pa.Q, 8) + 1, 256, 0, st>>>(pa, flags);
+    rc = launch_overlapped(pref_flags_kernel, dim3((unsigned)ceil_div(pa.Q, 8) + 1), 256, 0, 0, st, pa, flags, need, need_words);
+    if (rc != SAPO_OK) return rc;
   }
-  if ((choose || !one_pass) &&
-      cudaMemsetAsync(need, 0, (size_t)ceil_div<int64_t>(ceil_div<int64_t>(T, BM), 32) * 4, st) != cudaSuccess)
-    return SAPO_ERR_CUDA;
+  if (!one_pass && cudaMemsetAsync(need, 0, (size_t)need_words * 4, st) != cudaSuccess) return SAPO_ERR_CUDA;
   // 1. chosen-token logits and the reference of the exponentials
   {
     KernelScope scope(SAPO_K_TARGET_LOGIT, st);
-    target_logit_kernel<<<token_blocks(T), 256, 0, st>>>(RowSource{hidden, nullptr, ld_hidden, nullptr, 0, 0}, W, ld_W, ids,
-                                                         ref_logp, T, H, V, zy, c2, flags, pa.cu, pa.S, choose ? need : nullptr);
+    rc = launch_overlapped(target_logit_kernel, dim3((unsigned)token_blocks(T)), 256, 0, 0, st,
+                           RowSource{hidden, nullptr, ld_hidden, nullptr, 0, 0}, W, ld_W, ids, ref_logp, T, H, V, zy, c2, flags, pa.cu,
+                           pa.S, choose ? need : nullptr);
+    if (rc != SAPO_OK) return rc;
   }
   // 2. exponentials and their sums, then the log ratio of every token
   CUtensorMap map_w;
@@ -1494,35 +1515,36 @@ static int preference_impl(const __nv_bfloat16* hidden, const __nv_bfloat16* W, 
     fs.n_cover = (int32_t)Vp;
     ExpEpi::Params ep{c2 + t0, ps, nullptr, tc, V, nvt, panel, ceil_div<int64_t>(tc, BM) * nvt * BM, 2 * FUSED_MAX_SPLITS,
                       choose || !one_pass ? need : nullptr, (int32_t)(t0 / BM), LOG2E * z_compensation(H)};
-    const int rc = launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES>(map_h, map_w, fs, ep, pa.status, st, SAPO_K_FWD_EXP);
+    rc = launch_gemm<0, false, ExpEpi, FWD_BK, FWD_STAGES>(map_h, map_w, fs, ep, pa.status, st, SAPO_K_FWD_EXP, NoGather{}, /*overlap=*/true);
     if (rc != SAPO_OK) return rc;
     KernelScope scope(SAPO_K_PREF_SCORE, st);
-    pref_score_kernel<<<token_blocks(tc), 256, 0, st>>>(PrefTailArgs{ps, 2 * fs.units_per_m, t0, tc, zy, c2, sum, ids, V, ref_logp,
-                                                                     pa.cu, pa.S, T, logp, lse, log_ratio, pa.status});
+    rc = launch_overlapped(pref_score_kernel, dim3((unsigned)token_blocks(tc)), 256, 0, 0, st,
+                           PrefTailArgs{ps, 2 * fs.units_per_m, t0, tc, zy, c2, sum, ids, V, ref_logp, pa.cu, pa.S, T, logp, lse, log_ratio,
+                                        pa.status, choose ? active_mask : nullptr});
+    if (rc != SAPO_OK) return rc;
   }
   // 3. the loss and every token's factor
   pa.logp = log_ratio;
   pa.ref_logp = nullptr;
-  int rc = launch_preference(pa, st);
-  if (rc != SAPO_OK) return rc;
+  if ((rc = launch_preference(pa, st)) != SAPO_OK) return rc;
   // 4. the gradients
   if (!one_pass)
     return bwd_impl(hidden, W, SAPO_DTYPE_BF16, T, H, V, ld_hidden, ld_W, ids, 0, lse, pa.gscale, dhidden, dW_head, out_dtype,
                     accumulate_dW, ws, workspace_bytes, pa.status, st);
   const int64_t panel_rows = ceil_div<int64_t>(T, BM) * nvt * BM;
   float* row_scale = reinterpret_cast<float*>(ws + CL.row_scale);
-  if (by_block && cudaMemsetAsync(active_mask, 0, (size_t)MASK_WORDS_MAX * 4, st) != cudaSuccess) return SAPO_ERR_CUDA;
   {
     KernelScope scope(SAPO_K_FUSED_TAIL, st);
-    pref_scale_kernel<<<token_blocks(T), 256, 0, st>>>(PrefScaleArgs{sum, zy, c2, ids, V, pa.gscale, T, row_scale, panel, nvt,
-                                                                     panel_rows, hidden, ld_hidden, H, hs,
-                                                                     by_block ? active_mask : nullptr});
+    rc = launch_overlapped(pref_scale_kernel, dim3((unsigned)token_blocks(T)), 256, 0, 0, st,
+                           PrefScaleArgs{sum, zy, c2, ids, V, pa.gscale, T, row_scale, panel, nvt, panel_rows, hidden, ld_hidden, H, hs,
+                                         choose ? active_mask : nullptr});
+    if (rc != SAPO_OK) return rc;
   }
   const bool dw_via_acc = out_bf16 && accumulate_dW;
   float* dw_acc = reinterpret_cast<float*>(ws + L.dw_acc);
   rc = launch_grad_gemms(panel, panel_rows, nvt, W, ld_W, hs, H, T, H, V, Vp, dhidden, out_bf16, row_scale,
                          dw_via_acc ? (void*)dw_acc : dW_head, out_bf16 && !dw_via_acc, dw_via_acc ? 0 : accumulate_dW,
-                         reinterpret_cast<float*>(ws + L.partials), by_block ? active_mask : nullptr, pa.status, st);
+                         reinterpret_cast<float*>(ws + L.partials), choose ? active_mask : nullptr, pa.status, st, /*overlap=*/true);
   if (rc != SAPO_OK || !dw_via_acc) return rc;
   return launch_round_to_bf16(dw_acc, dW_head, (int64_t)V * H, 1, st);
 }

@@ -255,6 +255,8 @@ target_logit_kernel(const RowSource rows, const __nv_bfloat16* __restrict__ W,
                     int64_t T, int32_t H, int32_t V, float* __restrict__ zy, float* __restrict__ c2,
                     const float* __restrict__ adv, const int32_t* __restrict__ cu, int32_t S,
                     uint32_t* __restrict__ need) {
+  wait_for_previous();
+  let_next_start();
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   const int64_t n_warps = (int64_t)gridDim.x * 8;

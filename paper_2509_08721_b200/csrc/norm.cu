@@ -102,8 +102,7 @@ static int launch_fwd_ring_full(const NormFwdArgs& a, const RingPlan& p, int sms
   int64_t blocks = ceil_div<int64_t>(a.T, p.rows_per_block);
   if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
   KernelScope scope(SAPO_K_NORM_FWD, st);
-  kernel<<<(int)blocks, p.threads, smem, st>>>(a, p.wpr);
-  return check_launch();
+  return launch_overlapped(kernel, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
 }
 // FULL: the row's last warp has all its columns too, so that nothing is predicated
 template <class TX, int VPL>
@@ -136,8 +135,7 @@ static int bwd_ring_full(const NormBwdArgs& a, const RingPlan& p, int blocks, bo
     if (p.rows_per_block > 1 && smem < (size_t)2 * a.H * sizeof(float)) smem = (size_t)2 * a.H * sizeof(float);
     if (!launch) return resident_blocks(kernel, p.threads, smem, cache[p.threads / 32]);
     KernelScope scope(SAPO_K_NORM_BWD, st);
-    kernel<<<blocks, p.threads, smem, st>>>(a, p.wpr);
-    return check_launch();
+    return launch_overlapped(kernel, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
   }
 }
 template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS>
@@ -189,8 +187,7 @@ static int launch_fwd_any_shape(const NormFwdArgs& a, const AnyPlan& p, int sms,
   int64_t blocks = ceil_div<int64_t>(a.T, p.rows_per_block);
   if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
   KernelScope scope(SAPO_K_NORM_FWD, st);
-  kernel<<<(int)blocks, p.threads, 0, st>>>(a, p.wpr);
-  return check_launch();
+  return launch_overlapped(kernel, dim3((unsigned)blocks), p.threads, 0, 0, st, a, p.wpr);
 }
 template <class TX, int W>
 static int launch_fwd_any_w(const NormFwdArgs& a, const AnyPlan& p, int sms, cudaStream_t st) {
@@ -229,8 +226,7 @@ template <class TX, class A, int U>
 static int launch_bwd_any_shape(const NormBwdArgs& a, const AnyPlan& p, int blocks, cudaStream_t st) {
   const size_t smem = p.rows_per_block > 1 ? (size_t)2 * a.H * sizeof(float) : 0;      // rows_per_block > 1: H <= 2048
   KernelScope scope(SAPO_K_NORM_BWD, st);
-  norm_bwd_any_kernel<TX, A, U><<<blocks, p.threads, smem, st>>>(a, p.wpr);
-  return check_launch();
+  return launch_overlapped(norm_bwd_any_kernel<TX, A, U>, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
 }
 template <class TX, int W>
 static int launch_bwd_any_w(const NormBwdArgs& a, const AnyPlan& p, int blocks, cudaStream_t st) {
@@ -254,8 +250,7 @@ static int launch_ckpt8_warps(Kernel kernel, int64_t units, int32_t per_row, int
   if (per_sm == 0) return SAPO_ERR_CUDA;
   int64_t blocks = ceil_div<int64_t>(units, (int64_t)8 * n);
   if (blocks > (int64_t)sms * per_sm) blocks = (int64_t)sms * per_sm;
-  launch((int)blocks, blocks * 8 / per_row, (int32_t)(blocks * 8 % per_row));
-  return check_launch();
+  return launch(dim3((unsigned)blocks), blocks * 8 / per_row, (int32_t)(blocks * 8 % per_row));
 }
 template <class TX, int L, int N, bool RESTORE>
 static int launch_ckpt8_rows(const Ckpt8Args& a, int sms, cudaStream_t st) {
@@ -264,8 +259,8 @@ static int launch_ckpt8_rows(const Ckpt8Args& a, int sms, cudaStream_t st) {
   const int32_t segments = L == 32 ? ceil_div(a.H, N * 256) : 1;
   const int64_t units = ceil_div<int64_t>(a.T, L == 32 ? 1 : N * (32 / L)) * segments;
   KernelScope scope(SAPO_K_CKPT8, st);
-  return launch_ckpt8_warps(kernel, units, segments, 1, cache, sms, [&](int blocks, int64_t rows, int32_t segs) {
-    kernel<<<blocks, 256, 0, st>>>(a, segments, rows, segs);
+  return launch_ckpt8_warps(kernel, units, segments, 1, cache, sms, [&](dim3 blocks, int64_t rows, int32_t segs) {
+    return launch_overlapped(kernel, blocks, 256, 0, 0, st, a, segments, rows, segs);
   });
 }
 template <class TX, int W, bool RESTORE>
@@ -274,8 +269,8 @@ static int launch_ckpt8_any(const Ckpt8Args& a, int sms, cudaStream_t st) {
   auto kernel = ckpt8_any_kernel<TX, W, RESTORE>;
   const int32_t groups = ceil_div(a.H, Q8_GROUP);
   KernelScope scope(SAPO_K_CKPT8, st);
-  return launch_ckpt8_warps(kernel, a.T * groups, groups, CkptAny<RESTORE>::GROUPS, cache, sms, [&](int blocks, int64_t rows, int32_t g) {
-    kernel<<<blocks, 256, 0, st>>>(a, rows, g);
+  return launch_ckpt8_warps(kernel, a.T * groups, groups, CkptAny<RESTORE>::GROUPS, cache, sms, [&](dim3 blocks, int64_t rows, int32_t g) {
+    return launch_overlapped(kernel, blocks, 256, 0, 0, st, a, rows, g);
   });
 }
 template <class TX, bool RESTORE>
@@ -394,18 +389,8 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
   else if (h_ckpt) rc = launch_bwd_any<int8_t>(a, p, pairs, blocks, st);
   else rc = x_dtype == SAPO_DTYPE_F32 ? launch_bwd_any<float>(a, p, pairs, blocks, st) : launch_bwd_any<__nv_bfloat16>(a, p, pairs, blocks, st);
   if (rc != SAPO_OK || !reduce || blocks == 1) return rc;
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(ceil_div(H, 32), 2);
-  cfg.blockDim = dim3(1024);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
   KernelScope scope(SAPO_K_NORM_REDUCE, st);
-  return cudaLaunchKernelEx(&cfg, norm_reduce_kernel, (const float*)a.part, blocks, H, dgamma, dbeta, (int)accumulate) == cudaSuccess
-             ? SAPO_OK : SAPO_ERR_CUDA;
+  return launch_overlapped(norm_reduce_kernel, dim3((unsigned)ceil_div(H, 32), 2), 1024, 0, 0, st, a.part, blocks, H, dgamma, dbeta, accumulate);
 }
 
 extern "C" int sapo_ckpt8_store(const void* x, int32_t x_dtype, int64_t T, int32_t H, int64_t ld_x,

@@ -117,6 +117,8 @@ constexpr int ANY_RED = 2 * (NORM_MAX_THREADS / 32 / 2) * ANY_SLOTS;   // groups
 // (16 columns and one row a lane: 96 registers, so that two blocks of up to 10 warps fit on an SM)
 template <class TX, class A, int U>
 __global__ void __maxnreg__((A::PAIRS == 8 && U == 1) ? 96 : 128) norm_fwd_any_kernel(NormFwdArgs a, int wpr) {
+  wait_for_previous();
+  let_next_start();
   constexpr bool REPLAY = sizeof(TX) == 1;
   constexpr int P = A::PAIRS, G = A::GROUPS, L = A::LANES, PER_WARP = U * (32 / L);
   constexpr bool ONE_WARP = L < 32 || U > 2;            // a row never crosses warps
@@ -242,6 +244,8 @@ __global__ void __maxnreg__((A::PAIRS == 8 && U == 1) ? 96 : 128) norm_fwd_any_k
 
 template <class TX, class A, int U>
 __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_any_kernel(NormBwdArgs a, int wpr) {
+  wait_for_previous();
+  let_next_start();
   constexpr bool FROM_Q8 = sizeof(TX) == 1;
   constexpr int P = A::PAIRS, G = A::GROUPS, L = A::LANES, PER_WARP = U * (32 / L);
   constexpr bool ONE_WARP = L < 32 || U > 1;
@@ -324,7 +328,6 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_any_kernel(NormBwdA
     };
     if (a.dx.dtype == SAPO_DTYPE_F32) finish(static_cast<float*>(a.dx.p)); else finish(static_cast<__nv_bfloat16*>(a.dx.p));
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the rows that shared a warp, then the groups' sums one after the other
   #pragma unroll
@@ -363,6 +366,8 @@ template <bool RESTORE> struct CkptAny { static constexpr int GROUPS = RESTORE ?
 // stepped from group to group.
 template <class TX, int W, bool RESTORE>
 __global__ void __launch_bounds__(256) ckpt8_any_kernel(Ckpt8Args a, int64_t step_rows, int32_t step_groups) {
+  wait_for_previous();
+  let_next_start();
   constexpr int N = CkptAny<RESTORE>::GROUPS;
   using A = Cols<W, 4>;
   using S = Slots<N, 32>;

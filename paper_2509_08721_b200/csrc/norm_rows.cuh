@@ -79,6 +79,8 @@ __device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stage
 // TX int8_t: replay from a checkpoint (a.q), statistics given.
 template <class TX, int VPL, bool FULL>
 __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdArgs a, int wpr) {
+  wait_for_previous();
+  let_next_start();
   constexpr bool REPLAY = sizeof(TX) == 1;
   constexpr int S = FwdRing<TX, VPL>::STAGES, WARPS = NORM_THREADS / 32;
   using Row = WarpRow<TX, VPL>;
@@ -238,6 +240,8 @@ template <class TX, class TDY, int VPL, int MAX_THREADS> struct BwdRing {
 
 template <class TX, class TDY, int VPL, int MAX_THREADS, int SLOTS, bool FULL>
 __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_bwd_ring_kernel(NormBwdArgs a, int wpr) {
+  wait_for_previous();
+  let_next_start();
   constexpr bool FROM_Q8 = sizeof(TX) == 1;
   using Ring = BwdRing<TX, TDY, VPL, MAX_THREADS>;
   constexpr int S = Ring::STAGES;
@@ -370,7 +374,6 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     if (a.dx.dtype == SAPO_DTYPE_F32) finish(std::true_type{}); else finish(std::false_type{});
     dx_row += dx_step;
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
   // the groups' sums one after the other, through the ring (no copy is in flight any more)
   copy_wait<0>();
@@ -416,11 +419,12 @@ __global__ void __launch_bounds__(1024)
 norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float* dgamma, float* dbeta, int accumulate) {
   __shared__ float sh[32][33];
   float* out = blockIdx.y == 0 ? dgamma : dbeta;
-  if (out == nullptr) { asm volatile("griddepcontrol.wait;" ::: "memory"); return; }
+  wait_for_previous();
+  let_next_start();
+  if (out == nullptr) return;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + lane;
   float s = 0.f;
-  asm volatile("griddepcontrol.wait;" ::: "memory");      // launched while the backward's last blocks still run
   if (col < H)
     for (int b = w; b < n_parts; b += 32) s += part[((int64_t)b * 2 + blockIdx.y) * H + col];
   sh[w][lane] = s;
@@ -438,6 +442,8 @@ norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float
 // L < 32: rows of up to 8 L columns, 32 / L rows a warp at a time and N of those a lane.
 template <class TX, int L, int N, bool RESTORE>
 __global__ void __launch_bounds__(256) ckpt8_rows_kernel(Ckpt8Args a, int32_t segments, int64_t step_rows, int32_t step_segments) {
+  wait_for_previous();
+  let_next_start();
   constexpr int ROWS = L == 32 ? 1 : N * (32 / L), G = L < 16 ? L : 16;       // rows of a warp's step, lanes of a group
   using S = Slots<PowerOfTwo<N>::value, G>;
   const int lane = threadIdx.x & 31;

@@ -99,6 +99,8 @@ __device__ __forceinline__ float load_from_first(const float* p) {
 // up to PREF_SEQS completions.
 template <bool SOLO>
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
+  wait_for_previous();
+  let_next_start();
   __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
   __shared__ int32_t cu_s[PREF_SEQS + 1];
   __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS], g_s[PREF_SEQS];     // sums, rewards, factors
@@ -380,35 +382,23 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
     wide[dev] = true;
   }
   int cluster = pref_cluster(a.T, a.Q, sms);
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute attr[1];
-  cfg.blockDim = dim3(PREF_THREADS);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   // Few questions of few tokens: one cluster has a block for each and one for what they do not cover, and its barrier
   // takes the place of the count of finished clusters.
   if (cluster == 1 && a.Q < PREF_MAX_CLUSTER && a.T <= 65536) {
     while (cluster <= a.Q) cluster <<= 1;
     a.q_clusters = a.Q;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    cfg.gridDim = dim3((unsigned)cluster);
     KernelScope scope(SAPO_K_PREFERENCE, st);
-    return cudaLaunchKernelEx(&cfg, preference_kernel<true>, a) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
+    return launch_overlapped(preference_kernel<true>, dim3((unsigned)cluster), PREF_THREADS, 0, cluster, st, a);
   }
   const int64_t most = (int64_t)sms * 4 / cluster;
   a.q_clusters = (int32_t)(a.Q < most ? a.Q : most);
   // clusters for what no question covers: a capacity behind the last token can be large
   int64_t outside = ceil_div<int64_t>(a.T, (int64_t)65536 * cluster);
   outside = outside < 1 ? 1 : (outside > 32 ? 32 : outside);
-  attr[0].val.clusterDim.x = (unsigned)cluster;
-  cfg.gridDim = dim3((unsigned)((a.q_clusters + outside) * cluster));
   a.ticket = next_ticket(dev);
   if (a.ticket == nullptr) return SAPO_ERR_CUDA;
   KernelScope scope(SAPO_K_PREFERENCE, st);
-  return cudaLaunchKernelEx(&cfg, preference_kernel<false>, a) == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;
+  return launch_overlapped(preference_kernel<false>, dim3((unsigned)((a.q_clusters + outside) * cluster)), PREF_THREADS, 0, cluster, st, a);
 }
 
 }  // namespace sapo
