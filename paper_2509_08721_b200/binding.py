@@ -213,12 +213,13 @@ def _p(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream() -> int:
     """The current stream's handle (without building a Stream object, which costs 3 us, where torch allows it)."""
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -573,6 +574,13 @@ def _pref_cfg(*key) -> PrefCfgC:
     return cfg
 
 
+def _at_least(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> int:
+    """Device pointer of a vector of n elements or more."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+        raise SapoError(f"{what} must be contiguous {dtype} with {n} elements on the GPU")
+    return t.data_ptr()
+
+
 def alloc_preference_outputs(T: int, S: int, Q: int, device="cuda", scores: bool = False) -> Dict[str, torch.Tensor]:
     """Outputs of the preference loss; scores=True adds logp and lse (the call through the LM head)."""
     f = lambda n: torch.empty(n, dtype=torch.float32, device=device)
@@ -590,12 +598,17 @@ def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens:
     """Loss over the preference pairs of every question and its gradient factor per token; `out` comes
     from alloc_preference_outputs."""
     _require_cuda()
-    margin, pairs_out = out.get("q_margin"), out.get("q_pairs")
+    f32, i32, n = torch.float32, torch.int32, logp.numel()
+    seqs, Q = cu_seqlens.numel() - 1, group_offsets.numel() - 1
+    factors, ratio, grad, q_loss = out["gscale"], out["seq_logratio"], out["seq_grad"], out["q_loss"]
+    if factors.numel() < n or ratio.numel() < seqs or grad.numel() < seqs or q_loss.numel() < Q:
+        raise SapoError("the outputs are too small for these tokens, sequences and questions")
     rc = load().sapo_preference_loss(
-        logp.data_ptr(), ref_logp.data_ptr(), logp.shape[0], cu_seqlens.data_ptr(), cu_seqlens.shape[0] - 1,
-        rewards.data_ptr(), group_offsets.data_ptr(), group_offsets.shape[0] - 1,
-        _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale), out["gscale"].data_ptr(),
-        out["seq_logratio"].data_ptr(), out["seq_grad"].data_ptr(), out["q_loss"].data_ptr(), _p(margin), _p(pairs_out),
+        _at_least(logp, f32, n, "logp"), _at_least(ref_logp, f32, n, "ref_logp"), n,
+        _at_least(cu_seqlens, i32, 1, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
+        _at_least(group_offsets, i32, 1, "group_offsets"), Q,
+        _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale), factors.data_ptr(),
+        ratio.data_ptr(), grad.data_ptr(), q_loss.data_ptr(), _p(out.get("q_margin")), _p(out.get("q_pairs")),
         out["loss"].data_ptr(), status.data_ptr(), _stream())
     _check(rc, "sapo_preference_loss")
 
@@ -612,10 +625,21 @@ def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids
     _require_cuda()
     T = int(hidden.shape[0]) if T is None else int(T)
     H, V = int(hidden.shape[1]), int(W_head.shape[0])
+    f32, i32, seqs, Q = torch.float32, torch.int32, cu_seqlens.numel() - 1, group_offsets.numel() - 1
+    if W_head.dtype != hidden.dtype or W_head.shape[1] != H or hidden.shape[0] < T:
+        raise SapoError("hidden must be [T, H] and W_head [V, H] of the same element type")
+    if dhidden.shape[0] < T or dhidden.shape[1] != H or dW_head.shape != (V, H) \
+            or not (dhidden.is_contiguous() and dW_head.is_contiguous()):
+        raise SapoError("dhidden must be [T, H] and dW_head [V, H], both contiguous")
+    if (min(out[k].numel() for k in ("logp", "lse", "gscale")) < T or out["q_loss"].numel() < Q
+            or min(out["seq_logratio"].numel(), out["seq_grad"].numel()) < seqs):
+        raise SapoError("the outputs are too small for these tokens, sequences and questions")
     cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
     rc = load().sapo_preference_loss_fwd_bwd(
-        _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0), _p(ids), _p(ref_logp),
-        _p(cu_seqlens), int(cu_seqlens.numel() - 1), _p(rewards), _p(group_offsets), int(group_offsets.numel() - 1),
+        _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0),
+        _at_least(ids, i32, T, "ids"), _at_least(ref_logp, f32, T, "ref_logp"),
+        _at_least(cu_seqlens, i32, 1, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
+        _at_least(group_offsets, i32, 1, "group_offsets"), Q,
         cfg, _p(out["logp"]), _p(out["lse"]), _p(out["gscale"]), _p(out["seq_logratio"]), _p(out["seq_grad"]),
         _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]), _p(dhidden), _p(dW_head),
         _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
@@ -652,8 +676,8 @@ def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:
 def _rows(t: torch.Tensor, T: int, H: int, what: str):
     """(device pointer, element type, row pitch) of a [T, H] matrix whose columns are contiguous."""
     stride = t.stride()
-    if t.shape != (T, H) or (stride[1] != 1 and H > 1):
-        raise SapoError(f"{what} must be [{T}, {H}] with contiguous columns")
+    if t.shape != (T, H) or (stride[1] != 1 and H > 1) or not t.is_cuda:
+        raise SapoError(f"{what} must be [{T}, {H}] with contiguous columns on the GPU")
     code = _DTYPE_CODES.get(t.dtype)
     if code is None:
         raise SapoError(f"unsupported element type {t.dtype}")
@@ -664,16 +688,16 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     """Device pointer of an optional float32 vector of n elements."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
-        raise SapoError(f"{what} must be contiguous float32 with {n} elements")
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise SapoError(f"{what} must be contiguous float32 with {n} elements on the GPU")
     return t.data_ptr()
 
 
 def _weight(t: Optional[torch.Tensor], H: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    if t.shape != (H,) or not t.is_contiguous():
-        raise SapoError(f"{what} must be contiguous with {H} elements")
+    if t.numel() != H or not t.is_contiguous() or not t.is_cuda:
+        raise SapoError(f"{what} must be contiguous with {H} elements on the GPU")
     return t.data_ptr()
 
 

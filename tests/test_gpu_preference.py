@@ -342,3 +342,33 @@ def test_many_calls_on_two_streams_repeat_bit_for_bit():
     torch.cuda.synchronize()
     assert torch.isfinite(losses).all() and (losses == losses[0]).all() and status.item() == 0
     check(c, dict(run(c, 0.1)), 0.1)
+
+
+def test_binding_refuses_arrays_that_do_not_fit():
+    c = case([3, 4, 5], [2, 1], 5)
+    good = {k: torch.from_numpy(c[k]).cuda() for k in ("logp", "ref", "cu", "go", "rewards")}
+    out, status = B.alloc_preference_outputs(c["T"], c["S"], c["Q"]), B.new_status()
+    for key, bad in [("ref", good["ref"][:-1]), ("ref", good["ref"].double()), ("ref", good["ref"].cpu()),
+                     ("logp", torch.zeros(2 * c["T"], device="cuda")[::2]), ("cu", good["cu"].long()),
+                     ("go", good["go"].float()), ("rewards", good["rewards"][:2])]:
+        d = dict(good, **{key: bad})
+        with pytest.raises(B.SapoError):
+            B.sapo_preference_loss(d["logp"], d["ref"], d["cu"], d["rewards"], d["go"], 0.1, out, status)
+    for key in ("gscale", "seq_logratio", "seq_grad", "q_loss"):
+        with pytest.raises(B.SapoError):
+            B.sapo_preference_loss(good["logp"], good["ref"], good["cu"], good["rewards"], good["go"], 0.1,
+                                   dict(out, **{key: out[key][:-1]}), status)
+    hidden, W = torch.zeros(c["T"], 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(128, 64, dtype=torch.bfloat16, device="cuda")
+    ids, out = torch.zeros(c["T"], dtype=torch.int32, device="cuda"), B.alloc_preference_outputs(c["T"], c["S"], c["Q"], scores=True)
+    ws = torch.empty(B.sapo_workspace_bytes(B.WS_PREFERENCE | B.WS_OUT_BF16, c["T"], 64, 128, B.DTYPE_BF16), dtype=torch.uint8, device="cuda")
+
+    def through_head(hidden=hidden, W=W, ids=ids, ref=good["ref"], dhidden=torch.empty_like(hidden), dW=torch.empty_like(W)):
+        B.sapo_preference_loss_fwd_bwd(hidden, W, ids, ref, good["cu"], good["rewards"], good["go"], 0.1, out, dhidden, dW,
+                                       False, ws, status)
+    through_head()
+    assert status.item() == 0 and torch.isfinite(out["loss"]).all()
+    for bad in [dict(W=W.float()), dict(W=W[:, :32]), dict(ids=ids.long()), dict(ids=ids[:-1]), dict(ref=good["ref"].cpu()),
+                dict(dhidden=torch.empty(c["T"], 32, dtype=torch.bfloat16, device="cuda")), dict(dhidden=torch.empty(c["T"] - 1, 64, dtype=torch.bfloat16, device="cuda")),
+                dict(dW=torch.empty(64, 64, dtype=torch.bfloat16, device="cuda")), dict(dW=torch.empty(64, 128, dtype=torch.bfloat16, device="cuda").t())]:
+        with pytest.raises(B.SapoError):
+            through_head(**bad)
