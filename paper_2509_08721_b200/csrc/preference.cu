@@ -85,6 +85,14 @@ __device__ __forceinline__ float load_from_first(const float* p) {
   return x;
 }
 
+// Mean of the questions' losses, added up in their order by one warp.
+__device__ __forceinline__ void mean_loss(const float* q_loss, int32_t Q, float* loss, int lane) {
+  double x = 0.0;
+  for (int32_t q = lane; q < Q; q += 32) x += (double)__ldcg(q_loss + q);
+  x = warp_sum(x);
+  if (lane == 0) *loss = (float)(x / (double)Q);
+}
+
 // A cluster of blocks per question.  The question's tokens are one range, cut into equal pieces for the
 // cluster's warps whatever its sequences' lengths are, so that few long sequences keep as many SMs
 // busy as many short ones:
@@ -321,6 +329,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   // first, behind the barrier).
   if (rank != 0 || warp != 0 || (SOLO && blockIdx.x != 0)) return;
   if (!SOLO) {
+    if (a.ticket == nullptr) return;                       // preference_mean_kernel follows
     uint32_t before = 0;
     if (lane == 0) {
       __threadfence();                                     // this block's q_loss before its ticket
@@ -330,15 +339,20 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     __threadfence();
     if (lane == 0) *a.ticket = 0u;
   }
-  double x = 0.0;
-  for (int32_t q = lane; q < a.Q; q += 32) x += (double)__ldcg(a.q_loss + q);
-  x = warp_sum(x);
-  if (lane == 0) *a.loss = (float)(x / (double)a.Q);
+  mean_loss(a.q_loss, a.Q, a.loss, lane);
+}
+
+// The last step of preference_kernel<false> in a launch of its own (one warp).
+__global__ void __launch_bounds__(32) preference_mean_kernel(const float* q_loss, int32_t Q, float* loss) {
+  let_next_start();
+  wait_for_previous();
+  mean_loss(q_loss, Q, loss, threadIdx.x);
 }
 
 // How many clusters of a launch have finished: one counter per launch, left at zero by it.  Launches take them in turn,
-// so two that run at the same time (other streams, other threads) share one only if 16384 launches were made
-// between them; a captured graph keeps the counters of its capture, which is fine as a graph does not run beside itself.
+// so two that run at the same time (other streams, other threads) would share one only with 16384 launches in
+// flight between them.  A graph would replay its launch with the same counter for good, beside later launches that
+// get it in turn: a launch that is captured takes none, and preference_mean_kernel adds the losses up behind it.
 constexpr int PREF_TICKETS = 16384;
 static __device__ uint32_t g_pref_tickets[PREF_TICKETS];
 static uint32_t* next_ticket(int dev) {
@@ -395,10 +409,15 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
   // clusters for what no question covers: a capacity behind the last token can be large
   int64_t outside = ceil_div<int64_t>(a.T, (int64_t)65536 * cluster);
   outside = outside < 1 ? 1 : (outside > 32 ? 32 : outside);
-  a.ticket = next_ticket(dev);
-  if (a.ticket == nullptr) return SAPO_ERR_CUDA;
+  cudaStreamCaptureStatus capture;
+  if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) return SAPO_ERR_CUDA;
+  a.ticket = nullptr;
+  if (capture == cudaStreamCaptureStatusNone && (a.ticket = next_ticket(dev)) == nullptr) return SAPO_ERR_CUDA;
   KernelScope scope(SAPO_K_PREFERENCE, st);
-  return launch_overlapped(preference_kernel<false>, dim3((unsigned)((a.q_clusters + outside) * cluster)), PREF_THREADS, 0, cluster, st, a);
+  const int rc = launch_overlapped(preference_kernel<false>, dim3((unsigned)((a.q_clusters + outside) * cluster)), PREF_THREADS, 0, cluster, st, a);
+  if (rc != SAPO_OK || a.ticket != nullptr) return rc;
+  ++kernel_timer().launches;
+  return launch_overlapped(preference_mean_kernel, dim3(1), 32, 0, 0, st, (const float*)a.q_loss, a.Q, a.loss);
 }
 
 }  // namespace sapo

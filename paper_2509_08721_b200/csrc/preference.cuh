@@ -14,6 +14,7 @@ struct PrefArgs {
   float* gscale; float* seq_logratio; float* seq_grad; float* q_loss; float* q_margin; int32_t* q_pairs; float* loss;
   int32_t* status;
   // set by launch_preference: clusters of blocks that take questions, and the counter of those that have finished
+  // (NULL: none, the loss is added up by a launch behind)
   int32_t q_clusters; uint32_t* ticket;
 };
 

@@ -329,3 +329,43 @@ def test_binding_refuses_wrong_shapes_and_types():
                  lambda: B.sapo_norm_replay(B.alloc_ckpt8(4, 32), None, None, "rms", None, m, y)):
         with pytest.raises(B.SapoError):
             call()
+
+
+def test_captured_calls_replay():
+    """Norm forward with a checkpoint, replay and backward in a graph, on new inputs: the results of direct calls, bit for bit."""
+    data = []
+    for T, H, kind in [(1, 8, "rms"), (37, 1001, "layer"), (500, 896, "rms")]:
+        x = torch.randn(T, H, device="cuda").bfloat16()
+        e = lambda *s: torch.empty(*s, device="cuda")
+        data.append(dict(x=x, dy=torch.randn(T, H, device="cuda"), gamma=torch.randn(H, device="cuda"), kind=kind,
+                         y=torch.empty_like(x), back=torch.empty_like(x), mean=e(T) if kind == "layer" else None, rstd=e(T),
+                         ckpt=B.alloc_ckpt8(T, H), dx=e(T, H), dgamma=e(H), dbeta=e(H),
+                         ws=torch.empty(B.sapo_norm_workspace_bytes(T, H), dtype=torch.uint8, device="cuda")))
+    status = B.new_status()
+    outputs = ("y", "back", "dx", "dgamma", "dbeta")
+
+    def calls():
+        for d in data:
+            B.sapo_norm_fwd(d["x"], d["gamma"], None, 1e-6, d["kind"], d["y"], d["mean"], d["rstd"], d["ckpt"], status)
+            B.sapo_ckpt8_restore(d["ckpt"], d["back"])
+            B.sapo_norm_bwd(d["dy"], d["ckpt"], d["gamma"], d["mean"], d["rstd"], d["kind"], d["dx"], d["dgamma"],
+                            d["dbeta"], d["ws"])
+
+    def results():
+        torch.cuda.synchronize()
+        return [d[k].clone() for d in data for k in outputs]
+
+    calls()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(2):
+        for d in data:
+            d["x"].copy_(torch.randn(d["x"].shape, device="cuda"))
+        calls()
+        want = results()
+        for d in data:
+            for k in outputs:
+                d[k].zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, results())) and status.item() == 0

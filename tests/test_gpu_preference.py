@@ -372,3 +372,49 @@ def test_binding_refuses_arrays_that_do_not_fit():
                 dict(dW=torch.empty(64, 64, dtype=torch.bfloat16, device="cuda")), dict(dW=torch.empty(64, 128, dtype=torch.bfloat16, device="cuda").t())]:
         with pytest.raises(B.SapoError):
             through_head(**bad)
+
+
+def test_captured_calls_replay():
+    """Captured in a graph (both forms, and the call through the head), calls beside the replays, new inputs: the
+    results of direct calls, bit for bit."""
+    cases = [case([9, 30, 4, 17], [2, 2], 21), case(list(RNG.integers(20, 60, size=80)), [2] * 40, seed=22)]
+    H, V, status = 64, 300, B.new_status()
+    gen_ = torch.Generator(device="cuda").manual_seed(23)
+    data = []
+    for c in cases:
+        d = {k: torch.from_numpy(c[k]).cuda() for k in ("logp", "ref", "cu", "go", "rewards")}
+        d["out"] = B.alloc_preference_outputs(c["T"], c["S"], c["Q"])
+        d["hidden"] = torch.randn(c["T"], H, generator=gen_, device="cuda").bfloat16()
+        d["W"] = torch.randn(V, H, generator=gen_, device="cuda").bfloat16()
+        d["ids"] = torch.randint(0, V, (c["T"],), generator=gen_, device="cuda").int()
+        d["scored"] = B.alloc_preference_outputs(c["T"], c["S"], c["Q"], scores=True)
+        d["dh"], d["dW"] = torch.empty_like(d["hidden"]), torch.empty_like(d["W"])
+        d["ws"] = torch.empty(B.sapo_workspace_bytes(B.WS_PREFERENCE | B.WS_OUT_BF16, c["T"], H, V, B.DTYPE_BF16),
+                              dtype=torch.uint8, device="cuda")
+        data.append(d)
+
+    def calls():
+        for d in data:
+            B.sapo_preference_loss(d["logp"], d["ref"], d["cu"], d["rewards"], d["go"], 0.1, d["out"], status)
+            B.sapo_preference_loss_fwd_bwd(d["hidden"], d["W"], d["ids"], d["ref"], d["cu"], d["rewards"], d["go"], 0.1,
+                                           d["scored"], d["dh"], d["dW"], False, d["ws"], status)
+
+    def results():
+        torch.cuda.synchronize()
+        return [v.clone() for d in data for v in (*d["out"].values(), *d["scored"].values(), d["dh"], d["dW"])]
+
+    calls()                                                    # first calls set up what a capture may not
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(2):
+        for d in data:
+            d["ref"].add_(0.25 * torch.randn(d["ref"].shape, generator=gen_, device="cuda"))
+        calls()
+        want = results()
+        for d in data:
+            for v in (*d["out"].values(), *d["scored"].values(), d["dh"], d["dW"]):
+                v.zero_()
+        for _ in range(3):
+            graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, results())) and status.item() == 0
