@@ -130,9 +130,7 @@ static int bwd_ring_full(const NormBwdArgs& a, const RingPlan& p, int blocks, bo
   } else {
     static int cache[33][MAX_DEVICES] = {{0}};                       // by warps of the block
     auto kernel = norm_bwd_ring_kernel<TX, TDY, VPL, MAX_THREADS, SLOTS, FULL>;
-    // the ring, or the columns' sums that take its place at the end
-    size_t smem = (size_t)Ring::STAGES * (p.threads / 32) * Ring::WARP_BYTES;
-    if (p.rows_per_block > 1 && smem < (size_t)2 * a.H * sizeof(float)) smem = (size_t)2 * a.H * sizeof(float);
+    const size_t smem = (size_t)Ring::STAGES * (p.threads / 32) * Ring::WARP_BYTES;
     if (!launch) return resident_blocks(kernel, p.threads, smem, cache[p.threads / 32]);
     KernelScope scope(SAPO_K_NORM_BWD, st);
     return launch_overlapped(kernel, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
@@ -224,7 +222,8 @@ static int launch_fwd(const NormFwdArgs& a, bool replay, cudaStream_t st) {
 
 template <class TX, class A, int U>
 static int launch_bwd_any_shape(const NormBwdArgs& a, const AnyPlan& p, int blocks, cudaStream_t st) {
-  const size_t smem = p.rows_per_block > 1 ? (size_t)2 * a.H * sizeof(float) : 0;      // rows_per_block > 1: H <= 2048
+  const int groups = p.threads / 32 / p.wpr;
+  const size_t smem = groups > 1 ? (size_t)groups * 2 * a.H * sizeof(float) : 0;      // 8 warps with up to 512 columns each: 32 KB
   KernelScope scope(SAPO_K_NORM_BWD, st);
   return launch_overlapped(norm_bwd_any_kernel<TX, A, U>, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
 }
@@ -342,7 +341,7 @@ extern "C" size_t sapo_norm_workspace_bytes(int64_t T, int32_t H) {
   int64_t blocks = bwd_blocks(T > 0 ? T : 1, few < fewer ? few : fewer, 2, sms);
   const int64_t ring = bwd_blocks(T > 0 ? T : 1, bwd_ring_plan(H).rows_per_block, 2, sms);
   if (ring > blocks) blocks = ring;
-  return round_up<size_t>((size_t)blocks * 2 * H * sizeof(float), 256);
+  return round_up<size_t>((size_t)blocks * 2 * part_pitch(H) * sizeof(float), 256);
 }
 
 extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
@@ -382,7 +381,7 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
   const int blocks = (int)bwd_blocks(T, ring ? rp.rows_per_block : p.rows_per_block, ring && resident < 2 ? resident : 2, sms);
   if (reduce && blocks > 1) {
     if (!workspace || !aligned16(workspace)) return SAPO_ERR_INVALID_ARG;
-    if (workspace_bytes < (size_t)blocks * 2 * H * sizeof(float)) return SAPO_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < (size_t)blocks * 2 * part_pitch(H) * sizeof(float)) return SAPO_ERR_WORKSPACE_TOO_SMALL;
   }
   const bool pairs = H % 2 == 0 && pairs_ok(mdy) && pairs_ok(mdx) && (h_ckpt ? pairs_ok(a.q) : pairs_ok(mx));
   if (ring) rc = bwd_ring(a, rp, blocks, true, st);
@@ -390,7 +389,7 @@ extern "C" int sapo_norm_bwd(const void* dy, int32_t dy_dtype, int64_t ld_dy,
   else rc = x_dtype == SAPO_DTYPE_F32 ? launch_bwd_any<float>(a, p, pairs, blocks, st) : launch_bwd_any<__nv_bfloat16>(a, p, pairs, blocks, st);
   if (rc != SAPO_OK || !reduce || blocks == 1) return rc;
   KernelScope scope(SAPO_K_NORM_REDUCE, st);
-  return launch_overlapped(norm_reduce_kernel, dim3((unsigned)ceil_div(H, 32), 2), 1024, 0, 0, st, a.part, blocks, H, dgamma, dbeta, accumulate);
+  return launch_overlapped(norm_reduce_kernel, dim3((unsigned)ceil_div(H, 32), dgamma && dbeta ? 2 : 1), REDUCE_WARPS * 32, 0, 0, st, a.part, blocks, H, dgamma, dbeta, accumulate);
 }
 
 extern "C" int sapo_ckpt8_store(const void* x, int32_t x_dtype, int64_t T, int32_t H, int64_t ld_x,

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_any_kernel(NormBwdA
   constexpr int P = A::PAIRS, G = A::GROUPS, L = A::LANES, PER_WARP = U * (32 / L);
   constexpr bool ONE_WARP = L < 32 || U > 1;
   using Sums = Slots<2 * U, L>;                         // slot 2 u: sum of g, 2 u + 1: sum of g xh, of row u
-  extern __shared__ __align__(16) float cols_acc[];     // [2][H], when the block holds several rows
+  extern __shared__ __align__(16) float cols_acc[];     // [groups][2][H], of two groups or more
   __shared__ __align__(16) float2 red[ANY_RED];
   for (int i = threadIdx.x; i < ANY_RED; i += blockDim.x) red[i] = make_float2(0.f, 0.f);
   __syncthreads();
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_any_kernel(NormBwdA
     if (a.dx.dtype == SAPO_DTYPE_F32) finish(static_cast<float*>(a.dx.p)); else finish(static_cast<__nv_bfloat16*>(a.dx.p));
   }
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
-  // the rows that shared a warp, then the groups' sums one after the other
+  // the rows that shared a warp, then the groups' sums
   #pragma unroll
   for (int d = 16; d >= L; d >>= 1)
     #pragma unroll
@@ -337,28 +337,28 @@ __global__ void __launch_bounds__(NORM_MAX_THREADS) norm_bwd_any_kernel(NormBwdA
       dg[p] = add2(dg[p], make_float2(__shfl_xor_sync(0xffffffffu, dg[p].x, d), __shfl_xor_sync(0xffffffffu, dg[p].y, d)));
       db[p] = add2(db[p], make_float2(__shfl_xor_sync(0xffffffffu, db[p].x, d), __shfl_xor_sync(0xffffffffu, db[p].y, d)));
     }
-  for (int k = 0; k < at.groups; ++k) {
-    if (k == at.group && lane < L) {
+  const bool alone = at.groups == 1;
+  float* to = alone ? a.part + (int64_t)blockIdx.x * 2 * part_pitch(a.H) : cols_acc + at.group * 2 * a.H;
+  const int second = alone ? part_pitch(a.H) : a.H;
+  if (lane < L) {
+    #pragma unroll
+    for (int p = 0; p < P; ++p)
       #pragma unroll
-      for (int p = 0; p < P; ++p)
-        #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!A::has(p, h, left)) continue;
-          const int c = col + A::col_of(p, h);
-          float vg = h ? dg[p].y : dg[p].x, vb = h ? db[p].y : db[p].x;
-          if (k > 0) { vg += cols_acc[c]; vb += cols_acc[a.H + c]; }
-          if (k + 1 < at.groups) { cols_acc[c] = vg; cols_acc[a.H + c] = vb; continue; }
-          if (gridDim.x > 1) {
-            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H;
-            out[c] = vg; out[a.H + c] = vb;
-          } else {
-            if (a.dgamma != nullptr) a.dgamma[c] = a.accumulate ? a.dgamma[c] + vg : vg;
-            if (a.dbeta != nullptr) a.dbeta[c] = a.accumulate ? a.dbeta[c] + vb : vb;
-          }
+      for (int h = 0; h < 2; ++h) {
+        if (!A::has(p, h, left)) continue;
+        const int c = col + A::col_of(p, h);
+        const float vg = h ? dg[p].y : dg[p].x, vb = h ? db[p].y : db[p].x;
+        if (alone && gridDim.x == 1) {
+          if (a.dgamma != nullptr) a.dgamma[c] = a.accumulate ? a.dgamma[c] + vg : vg;
+          if (a.dbeta != nullptr) a.dbeta[c] = a.accumulate ? a.dbeta[c] + vb : vb;
+        } else {
+          to[c] = vg; to[second + c] = vb;
         }
-    }
-    __syncthreads();
+      }
   }
+  if (alone) return;
+  __syncthreads();
+  finish_columns<1>(a, cols_acc, at.groups, a.H);
 }
 
 template <bool RESTORE> struct CkptAny { static constexpr int GROUPS = RESTORE ? 4 : 2; };    // groups a warp takes at a time

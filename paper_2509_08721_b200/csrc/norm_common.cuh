@@ -243,4 +243,33 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, int wpr, int w, i
   return t;
 }
 
+// The end of a backward block.  acc holds the sums over the rows of each of the block's groups of warps,
+// [groups][2][pitch] with dgamma's columns first; they are added up in the groups' order, W columns a thread at a time, and
+// become the outputs, or with several blocks the block's part of them, [2][part_pitch(H)].
+__host__ __device__ constexpr int32_t part_pitch(int32_t H) { return (H + 3) & ~3; }
+template <int W>
+__device__ __forceinline__ void finish_columns(const NormBwdArgs& a, const float* acc, int groups, int pitch) {
+  const int n = a.H / W, first = a.dgamma != nullptr ? 0 : n, last = a.dbeta != nullptr ? 2 * n : n;
+  for (int i = first + threadIdx.x; i < last; i += blockDim.x) {
+    const bool beta = i >= n;
+    const int c = (beta ? i - n : i) * W;
+    const float* from = acc + (beta ? pitch : 0) + c;
+    float s[W];
+    for (int k = 0; k < groups; ++k, from += 2 * pitch) {
+      float x[W];
+      if constexpr (W == 4) *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(from); else x[0] = *from;
+      #pragma unroll
+      for (int j = 0; j < W; ++j) s[j] = k == 0 ? x[j] : s[j] + x[j];
+    }
+    if (gridDim.x > 1) {
+      float* out = a.part + ((int64_t)blockIdx.x * 2 + beta) * part_pitch(a.H) + c;
+      if constexpr (W == 4) *reinterpret_cast<float4*>(out) = *reinterpret_cast<const float4*>(s); else *out = s[0];
+    } else {
+      float* out = (beta ? a.dbeta : a.dgamma) + c;
+      #pragma unroll
+      for (int j = 0; j < W; ++j) out[j] = a.accumulate ? out[j] + s[j] : s[j];
+    }
+  }
+}
+
 }  // namespace sapo

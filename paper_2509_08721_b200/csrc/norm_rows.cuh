@@ -375,66 +375,63 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
     dx_row += dx_step;
   }
   if (a.dgamma == nullptr && a.dbeta == nullptr) return;
-  // the groups' sums one after the other, through the ring (no copy is in flight any more)
+  // the groups' sums take the ring's place (no copy is in flight any more)
   copy_wait<0>();
   __syncthreads();
-  float* acc = reinterpret_cast<float*>(ring);           // [2][H]
-  for (int k = 0; k < groups; ++k) {
-    if (k == group) {
-      #pragma unroll
-      for (int v = 0; v < VPL; ++v) {
-        const int col = col0 + 256 * v;
-        if (col >= a.H) continue;
-        #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float2* pg = reinterpret_cast<float2*>(acc + col + 2 * j);
-          float2* pb = reinterpret_cast<float2*>(acc + a.H + col + 2 * j);
-          if (k > 0) { dg[v][j] = add2(dg[v][j], *pg); db[v][j] = add2(db[v][j], *pb); }
-          if (k + 1 < groups) { *pg = dg[v][j]; *pb = db[v][j]; continue; }
-          if (gridDim.x > 1) {
-            float* out = a.part + (int64_t)blockIdx.x * 2 * a.H + col + 2 * j;
-            *reinterpret_cast<float2*>(out) = dg[v][j];
-            *reinterpret_cast<float2*>(out + a.H) = db[v][j];
-          } else {
-            const int c = col + 2 * j;
-            if (a.dgamma != nullptr) {
-              a.dgamma[c] = a.accumulate ? a.dgamma[c] + dg[v][j].x : dg[v][j].x;
-              a.dgamma[c + 1] = a.accumulate ? a.dgamma[c + 1] + dg[v][j].y : dg[v][j].y;
-            }
-            if (a.dbeta != nullptr) {
-              a.dbeta[c] = a.accumulate ? a.dbeta[c] + db[v][j].x : db[v][j].x;
-              a.dbeta[c + 1] = a.accumulate ? a.dbeta[c + 1] + db[v][j].y : db[v][j].y;
-            }
-          }
-        }
-      }
+  static_assert(S * Ring::WARP_BYTES >= 2 * VPL * 256 * (int)sizeof(float), "a warp's sums in its share of the ring");
+  float* acc = reinterpret_cast<float*>(ring);
+  const int pitch = wpr * VPL * 256;
+  float4* to = reinterpret_cast<float4*>(acc + group * 2 * pitch + col0);
+  #pragma unroll
+  for (int v = 0; v < VPL; ++v) {
+    #pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      to[64 * v + h] = make_float4(dg[v][2 * h].x, dg[v][2 * h].y, dg[v][2 * h + 1].x, dg[v][2 * h + 1].y);
+      to[pitch / 4 + 64 * v + h] = make_float4(db[v][2 * h].x, db[v][2 * h].y, db[v][2 * h + 1].x, db[v][2 * h + 1].y);
     }
-    __syncthreads();
   }
+  __syncthreads();
+  finish_columns<4>(a, acc, groups, pitch);
 }
 
-// dgamma (blockIdx.y 0) and dbeta (1): the sum over the blocks' parts, 32 columns per block, one warp
-// for every 32nd part.
-__global__ void __launch_bounds__(1024)
-norm_reduce_kernel(const float* __restrict__ part, int n_parts, int32_t H, float* dgamma, float* dbeta, int accumulate) {
-  __shared__ float sh[32][33];
-  float* out = blockIdx.y == 0 ? dgamma : dbeta;
+// dgamma and dbeta (blockIdx.y) as the sums of the blocks' parts, 32 columns a block: 8 lanes hold 4 columns each of every
+// 64th part, all of a thread's loads before the first use.  What it takes is their latency and a launch's.
+constexpr int REDUCE_WARPS = 16;
+__global__ void __launch_bounds__(REDUCE_WARPS * 32)
+norm_reduce_kernel(const float* part, int n_parts, int32_t H, float* dgamma, float* dbeta, int accumulate) {
+  constexpr int STEP = REDUCE_WARPS * 4, N = 5;          // 5 * 64 parts: two blocks' of each of up to 160 SMs at a time
+  __shared__ __align__(16) float sums[REDUCE_WARPS][32];
   wait_for_previous();
   let_next_start();
-  if (out == nullptr) return;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int col = blockIdx.x * 32 + lane;
-  float s = 0.f;
-  if (col < H)
-    for (int b = w; b < n_parts; b += 32) s += part[((int64_t)b * 2 + blockIdx.y) * H + col];
-  sh[w][lane] = s;
-  __syncthreads();
-  // transposed: warp w now holds the 32 sums of column w
-  float t = sh[lane][w];
+  const bool beta = dgamma == nullptr || blockIdx.y != 0;
+  float* out = beta ? dbeta : dgamma;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, pitch = part_pitch(H);
+  const int col = blockIdx.x * 32 + (lane & 7) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (col < H) {
+    const float* src = part + (beta ? pitch : 0) + col;
+    for (int b = w * 4 + (lane >> 3); b < n_parts; b += N * STEP) {
+      float4 x[N];
+      #pragma unroll
+      for (int j = 0; j < N; ++j)
+        x[j] = b + j * STEP < n_parts ? __ldcg(reinterpret_cast<const float4*>(src + (int64_t)(b + j * STEP) * 2 * pitch)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      #pragma unroll
+      for (int j = 0; j < N; ++j) { s.x += x[j].x; s.y += x[j].y; s.z += x[j].z; s.w += x[j].w; }
+    }
+  }
   #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-  const int c = blockIdx.x * 32 + w;
-  if (lane == 0 && c < H) out[c] = accumulate ? out[c] + t : t;
+  for (int d = 16; d >= 8; d >>= 1) {
+    s.x += __shfl_xor_sync(0xffffffffu, s.x, d); s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
+    s.z += __shfl_xor_sync(0xffffffffu, s.z, d); s.w += __shfl_xor_sync(0xffffffffu, s.w, d);
+  }
+  if (lane < 8) *reinterpret_cast<float4*>(&sums[w][lane * 4]) = s;
+  __syncthreads();
+  if (w != 0 || blockIdx.x * 32 + lane >= H) return;
+  float t = 0.f;
+  #pragma unroll
+  for (int k = 0; k < REDUCE_WARPS; ++k) t += sums[k][lane];
+  float* to = out + blockIdx.x * 32 + lane;
+  *to = accumulate ? *to + t : t;
 }
 
 // Checkpoints alone, rows on 16-byte boundaries in whole vectors.  L = 32: a warp takes N * 256 neighbouring columns of a
