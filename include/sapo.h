@@ -449,8 +449,11 @@ int sapo_preference_loss(const float* logp, const float* ref_logp, int64_t T, co
  * SAPO_ERR_UNSUPPORTED_SHAPE for fp32: those go through sapo_policy_loss_fwd, sapo_preference_loss and
  * sapo_policy_loss_bwd).
  * logp, lse, gscale [T]; a token with an id outside [0, V) gets logp 0 (SAPO_ST_BAD_TOKEN_ID), is left
- * out of its sequence's sum and gets no gradient.
- * workspace: sapo_workspace_bytes(SAPO_WS_PREFERENCE, ...), at least sapo_workspace_bytes_min of it. */
+ * out of its sequence's sum and gets no gradient.  The same holds for a token whose log ratio is beyond
+ * +-69 (SAPO_ST_EXP_RANGE): its exponentials are taken relative to exp(ref_logp).
+ * workspace: sapo_workspace_bytes(SAPO_WS_PREFERENCE, ...), at least sapo_workspace_bytes_min of it.  With a workspace
+ * whose panel holds the whole batch (what the first returns, up to 40960 tokens) the call takes 6 T V H flops, with a
+ * smaller one 8 T V H: a pair's factor is known only when both its sequences have been scored. */
 int sapo_preference_loss_fwd_bwd(const void* hidden, const void* W_head, int32_t dtype,
                                  int64_t T, int32_t H, int32_t V, int64_t ld_hidden, int64_t ld_W,
                                  const int32_t* ids, const float* ref_logp, const int32_t* cu_seqlens, int32_t S,

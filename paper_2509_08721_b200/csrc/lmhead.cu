@@ -529,8 +529,8 @@ static int fwd_check_args(const void* hidden, const void* W_head, int32_t dtype,
 }
 
 // Panel rows the workspace query asks for a preference call: the whole batch up to 40 960 tokens (12.5 GB at a
-// vocabulary of 152 000), because a smaller panel costs a second pass over the logits; beyond that, what the
-// backward asks for.
+// vocabulary of 152 000), because a smaller panel costs a second pass over the logits (9216 tokens, hidden 896,
+// vocabulary 151936: 5.4 ms in one pass, 7.5 in two); beyond that, what the backward asks for.
 constexpr int64_t PREF_ROWS_ONE_PIECE = 40960;
 static int64_t preference_panel_rows(int64_t T, int32_t H, int32_t V) {
   return T <= PREF_ROWS_ONE_PIECE ? round_up<int64_t>(T, BM) : preferred_panel_rows(T, H, V);
@@ -1289,7 +1289,8 @@ static float z_compensation(int32_t H) { return 1.f + 1.5e-8f * (float)(H / 16);
 
 // flags[s] = 1 for every sequence that may enter a pair, else 0, one warp per question: a sequence with a token and a
 // finite reward, in a question with two different such rewards; with best against worst, those two.  Also zero
-// for sequences of no question, and the words of `need` that target_logit_kernel sets bits in.  (A pair can still drop out for its log ratios; none can come in.)
+// for sequences of no question, and the words of `need` that target_logit_kernel sets bits in.  (A pair can still
+// drop out for its log ratios; none can come in.)
 __global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __restrict__ flags, uint32_t* need, int32_t need_words) {
   wait_for_previous();
   let_next_start();
@@ -1346,8 +1347,10 @@ struct PrefTailArgs {
 // After the forward pass of a chunk, one warp per token:  sum = sum_v exp(z - c) with c = z_y - ref (nearly),
 //   lse = c + log sum,  log ratio = z_y - lse - ref = (z_y - ref - c) - log sum.
 // The bracket is the rounding of c, taken in 64 bits: formed this way the log ratio, which a sequence's
-// hundreds of tokens are summed over, is free of the rounding of lse (1e-6 for an lse around 12).
+// hundreds of tokens are summed over, is free of the rounding of lse (1e-6 for an lse around 12): its error
+// against 64-bit arithmetic went from 7e-7 to 7e-8 a token, with z_compensation's part.
 // A masked token gets the log ratio NaN.
+// Reads the partial sums (n_parts floats a token): 11 us for 9216 tokens, 0.2 % of the call.
 __global__ void __launch_bounds__(256) pref_score_kernel(PrefTailArgs a) {
   wait_for_previous();
   let_next_start();
@@ -1394,6 +1397,7 @@ struct PrefScaleArgs {
 // Once the factors g_t are known, one warp per token: what turns the stored exponentials into dz, as in
 // fused_tail_kernel: the row scale a_t = -g_t / sum_t, the chosen token's entry e_y - sum_t, hs = a_t hidden.
 // A token without a gradient only needs a zero scale and row.
+// Reads and writes hidden once: 20 us for 9216 x 896 beside a forward pass of 1.8 ms and two contractions of 1.6 ms.
 __global__ void __launch_bounds__(256) pref_scale_kernel(PrefScaleArgs a) {
   wait_for_previous();
   let_next_start();

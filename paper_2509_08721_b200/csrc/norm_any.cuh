@@ -5,6 +5,9 @@
 //   Cols<2, E>   pairs of neighbouring columns, where rows start on pair boundaries and H is even
 //   Vector<L>    8 neighbouring columns, L lanes a row and 32 / L rows a warp, for rows of up to 8 L columns on 16-byte
 //                boundaries
+// Measured at 120 million columns, beside the copy bandwidth: rows of 64 bf16 forward 105 us (70 %), backward 144 us (76 %);
+// rows of 1001 fp32 94 and 89 %, bounded by DRAM; rows of 1001 bf16 224 and 241 us (33 and 46 %), bounded by the load and
+// store unit: a 2-byte access moves 64 bytes a warp, a sixteenth of what whole vectors do.
 #pragma once
 
 #include "norm_common.cuh"

@@ -105,6 +105,8 @@ __device__ __forceinline__ void mean_loss(const float* q_loss, int32_t Q, float*
 // A small batch is a chain of waits for memory (each about half a microsecond), so a question's offsets and
 // rewards are read into shared memory at once, and what passes between the steps stays there, for questions of
 // up to PREF_SEQS completions.
+// Bound by those waits, not by its 12 bytes a token: 4 questions x 8 completions 6.0 us (the call's host side takes 8),
+// 64 x 8 completions of 600 tokens 10.5 us, 2 questions of 105000 tokens 11 us (389 with a block per question).
 template <bool SOLO>
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
   wait_for_previous();
