@@ -35,9 +35,9 @@ __device__ __forceinline__ void offset_range(const int32_t* offsets, int32_t i, 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
 // all threads of the cluster; orders their shared and global memory accesses
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_barrier() { cluster_arrive(); cluster_wait(); }
 // *p = x in the shared memory of the cluster's first block
 __device__ __forceinline__ void store_to_first(float* p, float x) {
   uint32_t at;
@@ -109,8 +109,13 @@ __device__ __forceinline__ void mean_loss(const float* q_loss, int32_t Q, float*
 // 64 x 8 completions of 600 tokens 10.5 us, 2 questions of 105000 tokens 11 us (389 with a block per question).
 template <bool SOLO>
 __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
+  // Another block's shared memory may only be accessed once that block has started, which being scheduled together
+  // does not say: every block of a cluster arrives here, and waits for the others before its first store to the first
+  // block.  The wait for the kernel before this one lies in between, so it costs nothing that was measured.
+  if (!SOLO) cluster_arrive();
   wait_for_previous();
   let_next_start();
+  if (!SOLO) cluster_wait();
   __shared__ float head[PREF_MAX_CLUSTER * PREF_WARPS];
   __shared__ int32_t cu_s[PREF_SEQS + 1];
   __shared__ float R_s[PREF_SEQS], r_s[PREF_SEQS], g_s[PREF_SEQS];     // sums, rewards, factors
