@@ -574,6 +574,13 @@ def _pref_cfg(*key) -> PrefCfgC:
     return cfg
 
 
+def _elements(t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
+    """Device pointer of a vector whose length the call goes by."""
+    if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
+        raise SapoError(f"{what} must be contiguous {dtype} on the GPU")
+    return t.data_ptr()
+
+
 def _at_least(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> int:
     """Device pointer of a vector of n elements or more."""
     if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
@@ -581,14 +588,54 @@ def _at_least(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> int:
     return t.data_ptr()
 
 
+class PreferenceOutputs(dict):
+    """Outputs of the preference loss by name.  `known` holds them while they are what alloc_preference_outputs made,
+    contiguous vectors of the right types on the GPU: a call then only looks at their lengths (asking eight tensors for
+    their type, layout and place takes 2.4 us of a call's 8).  A change of the dict ends that; a plain dict is always asked."""
+    known: Optional[tuple] = None
+
+
+def _forgets(name: str):
+    change = getattr(dict, name)
+
+    def method(self, *args, **kw):
+        self.known = None
+        return change(self, *args, **kw)
+    return method
+
+
+for _name in ("__setitem__", "__delitem__", "__ior__", "update", "setdefault", "pop", "popitem", "clear"):
+    setattr(PreferenceOutputs, _name, _forgets(_name))
+_PREF_OUTPUTS = ("gscale", "seq_logratio", "seq_grad", "q_loss", "q_margin", "q_pairs", "loss")
+
+
 def alloc_preference_outputs(T: int, S: int, Q: int, device="cuda", scores: bool = False) -> Dict[str, torch.Tensor]:
     """Outputs of the preference loss; scores=True adds logp and lse (the call through the LM head)."""
     f = lambda n: torch.empty(n, dtype=torch.float32, device=device)
-    out = {"loss": f(1), "gscale": f(T), "seq_logratio": f(S), "seq_grad": f(S), "q_loss": f(Q), "q_margin": f(Q),
-           "q_pairs": torch.empty(Q, dtype=torch.int32, device=device)}
+    out = PreferenceOutputs(loss=f(1), gscale=f(T), seq_logratio=f(S), seq_grad=f(S), q_loss=f(Q), q_margin=f(Q),
+                            q_pairs=torch.empty(Q, dtype=torch.int32, device=device))
     if scores:
         out["logp"], out["lse"] = f(T), f(T)
+    out.known = tuple(out[k] for k in _PREF_OUTPUTS) if out["loss"].is_cuda else None
     return out
+
+
+def _pref_outputs(out: Dict[str, torch.Tensor], T: int, S: int, Q: int) -> tuple:
+    """Device pointers of gscale, seq_logratio, seq_grad, q_loss, q_margin, q_pairs (these two may be missing) and loss."""
+    if type(out) is PreferenceOutputs and out.known is not None:
+        gscale, ratio, grad, q_loss, margin, pairs, loss = out.known
+        if (gscale.numel() < T or ratio.numel() < S or grad.numel() < S or q_loss.numel() < Q or margin.numel() < Q
+                or pairs.numel() < Q or loss.numel() < 1):
+            raise SapoError("the outputs are too small for these tokens, sequences and questions")
+        return (gscale.data_ptr(), ratio.data_ptr(), grad.data_ptr(), q_loss.data_ptr(), margin.data_ptr(),
+                pairs.data_ptr(), loss.data_ptr())
+    pointers = []
+    for name, n in zip(_PREF_OUTPUTS, (T, S, S, Q, Q, Q, 1)):
+        t = out.get(name)
+        if t is None and name not in ("q_margin", "q_pairs"):
+            raise SapoError(f"the outputs must hold {name}")
+        pointers.append(None if t is None else _at_least(t, torch.int32 if name == "q_pairs" else torch.float32, n, name))
+    return tuple(pointers)
 
 
 def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens: torch.Tensor, rewards: torch.Tensor,
@@ -600,16 +647,12 @@ def sapo_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor, cu_seqlens:
     _require_cuda()
     f32, i32, n = torch.float32, torch.int32, logp.numel()
     seqs, Q = cu_seqlens.numel() - 1, group_offsets.numel() - 1
-    factors, ratio, grad, q_loss = out["gscale"], out["seq_logratio"], out["seq_grad"], out["q_loss"]
-    if factors.numel() < n or ratio.numel() < seqs or grad.numel() < seqs or q_loss.numel() < Q:
-        raise SapoError("the outputs are too small for these tokens, sequences and questions")
     rc = load().sapo_preference_loss(
-        _at_least(logp, f32, n, "logp"), _at_least(ref_logp, f32, n, "ref_logp"), n,
-        _at_least(cu_seqlens, i32, 1, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
-        _at_least(group_offsets, i32, 1, "group_offsets"), Q,
-        _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale), factors.data_ptr(),
-        ratio.data_ptr(), grad.data_ptr(), q_loss.data_ptr(), _p(out.get("q_margin")), _p(out.get("q_pairs")),
-        out["loss"].data_ptr(), status.data_ptr(), _stream())
+        _elements(logp, f32, "logp"), _at_least(ref_logp, f32, n, "ref_logp"), n,
+        _elements(cu_seqlens, i32, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
+        _elements(group_offsets, i32, "group_offsets"), Q,
+        _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale), *_pref_outputs(out, n, seqs, Q),
+        _at_least(status, i32, 1, "status"), _stream())
     _check(rc, "sapo_preference_loss")
 
 
@@ -631,19 +674,15 @@ def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids
     if dhidden.shape[0] < T or dhidden.shape[1] != H or dW_head.shape != (V, H) \
             or not (dhidden.is_contiguous() and dW_head.is_contiguous()):
         raise SapoError("dhidden must be [T, H] and dW_head [V, H], both contiguous")
-    if (min(out[k].numel() for k in ("logp", "lse", "gscale")) < T or out["q_loss"].numel() < Q
-            or min(out["seq_logratio"].numel(), out["seq_grad"].numel()) < seqs):
-        raise SapoError("the outputs are too small for these tokens, sequences and questions")
     cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
     rc = load().sapo_preference_loss_fwd_bwd(
         _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0),
         _at_least(ids, i32, T, "ids"), _at_least(ref_logp, f32, T, "ref_logp"),
-        _at_least(cu_seqlens, i32, 1, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
-        _at_least(group_offsets, i32, 1, "group_offsets"), Q,
-        cfg, _p(out["logp"]), _p(out["lse"]), _p(out["gscale"]), _p(out["seq_logratio"]), _p(out["seq_grad"]),
-        _p(out["q_loss"]), _p(out.get("q_margin")), _p(out.get("q_pairs")), _p(out["loss"]), _p(dhidden), _p(dW_head),
-        _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
-        _p(workspace), workspace.numel() * workspace.element_size(), _p(status), _stream())
+        _elements(cu_seqlens, i32, "cu_seqlens"), seqs, _at_least(rewards, f32, seqs, "rewards"),
+        _elements(group_offsets, i32, "group_offsets"), Q,
+        cfg, _at_least(out["logp"], f32, T, "logp"), _at_least(out["lse"], f32, T, "lse"), *_pref_outputs(out, T, seqs, Q),
+        _p(dhidden), _p(dW_head), _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
+        _p(workspace), workspace.numel() * workspace.element_size(), _at_least(status, i32, 1, "status"), _stream())
     _check(rc, "sapo_preference_loss_fwd_bwd")
 
 
