@@ -669,11 +669,12 @@ def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids
     T = int(hidden.shape[0]) if T is None else int(T)
     H, V = int(hidden.shape[1]), int(W_head.shape[0])
     f32, i32, seqs, Q = torch.float32, torch.int32, cu_seqlens.numel() - 1, group_offsets.numel() - 1
-    if W_head.dtype != hidden.dtype or W_head.shape[1] != H or hidden.shape[0] < T:
-        raise SapoError("hidden must be [T, H] and W_head [V, H] of the same element type")
+    if (W_head.dtype != hidden.dtype or W_head.shape[1] != H or hidden.shape[0] < T or not hidden.is_cuda or not W_head.is_cuda
+            or hidden.stride(1) != 1 or W_head.stride(1) != 1):
+        raise SapoError("hidden must be [T, H] and W_head [V, H] of the same element type, with contiguous columns, on the GPU")
     if dhidden.shape[0] < T or dhidden.shape[1] != H or dW_head.shape != (V, H) \
-            or not (dhidden.is_contiguous() and dW_head.is_contiguous()):
-        raise SapoError("dhidden must be [T, H] and dW_head [V, H], both contiguous")
+            or not (dhidden.is_contiguous() and dW_head.is_contiguous() and dhidden.is_cuda and dW_head.is_cuda):
+        raise SapoError("dhidden must be [T, H] and dW_head [V, H], both contiguous, on the GPU")
     cfg = _pref_cfg(beta, kind, pairs, label_smoothing, length_norm, grad_scale)
     rc = load().sapo_preference_loss_fwd_bwd(
         _p(hidden), _p(W_head), _dtype_code(hidden), T, H, V, hidden.stride(0), W_head.stride(0),

@@ -112,3 +112,13 @@ def test_allocated_outputs_are_checked_once_an_entry_changes(lib, through_head):
     refuses(lib, lambda: preference(out, i(1), through_head))
     out = B.alloc_preference_outputs(T, S, Q, device="cpu", scores=through_head)          # on the host
     refuses(lib, lambda: preference(out, i(1), through_head))
+
+
+def test_head_operands_with_gaps_between_columns_or_on_the_host(lib):
+    good = outputs(True)
+    preference(good, i(1), True)
+    bf = torch.bfloat16
+    for change in (dict(hidden=f(T, 2 * H, dt=bf)[:, ::2]), dict(W=f(V, 2 * H, dt=bf)[:, ::2]), dict(hidden=torch.zeros(T, H, dtype=bf)),
+                   dict(W=torch.zeros(V, H, dtype=bf)), dict(dhidden=torch.zeros(T, H)), dict(dW=torch.zeros(V, H))):
+        refuses(lib, lambda: preference(good, i(1), True, **change))
+    preference(good, i(1), True, hidden=f(T, 2 * H, dt=bf)[:, :H], W=f(V, 2 * H, dt=bf)[:, H:])      # a pitch is fine
