@@ -702,9 +702,12 @@ class Ckpt8:
         n = -(-H // Q8_GROUP)
         if (self.H != H or data.shape[0] != T or data.shape[1] < H or scale.shape[0] != T or scale.shape[1] < n
                 or data.dtype != torch.int8 or scale.dtype != torch.float32 or data.stride(1) != 1
-                or scale.stride(1) != 1):
-            raise SapoError("the checkpoint must have the shape of the activation")
-        return Ckpt8C(data.data_ptr(), scale.data_ptr(), max(data.stride(0), H), max(scale.stride(0), n))
+                or scale.stride(1) != 1 or not data.is_cuda or not scale.is_cuda):
+            raise SapoError("the checkpoint must have the shape of the activation, on the GPU")
+        ld, ld_scale = data.stride(0), scale.stride(0)
+        if T > 1 and (ld < H or ld_scale < n):
+            raise SapoError("rows of the checkpoint overlap")
+        return Ckpt8C(data.data_ptr(), scale.data_ptr(), max(ld, H), max(ld_scale, n))
 
 
 def alloc_ckpt8(T: int, H: int, device="cuda") -> Ckpt8:

@@ -122,3 +122,22 @@ def test_head_operands_with_gaps_between_columns_or_on_the_host(lib):
                    dict(W=torch.zeros(V, H, dtype=bf)), dict(dhidden=torch.zeros(T, H)), dict(dW=torch.zeros(V, H))):
         refuses(lib, lambda: preference(good, i(1), True, **change))
     preference(good, i(1), True, hidden=f(T, 2 * H, dt=bf)[:, :H], W=f(V, 2 * H, dt=bf)[:, H:])      # a pitch is fine
+
+
+def test_checkpoints_with_overlapping_rows_or_on_the_host(lib):
+    x, st = f(T, H, dt=torch.bfloat16), i(1)
+    data, scale = f(T, H, dt=torch.int8), f(T, 1)
+    calls = (lambda c: B.sapo_ckpt8_store(x, c, st), lambda c: B.sapo_ckpt8_restore(c, x),
+             lambda c: B.sapo_norm_fwd(x, None, None, 1e-6, "rms", x, None, None, c, st),
+             lambda c: B.sapo_norm_bwd(x, c, None, None, f(T), "rms", x, None, None, None),
+             lambda c: B.sapo_norm_replay(c, None, None, "rms", None, f(T), x))
+    for call in calls:
+        call(B.Ckpt8(data, scale, H))
+    assert len(lib.calls) == 5
+    one_row, one_scale = f(1, H, dt=torch.int8).expand(T, H), f(1, 1).expand(T, 1)
+    for bad in (B.Ckpt8(one_row, scale, H), B.Ckpt8(f(2 * T * H, dt=torch.int8).as_strided((T, H), (H // 2, 1)), scale, H),
+                B.Ckpt8(data, one_scale, H), B.Ckpt8(torch.zeros(T, H, dtype=torch.int8), scale, H), B.Ckpt8(data, torch.zeros(T, 1), H)):
+        for call in calls:
+            refuses(lib, lambda: call(bad))
+    one = B.Ckpt8(f(1, H, dt=torch.int8).expand(1, H), f(1, 1), H)                        # a single row has no pitch
+    B.sapo_ckpt8_restore(one, f(1, H))
