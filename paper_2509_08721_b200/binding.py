@@ -583,7 +583,7 @@ def _elements(t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
 
 def _at_least(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> int:
     """Device pointer of a vector of n elements or more."""
-    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
+    if t is None or t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
         raise SapoError(f"{what} must be contiguous {dtype} with {n} elements on the GPU")
     return t.data_ptr()
 
@@ -683,7 +683,7 @@ def sapo_preference_loss_fwd_bwd(hidden: torch.Tensor, W_head: torch.Tensor, ids
         _elements(group_offsets, i32, "group_offsets"), Q,
         cfg, _at_least(out["logp"], f32, T, "logp"), _at_least(out["lse"], f32, T, "lse"), *_pref_outputs(out, T, seqs, Q),
         _p(dhidden), _p(dW_head), _out_dtype_code(dhidden, dW_head), 1 if accumulate_dW else 0,
-        _p(workspace), workspace.numel() * workspace.element_size(), _at_least(status, i32, 1, "status"), _stream())
+        *_scratch(workspace), _at_least(status, i32, 1, "status"), _stream())
     _check(rc, "sapo_preference_loss_fwd_bwd")
 
 
@@ -736,6 +736,15 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     return t.data_ptr()
 
 
+def _scratch(t: Optional[torch.Tensor]):
+    """(device pointer, bytes) of an optional workspace."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise SapoError("the workspace must be contiguous, on the GPU")
+    return t.data_ptr(), t.nbytes
+
+
 def _weight(t: Optional[torch.Tensor], H: int, what: str) -> Optional[int]:
     if t is None:
         return None
@@ -774,7 +783,8 @@ def sapo_norm_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional
     py, ty, ldy = _rows(y, T, H, "y")
     rc = load().sapo_norm_fwd(px, tx, T, H, ldx, _weight(gamma, H, "gamma"), _weight(beta, H, "beta"),
                               _norm_cfg(kind, eps, gamma, beta), py, ty, ldy, _vector(mean, T, "mean"),
-                              _vector(rstd, T, "rstd"), None if ckpt is None else ckpt.c(T, H), _p(status), _stream())
+                              _vector(rstd, T, "rstd"), None if ckpt is None else ckpt.c(T, H),
+                              None if ckpt is None else _at_least(status, torch.int32, 1, "status"), _stream())
     _check(rc, "sapo_norm_fwd")
 
 
@@ -807,8 +817,7 @@ def sapo_norm_bwd(dy: torch.Tensor, x, gamma: Optional[torch.Tensor], mean: Opti
     rc = load().sapo_norm_bwd(pd, td, ldd, px, tx, ldx, x.c(T, H) if held else None, T, H, _weight(gamma, H, "gamma"),
                               _norm_cfg(kind, 0.0, gamma, None), _vector(mean, T, "mean"), _vector(rstd, T, "rstd"),
                               po, to, ldo, _vector(dgamma, H, "dgamma"), _vector(dbeta, H, "dbeta"),
-                              1 if accumulate else 0, _p(workspace), 0 if workspace is None else workspace.nbytes,
-                              _stream())
+                              1 if accumulate else 0, *_scratch(workspace), _stream())
     _check(rc, "sapo_norm_bwd")
 
 
@@ -817,7 +826,8 @@ def sapo_ckpt8_store(x: torch.Tensor, ckpt: Ckpt8, status: torch.Tensor) -> None
     _require_cuda()
     T, H = x.shape
     px, tx, ldx = _rows(x, T, H, "x")
-    _check(load().sapo_ckpt8_store(px, tx, T, H, ldx, ckpt.c(T, H), _p(status), _stream()), "sapo_ckpt8_store")
+    rc = load().sapo_ckpt8_store(px, tx, T, H, ldx, ckpt.c(T, H), _at_least(status, torch.int32, 1, "status"), _stream())
+    _check(rc, "sapo_ckpt8_store")
 
 
 def sapo_ckpt8_restore(ckpt: Ckpt8, x: torch.Tensor) -> None:

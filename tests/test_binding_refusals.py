@@ -141,3 +141,19 @@ def test_checkpoints_with_overlapping_rows_or_on_the_host(lib):
             refuses(lib, lambda: call(bad))
     one = B.Ckpt8(f(1, H, dt=torch.int8).expand(1, H), f(1, 1), H)                        # a single row has no pitch
     B.sapo_ckpt8_restore(one, f(1, H))
+
+
+def test_workspaces_and_status_words_that_are_not_on_the_gpu(lib):
+    x, c = f(T, H, dt=torch.bfloat16), B.Ckpt8(f(T, H, dt=torch.int8), f(T, 1), H)
+    back = lambda ws: B.sapo_norm_bwd(x, x, None, None, f(T), "rms", x, f(H), None, ws)
+    head = lambda ws: preference(outputs(True), i(1), True, ws=ws)
+    for call in (back, head):
+        call(f(64, dt=torch.uint8))
+        for bad in (torch.zeros(64, dtype=torch.uint8), f(64, dt=torch.uint8)[::2]):
+            refuses(lib, lambda: call(bad))
+    back(None)                                                    # the library says whether it needs one
+    for call in (lambda st: B.sapo_norm_fwd(x, None, None, 1e-6, "rms", x, None, None, c, st), lambda st: B.sapo_ckpt8_store(x, c, st)):
+        call(i(1))
+        for bad in (None, i(0), f(1), torch.zeros(1, dtype=torch.int32)):
+            refuses(lib, lambda: call(bad))
+    B.sapo_norm_fwd(x, None, None, 1e-6, "rms", x, None, None)    # without a checkpoint the status is not used
