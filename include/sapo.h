@@ -451,6 +451,9 @@ int sapo_preference_loss(const float* logp, const float* ref_logp, int64_t T, co
  * logp, lse, gscale [T]; a token with an id outside [0, V) gets logp 0 (SAPO_ST_BAD_TOKEN_ID), is left
  * out of its sequence's sum and gets no gradient.  The same holds for a token whose log ratio is beyond
  * +-69 (SAPO_ST_EXP_RANGE): its exponentials are taken relative to exp(ref_logp).
+ * lse and logp are not sapo_policy_loss_fwd's to the bit: here a part of what the tensor cores truncate from a logit is put
+ * back (they add in fp32 rounded towards zero; lse is short by about 1e-9 H E_p[z] without it, and a sequence sums that),
+ * and a log ratio is formed without the rounding of its lse.
  * workspace: sapo_workspace_bytes(SAPO_WS_PREFERENCE, ...), at least sapo_workspace_bytes_min of it.  With a workspace
  * whose panel holds the whole batch (what the first returns, up to 40960 tokens) the call takes 6 T V H flops, with a
  * smaller one 8 T V H: a pair's factor is known only when both its sequences have been scored. */
