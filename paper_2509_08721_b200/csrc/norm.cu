@@ -106,16 +106,19 @@ static int launch_fwd_ring_full(const NormFwdArgs& a, const RingPlan& p, int sms
   KernelScope scope(SAPO_K_NORM_FWD, st);
   return launch_overlapped(kernel, dim3((unsigned)blocks), p.threads, smem, 0, st, a, p.wpr);
 }
-// FULL: the row's last warp has all its columns too, so that nothing is predicated
+// FULL: the row's last warp has all its columns too, so that nothing is predicated.  (With 8 vectors a thread that is
+// the widest row only, which does not fit in fp32.)
 template <class TX, int VPL>
 static int launch_fwd_ring_vpl(const NormFwdArgs& a, const RingPlan& p, int sms, cudaStream_t st) {
-  return a.H == p.wpr * VPL * 256 ? launch_fwd_ring_full<TX, VPL, true>(a, p, sms, st) : launch_fwd_ring_full<TX, VPL, false>(a, p, sms, st);
+  if constexpr (VPL < 8 || FwdRing<TX, VPL>::smem(NORM_MAX_H) <= SMEM_MAX) {
+    if (a.H == p.wpr * VPL * 256) return launch_fwd_ring_full<TX, VPL, true>(a, p, sms, st);
+  }
+  return launch_fwd_ring_full<TX, VPL, false>(a, p, sms, st);
 }
 template <class TX>
 static int launch_fwd_ring(const NormFwdArgs& a, int sms, cudaStream_t st) {
   const RingPlan p = fwd_ring_plan(a.H);
-  switch (p.vpl) {
-    case 1: return launch_fwd_ring_vpl<TX, 1>(a, p, sms, st);
+  switch (p.vpl) {                         // (rows of more than FWD_RING_ABOVE columns: two vectors at least)
     case 2: return launch_fwd_ring_vpl<TX, 2>(a, p, sms, st);
     case 3: return launch_fwd_ring_vpl<TX, 3>(a, p, sms, st);
     case 4: return launch_fwd_ring_vpl<TX, 4>(a, p, sms, st);
@@ -280,14 +283,13 @@ static int launch_ckpt8(const Ckpt8Args& a, int sms, cudaStream_t st) {
     if (a.H <= 32) return launch_ckpt8_rows<TX, 4, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
     if (a.H <= 64) return launch_ckpt8_rows<TX, 8, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
     if (a.H <= 128) return launch_ckpt8_rows<TX, 16, RESTORE ? 2 : 4, RESTORE>(a, sms, st);
-    // vectors a lane takes of a row: up to 4, as many as leave the fewest of the row's last segment unused
-    const int steps = ceil_div(a.H, 256), segments = ceil_div(steps, RESTORE ? 2 : 4);
-    switch (ceil_div(steps, segments)) {
-      case 1: return launch_ckpt8_rows<TX, 32, 1, RESTORE>(a, sms, st);
-      case 2: return launch_ckpt8_rows<TX, 32, 2, RESTORE>(a, sms, st);
-      case 3: return launch_ckpt8_rows<TX, 32, 3, RESTORE>(a, sms, st);
-      default: return launch_ckpt8_rows<TX, 32, 4, RESTORE>(a, sms, st);
+    // vectors a lane takes of a row: up to 4 (2 on the way back), as many as leave the fewest of the row's last segment unused
+    const int steps = ceil_div(a.H, 256), segments = ceil_div(steps, RESTORE ? 2 : 4), n = ceil_div(steps, segments);
+    if constexpr (!RESTORE) {
+      if (n == 3) return launch_ckpt8_rows<TX, 32, 3, RESTORE>(a, sms, st);
+      if (n == 4) return launch_ckpt8_rows<TX, 32, 4, RESTORE>(a, sms, st);
     }
+    return n == 1 ? launch_ckpt8_rows<TX, 32, 1, RESTORE>(a, sms, st) : launch_ckpt8_rows<TX, 32, 2, RESTORE>(a, sms, st);
   }
   if (a.H % 2 == 0 && pairs_ok(a.x) && pairs_ok(a.q)) return launch_ckpt8_any<TX, 2, RESTORE>(a, sms, st);
   return launch_ckpt8_any<TX, 1, RESTORE>(a, sms, st);

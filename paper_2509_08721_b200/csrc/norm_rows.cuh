@@ -71,7 +71,7 @@ struct WarpRow {
 template <class TX, int VPL> struct FwdRing {
   static constexpr int STAGE_BYTES = NORM_THREADS / 32 * WarpRow<TX, VPL>::BYTES;
   static constexpr int STAGES = sizeof(TX) == 1 ? 4 : (VPL <= 4 ? 3 : 2);
-  static int smem(int H) { return STAGES * STAGE_BYTES + 2 * H * (int)sizeof(float); }   // and the weights
+  static constexpr int smem(int H) { return STAGES * STAGE_BYTES + 2 * H * (int)sizeof(float); }   // and the weights
 };
 
 // Zeros where the warp's columns do not exist: nothing is ever copied there, and zeros add nothing to sums.
