@@ -31,6 +31,8 @@ static inline long long read_bounds_violations() { return 0; }
 #endif
 long long bounds_violations_pack();
 long long bounds_violations_lmhead();
+long long bounds_violations_norm();
+long long bounds_violations_preference();
 
 inline int check_launch() {
   return cudaGetLastError() == cudaSuccess ? SAPO_OK : SAPO_ERR_CUDA;

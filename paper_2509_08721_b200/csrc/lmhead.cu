@@ -1340,6 +1340,7 @@ __global__ void __launch_bounds__(256) pref_flags_kernel(PrefArgs a, float* __re
   }
   for (int32_t s = s0 + lane; s < s1; s += 32) {
     const float r = reward(s);
+    if (!SAPO_IN_BOUNDS(s >= 0 && s < a.S)) continue;
     flags[s] = hi > lo && r == r && (a.pairs == SAPO_PREF_ALL || s == best || s == worst) ? 1.f : 0.f;
   }
 }

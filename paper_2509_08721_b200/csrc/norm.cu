@@ -302,6 +302,7 @@ static int launch_ckpt8_x(const Ckpt8Args& a, cudaStream_t st) {
   return a.x.dtype == SAPO_DTYPE_F32 ? launch_ckpt8<float, RESTORE>(a, sms, st) : launch_ckpt8<__nv_bfloat16, RESTORE>(a, sms, st);
 }
 
+long long bounds_violations_norm() { return read_bounds_violations(); }
 }  // namespace sapo
 
 // =============================================================================== C ABI

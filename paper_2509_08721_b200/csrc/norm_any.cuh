@@ -387,6 +387,9 @@ __global__ void __launch_bounds__(256) ckpt8_any_kernel(Ckpt8Args a, int64_t ste
   const int64_t s_step = step_rows * a.q.ld_scale + step_groups, s_wrap = a.q.ld_scale - groups;
   const int32_t last_left = a.H - (groups - 1) * Q8_GROUP - col;       // columns from the lane's first one on, last group
   while (row < a.T) {
+    if (!SAPO_IN_BOUNDS(row >= 0 && g >= 0 && g < groups && x - static_cast<TX*>(a.x.p) == row * a.x.ld + g * Q8_GROUP + col &&
+                        q - a.q.p == row * a.q.ld + g * Q8_GROUP + col && s - a.q.scale == row * a.q.ld_scale + g))
+      break;
     TX* xs[N]; int8_t* qs[N]; float* ss[N];
     int left[N]; bool in[N];
     float2 v[N][2]; float scale_of[N];

@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 2) norm_fwd_ring_kernel(NormFwdA
   const int n_rows = row0 < a.T ? (int)((a.T - row0 + step - 1) / step) : 0;
   int to_fetch = n_rows;
   auto fetch = [&](int stage) {
-    if (to_fetch > 0) Row::template copy<FULL>(dst + stage * STAGE_BYTES, src, cols, lane);
+    if (to_fetch > 0 && SAPO_IN_BOUNDS(row0 + (n_rows - to_fetch) * step < a.T && stage >= 0 && stage < S))
+      Row::template copy<FULL>(dst + stage * STAGE_BYTES, src, cols, lane);
     copy_commit();
     --to_fetch;
     src += step * ld;
@@ -290,7 +291,7 @@ __global__ void __launch_bounds__(MAX_THREADS, MAX_THREADS == 256 ? 2 : 1) norm_
   int to_fetch = n_rows;
   stat += row0;
   auto fetch = [&](int stage) {
-    if (to_fetch > 0) {
+    if (to_fetch > 0 && SAPO_IN_BOUNDS(row0 + (n_rows - to_fetch) * step < a.T && stage >= 0 && stage < S)) {
       const uint32_t off = stage * stage_bytes;
       RowX::template copy<FULL>(dst_x + off, xp, cols, lane);
       RowD::template copy<FULL>(dst_d + off, dyp, cols, lane);
@@ -469,6 +470,7 @@ __global__ void __launch_bounds__(256) ckpt8_rows_kernel(Ckpt8Args a, int32_t se
     const int64_t x_next = L == 32 ? 256 : a.x.ld, q_next = L == 32 ? 256 : a.q.ld;
     // vector k of the lane: 256 k columns on (L = 32), or k rows on
     auto exists = [&](int k) { return L == 32 ? col + 256 * k < a.H : row + k < a.T && col < a.H; };
+    if (!SAPO_IN_BOUNDS(unit >= 0 && seg >= 0 && seg < segments)) break;
     float2 v[N][4];
     if constexpr (RESTORE) {
       float s[N];

@@ -74,6 +74,7 @@ __device__ __forceinline__ void pair_loss(const PrefArgs& a, float h, float& l, 
 
 // log ratio of token t, NaN or infinite where the token is masked
 __device__ __forceinline__ float token_ratio(const PrefArgs& a, int32_t t) {
+  if (!SAPO_IN_BOUNDS(t >= 0 && t < a.T)) return NAN;
   return a.ref_logp != nullptr ? a.logp[t] - a.ref_logp[t] : a.logp[t];
 }
 
@@ -143,9 +144,13 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
     if (t_hi < t_lo) t_hi = t_lo;
     const int64_t skip = (int64_t)a.q_clusters * size;
     const int64_t first = (blockIdx.x - skip) * PREF_THREADS + threadIdx.x, step = (gridDim.x - skip) * PREF_THREADS;
-    for (int64_t i = first; i < (int64_t)t_lo + (Tc - t_hi); i += step) a.gscale[i < t_lo ? i : t_hi + (i - t_lo)] = 0.f;
+    for (int64_t i = first; i < (int64_t)t_lo + (Tc - t_hi); i += step) {
+      const int64_t t = i < t_lo ? i : t_hi + (i - t_lo);
+      if (SAPO_IN_BOUNDS(t >= 0 && t < a.T)) a.gscale[t] = 0.f;
+    }
     for (int64_t i = first; i < (int64_t)s_lo + (a.S - s_hi); i += step) {
       const int64_t s = i < s_lo ? i : s_hi + (i - s_lo);
+      if (!SAPO_IN_BOUNDS(s >= 0 && s < a.S)) continue;
       a.seq_logratio[s] = 0.f;
       a.seq_grad[s] = 0.f;
     }
@@ -159,6 +164,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
       // (the previous question's readers are behind the barrier that ended its step 2, or read their own block's)
       __syncthreads();
       for (int32_t i = threadIdx.x; i <= s1 - s0; i += PREF_THREADS) {
+        if (!SAPO_IN_BOUNDS(s0 >= 0 && s0 + i <= a.S && i <= PREF_SEQS)) continue;
         cu_s[i] = a.cu[s0 + i];
         if (i < s1 - s0) r_s[i] = a.rewards[s0 + i];
       }
@@ -203,7 +209,7 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           if (isfinite(d)) part[0] += d; else masked = true;
         }
         const float sum = warp_sum((part[0] + part[1]) + (part[2] + part[3]));
-        if (lane == 0) {
+        if (lane == 0 && SAPO_IN_BOUNDS(gw < PREF_MAX_CLUSTER * PREF_WARPS && s >= 0 && s < a.S)) {
           if (t0 <= begin) to_first(&head[gw], sum);
           else if (kept) to_first(&R_s[s - s0], sum);
           else a.seq_logratio[s] = sum;
@@ -227,12 +233,13 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
           if (w1 >= n_warps) w1 = n_warps - 1;
           const bool inside = t0 - ta > w0 * piece;
           float x = 0.f;
-          for (int32_t w = w0 + (inside ? 1 : 0) + lane; w <= w1; w += 32) x += head[w];
+          for (int32_t w = w0 + (inside ? 1 : 0) + lane; w <= w1; w += 32)
+            if (SAPO_IN_BOUNDS(w >= 0 && w < n_warps)) x += head[w];
           R = warp_sum(x) + (inside ? (kept ? R_s[s - s0] : __ldcg(a.seq_logratio + s)) : 0.f);
           if (a.length_norm) R /= (float)n;
         }
         __syncwarp();
-        if (lane == 0) {
+        if (lane == 0 && SAPO_IN_BOUNDS(s >= 0 && s < a.S)) {
           const float r = kept ? r_s[s - s0] : a.rewards[s];
           if (!isfinite(r)) bad_reward = true;
           a.seq_logratio[s] = R;
@@ -323,7 +330,8 @@ __global__ void __launch_bounds__(PREF_THREADS) preference_kernel(PrefArgs a) {
         float g = !kept ? __ldcg(a.seq_grad + s) : (SOLO ? g_s[s - s0] : load_from_first(&g_s[s - s0]));
         if (a.length_norm) g /= (float)(t1 - t0);
         // the lane that summed a token writes its factor, and knows whether any of its tokens was masked
-        for (int32_t t = from + lane; t < to; t += 32) a.gscale[t] = masked && !isfinite(token_ratio(a, t)) ? 0.f : g;
+        for (int32_t t = from + lane; t < to; t += 32)
+          if (SAPO_IN_BOUNDS(t >= 0 && t < a.T)) a.gscale[t] = masked && !isfinite(token_ratio(a, t)) ? 0.f : g;
       }
     }
   }
@@ -427,6 +435,7 @@ int launch_preference(PrefArgs a, cudaStream_t st) {
   return launch_overlapped(preference_mean_kernel, dim3(1), 32, 0, 0, st, (const float*)a.q_loss, a.Q, a.loss);
 }
 
+long long bounds_violations_preference() { return read_bounds_violations(); }
 }  // namespace sapo
 
 extern "C" int sapo_preference_loss(const float* logp, const float* ref_logp, int64_t T, const int32_t* cu_seqlens,

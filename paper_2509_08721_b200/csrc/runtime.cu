@@ -41,8 +41,11 @@ extern "C" int sapo_timing_read(float* h_ms, int32_t* h_launches) {
 
 extern "C" int64_t sapo_debug_bounds_violations(void) {
 #ifdef SAPO_BOUNDS_CHECK
-  const long long a = sapo::bounds_violations_pack(), b = sapo::bounds_violations_lmhead();
-  return (a < 0 || b < 0) ? -2 : a + b;
+  const long long counts[] = {sapo::bounds_violations_pack(), sapo::bounds_violations_lmhead(),
+                              sapo::bounds_violations_norm(), sapo::bounds_violations_preference()};
+  long long sum = 0;
+  for (long long n : counts) { if (n < 0) return -2; sum += n; }
+  return sum;
 #else
   return -1;      // not a checked build
 #endif
