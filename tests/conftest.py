@@ -13,6 +13,9 @@ def pytest_configure(config):
 
 
 def pytest_collection_modifyitems(config, items):
+    # The full-size workloads last: without the cache of tests/golden/write_oracle_cache.py their oracle runs on the host
+    # for most of an hour, and a run that is cut off should have run everything else by then.
+    items.sort(key=lambda item: os.path.basename(str(item.fspath)) == "test_gpu_full_size.py")
     try:
         import torch
         has_gpu = torch.cuda.is_available()
