@@ -14,10 +14,11 @@ namespace sapo {
 // same warp read what a lane copied: the wait for a row is one __syncwarp.
 // What then bounds a row kernel is instruction issue (at the copy bandwidth an SM has to finish 4 to 6
 // columns per clock), so the arithmetic is done in pairs and every vector is whole.
-// Measured on long runs of rows, beside a copy (forward) or an addition of two arrays (backward) of the same bytes:
-//   forward    146382 x 1536 bf16  150 to 160 us (copy 142), 500000 x 512  160 us (copy 158)
-//   backward   143347 x 3584 bf16  475 us (addition 435), 146382 x 1536  240 us (193), where the fewer warps of a
-//              row leave the waits for its sums less covered (45 % of issue slots used, 75 % of the DRAM rate)
+// Measured on long runs of rows, beside a copy (forward) or an addition of two arrays (backward) of the same bytes; 30 calls
+// in a row, then 1.5 s of them (boxes and their state move either by up to 10 %):
+//   forward    146382 x 1536 bf16  150 and 157 us (copy 143), 500000 x 512  165 and 160 us (copy 160)
+//   backward   143347 x 3584 bf16  476 and 514 us (addition 437), 146382 x 1536  237 and 213 us (194), where the fewer
+//              warps of a row leave the waits for its sums less covered (45 % of issue slots used, 75 % of the DRAM rate)
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 // (predicated, not branched around: a lane whose columns do not exist copies nothing)
 template <int BYTES, bool ALWAYS>
@@ -82,7 +83,7 @@ __device__ __forceinline__ void clear_stages(uint8_t* mine, int bytes, int stage
 }
 // y = (x - mean) rstd gamma + beta; the row stays in registers between its mean, its sum of squares about the mean
 // and y, so it is read once and nothing is subtracted from a sum of squares.  With a checkpoint the groups of 128
-// columns are quantised on the way (146382 x 1536: 150 us for 0.90 GB without, 196 us for 1.13 GB with).
+// columns are quantised on the way (146382 x 1536: 150 us for 0.90 GB without, 206 us for 1.13 GB with).
 // The weights are kept in shared memory in fp32, in the order in which a warp reads them without bank conflicts.
 // TX int8_t: replay from a checkpoint (a.q), statistics given.
 template <class TX, int VPL, bool FULL>
