@@ -31,6 +31,10 @@
  *   sapo_norm_fwd, sapo_norm_bwd    the norm in front of the LM head (layer norm, RMS norm)
  *   sapo_ckpt8_store, sapo_ckpt8_restore, sapo_norm_replay
  *                                   activations kept in 8 bits between forward and backward
+ *   sapo_sample                     draws the next tokens from logits (the answers of a round)
+ *   sapo_fp8_store, sapo_fp8_matmul matrices in 8-bit floating point and their product (the head that
+ *                                   answers)
+ *   sapo_adamw_step                 AdamW over many tensors, states in 32 or 8 bits
  *   sapo_policy_loss_fwd_static     the forward for callers that may not allocate device memory
  *   sapo_group_advantages_warp, sapo_workspace_bytes[_min], sapo_status_string, sapo_timing_*,
  *   sapo_launch_count, sapo_debug_wait_timeout, sapo_debug_bounds_violations
@@ -546,6 +550,115 @@ int sapo_adam_step(float* master, float* m, float* v, const float* grad, void* w
                    int64_t rows, int32_t cols, int64_t ld_w, int32_t step,
                    float lr, float beta1, float beta2, float eps, void* stream);
 
+/* AdamW over a list of tensors (Loshchilov & Hutter; no counterpart in the paper, whose run is plain
+ * Adam: sapo_adam_step).  Per element, with g = grad (* *grad_scale), lr_i = lr lr_factor:
+ *   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g g;
+ *   master <- master (1 - lr_i weight_decay) - lr_i (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
+ * and copy_bf16 (may be NULL) = master rounded to bf16.  An element whose g is not finite is left as it
+ * was (SAPO_ST_NONFINITE_INPUT); v stops at the largest fp32.
+ * A tensor has n elements in one run of memory, of any n (0 too) and any alignment of its element type;
+ * arrays on 16-byte boundaries are faster.  The _out arrays receive the new values: the same pointers as
+ * the old ones for a step in place, or other arrays (the weights of the policy before the step stay).
+ * state_bits 32: m, v are fp32.  state_bits 8: m and v are e4m3 codes [n] with an fp32 scale per 128
+ * elements, [ceil(n / 128)]: m = code * m_scale, and the SECOND array holds the root: sqrt(v) = code *
+ * v_scale.  The step itself uses the new m and v before they are rounded.  With a the largest magnitude of
+ * a group, scale = a (1/448) (0, and codes 0, if a < 2^-119); m (448 (1/a)) is rounded to the nearest code.  For the
+ * root, t = max(sqrt(v) (448 (1/a)), 2^-6) (0 if v is 0) is rounded up or down to a code so that it is right on average: of
+ * the bits of t as fp32 those of weight below 2^20 are cut off after 16 r + 8 has been added, r being 16 random
+ * bits; element i of tensor `number` in the list takes half i % 8 (low half of a word first) of
+ * philox4x32-10(counter = (i / 8 low, i / 8 high, number, step), key = (seed low, seed high)).  Each product and sum of
+ * the state is rounded to fp32 by itself, so that the state is defined to the bit.  Zeroed codes and scales are a fresh state. */
+typedef struct sapo_adamw_tensor {
+  const float* master;
+  float*       master_out;
+  const void*  grad;          /* grad_dtype */
+  const void*  m;
+  const void*  v;
+  void*        m_out;
+  void*        v_out;
+  const float* m_scale;       /* state_bits 8 only */
+  const float* v_scale;
+  float*       m_scale_out;
+  float*       v_scale_out;
+  void*        copy_bf16;
+  int64_t      n;
+  float        lr_factor;
+  float        weight_decay;
+  int32_t      grad_dtype;
+  int32_t      state_bits;
+} sapo_adamw_tensor;
+
+/* step counts from 1.  lr_dev, step_dev (each may be NULL): device memory that is read instead of lr and
+ * step, so that a captured call follows a schedule.  grad_scale (may be NULL): one float in device memory, e.g. the
+ * factor of a clipped gradient norm. */
+typedef struct sapo_adamw_cfg {
+  double   lr, beta1, beta2, eps;
+  uint64_t seed;
+  int32_t  step;
+  const int32_t* step_dev;
+  const float*   lr_dev;
+  const float*   grad_scale;
+} sapo_adamw_cfg;
+
+int sapo_adamw_step(const sapo_adamw_tensor* h_tensors, int32_t n_tensors, const sapo_adamw_cfg* h_cfg,
+                    int32_t* status, void* stream);
+
+/* A matrix [R, C] in 8-bit floating point: e4m3 codes data [R, ld], and one fp32 scale per row and 128
+ * columns (blocks 0: scale [R, ld_scale]) or per block of 128 rows and 128 columns (blocks 1: scale
+ * [ceil(R / 128), ld_scale]), ld_scale >= ceil(C / 128).  An element stands for code * scale. */
+typedef struct sapo_fp8 {
+  void*   data;
+  float*  scale;
+  int64_t ld, ld_scale;
+  int32_t blocks;
+} sapo_fp8;
+
+/* x [R, ld_x] (bf16 or fp32) into 8 bits: a = the largest |x| of a group, scale = a (1/448), code = x (448 (1/a)) rounded
+ * to the nearest, each product and quotient rounded to fp32 (a below 2^-119: scale and codes 0).  A group that holds a NaN or an infinity gets scale NaN and
+ * codes 0 (SAPO_ST_NONFINITE_INPUT).  Any C and any leading dimension from C up; R may be 0. */
+int sapo_fp8_store(const void* x, int32_t x_dtype, int64_t R, int32_t C, int64_t ld_x, const sapo_fp8* h_out,
+                   int32_t* status, void* stream);
+
+/* y [T, ld_y] (bf16 or fp32) = x W^T for x [T, K] with scales per row (blocks 0) and W [N, K] with scales
+ * per block (blocks 1); products of one block of 128 along K are formed on the tensor cores, scaled and added up in
+ * fp32, and rounded once.  data of both 16-byte aligned, ld a multiple of 16 where there is more than one row (codes
+ * behind column K are not read).  Any N, K >= 1, T >= 0; y on 16-byte boundaries with ld_y in bytes a multiple of 16 is
+ * written faster.  *status: SAPO_ST_WAIT_TIMEOUT. */
+int sapo_fp8_matmul(const sapo_fp8* h_x, int64_t T, const sapo_fp8* h_w, int32_t N, int32_t K, void* y, int32_t y_dtype,
+                    int64_t ld_y, int32_t* status, void* stream);
+
+/* How a row is drawn: temperature >= 0 (0: the largest logit), top_k (<= 0: off), top_p (>= 1: off; <= 0: the
+ * largest logit), min_p in [0, 1] (0: off).  The _rows pointers (device, [B], each may be NULL) give every row a value of its own
+ * in place of the common one. */
+typedef struct sapo_sample_cfg {
+  float   temperature;
+  int32_t top_k;
+  float   top_p;
+  float   min_p;
+  const float*   temperature_rows;
+  const int32_t* top_k_rows;
+  const float*   top_p_rows;
+  const float*   min_p_rows;
+} sapo_sample_cfg;
+
+/* Draws one token of every row of logits [B, ld] (V columns, bf16 or fp32): the answers of a round
+ * (Section 3.1: a node's own completions), whose log-probs the training batch keeps as old_logp.
+ * With w_i = exp((z_i - max z) / temperature), tokens stay in the draw that are
+ *   among the top_k largest logits (equal logits: lower index first),
+ *   in that order the first ones whose predecessors' weight is below top_p of the top_k tokens' weight,
+ *   and have w_i >= min_p;
+ * the largest always stays.  Of these, token i wins with probability w_i / sum w: ids[b] = the one with the smallest
+ * e_i / w_i, e_i = -log(1 - (n_i + 1/2) 2^-32), where the 32 bits n_i come from the row's random number
+ * seeds[b]: upper 16 bits half i % 8 (low half of a word first) of philox4x32-10(counter = (i / 8, 0, 0, 0), key = (seed low,
+ * seed high)), lower 16 bits the same of counter (i / 8, 1, 0, 0).  The same number draws the same token.
+ * logp[b] = log softmax(z)[ids[b]], at temperature 1 and over all tokens: old_logp of the loss calls.
+ * Logits of -inf rule a token out.  A row of -inf only gets id -1 and logp 0; so does a row with a NaN, with
+ * +inf, or with a temperature, top_p or min_p that is NaN or out of range (SAPO_ST_NONFINITE_INPUT).
+ * V >= 1, up to 1474048 bytes of logits a row (SAPO_ERR_UNSUPPORTED_SHAPE beyond); B may be 0.  Rows on 16-byte boundaries
+ * are read faster; ld may be 0 (several draws from one row). */
+int sapo_sample(const void* logits, int32_t dtype, int32_t B, int32_t V, int64_t ld, const int64_t* seeds,
+                const sapo_sample_cfg* h_cfg, int32_t* ids, float* logp, int32_t* status, void* stream);
+
 /* Bytes of scratch the forward (SAPO_WS_FWD), backward (SAPO_WS_BWD, SAPO_WS_BWD_ACTIVE),
  * fused (SAPO_WS_FUSED) or preference (SAPO_WS_PREFERENCE) call wants for these sizes; OR SAPO_WS_OUT_BF16 into `which` for a call
  * with bf16 gradient outputs.  Returns 0 for invalid arguments. */
@@ -613,7 +726,11 @@ int sapo_policy_loss_fwd_static(const void* hidden, const void* W_head, int32_t 
 #define SAPO_K_CKPT8      20
 #define SAPO_K_PREFERENCE 21
 #define SAPO_K_PREF_SCORE 22
-#define SAPO_K_COUNT      23
+#define SAPO_K_SAMPLE     23
+#define SAPO_K_FP8_STORE  24
+#define SAPO_K_FP8_MATMUL 25
+#define SAPO_K_ADAMW      26
+#define SAPO_K_COUNT      27
 int sapo_timing_enable(int32_t on);
 int sapo_timing_read(float* h_ms, int32_t* h_launches);
 int64_t sapo_launch_count(void);

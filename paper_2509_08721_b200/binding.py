@@ -38,16 +38,16 @@ EXPORTS = ("sapo_pack_rollouts", "sapo_group_advantages", "sapo_policy_loss_fwd"
            "sapo_policy_loss_fwd_bwd_gather", "sapo_lmhead_lse_partial", "sapo_policy_loss_from_partials", "sapo_policy_loss_bwd_shard",
            "sapo_select_workspace_bytes", "sapo_adam_step", "sapo_preference_loss", "sapo_preference_loss_fwd_bwd",
            "sapo_norm_fwd", "sapo_norm_replay", "sapo_norm_bwd", "sapo_norm_workspace_bytes", "sapo_ckpt8_store",
-           "sapo_ckpt8_restore")
+           "sapo_ckpt8_restore", "sapo_sample", "sapo_fp8_store", "sapo_fp8_matmul", "sapo_adamw_step")
 NORM_KINDS = {"layer": 0, "rms": 1}
 PREF_KINDS = {"sigmoid": 0, "squared": 1, "hinge": 2}
 PREF_PAIRS = {"all": 0, "best_worst": 1}
-Q8_GROUP = 128               # columns of an 8-bit checkpoint that share one scale
+Q8_GROUP = 128               # columns of an 8-bit checkpoint, or elements of an 8-bit state, that share one scale
 STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 KERNEL_NAMES = ("pack_scan", "pack_copy", "group_adv", "split_bf16", "fwd_gemm", "loss_tail",
                 "loss_final", "bwd_dz", "bwd_dh", "bwd_dw", "streamk_fixup", "compact", "select", "adam",
                 "target_logit", "fwd_exp", "fused_tail", "norm_fwd", "norm_bwd", "norm_reduce", "ckpt8", "preference",
-                "pref_score")
+                "pref_score", "sample", "fp8_store", "fp8_matmul", "adamw")
 
 
 class RolloutBufC(C.Structure):
@@ -86,6 +86,29 @@ class Ckpt8C(C.Structure):
 
 class NormCfgC(C.Structure):
     _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("w_dtype", C.c_int32)]
+
+
+class SampleCfgC(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("temperature_rows", C.c_void_p), ("top_k_rows", C.c_void_p), ("top_p_rows", C.c_void_p),
+                ("min_p_rows", C.c_void_p)]
+
+
+class Fp8C(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("ld_scale", C.c_int64),
+                ("blocks", C.c_int32)]
+
+
+class AdamWTensorC(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("master", "master_out", "grad", "m", "v", "m_out", "v_out", "m_scale", "v_scale",
+                                          "m_scale_out", "v_scale_out", "copy_bf16")] + \
+               [("n", C.c_int64), ("lr_factor", C.c_float), ("weight_decay", C.c_float), ("grad_dtype", C.c_int32),
+                ("state_bits", C.c_int32)]
+
+
+class AdamWCfgC(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("seed", C.c_uint64),
+                ("step", C.c_int32), ("step_dev", C.c_void_p), ("lr_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -180,6 +203,14 @@ def load() -> C.CDLL:
     lib.sapo_ckpt8_store.argtypes = [vp, i32, i64, i32, i64, C.POINTER(Ckpt8C), vp, vp]
     lib.sapo_ckpt8_restore.restype = C.c_int
     lib.sapo_ckpt8_restore.argtypes = [C.POINTER(Ckpt8C), i64, i32, vp, i32, i64, vp]
+    lib.sapo_sample.restype = C.c_int
+    lib.sapo_sample.argtypes = [vp, i32, i32, i32, i64, vp, C.POINTER(SampleCfgC), vp, vp, vp, vp]
+    lib.sapo_fp8_store.restype = C.c_int
+    lib.sapo_fp8_store.argtypes = [vp, i32, i64, i32, i64, C.POINTER(Fp8C), vp, vp]
+    lib.sapo_fp8_matmul.restype = C.c_int
+    lib.sapo_fp8_matmul.argtypes = [C.POINTER(Fp8C), i64, C.POINTER(Fp8C), i32, i32, vp, i32, i64, vp, vp]
+    lib.sapo_adamw_step.restype = C.c_int
+    lib.sapo_adamw_step.argtypes = [C.POINTER(AdamWTensorC), i32, C.POINTER(AdamWCfgC), vp, vp]
     lib.sapo_launch_count.restype = C.c_int64
     lib.sapo_launch_count.argtypes = []
     lib.sapo_status_string.restype = C.c_char_p
@@ -221,6 +252,20 @@ def _stream() -> int:
     if _raw_stream is not None:
         return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """All tensors of a call are on the current device, whose stream its kernels go to."""
+    first = None
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if first is None:
+                first = at
+            elif at != first:
+                raise SapoError("the tensors of a call must be on one device")
+    if first is not None and first >= 0 and first != _raw_device():
+        raise SapoError(f"the tensors are on device {first}, which is not the current one")
 
 
 def _out_dtype_code(dhidden: torch.Tensor, dW_head: torch.Tensor) -> int:
@@ -836,3 +881,190 @@ def sapo_ckpt8_restore(ckpt: Ckpt8, x: torch.Tensor) -> None:
     T, H = x.shape
     px, tx, ldx = _rows(x, T, H, "x")
     _check(load().sapo_ckpt8_restore(ckpt.c(T, H), T, H, px, tx, ldx, _stream()), "sapo_ckpt8_restore")
+
+
+# ------------------------------------------------------------------------------------------
+# answering: matrices in 8-bit floating point, their product, and the draw of the next tokens
+@dataclass
+class Fp8:
+    """A matrix [R, C] in 8-bit floating point (e4m3): data [R, ld], one fp32 scale per row and 128 columns, or
+    (blocks=True) per block of 128 x 128."""
+    data: torch.Tensor
+    scale: torch.Tensor
+    C: int
+    blocks: bool = False
+
+    def c(self) -> Fp8C:
+        data, scale, n = self.data, self.scale, -(-self.C // Q8_GROUP)
+        if data.dtype != torch.float8_e4m3fn or data.dim() != 2 or data.shape[1] < self.C or self.C < 1 or not data.is_cuda:
+            raise SapoError("the 8-bit values must be float8_e4m3fn [R, C] on the GPU")
+        R = data.shape[0]
+        if (scale.dtype != torch.float32 or scale.dim() != 2 or scale.shape[0] != (-(-R // Q8_GROUP) if self.blocks else R)
+                or scale.shape[1] < n or not scale.is_cuda):
+            raise SapoError("the scales must be float32, one per row (or 128 rows) and 128 columns, on the GPU")
+        (ld, one), (ld_scale, one_scale) = data.stride(), scale.stride()
+        if (one != 1 and self.C > 1) or (one_scale != 1 and n > 1):
+            raise SapoError("columns of the 8-bit values and of their scales must be contiguous")
+        if (R > 1 and ld < self.C) or (scale.shape[0] > 1 and ld_scale < n):
+            raise SapoError("rows of the 8-bit matrix overlap")
+        return Fp8C(data.data_ptr(), scale.data_ptr(), max(ld, self.C), max(ld_scale, n), 1 if self.blocks else 0)
+
+
+def alloc_fp8(R: int, C: int, blocks: bool = False, device="cuda") -> Fp8:
+    ld = -(-C // 16) * 16                     # rows start on 16-byte boundaries, as the product needs them
+    return Fp8(torch.zeros(R, ld, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
+               torch.zeros(-(-R // Q8_GROUP) if blocks else R, -(-C // Q8_GROUP), dtype=torch.float32, device=device), C, blocks)
+
+
+def sapo_fp8_store(x: torch.Tensor, out: Fp8, status: torch.Tensor) -> None:
+    """x [R, C] into 8-bit floating point; `out` comes from alloc_fp8."""
+    _require_cuda()
+    R, C_ = x.shape
+    if out.C != C_ or out.data.shape[0] != R:
+        raise SapoError("the 8-bit matrix must have the shape of x")
+    _here(x, out.data, out.scale, status)
+    px, tx, ldx = _rows(x, R, C_, "x")
+    _check(load().sapo_fp8_store(px, tx, R, C_, ldx, out.c(), _at_least(status, torch.int32, 1, "status"), _stream()),
+           "sapo_fp8_store")
+
+
+def sapo_fp8_matmul(x: Fp8, w: Fp8, y: torch.Tensor, status: torch.Tensor) -> None:
+    """y [T, N] = x W^T for x [T, K] with scales per row and W [N, K] with scales per 128 x 128 block."""
+    _require_cuda()
+    T, N, K = x.data.shape[0], w.data.shape[0], x.C
+    if w.C != K or x.blocks or not w.blocks:
+        raise SapoError("x [T, K] has scales per row and w [N, K] scales per block, with the same K")
+    _here(y, x.data, x.scale, w.data, w.scale, status)
+    py, ty, ldy = _rows(y, T, N, "y")
+    if T > 1 and ldy < N:
+        raise SapoError("rows of y overlap")
+    _check(load().sapo_fp8_matmul(x.c(), T, w.c(), N, K, py, ty, ldy, _at_least(status, torch.int32, 1, "status"), _stream()),
+           "sapo_fp8_matmul")
+
+
+_sample_cfgs: Dict[tuple, SampleCfgC] = {}
+
+
+def _sample_cfg(B: int, temperature, top_k, top_p, min_p) -> SampleCfgC:
+    """The settings of a draw: numbers (those blocks are read only and few, so they are kept), or one value a row."""
+    rows = [isinstance(v, torch.Tensor) for v in (temperature, top_k, top_p, min_p)]
+    if not any(rows):
+        key = (temperature, top_k, top_p, min_p)
+        cfg = _sample_cfgs.get(key)
+        if cfg is None:
+            cfg = SampleCfgC(float(temperature), int(top_k), float(top_p), float(min_p), None, None, None, None)
+            if len(_sample_cfgs) < 64:
+                _sample_cfgs[key] = cfg
+    else:
+        cfg = SampleCfgC(1.0 if rows[0] else float(temperature), 0 if rows[1] else int(top_k), 1.0 if rows[2] else float(top_p),
+                         0.0 if rows[3] else float(min_p),
+                         _at_least(temperature, torch.float32, B, "temperature") if rows[0] else None,
+                         _at_least(top_k, torch.int32, B, "top_k") if rows[1] else None,
+                         _at_least(top_p, torch.float32, B, "top_p") if rows[2] else None,
+                         _at_least(min_p, torch.float32, B, "min_p") if rows[3] else None)
+    if not cfg.temperature >= 0.0 or not 0.0 <= cfg.min_p <= 1.0 or cfg.top_p != cfg.top_p:
+        raise SapoError("temperature must be at least 0, min_p in [0, 1], top_p a number")
+    return cfg
+
+
+def sapo_sample(logits: torch.Tensor, seeds: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, status: torch.Tensor,
+                temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) -> None:
+    """One token of every row of logits [B, V], from the rows' random numbers seeds (int64 [B]); ids int32 [B], logp
+    float32 [B] (at temperature 1, over all tokens).  Each setting is a number or a tensor with one value a row."""
+    _require_cuda()
+    B, V = logits.shape
+    _here(logits, seeds, ids, logp, status, *(v for v in (temperature, top_k, top_p, min_p) if isinstance(v, torch.Tensor)))
+    pz, tz, ldz = _rows(logits, B, V, "logits")
+    rc = load().sapo_sample(pz, tz, B, V, ldz, _at_least(seeds, torch.int64, B, "seeds"),
+                            _sample_cfg(B, temperature, top_k, top_p, min_p), _at_least(ids, torch.int32, B, "ids"),
+                            _at_least(logp, torch.float32, B, "logp"), _at_least(status, torch.int32, 1, "status"), _stream())
+    _check(rc, "sapo_sample")
+
+
+# ------------------------------------------------------------------------------------------
+# AdamW over many tensors
+@dataclass
+class AdamWState:
+    """Moments of one tensor: m, v float32 like the tensor; or both float8_e4m3fn [n], m_scale and v_scale float32
+    [ceil(n / 128)], where v and v_scale hold the root of v."""
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+def alloc_adamw_state(n: int, bits: int = 32, device="cuda") -> AdamWState:
+    """Moments of zero for n elements."""
+    if bits == 32:
+        return AdamWState(torch.zeros(n, device=device), torch.zeros(n, device=device))
+    if bits != 8:
+        raise SapoError("a state has 32 or 8 bits")
+    code = lambda: torch.zeros(n, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+    scale = lambda: torch.zeros(-(-n // Q8_GROUP), device=device)
+    return AdamWState(code(), code(), scale(), scale())
+
+
+class AdamWTensors:
+    """The tensors of an optimiser: float32 weights (any contiguous shape) with their states and, where wanted, bf16
+    copies that a step rewrites; lr_factor and weight_decay may differ from tensor to tensor (weight_decay None: the one
+    of the call).  Checked when it is made; afterwards the tensors may change their values, not their size or type."""
+
+    def __init__(self, params, states, copies=None, lr_factor=None, weight_decay=None):
+        self.params, self.states = list(params), list(states)
+        n = len(self.params)
+        each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * n
+        self.copies, self.lr_factor, self.weight_decay = each(copies), each(1.0 if lr_factor is None else lr_factor), each(weight_decay)
+        if not len(self.states) == len(self.copies) == len(self.lr_factor) == len(self.weight_decay) == n:
+            raise SapoError("one state, copy, lr_factor and weight_decay per tensor")
+        self.sizes, self.bits = [], []
+        for p, st, copy in zip(self.params, self.states, self.copies):
+            k = p.numel()
+            self.sizes.append(k)
+            self.bits.append(8 if st.m.dtype == torch.float8_e4m3fn else 32)
+            held = torch.float8_e4m3fn if self.bits[-1] == 8 else torch.float32
+            wanted = [(p, torch.float32, k, "a weight"), (st.m, held, k, "m"), (st.v, held, k, "v")]
+            if self.bits[-1] == 8:
+                wanted += [(st.m_scale, torch.float32, -(-k // Q8_GROUP), "m_scale"), (st.v_scale, torch.float32, -(-k // Q8_GROUP), "v_scale")]
+            if copy is not None:
+                wanted.append((copy, torch.bfloat16, k, "a copy"))
+            for t, dtype, size, what in wanted:
+                if t is None or t.dtype != dtype or t.numel() != size or not t.is_contiguous() or not t.is_cuda:
+                    raise SapoError(f"{what} must be contiguous {dtype} with {size} elements on the GPU")
+                if t.get_device() != self.params[0].get_device():
+                    raise SapoError("the tensors of an optimiser must be on one device")
+
+    def arrays(self, i: int):
+        """(tensors of number i, in the order of the C struct: weight, m, v, m_scale, v_scale)"""
+        st = self.states[i]
+        return self.params[i], st.m, st.v, st.m_scale, st.v_scale
+
+
+def sapo_adamw_step(tensors: AdamWTensors, grads, step, lr, status: torch.Tensor, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0, grad_scale: Optional[torch.Tensor] = None,
+                    out: Optional[AdamWTensors] = None) -> None:
+    """One AdamW step from the gradients (a list like the tensors, each bf16 or float32).  In place; or, with out, into
+    the weights, states and copies of `out`.  step (from 1) and lr are numbers, or device tensors (int32, float32) that
+    a captured call reads anew; grad_scale: float32 [1], a factor of all gradients; seed: of the 8-bit states' rounding."""
+    _require_cuda()
+    to = tensors if out is None else out
+    n = len(tensors.params)
+    if len(grads) != n or to.sizes != tensors.sizes or to.bits != tensors.bits:
+        raise SapoError("one gradient per tensor, and outputs of the same sizes and states")
+    _here(status, *grads, *tensors.params[:1], *to.params[:1], *(v for v in (step, lr, grad_scale) if isinstance(v, torch.Tensor)))
+    list_c = (AdamWTensorC * max(n, 1))()
+    for i, g in enumerate(grads):
+        code = _DTYPE_CODES.get(g.dtype)
+        if code is None or g.numel() != tensors.sizes[i] or not g.is_contiguous() or not g.is_cuda:
+            raise SapoError(f"gradient {i} must be contiguous bf16 or float32 with {tensors.sizes[i]} elements on the GPU")
+        w, m, v, ms, vs = tensors.arrays(i)
+        w2, m2, v2, ms2, vs2 = to.arrays(i)
+        decay = tensors.weight_decay[i]
+        list_c[i] = AdamWTensorC(w.data_ptr(), w2.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), m2.data_ptr(), v2.data_ptr(),
+                                 _p(ms), _p(vs), _p(ms2), _p(vs2), _p(to.copies[i]), tensors.sizes[i], tensors.lr_factor[i],
+                                 weight_decay if decay is None else decay, code, tensors.bits[i])
+    on_device = lambda t, dtype, what: _at_least(t, dtype, 1, what) if isinstance(t, torch.Tensor) else None
+    step_dev, lr_dev = on_device(step, torch.int32, "step"), on_device(lr, torch.float32, "lr")
+    cfg = AdamWCfgC(0.0 if lr_dev else lr, beta1, beta2, eps, int(seed) & (2**64 - 1), 1 if step_dev else int(step), step_dev, lr_dev,
+                    on_device(grad_scale, torch.float32, "grad_scale"))
+    rc = load().sapo_adamw_step(list_c, n, C.byref(cfg), _at_least(status, torch.int32, 1, "status"), _stream())
+    _check(rc, "sapo_adamw_step")

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsapo_b200.so")
 LIB_CHECKED = os.path.join(HERE, "libsapo_b200_checked.so")     # the same sources with -DSAPO_BOUNDS_CHECK
 LIB_STATS = os.path.join(HERE, "libsapo_b200_stats.so")         # ... with -DSAPO_WAIT_STATS (cycle counters)
-SOURCES = ["runtime.cu", "pack.cu", "advantages.cu", "select.cu", "adam.cu", "norm.cu", "preference.cu", "lmhead.cu"]
+SOURCES = ["runtime.cu", "pack.cu", "advantages.cu", "select.cu", "adam.cu", "norm.cu", "preference.cu", "sample.cu", "fp8.cu", "fp8_gemm.cu",
+           "adamw.cu", "lmhead.cu"]
 FLAGS = ["--threads", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "--shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=default"]
 

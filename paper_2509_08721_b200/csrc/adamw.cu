@@ -1,0 +1,299 @@
+// sapo_adamw_step: one AdamW step (Loshchilov & Hutter: Adam with the decay of the weights outside the moments) over a
+// list of tensors in as few launches as their number allows; moments in 32 bits, or in 8 with an fp32 scale per 128.
+//
+// The 8-bit state holds m and the ROOT of v, which halves v's span of exponents.  m is rounded to the nearest code: its
+// average moves by a tenth of a gradient a step, more than half a code.  v moves by a thousandth a step, far less than a
+// code: to the nearest it would stand still once about ten gradients are in it, so its root is rounded up or down by a
+// random number (16 bits of Philox, counted by element, tensor and step) that makes it right on average, and a root that
+// is not zero never becomes zero (its smallest code is 2^-6 / 448 of the group's largest), so that no weight is divided by
+// eps alone.
+//
+// HBM-bound: per weight 4 + 4 (master) + 2 or 4 (gradient) + 2 (bf16 copy) + 16 (32 bits) or 4.13 (8 bits) bytes.  A
+// warp takes 512 consecutive elements, four groups, all loads before the first use.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "float8.cuh"
+#include "philox.cuh"
+
+namespace sapo {
+
+constexpr int ADW_THREADS = 256;
+constexpr int ADW_GROUPS = 4;                                       // groups of 128 a warp takes at a time
+constexpr int ADW_WARP = ADW_GROUPS * F8_GROUP;
+constexpr int ADW_BLOCK = ADW_WARP * ADW_THREADS / 32;              // elements a block takes
+constexpr int ADW_TENSORS = 32;                                     // tensors a launch takes (its parameters hold the list)
+
+struct AdamWEntry {
+  const float* master; float* master_out;
+  const void* grad;
+  const void* m; const void* v; void* m_out; void* v_out;
+  const float* m_scale; const float* v_scale; float* m_scale_out; float* v_scale_out;
+  __nv_bfloat16* copy;
+  int64_t n;
+  float lr_factor, decay;
+  int32_t first_block;      // blocks of the launch before this tensor's
+  int32_t number;           // of the tensor in the caller's list: part of the random counter
+  int32_t vectors;          // every array starts on a boundary for vectors of four elements
+};
+
+struct AdamWArgs {
+  AdamWEntry t[ADW_TENSORS];
+  int32_t n_tensors;
+  double lr, beta1, beta2;
+  const float* lr_dev; const int32_t* step_dev; const float* grad_scale;
+  float b1, b2, one_minus_b1, one_minus_b2, eps, inv_bias1, inv_bias2_root;
+  uint32_t step, k0, k1;
+  int32_t* status;
+};
+
+// 1 - b^t in 64 bits
+__host__ __device__ inline double one_minus_power(double b, uint32_t t) {
+  double p = 1.0;
+  for (; t; t >>= 1, b *= b) if (t & 1u) p *= b;
+  return 1.0 - p;
+}
+
+struct Four { float v[4]; };
+template <class G> __device__ __forceinline__ Four load4(const G* p, int64_t at, int64_t n, bool vec);
+template <> __device__ __forceinline__ Four load4<float>(const float* p, int64_t at, int64_t n, bool vec) {
+  Four f;
+  if (vec) { const float4 x = *reinterpret_cast<const float4*>(p + at); f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w; }
+  else {
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = at + i < n ? p[at + i] : 0.f;
+  }
+  return f;
+}
+template <> __device__ __forceinline__ Four load4<__nv_bfloat16>(const __nv_bfloat16* p, int64_t at, int64_t n, bool vec) {
+  Four f;
+  if (vec) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p + at);
+    f.v[0] = __uint_as_float(x.x << 16); f.v[1] = __uint_as_float(x.x & 0xFFFF0000u);
+    f.v[2] = __uint_as_float(x.y << 16); f.v[3] = __uint_as_float(x.y & 0xFFFF0000u);
+  } else {
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = at + i < n ? __bfloat162float(p[at + i]) : 0.f;
+  }
+  return f;
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t at, int64_t n, bool vec) {
+  if (vec) return *reinterpret_cast<const uint32_t*>(p + at);
+  uint32_t q = 0;
+  #pragma unroll
+  for (int i = 0; i < 4; ++i) if (at + i < n) q |= (uint32_t)p[at + i] << (8 * i);
+  return q;
+}
+__device__ __forceinline__ void store4(float* p, int64_t at, int64_t n, bool vec, const float (&v)[4]) {
+  if (vec) *reinterpret_cast<float4*>(p + at) = make_float4(v[0], v[1], v[2], v[3]);
+  else {
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = v[i];
+  }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t at, int64_t n, bool vec, const float (&v)[4]) {
+  if (vec) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = __float2bfloat16_rn(v[i]);
+  }
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t at, int64_t n, bool vec, uint32_t q) {
+  if (vec) *reinterpret_cast<uint32_t*>(p + at) = q;
+  else {
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = (uint8_t)(q >> (8 * i));
+  }
+}
+
+// A root in units of its scale, rounded to one of the two codes around it: bits is uniform on [0, 65536).
+__device__ __forceinline__ float round_root(float t, uint32_t bits) {
+  const uint32_t up = (__float_as_uint(fmaxf(t, 0.015625f)) + 16u * bits + 8u) & 0xFFF00000u;
+  return t > 0.f ? fminf(__uint_as_float(up), F8_TOP) : 0.f;
+}
+
+template <bool BITS8, class G>
+__global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constant__ AdamWArgs a) {
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int lo = 0, hi = a.n_tensors - 1;            // the last tensor whose first block is not behind this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.t[mid].first_block <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+  }
+  const AdamWEntry& t = a.t[lo];
+  float inv_bias1 = a.inv_bias1, inv_bias2_root = a.inv_bias2_root;
+  uint32_t step = a.step;
+  if (a.step_dev != nullptr) {
+    __shared__ float bias[2];
+    step = (uint32_t)max(*a.step_dev, 1);
+    if (threadIdx.x == 0) { bias[0] = (float)(1.0 / one_minus_power(a.beta1, step)); bias[1] = (float)(1.0 / sqrt(one_minus_power(a.beta2, step))); }
+    __syncthreads();
+    inv_bias1 = bias[0]; inv_bias2_root = bias[1];
+  }
+  const double lr64 = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
+  const float lr = (float)lr64, shrink = (float)(1.0 - lr64 * (double)t.decay);
+  const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
+
+  const int64_t n = t.n, base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK + (int64_t)warp * ADW_WARP;
+  if (base >= n) return;
+  const bool vec = t.vectors && base + ADW_WARP <= n;      // whole vectors everywhere: no bounds to look at
+  Four g[ADW_GROUPS], w[ADW_GROUPS], m[ADW_GROUPS], v[ADW_GROUPS];
+  uint32_t qm[ADW_GROUPS], qv[ADW_GROUPS];
+  float sm[ADW_GROUPS], sv[ADW_GROUPS];
+  #pragma unroll
+  for (int u = 0; u < ADW_GROUPS; ++u) {
+    const int64_t at = base + u * F8_GROUP + 4 * lane;
+    g[u] = load4(static_cast<const G*>(t.grad), at, n, vec);
+    w[u] = load4(t.master, at, n, vec);
+    if (BITS8) {
+      qm[u] = load_codes(static_cast<const uint8_t*>(t.m), at, n, vec);
+      qv[u] = load_codes(static_cast<const uint8_t*>(t.v), at, n, vec);
+      const int64_t group = (base >> 7) + u;
+      const bool there = group * F8_GROUP < n;
+      sm[u] = there ? t.m_scale[group] : 0.f;
+      sv[u] = there ? t.v_scale[group] : 0.f;
+    } else {
+      m[u] = load4(static_cast<const float*>(t.m), at, n, vec);
+      v[u] = load4(static_cast<const float*>(t.v), at, n, vec);
+    }
+  }
+  // random words: the eight elements of a counter belong to two lanes; each of them makes the counters of every other group
+  uint32_t rnd[ADW_GROUPS][2];
+  if (BITS8) {
+    #pragma unroll
+    for (int u = 0; u < ADW_GROUPS; u += 2) {
+      const uint64_t c = (uint64_t)(base + (u + (lane & 1)) * F8_GROUP + 4 * (lane & ~1)) >> 3;
+      const uint4 r = philox4x32_10((uint32_t)c, (uint32_t)(c >> 32), (uint32_t)t.number, step, a.k0, a.k1);
+      const bool odd = lane & 1;
+      const uint32_t p = __shfl_xor_sync(0xFFFFFFFFu, odd ? r.x : r.z, 1), q = __shfl_xor_sync(0xFFFFFFFFu, odd ? r.y : r.w, 1);
+      rnd[u][0] = odd ? p : r.x; rnd[u][1] = odd ? q : r.y;
+      rnd[u + 1][0] = odd ? r.z : p; rnd[u + 1][1] = odd ? r.w : q;
+    }
+  }
+  bool bad = false;
+  #pragma unroll
+  for (int u = 0; u < ADW_GROUPS; ++u) {
+    const int64_t at = base + u * F8_GROUP + 4 * lane;
+    float root[4];
+    if (BITS8) { f8_unpack4(qm[u], m[u].v); f8_unpack4(qv[u], root); }
+    float most_m = 0.f, most_r = 0.f;
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (BITS8) { m[u].v[i] = __fmul_rn(m[u].v[i], sm[u]); const float r = __fmul_rn(root[i], sv[u]); v[u].v[i] = __fmul_rn(r, r); }
+      const float x = __fmul_rn(g[u].v[i], gs);
+      const bool fine = fabsf(x) < __int_as_float(0x7f800000);
+      bad |= !fine;
+      // the products and sums are rounded one by one: the state is the same to the bit however a compiler would fuse them
+      const float m1 = __fadd_rn(__fmul_rn(a.b1, m[u].v[i]), __fmul_rn(a.one_minus_b1, x));
+      const float v1 = fminf(__fadd_rn(__fmul_rn(a.b2, v[u].v[i]), __fmul_rn(__fmul_rn(a.one_minus_b2, x), x)), 3.402823466e38f);
+      const float r1 = sqrtf(fine ? v1 : v[u].v[i]);
+      if (fine) {
+        m[u].v[i] = m1; v[u].v[i] = v1;
+        w[u].v[i] = w[u].v[i] * shrink - lr * __fdividef(m1 * inv_bias1, r1 * inv_bias2_root + a.eps);
+      }
+      root[i] = r1;
+      most_m = fmaxf(most_m, fabsf(m[u].v[i])); most_r = fmaxf(most_r, r1);
+    }
+    store4(t.master_out, at, n, vec, w[u].v);
+    if (t.copy != nullptr) store4(t.copy, at, n, vec, w[u].v);
+    if (BITS8) {
+      most_m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most_m)));
+      most_r = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most_r)));
+      float scale_m, inv_m, scale_r, inv_r;
+      f8_group(most_m, scale_m, inv_m);
+      f8_group(most_r, scale_r, inv_r);
+      const float* x = m[u].v;
+      store_codes(static_cast<uint8_t*>(t.m_out), at, n, vec,
+                  f8_pack4(__fmul_rn(x[0], inv_m), __fmul_rn(x[1], inv_m), __fmul_rn(x[2], inv_m), __fmul_rn(x[3], inv_m)));
+      store_codes(static_cast<uint8_t*>(t.v_out), at, n, vec,
+                  f8_pack4(round_root(__fmul_rn(root[0], inv_r), rnd[u][0] & 0xFFFFu), round_root(__fmul_rn(root[1], inv_r), rnd[u][0] >> 16),
+                           round_root(__fmul_rn(root[2], inv_r), rnd[u][1] & 0xFFFFu), round_root(__fmul_rn(root[3], inv_r), rnd[u][1] >> 16)));
+      const int64_t group = (base >> 7) + u;
+      if (lane == 0 && group * F8_GROUP < n) { t.m_scale_out[group] = scale_m; t.v_scale_out[group] = scale_r; }
+    } else {
+      store4(static_cast<float*>(t.m_out), at, n, vec, m[u].v);
+      store4(static_cast<float*>(t.v_out), at, n, vec, v[u].v);
+    }
+  }
+  if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+}
+
+static bool multiple_of(const void* p, size_t k) { return reinterpret_cast<uintptr_t>(p) % k == 0; }
+
+// one launch per 32 tensors of the list that are of this kind
+template <bool BITS8, class G>
+static int launch_adamw(const sapo_adamw_tensor* list, int32_t n, AdamWArgs& a, cudaStream_t st) {
+  constexpr int g_dtype = sizeof(G) == 2 ? SAPO_DTYPE_BF16 : SAPO_DTYPE_F32;
+  int64_t blocks = 0;
+  a.n_tensors = 0;
+  const auto launch = [&]() -> int {
+    if (a.n_tensors == 0) return SAPO_OK;
+    KernelScope scope(SAPO_K_ADAMW, st);
+    const int rc = launch_overlapped(adamw_kernel<BITS8, G>, dim3((unsigned)blocks), ADW_THREADS, 0, 0, st, a);
+    blocks = 0; a.n_tensors = 0;
+    return rc;
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const sapo_adamw_tensor& t = list[i];
+    if (t.n == 0 || (t.state_bits == 8) != BITS8 || t.grad_dtype != g_dtype) continue;
+    const int64_t need = ceil_div<int64_t>(t.n, ADW_BLOCK);
+    if (a.n_tensors == ADW_TENSORS || blocks + need > 0x7FFFFFFF) {
+      const int rc = launch();
+      if (rc != SAPO_OK) return rc;
+    }
+    const size_t state = BITS8 ? 4 : 16;
+    const bool vectors = aligned16(t.master) && aligned16(t.master_out) && multiple_of(t.grad, 4 * sizeof(G)) && multiple_of(t.m, state) &&
+                         multiple_of(t.v, state) && multiple_of(t.m_out, state) && multiple_of(t.v_out, state) && multiple_of(t.copy_bf16, 8);
+    a.t[a.n_tensors++] = AdamWEntry{t.master, t.master_out, t.grad, t.m, t.v, t.m_out, t.v_out, t.m_scale, t.v_scale, t.m_scale_out,
+                                    t.v_scale_out, static_cast<__nv_bfloat16*>(t.copy_bf16), t.n, t.lr_factor, t.weight_decay,
+                                    (int32_t)blocks, i, vectors ? 1 : 0};
+    blocks += need;
+  }
+  return launch();
+}
+
+}  // namespace sapo
+
+extern "C" int sapo_adamw_step(const sapo_adamw_tensor* h_tensors, int32_t n_tensors, const sapo_adamw_cfg* h_cfg, int32_t* status,
+                               void* stream) {
+  using namespace sapo;
+  if (n_tensors < 0 || (n_tensors > 0 && !h_tensors) || !h_cfg || !status) return SAPO_ERR_INVALID_ARG;
+  const sapo_adamw_cfg& c = *h_cfg;
+  if (!(c.beta1 >= 0. && c.beta1 < 1.) || !(c.beta2 >= 0. && c.beta2 < 1.) || !(c.eps >= 0. && c.eps < 1e30) || !(c.lr - c.lr == 0.)) return SAPO_ERR_INVALID_ARG;
+  if (!c.step_dev && c.step < 1) return SAPO_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const sapo_adamw_tensor& t = h_tensors[i];
+    if (t.n < 0 || (t.state_bits != 8 && t.state_bits != 32) || (t.grad_dtype != SAPO_DTYPE_BF16 && t.grad_dtype != SAPO_DTYPE_F32))
+      return SAPO_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (!t.master || !t.master_out || !t.grad || !t.m || !t.v || !t.m_out || !t.v_out) return SAPO_ERR_INVALID_ARG;
+    if (t.state_bits == 8 && (!t.m_scale || !t.v_scale || !t.m_scale_out || !t.v_scale_out)) return SAPO_ERR_INVALID_ARG;
+    const size_t g = t.grad_dtype == SAPO_DTYPE_BF16 ? 2 : 4, s = t.state_bits == 8 ? 1 : 4;
+    if (!multiple_of(t.master, 4) || !multiple_of(t.master_out, 4) || !multiple_of(t.grad, g) || !multiple_of(t.m, s) || !multiple_of(t.v, s) ||
+        !multiple_of(t.m_out, s) || !multiple_of(t.v_out, s) || !multiple_of(t.copy_bf16, 2))
+      return SAPO_ERR_INVALID_ARG;
+    if (!(t.weight_decay - t.weight_decay == 0.f) || !(t.lr_factor - t.lr_factor == 0.f)) return SAPO_ERR_INVALID_ARG;
+    if (ceil_div<int64_t>(t.n, ADW_BLOCK) > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  }
+  if (current_device() < 0) return SAPO_ERR_CUDA;
+  AdamWArgs a;
+  a.lr = c.lr; a.beta1 = c.beta1; a.beta2 = c.beta2;
+  a.lr_dev = c.lr_dev; a.step_dev = c.step_dev; a.grad_scale = c.grad_scale;
+  a.b1 = (float)c.beta1; a.b2 = (float)c.beta2;
+  a.one_minus_b1 = (float)(1. - c.beta1); a.one_minus_b2 = (float)(1. - c.beta2);
+  a.eps = (float)c.eps;
+  a.step = (uint32_t)(c.step < 1 ? 1 : c.step);
+  a.inv_bias1 = (float)(1. / one_minus_power(c.beta1, a.step));
+  a.inv_bias2_root = (float)(1. / sqrt(one_minus_power(c.beta2, a.step)));
+  a.k0 = (uint32_t)c.seed; a.k1 = (uint32_t)(c.seed >> 32);
+  a.status = status;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int rc = launch_adamw<true, __nv_bfloat16>(h_tensors, n_tensors, a, st);
+  if (rc == SAPO_OK) rc = launch_adamw<true, float>(h_tensors, n_tensors, a, st);
+  if (rc == SAPO_OK) rc = launch_adamw<false, __nv_bfloat16>(h_tensors, n_tensors, a, st);
+  if (rc == SAPO_OK) rc = launch_adamw<false, float>(h_tensors, n_tensors, a, st);
+  return rc;
+}

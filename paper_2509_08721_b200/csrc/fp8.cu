@@ -1,0 +1,177 @@
+// sapo_fp8_store: a matrix in 8-bit floating point (e4m3), one fp32 scale per row and 128 columns (activations) or per
+// 128 x 128 block (weights).  With a = the largest magnitude of a group, scale = a (1/448) and q = x (448 (1/a)) rounded to
+// the nearest code: the group's largest value uses the type's largest.
+// HBM-bound (3 bytes an element from bf16): rows are taken in pieces of 256 columns by warps, half a warp per group, four
+// pieces in flight; blocks of 128 x 128 stay in a block's registers between the search for a and the conversion.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+#include "float8.cuh"
+
+namespace sapo {
+
+constexpr int F8S_THREADS = 256;
+constexpr int F8S_PIECES = 4;       // pieces of 256 columns a warp has in flight
+
+struct Fp8StoreArgs {
+  const void* x; int64_t R; int32_t C; int64_t ld_x;
+  uint8_t* q; float* scale; int64_t ld, ld_scale;
+  int32_t vec_x, vec_q;             // rows start where eight values can be read, eight codes written, at once
+  int32_t* status;
+};
+
+struct Eight { float v[8]; };
+__device__ __forceinline__ Eight load8(const float* p, int left, bool vec) {      // left: columns up to the row's end
+  Eight e;
+  if (vec && left >= 8) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    e.v[0] = a.x; e.v[1] = a.y; e.v[2] = a.z; e.v[3] = a.w; e.v[4] = b.x; e.v[5] = b.y; e.v[6] = b.z; e.v[7] = b.w;
+  } else {
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i] = i < left ? p[i] : 0.f;
+  }
+  return e;
+}
+__device__ __forceinline__ Eight load8(const __nv_bfloat16* p, int left, bool vec) {
+  Eight e;
+  if (vec && left >= 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+    #pragma unroll
+    for (int i = 0; i < 4; ++i) { e.v[2 * i] = __uint_as_float(w[i] << 16); e.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+  } else {
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i] = i < left ? __bfloat162float(p[i]) : 0.f;
+  }
+  return e;
+}
+// largest magnitude, NaN if there is one (as an unsigned integer NaN is above infinity)
+__device__ __forceinline__ uint32_t largest(const Eight& e) {
+  uint32_t m = 0;
+  #pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(e.v[i]) & 0x7FFFFFFFu);
+  return m;
+}
+__device__ __forceinline__ void store8(uint8_t* p, int left, bool vec, const Eight& e, float inv) {
+  float x[8];
+  #pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = inv > 0.f ? __fmul_rn(e.v[i], inv) : 0.f;
+  const uint2 q = make_uint2(f8_pack4(x[0], x[1], x[2], x[3]), f8_pack4(x[4], x[5], x[6], x[7]));
+  if (vec && left >= 8) *reinterpret_cast<uint2*>(p) = q;
+  else {
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < left) p[i] = (uint8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArgs a) {
+  wait_for_previous();
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = ((int64_t)blockIdx.x * F8S_THREADS + threadIdx.x) >> 5, warps = (int64_t)gridDim.x * F8S_THREADS / 32;
+  const uint32_t per_row = (uint32_t)(a.C + 255) / 256;
+  const int64_t pieces = a.R * per_row;
+  bool bad = false;
+  for (int64_t first = warp * F8S_PIECES; first < pieces; first += warps * F8S_PIECES) {
+    Eight e[F8S_PIECES];
+    int64_t row[F8S_PIECES]; int col[F8S_PIECES];
+    #pragma unroll
+    for (int u = 0; u < F8S_PIECES; ++u) {
+      row[u] = (first + u) / per_row;
+      col[u] = (int)((first + u) - row[u] * per_row) * 256 + lane * 8;
+      const int left = first + u < pieces ? a.C - col[u] : 0;
+      if (left > 0) e[u] = load8(static_cast<const T*>(a.x) + row[u] * a.ld_x + col[u], left, a.vec_x);
+      else
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) e[u].v[i] = 0.f;
+    }
+    #pragma unroll
+    for (int u = 0; u < F8S_PIECES; ++u) {
+      uint32_t m = largest(e[u]);
+      #pragma unroll
+      for (int d = 8; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));      // the group's 16 lanes
+      float scale, inv;
+      f8_group(__uint_as_float(m), scale, inv);
+      const int left = first + u < pieces ? a.C - col[u] : 0;
+      if (left <= 0) continue;
+      bad |= m >= 0x7F800000u;
+      store8(a.q + row[u] * a.ld + col[u], left, a.vec_q, e[u], inv);
+      if ((lane & 15) == 0) a.scale[row[u] * a.ld_scale + (col[u] >> 7)] = scale;
+    }
+  }
+  if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+}
+
+// One block of 128 x 128: 16 threads a row, 16 rows at a time.
+template <class T>
+__global__ void __launch_bounds__(F8S_THREADS) fp8_blocks_kernel(const Fp8StoreArgs a) {
+  wait_for_previous();
+  __shared__ uint32_t warp_max[F8S_THREADS / 32];
+  const uint32_t across = (uint32_t)(a.C + 127) / 128;
+  const int64_t br = blockIdx.x / across;
+  const int bc = (int)(blockIdx.x - br * across);
+  const int col = bc * 128 + (threadIdx.x & 15) * 8, left = a.C - col;
+  const int64_t row0 = br * 128 + (threadIdx.x >> 4);
+  Eight e[8];
+  uint32_t m = 0;
+  #pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    if (left > 0 && row0 + 16 * u < a.R) e[u] = load8(static_cast<const T*>(a.x) + (row0 + 16 * u) * a.ld_x + col, left, a.vec_x);
+    else
+      #pragma unroll
+      for (int i = 0; i < 8; ++i) e[u].v[i] = 0.f;
+  }
+  #pragma unroll
+  for (int u = 0; u < 8; ++u) m = max(m, largest(e[u]));
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+  #pragma unroll
+  for (int w = 0; w < F8S_THREADS / 32; ++w) m = max(m, warp_max[w]);
+  float scale, inv;
+  f8_group(__uint_as_float(m), scale, inv);
+  #pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (left > 0 && row0 + 16 * u < a.R) store8(a.q + (row0 + 16 * u) * a.ld + col, left, a.vec_q, e[u], inv);
+  if (threadIdx.x == 0) {
+    a.scale[br * a.ld_scale + bc] = scale;
+    if (m >= 0x7F800000u) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+  }
+}
+
+template <class T>
+static int launch_fp8_store(const Fp8StoreArgs& a, bool blocks, cudaStream_t st) {
+  const int sms = sm_count();
+  if (sms <= 0) return SAPO_ERR_CUDA;
+  KernelScope scope(SAPO_K_FP8_STORE, st);
+  if (blocks) {
+    const int64_t n = ceil_div<int64_t>(a.R, 128) * ceil_div<int64_t>(a.C, 128);
+    if (n > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
+    return launch_overlapped(fp8_blocks_kernel<T>, dim3((unsigned)n), F8S_THREADS, 0, 0, st, a);
+  }
+  static int resident[MAX_DEVICES] = {0};
+  const int dev = current_device();
+  if (resident[dev] == 0) resident[dev] = resident_blocks_per_sm(fp8_rows_kernel<T>, F8S_THREADS);
+  const int64_t turns = ceil_div<int64_t>(a.R * ceil_div<int64_t>(a.C, 256), F8S_PIECES);
+  const int64_t most = (int64_t)sms * resident[dev], need = ceil_div<int64_t>(turns, F8S_THREADS / 32);
+  return launch_overlapped(fp8_rows_kernel<T>, dim3((unsigned)(need < most ? need : most)), F8S_THREADS, 0, 0, st, a);
+}
+
+}  // namespace sapo
+
+extern "C" int sapo_fp8_store(const void* x, int32_t x_dtype, int64_t R, int32_t C, int64_t ld_x, const sapo_fp8* h_out,
+                              int32_t* status, void* stream) {
+  using namespace sapo;
+  if (!h_out || !status || R < 0 || C < 1 || ld_x < C || (x_dtype != SAPO_DTYPE_BF16 && x_dtype != SAPO_DTYPE_F32)) return SAPO_ERR_INVALID_ARG;
+  const sapo_fp8& o = *h_out;
+  if (o.ld < C || o.ld_scale < ceil_div<int64_t>(C, 128) || (o.blocks != 0 && o.blocks != 1)) return SAPO_ERR_INVALID_ARG;
+  if (R == 0) return SAPO_OK;
+  if (!x || !o.data || !o.scale) return SAPO_ERR_INVALID_ARG;
+  const size_t size = x_dtype == SAPO_DTYPE_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(o.scale) % 4) return SAPO_ERR_INVALID_ARG;
+  const Fp8StoreArgs a{x, R, C, ld_x, static_cast<uint8_t*>(o.data), o.scale, o.ld, o.ld_scale,
+                       aligned16(x) && (R == 1 || (ld_x * (int64_t)size) % 16 == 0),
+                       (reinterpret_cast<uintptr_t>(o.data) & 7u) == 0 && (R == 1 || o.ld % 8 == 0), status};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return x_dtype == SAPO_DTYPE_BF16 ? launch_fp8_store<__nv_bfloat16>(a, o.blocks != 0, st) : launch_fp8_store<float>(a, o.blocks != 0, st);
+}

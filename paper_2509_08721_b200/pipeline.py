@@ -1,6 +1,7 @@
 """One policy-scoring step = pack -> group advantages -> loss forward -> loss backward,
 each a call into the CUDA library (PolicyScorer); one preference-training step = pack -> norm ->
-preference loss through the head -> norm's backward (PreferenceScorer).  This module only owns buffers
+preference loss through the head -> norm's backward (PreferenceScorer); the update of the head and the norm
+(HeadOptimizer) and the next tokens drawn from them (AnswerHead).  This module only owns buffers
 and sequences the calls (it is the API a training loop would use); it performs no arithmetic of its own.
 """
 from __future__ import annotations
@@ -276,6 +277,77 @@ class PreferenceScorer:
         dx = self.dhidden[:T]                      # the norm's gradient takes the place of its output's
         B.sapo_norm_bwd(dx, held, self.gamma, mean, rstd, self.norm, dx, self.dgamma, self.dbeta, self.workspace)
         return PreferenceResult(out["loss"], out, dx, self.dgamma, self.dbeta, self.dW, p)
+
+    def check_status(self) -> None:
+        word = int(self.status.item())
+        if word:
+            raise B.SapoError("device status: " + ",".join(B.decode_status(word)))
+
+
+class HeadOptimizer:
+    """AdamW on a policy's last layers: the bf16 head (with an fp32 master of its own) and the norm's fp32 weights, in
+    one call a step.  W_head, gamma and norm_beta are rewritten in place, so the scorers and the AnswerHead that hold them see the
+    new ones (AnswerHead.refresh lays the head out again).  bits: of the moments, 8 or 32.  The norm's weights do not
+    decay."""
+
+    def __init__(self, W_head: torch.Tensor, gamma: Optional[torch.Tensor] = None, norm_beta: Optional[torch.Tensor] = None,
+                 lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                 bits: int = 8, seed: int = 0):
+        self.lr = lr
+        self.options = dict(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay, seed=seed)
+        self.master = W_head.float()
+        params = [self.master] + [w for w in (gamma, norm_beta) if w is not None]
+        device = W_head.device
+        self.tensors = B.AdamWTensors(params, [B.alloc_adamw_state(p.numel(), bits, device) for p in params],
+                                      [W_head] + [None] * (len(params) - 1), weight_decay=[None] + [0.0] * (len(params) - 1))
+        self.steps = 0
+        self.status = B.new_status(device)
+
+    def step(self, dW: torch.Tensor, dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+             lr: Optional[float] = None, grad_scale: Optional[torch.Tensor] = None) -> None:
+        """One step from the gradients of a scorer's step."""
+        self.steps += 1
+        B.sapo_adamw_step(self.tensors, [dW] + [g for g in (dgamma, dbeta) if g is not None], self.steps,
+                          self.lr if lr is None else lr, self.status, grad_scale=grad_scale, **self.options)
+
+    def check_status(self) -> None:
+        word = int(self.status.item())
+        if word:
+            raise B.SapoError("device status: " + ",".join(B.decode_status(word)))
+
+
+class AnswerHead:
+    """The next tokens from the rows in front of a policy's last norm: norm -> rows in 8 bits -> product with the head in
+    8 bits -> draw.  Their log-probs (temperature 1, all tokens) are the old_logp of the rollouts."""
+
+    def __init__(self, W_head: torch.Tensor, gamma: Optional[torch.Tensor], norm_beta: Optional[torch.Tensor], max_rows: int,
+                 norm: str = "rms", eps: float = 1e-6, logits_dtype: torch.dtype = torch.float32):
+        self.W, self.gamma, self.norm_beta = W_head, gamma, norm_beta
+        self.V, self.H = int(W_head.shape[0]), int(W_head.shape[1])
+        self.norm, self.eps = norm, float(eps)
+        device, n = W_head.device, int(max_rows)
+        self.w8, self.x8 = B.alloc_fp8(self.V, self.H, True, device), B.alloc_fp8(n, self.H, False, device)
+        self.hidden = torch.empty(n, self.H, dtype=torch.bfloat16, device=device)
+        self.logits = torch.empty(n, -(-self.V // 8) * 8, dtype=logits_dtype, device=device)      # rows on 16-byte boundaries
+        self.ids = torch.empty(n, dtype=torch.int32, device=device)
+        self.logp = torch.empty(n, dtype=torch.float32, device=device)
+        self.status = B.new_status(device)
+        self.refresh()
+
+    def refresh(self) -> None:
+        """The head in 8 bits again, after its weights have changed."""
+        B.sapo_fp8_store(self.W, self.w8, self.status)
+
+    def next_tokens(self, x: torch.Tensor, seeds: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        """(ids, logp) of the rows of x [n, H]; seeds: one random number a row (int64)."""
+        n = int(x.shape[0])
+        hidden, x8 = self.hidden[:n], B.Fp8(self.x8.data[:n], self.x8.scale[:n], self.H)
+        logits, ids, logp = self.logits[:n, :self.V], self.ids[:n], self.logp[:n]
+        B.sapo_norm_fwd(x, self.gamma, self.norm_beta, self.eps, self.norm, hidden, None, None)
+        B.sapo_fp8_store(hidden, x8, self.status)
+        B.sapo_fp8_matmul(x8, self.w8, logits, self.status)
+        B.sapo_sample(logits, seeds, ids, logp, self.status, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        return ids, logp
 
     def check_status(self) -> None:
         word = int(self.status.item())
