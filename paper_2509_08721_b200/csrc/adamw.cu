@@ -14,6 +14,7 @@
 
 #include "common.cuh"
 #include "float8.cuh"
+#include "paired.cuh"
 #include "philox.cuh"
 
 namespace sapo {
@@ -108,14 +109,19 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t at, int64_t n, b
   }
 }
 
-// A root in units of its scale, rounded to one of the two codes around it: bits is uniform on [0, 65536).
-__device__ __forceinline__ float round_root(float t, uint32_t bits) {
-  const uint32_t up = (__float_as_uint(fmaxf(t, 0.015625f)) + 16u * bits + 8u) & 0xFFF00000u;
+// a b rounded by itself: the assembler fuses a paired product and a sum that follows into one rounding, so the products
+// whose sum makes the state are not paired
+__device__ __forceinline__ float2 product(float2 a, float2 b) { return make_float2(__fmul_rn(a.x, b.x), __fmul_rn(a.y, b.y)); }
+
+// A root in units of its scale, rounded to one of the two codes around it: bits16 is 16 times a number uniform on [0, 65536).
+__device__ __forceinline__ float round_root(float t, uint32_t bits16) {
+  const uint32_t up = (__float_as_uint(fmaxf(t, 0.015625f)) + (bits16 | 8u)) & 0xFFF00000u;
   return t > 0.f ? fminf(__uint_as_float(up), F8_TOP) : 0.f;
 }
 
 template <bool BITS8, class G>
 __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constant__ AdamWArgs a) {
+  constexpr uint32_t ALL = 0xFFFFFFFFu;
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int lo = 0, hi = a.n_tensors - 1;            // the last tensor whose first block is not behind this one
@@ -133,10 +139,6 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
     __syncthreads();
     inv_bias1 = bias[0]; inv_bias2_root = bias[1];
   }
-  const double lr64 = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
-  const float lr = (float)lr64, shrink = (float)(1.0 - lr64 * (double)t.decay);
-  const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
-
   const int64_t n = t.n, base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK + (int64_t)warp * ADW_WARP;
   if (base >= n) return;
   const bool vec = t.vectors && base + ADW_WARP <= n;      // whole vectors everywhere: no bounds to look at
@@ -160,6 +162,9 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
       v[u] = load4(static_cast<const float*>(t.v), at, n, vec);
     }
   }
+  const double lr64 = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
+  const float minus_lr = -(float)lr64, shrink = (float)(1.0 - lr64 * (double)t.decay);
+  const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
   // random words: the eight elements of a counter belong to two lanes; each of them makes the counters of every other group
   uint32_t rnd[ADW_GROUPS][2];
   if (BITS8) {
@@ -168,54 +173,88 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
       const uint64_t c = (uint64_t)(base + (u + (lane & 1)) * F8_GROUP + 4 * (lane & ~1)) >> 3;
       const uint4 r = philox4x32_10((uint32_t)c, (uint32_t)(c >> 32), (uint32_t)t.number, step, a.k0, a.k1);
       const bool odd = lane & 1;
-      const uint32_t p = __shfl_xor_sync(0xFFFFFFFFu, odd ? r.x : r.z, 1), q = __shfl_xor_sync(0xFFFFFFFFu, odd ? r.y : r.w, 1);
+      const uint32_t p = __shfl_xor_sync(ALL, odd ? r.x : r.z, 1), q = __shfl_xor_sync(ALL, odd ? r.y : r.w, 1);
       rnd[u][0] = odd ? p : r.x; rnd[u][1] = odd ? q : r.y;
       rnd[u + 1][0] = odd ? r.z : p; rnd[u + 1][1] = odd ? r.w : q;
     }
   }
+  // moments and weights; afterwards m and v hold the new m and (8 bits) the new root
+  uint32_t most_m[ADW_GROUPS], most_r[ADW_GROUPS];      // of the groups
   bool bad = false;
   #pragma unroll
   for (int u = 0; u < ADW_GROUPS; ++u) {
     const int64_t at = base + u * F8_GROUP + 4 * lane;
+    float big = 0.f, mm = 0.f, mr = 0.f;
+    float2 x[2], m0[2], v0[2];
     float root[4];
     if (BITS8) { f8_unpack4(qm[u], m[u].v); f8_unpack4(qv[u], root); }
-    float most_m = 0.f, most_r = 0.f;
     #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (BITS8) { m[u].v[i] = __fmul_rn(m[u].v[i], sm[u]); const float r = __fmul_rn(root[i], sv[u]); v[u].v[i] = __fmul_rn(r, r); }
-      const float x = __fmul_rn(g[u].v[i], gs);
-      const bool fine = fabsf(x) < __int_as_float(0x7f800000);
-      bad |= !fine;
-      // the products and sums are rounded one by one: the state is the same to the bit however a compiler would fuse them
-      const float m1 = __fadd_rn(__fmul_rn(a.b1, m[u].v[i]), __fmul_rn(a.one_minus_b1, x));
-      const float v1 = fminf(__fadd_rn(__fmul_rn(a.b2, v[u].v[i]), __fmul_rn(__fmul_rn(a.one_minus_b2, x), x)), 3.402823466e38f);
-      const float r1 = sqrtf(fine ? v1 : v[u].v[i]);
-      if (fine) {
-        m[u].v[i] = m1; v[u].v[i] = v1;
-        w[u].v[i] = w[u].v[i] * shrink - lr * __fdividef(m1 * inv_bias1, r1 * inv_bias2_root + a.eps);
+    for (int h = 0; h < 2; ++h) {
+      x[h] = mul2(make_float2(g[u].v[2 * h], g[u].v[2 * h + 1]), both(gs));
+      m0[h] = make_float2(m[u].v[2 * h], m[u].v[2 * h + 1]);
+      v0[h] = make_float2(v[u].v[2 * h], v[u].v[2 * h + 1]);
+      if (BITS8) {
+        m0[h] = mul2(m0[h], both(sm[u]));
+        const float2 r = mul2(make_float2(root[2 * h], root[2 * h + 1]), both(sv[u]));
+        v0[h] = mul2(r, r);
       }
-      root[i] = r1;
-      most_m = fmaxf(most_m, fabsf(m[u].v[i])); most_r = fmaxf(most_r, r1);
+      big = max_nan(big, max_nan(fabsf(x[h].x), fabsf(x[h].y)));
+    }
+    // Squares that may leave the fp32 range, and what is not finite, are looked at one by one.  Products and sums are
+    // rounded one by one: the state is the same to the bit however a compiler would fuse them.
+    const bool plain = __all_sync(ALL, big < 1e18f);
+    #pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float2 m1 = add2(product(both(a.b1), m0[h]), product(both(a.one_minus_b1), x[h]));
+      float2 v1 = add2(product(both(a.b2), v0[h]), product(mul2(both(a.one_minus_b2), x[h]), x[h]));
+      const float2 was = make_float2(w[u].v[2 * h], w[u].v[2 * h + 1]);
+      bool fine[2] = {true, true};
+      if (!plain) {
+        fine[0] = fabsf(x[h].x) < __int_as_float(0x7f800000); fine[1] = fabsf(x[h].y) < __int_as_float(0x7f800000);
+        bad = bad || !fine[0] || !fine[1];
+        m1 = make_float2(fine[0] ? m1.x : m0[h].x, fine[1] ? m1.y : m0[h].y);
+        v1 = make_float2(fine[0] ? fminf(v1.x, 3.402823466e38f) : v0[h].x, fine[1] ? fminf(v1.y, 3.402823466e38f) : v0[h].y);
+      }
+      const float2 r1 = make_float2(sqrtf(v1.x), sqrtf(v1.y));
+      const float2 above = mul2(m1, both(inv_bias1)), below = fma2(r1, both(inv_bias2_root), both(a.eps));
+      const float2 now = fma2(both(minus_lr), make_float2(__fdividef(above.x, below.x), __fdividef(above.y, below.y)), mul2(was, both(shrink)));
+      w[u].v[2 * h] = fine[0] ? now.x : was.x; w[u].v[2 * h + 1] = fine[1] ? now.y : was.y;
+      m[u].v[2 * h] = m1.x; m[u].v[2 * h + 1] = m1.y;
+      v[u].v[2 * h] = BITS8 ? r1.x : v1.x; v[u].v[2 * h + 1] = BITS8 ? r1.y : v1.y;
+      if (BITS8) { mm = fmaxf(mm, fmaxf(fabsf(m1.x), fabsf(m1.y))); mr = fmaxf(mr, fmaxf(r1.x, r1.y)); }
     }
     store4(t.master_out, at, n, vec, w[u].v);
     if (t.copy != nullptr) store4(t.copy, at, n, vec, w[u].v);
     if (BITS8) {
-      most_m = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most_m)));
-      most_r = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most_r)));
-      float scale_m, inv_m, scale_r, inv_r;
-      f8_group(most_m, scale_m, inv_m);
-      f8_group(most_r, scale_r, inv_r);
-      const float* x = m[u].v;
-      store_codes(static_cast<uint8_t*>(t.m_out), at, n, vec,
-                  f8_pack4(__fmul_rn(x[0], inv_m), __fmul_rn(x[1], inv_m), __fmul_rn(x[2], inv_m), __fmul_rn(x[3], inv_m)));
-      store_codes(static_cast<uint8_t*>(t.v_out), at, n, vec,
-                  f8_pack4(round_root(__fmul_rn(root[0], inv_r), rnd[u][0] & 0xFFFFu), round_root(__fmul_rn(root[1], inv_r), rnd[u][0] >> 16),
-                           round_root(__fmul_rn(root[2], inv_r), rnd[u][1] & 0xFFFFu), round_root(__fmul_rn(root[3], inv_r), rnd[u][1] >> 16)));
-      const int64_t group = (base >> 7) + u;
-      if (lane == 0 && group * F8_GROUP < n) { t.m_scale_out[group] = scale_m; t.v_scale_out[group] = scale_r; }
+      most_m[u] = __reduce_max_sync(ALL, __float_as_uint(mm));
+      most_r[u] = __reduce_max_sync(ALL, __float_as_uint(mr));
     } else {
       store4(static_cast<float*>(t.m_out), at, n, vec, m[u].v);
       store4(static_cast<float*>(t.v_out), at, n, vec, v[u].v);
+    }
+  }
+  if (BITS8) {
+    // the divisions of the eight groups (m and root of four) are done by a lane each
+    uint32_t mine = 0;
+    #pragma unroll
+    for (int u = 0; u < ADW_GROUPS; ++u) {
+      if ((lane & 7) == u) mine = most_m[u];
+      if ((lane & 7) == ADW_GROUPS + u) mine = most_r[u];
+    }
+    float scale, inv;
+    f8_group(__uint_as_float(mine), scale, inv);
+    const int64_t group = (base >> 7) + (lane & 3);
+    if (lane < 2 * ADW_GROUPS && group * F8_GROUP < n) (lane < ADW_GROUPS ? t.m_scale_out : t.v_scale_out)[group] = scale;
+    #pragma unroll
+    for (int u = 0; u < ADW_GROUPS; ++u) {
+      const int64_t at = base + u * F8_GROUP + 4 * lane;
+      const float2 im = both(__shfl_sync(ALL, inv, u)), ir = both(__shfl_sync(ALL, inv, ADW_GROUPS + u));
+      const float2 x = mul2(make_float2(m[u].v[0], m[u].v[1]), im), y = mul2(make_float2(m[u].v[2], m[u].v[3]), im);
+      store_codes(static_cast<uint8_t*>(t.m_out), at, n, vec, f8_pack4(x.x, x.y, y.x, y.y));
+      const float2 p = mul2(make_float2(v[u].v[0], v[u].v[1]), ir), q = mul2(make_float2(v[u].v[2], v[u].v[3]), ir);
+      store_codes(static_cast<uint8_t*>(t.v_out), at, n, vec,
+                  f8_pack4(round_root(p.x, (rnd[u][0] << 4) & 0xFFFF0u), round_root(p.y, (rnd[u][0] >> 12) & 0xFFFF0u),
+                           round_root(q.x, (rnd[u][1] << 4) & 0xFFFF0u), round_root(q.y, (rnd[u][1] >> 12) & 0xFFFF0u)));
     }
   }
   if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);

@@ -7,6 +7,7 @@
 
 #include "common.cuh"
 #include "float8.cuh"
+#include "paired.cuh"
 
 namespace sapo {
 
@@ -20,43 +21,58 @@ struct Fp8StoreArgs {
   int32_t* status;
 };
 
-struct Eight { float v[8]; };
-__device__ __forceinline__ Eight load8(const float* p, int left, bool vec) {      // left: columns up to the row's end
-  Eight e;
+// Eight neighbouring values as they are in memory: bf16 takes four registers until it is converted.
+template <class T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+  uint32_t w[4];
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float((i & 1) ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16); }
+};
+template <> struct Eight<float> {
+  uint32_t w[8];
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(w[i]); }
+};
+template <class T>
+__device__ __forceinline__ void load8(Eight<T>& e, const T* p, int left, bool vec) {      // left: columns up to the row's end
   if (vec && left >= 8) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    e.v[0] = a.x; e.v[1] = a.y; e.v[2] = a.z; e.v[3] = a.w; e.v[4] = b.x; e.v[5] = b.y; e.v[6] = b.z; e.v[7] = b.w;
-  } else {
     #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = i < left ? p[i] : 0.f;
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+      const uint4 a = reinterpret_cast<const uint4*>(p)[h];
+      e.w[4 * h] = a.x; e.w[4 * h + 1] = a.y; e.w[4 * h + 2] = a.z; e.w[4 * h + 3] = a.w;
+    }
+    return;
   }
-  return e;
-}
-__device__ __forceinline__ Eight load8(const __nv_bfloat16* p, int left, bool vec) {
-  Eight e;
-  if (vec && left >= 8) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-    #pragma unroll
-    for (int i = 0; i < 4; ++i) { e.v[2 * i] = __uint_as_float(w[i] << 16); e.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-  } else {
-    #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = i < left ? __bfloat162float(p[i]) : 0.f;
+  #pragma unroll
+  for (int i = 0; i < 2 * (int)sizeof(T); ++i) e.w[i] = 0;
+  #pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (i >= left) continue;
+    if (sizeof(T) == 4) e.w[i % (2 * sizeof(T))] = reinterpret_cast<const uint32_t*>(p)[i];
+    else e.w[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
   }
-  return e;
 }
-// largest magnitude, NaN if there is one (as an unsigned integer NaN is above infinity)
-__device__ __forceinline__ uint32_t largest(const Eight& e) {
-  uint32_t m = 0;
-  #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(e.v[i]) & 0x7FFFFFFFu);
-  return m;
+// largest magnitude, as an unsigned integer: a NaN is above infinity
+template <class T>
+__device__ __forceinline__ uint32_t largest(const Eight<T>& e) {
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162* b = reinterpret_cast<const __nv_bfloat162*>(e.w);
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(__habs2(b[0]), __habs2(b[1])), __hmax2_nan(__habs2(b[2]), __habs2(b[3])));
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&m);
+    return max(w << 16, w & 0xFFFF0000u);
+  } else {
+    uint32_t m = 0;
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, e.w[i] & 0x7FFFFFFFu);
+    return m;
+  }
 }
-__device__ __forceinline__ void store8(uint8_t* p, int left, bool vec, const Eight& e, float inv) {
-  float x[8];
+// codes of eight values; a group that holds no number below infinity, or only tiny ones, has inv 0 and gets zeros
+template <class T>
+__device__ __forceinline__ void store8(uint8_t* p, int left, bool vec, const Eight<T>& e, float inv) {
+  float2 x[4];
   #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = inv > 0.f ? __fmul_rn(e.v[i], inv) : 0.f;
-  const uint2 q = make_uint2(f8_pack4(x[0], x[1], x[2], x[3]), f8_pack4(x[4], x[5], x[6], x[7]));
+  for (int i = 0; i < 4; ++i) x[i] = mul2(make_float2(e.at(2 * i), e.at(2 * i + 1)), both(inv));
+  uint2 q = make_uint2(f8_pack4(x[0].x, x[0].y, x[1].x, x[1].y), f8_pack4(x[2].x, x[2].y, x[3].x, x[3].y));
+  if (inv == 0.f) q = make_uint2(0, 0);
   if (vec && left >= 8) *reinterpret_cast<uint2*>(p) = q;
   else {
     #pragma unroll
@@ -73,18 +89,17 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArg
   const int64_t pieces = a.R * per_row;
   bool bad = false;
   for (int64_t first = warp * F8S_PIECES; first < pieces; first += warps * F8S_PIECES) {
-    Eight e[F8S_PIECES];
-    int64_t row[F8S_PIECES]; int col[F8S_PIECES];
+    Eight<T> e[F8S_PIECES];
+    int64_t row = first / per_row;
+    int col = (int)(first - row * per_row) * 256 + lane * 8;
+    const int64_t row_first = row;
+    const int col_first = col;
     #pragma unroll
     for (int u = 0; u < F8S_PIECES; ++u) {
-      row[u] = (first + u) / per_row;
-      col[u] = (int)((first + u) - row[u] * per_row) * 256 + lane * 8;
-      const int left = first + u < pieces ? a.C - col[u] : 0;
-      if (left > 0) e[u] = load8(static_cast<const T*>(a.x) + row[u] * a.ld_x + col[u], left, a.vec_x);
-      else
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) e[u].v[i] = 0.f;
+      load8(e[u], static_cast<const T*>(a.x) + row * a.ld_x + col, first + u < pieces ? a.C - col : 0, a.vec_x);
+      if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
+    row = row_first; col = col_first;
     #pragma unroll
     for (int u = 0; u < F8S_PIECES; ++u) {
       uint32_t m = largest(e[u]);
@@ -92,11 +107,13 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArg
       for (int d = 8; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));      // the group's 16 lanes
       float scale, inv;
       f8_group(__uint_as_float(m), scale, inv);
-      const int left = first + u < pieces ? a.C - col[u] : 0;
-      if (left <= 0) continue;
-      bad |= m >= 0x7F800000u;
-      store8(a.q + row[u] * a.ld + col[u], left, a.vec_q, e[u], inv);
-      if ((lane & 15) == 0) a.scale[row[u] * a.ld_scale + (col[u] >> 7)] = scale;
+      const int left = first + u < pieces ? a.C - col : 0;
+      if (left > 0) {
+        bad |= m >= 0x7F800000u;
+        store8(a.q + row * a.ld + col, left, a.vec_q, e[u], inv);
+        if ((lane & 15) == 0) a.scale[row * a.ld_scale + (col >> 7)] = scale;
+      }
+      if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
   }
   if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
@@ -112,15 +129,10 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_blocks_kernel(const Fp8StoreA
   const int bc = (int)(blockIdx.x - br * across);
   const int col = bc * 128 + (threadIdx.x & 15) * 8, left = a.C - col;
   const int64_t row0 = br * 128 + (threadIdx.x >> 4);
-  Eight e[8];
+  Eight<T> e[8];
   uint32_t m = 0;
   #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    if (left > 0 && row0 + 16 * u < a.R) e[u] = load8(static_cast<const T*>(a.x) + (row0 + 16 * u) * a.ld_x + col, left, a.vec_x);
-    else
-      #pragma unroll
-      for (int i = 0; i < 8; ++i) e[u].v[i] = 0.f;
-  }
+  for (int u = 0; u < 8; ++u) load8(e[u], static_cast<const T*>(a.x) + (row0 + 16 * u) * a.ld_x + col, row0 + 16 * u < a.R ? left : 0, a.vec_x);
   #pragma unroll
   for (int u = 0; u < 8; ++u) m = max(m, largest(e[u]));
   m = __reduce_max_sync(0xFFFFFFFFu, m);

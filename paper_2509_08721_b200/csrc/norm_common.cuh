@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "paired.cuh"
 
 namespace sapo {
 
@@ -34,29 +35,6 @@ struct NormBwdArgs {
   int64_t T; int32_t H; float* part; float* dgamma; float* dbeta; int32_t accumulate;
 };
 struct Ckpt8Args { Mat x; Q8Mat q; int64_t T; int32_t H; int32_t* status; };
-
-// ---------------------------------------------------------------------------- paired fp32 arithmetic
-// (fma.rn.f32x2 and its kin, each half rounded like the scalar operation)
-#define SAPO_F32X2(name, ptx)                                                                             \
-  __device__ __forceinline__ float2 name(float2 a, float2 b) {                                            \
-    float2 d;                                                                                             \
-    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t" ptx                 \
-        " d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"                                                          \
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));                                 \
-    return d;                                                                                             \
-  }
-SAPO_F32X2(add2, "add.rn.f32x2")
-SAPO_F32X2(mul2, "mul.rn.f32x2")
-#undef SAPO_F32X2
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
-      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
 
 // ---------------------------------------------------------------------------- 8 neighbouring columns
 __device__ __forceinline__ void unpack8(uint4 u, float2 (&x)[4]) {       // bf16 to fp32: the upper half of the word
@@ -103,11 +81,6 @@ __device__ __forceinline__ void put8(void* p, int64_t at, const float2 (&x)[4]) 
   }
 }
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
 
 // ---------------------------------------------------------------------------- several reductions at once
 // N values (1, 2, 4 or 8) per lane, each reduced over WIDTH >= N lanes (a power of two): an exchange halves how many values a lane
