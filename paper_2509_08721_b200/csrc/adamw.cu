@@ -55,57 +55,63 @@ __host__ __device__ inline double one_minus_power(double b, uint32_t t) {
   return 1.0 - p;
 }
 
+// Four neighbouring elements from p on, `left` of which exist (WHOLE: all four, on a boundary for one access).
 struct Four { float v[4]; };
-template <class G> __device__ __forceinline__ Four load4(const G* p, int64_t at, int64_t n, bool vec);
-template <> __device__ __forceinline__ Four load4<float>(const float* p, int64_t at, int64_t n, bool vec) {
+template <bool WHOLE>
+__device__ __forceinline__ Four load4(const float* p, int left) {
   Four f;
-  if (vec) { const float4 x = *reinterpret_cast<const float4*>(p + at); f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w; }
+  if (WHOLE) { const float4 x = *reinterpret_cast<const float4*>(p); f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w; }
   else {
     #pragma unroll
-    for (int i = 0; i < 4; ++i) f.v[i] = at + i < n ? p[at + i] : 0.f;
+    for (int i = 0; i < 4; ++i) f.v[i] = i < left ? p[i] : 0.f;
   }
   return f;
 }
-template <> __device__ __forceinline__ Four load4<__nv_bfloat16>(const __nv_bfloat16* p, int64_t at, int64_t n, bool vec) {
+template <bool WHOLE>
+__device__ __forceinline__ Four load4(const __nv_bfloat16* p, int left) {
   Four f;
-  if (vec) {
-    const uint2 x = *reinterpret_cast<const uint2*>(p + at);
+  if (WHOLE) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
     f.v[0] = __uint_as_float(x.x << 16); f.v[1] = __uint_as_float(x.x & 0xFFFF0000u);
     f.v[2] = __uint_as_float(x.y << 16); f.v[3] = __uint_as_float(x.y & 0xFFFF0000u);
   } else {
     #pragma unroll
-    for (int i = 0; i < 4; ++i) f.v[i] = at + i < n ? __bfloat162float(p[at + i]) : 0.f;
+    for (int i = 0; i < 4; ++i) f.v[i] = i < left ? __bfloat162float(p[i]) : 0.f;
   }
   return f;
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t at, int64_t n, bool vec) {
-  if (vec) return *reinterpret_cast<const uint32_t*>(p + at);
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int left) {
+  if (WHOLE) return *reinterpret_cast<const uint32_t*>(p);
   uint32_t q = 0;
   #pragma unroll
-  for (int i = 0; i < 4; ++i) if (at + i < n) q |= (uint32_t)p[at + i] << (8 * i);
+  for (int i = 0; i < 4; ++i) if (i < left) q |= (uint32_t)p[i] << (8 * i);
   return q;
 }
-__device__ __forceinline__ void store4(float* p, int64_t at, int64_t n, bool vec, const float (&v)[4]) {
-  if (vec) *reinterpret_cast<float4*>(p + at) = make_float4(v[0], v[1], v[2], v[3]);
+template <bool WHOLE>
+__device__ __forceinline__ void store4(float* p, int left, const float (&v)[4]) {
+  if (WHOLE) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   else {
     #pragma unroll
-    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = v[i];
+    for (int i = 0; i < 4; ++i) if (i < left) p[i] = v[i];
   }
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t at, int64_t n, bool vec, const float (&v)[4]) {
-  if (vec) {
+template <bool WHOLE>
+__device__ __forceinline__ void store4(__nv_bfloat16* p, int left, const float (&v)[4]) {
+  if (WHOLE) {
     const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
-    *reinterpret_cast<uint2*>(p + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
   } else {
     #pragma unroll
-    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 4; ++i) if (i < left) p[i] = __float2bfloat16_rn(v[i]);
   }
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t at, int64_t n, bool vec, uint32_t q) {
-  if (vec) *reinterpret_cast<uint32_t*>(p + at) = q;
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(uint8_t* p, int left, uint32_t q) {
+  if (WHOLE) *reinterpret_cast<uint32_t*>(p) = q;
   else {
     #pragma unroll
-    for (int i = 0; i < 4; ++i) if (at + i < n) p[at + i] = (uint8_t)(q >> (8 * i));
+    for (int i = 0; i < 4; ++i) if (i < left) p[i] = (uint8_t)(q >> (8 * i));
   }
 }
 
@@ -119,59 +125,41 @@ __device__ __forceinline__ float round_root(float t, uint32_t bits16) {
   return t > 0.f ? fminf(__uint_as_float(up), F8_TOP) : 0.f;
 }
 
-template <bool BITS8, class G>
-__global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constant__ AdamWArgs a) {
+// What a step has in common for the elements of a tensor
+struct AdamWStep { float minus_lr, shrink, grad_scale, inv_bias1, inv_bias2_root; uint32_t step; };
+
+// 512 elements of tensor t from `base` on.  WHOLE: they all exist, and every array can be read and written four at a time.
+template <bool BITS8, class G, bool WHOLE>
+__device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& t, const AdamWStep& c, int64_t base) {
   constexpr uint32_t ALL = 0xFFFFFFFFu;
-  wait_for_previous();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int lo = 0, hi = a.n_tensors - 1;            // the last tensor whose first block is not behind this one
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.t[mid].first_block <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
-  }
-  const AdamWEntry& t = a.t[lo];
-  float inv_bias1 = a.inv_bias1, inv_bias2_root = a.inv_bias2_root;
-  uint32_t step = a.step;
-  if (a.step_dev != nullptr) {
-    __shared__ float bias[2];
-    step = (uint32_t)max(*a.step_dev, 1);
-    if (threadIdx.x == 0) { bias[0] = (float)(1.0 / one_minus_power(a.beta1, step)); bias[1] = (float)(1.0 / sqrt(one_minus_power(a.beta2, step))); }
-    __syncthreads();
-    inv_bias1 = bias[0]; inv_bias2_root = bias[1];
-  }
-  const int64_t n = t.n, base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK + (int64_t)warp * ADW_WARP;
-  if (base >= n) return;
-  const bool vec = t.vectors && base + ADW_WARP <= n;      // whole vectors everywhere: no bounds to look at
+  const int lane = threadIdx.x & 31;
+  const int64_t at = base + 4 * lane, group = base >> 7, groups = (t.n + F8_GROUP - 1) >> 7;
+  const int left = WHOLE ? ADW_WARP : (int)max((int64_t)-ADW_WARP, min((int64_t)ADW_WARP, t.n - at));      // elements from this lane's first on
   Four g[ADW_GROUPS], w[ADW_GROUPS], m[ADW_GROUPS], v[ADW_GROUPS];
   uint32_t qm[ADW_GROUPS], qv[ADW_GROUPS];
   float sm[ADW_GROUPS], sv[ADW_GROUPS];
   #pragma unroll
   for (int u = 0; u < ADW_GROUPS; ++u) {
-    const int64_t at = base + u * F8_GROUP + 4 * lane;
-    g[u] = load4(static_cast<const G*>(t.grad), at, n, vec);
-    w[u] = load4(t.master, at, n, vec);
+    g[u] = load4<WHOLE>(static_cast<const G*>(t.grad) + at + u * F8_GROUP, left - u * F8_GROUP);
+    w[u] = load4<WHOLE>(t.master + at + u * F8_GROUP, left - u * F8_GROUP);
     if (BITS8) {
-      qm[u] = load_codes(static_cast<const uint8_t*>(t.m), at, n, vec);
-      qv[u] = load_codes(static_cast<const uint8_t*>(t.v), at, n, vec);
-      const int64_t group = (base >> 7) + u;
-      const bool there = group * F8_GROUP < n;
-      sm[u] = there ? t.m_scale[group] : 0.f;
-      sv[u] = there ? t.v_scale[group] : 0.f;
+      qm[u] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.m) + at + u * F8_GROUP, left - u * F8_GROUP);
+      qv[u] = load_codes<WHOLE>(static_cast<const uint8_t*>(t.v) + at + u * F8_GROUP, left - u * F8_GROUP);
+      const bool there = WHOLE || group + u < groups;
+      sm[u] = there ? t.m_scale[group + u] : 0.f;
+      sv[u] = there ? t.v_scale[group + u] : 0.f;
     } else {
-      m[u] = load4(static_cast<const float*>(t.m), at, n, vec);
-      v[u] = load4(static_cast<const float*>(t.v), at, n, vec);
+      m[u] = load4<WHOLE>(static_cast<const float*>(t.m) + at + u * F8_GROUP, left - u * F8_GROUP);
+      v[u] = load4<WHOLE>(static_cast<const float*>(t.v) + at + u * F8_GROUP, left - u * F8_GROUP);
     }
   }
-  const double lr64 = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
-  const float minus_lr = -(float)lr64, shrink = (float)(1.0 - lr64 * (double)t.decay);
-  const float gs = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
   // random words: the eight elements of a counter belong to two lanes; each of them makes the counters of every other group
   uint32_t rnd[ADW_GROUPS][2];
   if (BITS8) {
     #pragma unroll
     for (int u = 0; u < ADW_GROUPS; u += 2) {
-      const uint64_t c = (uint64_t)(base + (u + (lane & 1)) * F8_GROUP + 4 * (lane & ~1)) >> 3;
-      const uint4 r = philox4x32_10((uint32_t)c, (uint32_t)(c >> 32), (uint32_t)t.number, step, a.k0, a.k1);
+      const uint64_t eight = (uint64_t)(base + (u + (lane & 1)) * F8_GROUP + 4 * (lane & ~1)) >> 3;
+      const uint4 r = philox4x32_10((uint32_t)eight, (uint32_t)(eight >> 32), (uint32_t)t.number, c.step, a.k0, a.k1);
       const bool odd = lane & 1;
       const uint32_t p = __shfl_xor_sync(ALL, odd ? r.x : r.z, 1), q = __shfl_xor_sync(ALL, odd ? r.y : r.w, 1);
       rnd[u][0] = odd ? p : r.x; rnd[u][1] = odd ? q : r.y;
@@ -183,14 +171,13 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
   bool bad = false;
   #pragma unroll
   for (int u = 0; u < ADW_GROUPS; ++u) {
-    const int64_t at = base + u * F8_GROUP + 4 * lane;
     float big = 0.f, mm = 0.f, mr = 0.f;
     float2 x[2], m0[2], v0[2];
     float root[4];
     if (BITS8) { f8_unpack4(qm[u], m[u].v); f8_unpack4(qv[u], root); }
     #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      x[h] = mul2(make_float2(g[u].v[2 * h], g[u].v[2 * h + 1]), both(gs));
+      x[h] = mul2(make_float2(g[u].v[2 * h], g[u].v[2 * h + 1]), both(c.grad_scale));
       m0[h] = make_float2(m[u].v[2 * h], m[u].v[2 * h + 1]);
       v0[h] = make_float2(v[u].v[2 * h], v[u].v[2 * h + 1]);
       if (BITS8) {
@@ -216,21 +203,21 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
         v1 = make_float2(fine[0] ? fminf(v1.x, 3.402823466e38f) : v0[h].x, fine[1] ? fminf(v1.y, 3.402823466e38f) : v0[h].y);
       }
       const float2 r1 = make_float2(sqrtf(v1.x), sqrtf(v1.y));
-      const float2 above = mul2(m1, both(inv_bias1)), below = fma2(r1, both(inv_bias2_root), both(a.eps));
-      const float2 now = fma2(both(minus_lr), make_float2(__fdividef(above.x, below.x), __fdividef(above.y, below.y)), mul2(was, both(shrink)));
+      const float2 above = mul2(m1, both(c.inv_bias1)), below = fma2(r1, both(c.inv_bias2_root), both(a.eps));
+      const float2 now = fma2(both(c.minus_lr), make_float2(__fdividef(above.x, below.x), __fdividef(above.y, below.y)), mul2(was, both(c.shrink)));
       w[u].v[2 * h] = fine[0] ? now.x : was.x; w[u].v[2 * h + 1] = fine[1] ? now.y : was.y;
       m[u].v[2 * h] = m1.x; m[u].v[2 * h + 1] = m1.y;
       v[u].v[2 * h] = BITS8 ? r1.x : v1.x; v[u].v[2 * h + 1] = BITS8 ? r1.y : v1.y;
       if (BITS8) { mm = fmaxf(mm, fmaxf(fabsf(m1.x), fabsf(m1.y))); mr = fmaxf(mr, fmaxf(r1.x, r1.y)); }
     }
-    store4(t.master_out, at, n, vec, w[u].v);
-    if (t.copy != nullptr) store4(t.copy, at, n, vec, w[u].v);
+    store4<WHOLE>(t.master_out + at + u * F8_GROUP, left - u * F8_GROUP, w[u].v);
+    if (t.copy != nullptr) store4<WHOLE>(t.copy + at + u * F8_GROUP, left - u * F8_GROUP, w[u].v);
     if (BITS8) {
       most_m[u] = __reduce_max_sync(ALL, __float_as_uint(mm));
       most_r[u] = __reduce_max_sync(ALL, __float_as_uint(mr));
     } else {
-      store4(static_cast<float*>(t.m_out), at, n, vec, m[u].v);
-      store4(static_cast<float*>(t.v_out), at, n, vec, v[u].v);
+      store4<WHOLE>(static_cast<float*>(t.m_out) + at + u * F8_GROUP, left - u * F8_GROUP, m[u].v);
+      store4<WHOLE>(static_cast<float*>(t.v_out) + at + u * F8_GROUP, left - u * F8_GROUP, v[u].v);
     }
   }
   if (BITS8) {
@@ -243,21 +230,47 @@ __global__ void __launch_bounds__(ADW_THREADS) adamw_kernel(const __grid_constan
     }
     float scale, inv;
     f8_group(__uint_as_float(mine), scale, inv);
-    const int64_t group = (base >> 7) + (lane & 3);
-    if (lane < 2 * ADW_GROUPS && group * F8_GROUP < n) (lane < ADW_GROUPS ? t.m_scale_out : t.v_scale_out)[group] = scale;
+    const int64_t own = group + (lane & (ADW_GROUPS - 1));
+    if (lane < 2 * ADW_GROUPS && (WHOLE || own < groups)) (lane < ADW_GROUPS ? t.m_scale_out : t.v_scale_out)[own] = scale;
     #pragma unroll
     for (int u = 0; u < ADW_GROUPS; ++u) {
-      const int64_t at = base + u * F8_GROUP + 4 * lane;
       const float2 im = both(__shfl_sync(ALL, inv, u)), ir = both(__shfl_sync(ALL, inv, ADW_GROUPS + u));
       const float2 x = mul2(make_float2(m[u].v[0], m[u].v[1]), im), y = mul2(make_float2(m[u].v[2], m[u].v[3]), im);
-      store_codes(static_cast<uint8_t*>(t.m_out), at, n, vec, f8_pack4(x.x, x.y, y.x, y.y));
+      store_codes<WHOLE>(static_cast<uint8_t*>(t.m_out) + at + u * F8_GROUP, left - u * F8_GROUP, f8_pack4(x.x, x.y, y.x, y.y));
       const float2 p = mul2(make_float2(v[u].v[0], v[u].v[1]), ir), q = mul2(make_float2(v[u].v[2], v[u].v[3]), ir);
-      store_codes(static_cast<uint8_t*>(t.v_out), at, n, vec,
+      store_codes<WHOLE>(static_cast<uint8_t*>(t.v_out) + at + u * F8_GROUP, left - u * F8_GROUP,
                   f8_pack4(round_root(p.x, (rnd[u][0] << 4) & 0xFFFF0u), round_root(p.y, (rnd[u][0] >> 12) & 0xFFFF0u),
                            round_root(q.x, (rnd[u][1] << 4) & 0xFFFF0u), round_root(q.y, (rnd[u][1] >> 12) & 0xFFFF0u)));
     }
   }
   if (bad) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+}
+
+template <bool BITS8, class G>
+__global__ void __launch_bounds__(ADW_THREADS, 3) adamw_kernel(const __grid_constant__ AdamWArgs a) {
+  wait_for_previous();
+  const int warp = threadIdx.x >> 5;
+  int lo = 0, hi = a.n_tensors - 1;            // the last tensor whose first block is not behind this one
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.t[mid].first_block <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+  }
+  const AdamWEntry& t = a.t[lo];
+  float inv_bias1 = a.inv_bias1, inv_bias2_root = a.inv_bias2_root;
+  uint32_t step = a.step;
+  if (a.step_dev != nullptr) {
+    __shared__ float bias[2];
+    step = (uint32_t)max(*a.step_dev, 1);
+    if (threadIdx.x == 0) { bias[0] = (float)(1.0 / one_minus_power(a.beta1, step)); bias[1] = (float)(1.0 / sqrt(one_minus_power(a.beta2, step))); }
+    __syncthreads();
+    inv_bias1 = bias[0]; inv_bias2_root = bias[1];
+  }
+  const int64_t base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK + (int64_t)warp * ADW_WARP;
+  if (base >= t.n) return;
+  const double lr = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
+  const AdamWStep c{-(float)lr, (float)(1.0 - lr * (double)t.decay), a.grad_scale != nullptr ? *a.grad_scale : 1.f, inv_bias1, inv_bias2_root, step};
+  if (t.vectors && base + ADW_WARP <= t.n) adamw_run<BITS8, G, true>(a, t, c, base);
+  else                                     adamw_run<BITS8, G, false>(a, t, c, base);
 }
 
 static bool multiple_of(const void* p, size_t k) { return reinterpret_cast<uintptr_t>(p) % k == 0; }

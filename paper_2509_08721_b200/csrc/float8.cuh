@@ -14,7 +14,7 @@ constexpr float F8_TINY = 1.504632769052528e-36f;   // 2^-119: below it 448 (1/a
 __device__ __forceinline__ void f8_group(float a, float& scale, float& inv) {
   const bool finite = a < __int_as_float(0x7f800000);
   scale = !finite ? __int_as_float(0x7fffffff) : (a >= F8_TINY ? __fmul_rn(a, 1.f / F8_TOP) : 0.f);
-  inv = finite && a >= F8_TINY ? __fmul_rn(F8_TOP, __fdiv_rn(1.f, a)) : 0.f;
+  inv = finite && a >= F8_TINY ? __fmul_rn(F8_TOP, __frcp_rn(a)) : 0.f;
 }
 __device__ __forceinline__ uint32_t f8_pack4(float a, float b, float c, float d) {
   const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);

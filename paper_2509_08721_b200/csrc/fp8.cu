@@ -99,20 +99,26 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArg
       load8(e[u], static_cast<const T*>(a.x) + row * a.ld_x + col, first + u < pieces ? a.C - col : 0, a.vec_x);
       if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
+    // largest magnitudes of the pieces' groups (16 lanes each); lane j of the 16 works out the scale of piece j
+    uint32_t m[F8S_PIECES], mine = 0;
+    #pragma unroll
+    for (int u = 0; u < F8S_PIECES; ++u) {
+      m[u] = largest(e[u]);
+      #pragma unroll
+      for (int d = 8; d > 0; d >>= 1) m[u] = max(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], d));
+      bad |= m[u] >= 0x7F800000u;
+      if ((lane & 15) == u) mine = m[u];
+    }
+    float scale, inv;
+    f8_group(__uint_as_float(mine), scale, inv);
     row = row_first; col = col_first;
     #pragma unroll
     for (int u = 0; u < F8S_PIECES; ++u) {
-      uint32_t m = largest(e[u]);
-      #pragma unroll
-      for (int d = 8; d > 0; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));      // the group's 16 lanes
-      float scale, inv;
-      f8_group(__uint_as_float(m), scale, inv);
+      const float inv_u = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + u);
       const int left = first + u < pieces ? a.C - col : 0;
-      if (left > 0) {
-        bad |= m >= 0x7F800000u;
-        store8(a.q + row * a.ld + col, left, a.vec_q, e[u], inv);
-        if ((lane & 15) == 0) a.scale[row * a.ld_scale + (col >> 7)] = scale;
-      }
+      if (left > 0) store8(a.q + row * a.ld + col, left, a.vec_q, e[u], inv_u);
+      const int group = col >> 7;
+      if ((lane & 15) == u && first + u < pieces && group * 128 < a.C) a.scale[row * a.ld_scale + group] = scale;
       if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
   }

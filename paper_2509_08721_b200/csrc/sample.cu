@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   int turn = 0;
 
   auto barrier = [&]() { if (C > 1) cluster.sync(); else __syncthreads(); };
-  // Tell every block of the cluster W words (the same in all threads) and wait; returns the words of all blocks.
+  // Tell every block of the cluster W words (of the first threads, the same in each) and wait; returns those of all blocks.
   auto exchange = [&](const uint32_t* v, int W) -> const uint32_t (*)[8] {
     const int t = turn;
     turn ^= 1;
@@ -123,22 +123,29 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     barrier();
     return sh.slots[t];
   };
-  // Combine the words of every thread of the cluster; op(x, y) folds y into x; all threads get the result.
+  // Combine the words of every thread of the cluster; op(x, y) folds y into x; all threads get the result.  One warp
+  // combines what the warps of a block have, and tells the blocks.
   auto reduce = [&](auto& v, auto op) {
     constexpr int W = sizeof(v) / 4;
-    #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      uint32_t o[W];
+    auto fold = [&](int widest) {
       #pragma unroll
-      for (int i = 0; i < W; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
-      op(v, o);
-    }
+      for (int d = 16; d > 0; d >>= 1) {
+        if (d > widest) continue;
+        uint32_t o[W];
+        #pragma unroll
+        for (int i = 0; i < W; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+        op(v, o);
+      }
+    };
+    fold(16);
     uint32_t (*each)[4] = sh.warp[turn];
     if (lane == 0)
       for (int i = 0; i < W; ++i) each[warp][i] = v[i];
     __syncthreads();
-    for (int i = 0; i < W; ++i) v[i] = each[0][i];
-    for (int w = 1; w < SMP_WARPS; ++w) op(v, each[w]);
+    if (warp == 0) {
+      for (int i = 0; i < W; ++i) v[i] = each[lane & (SMP_WARPS - 1)][i];
+      fold(SMP_WARPS / 2);
+    }
     const uint32_t (*all)[8] = exchange(v, W);
     for (int i = 0; i < W; ++i) v[i] = all[0][i];
     for (uint32_t r = 1; r < C; ++r) op(v, all[r]);
@@ -179,23 +186,36 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   if (tid == 0) { sh.n_list = 0; sh.n_sort = 0; }
   asm volatile("cp.async.wait_all;" ::: "memory");
 
-  // ---- the largest logit
+  // ---- the largest logit: of the block, and of the row.  Without top-k and top-p the sums below are formed against the
+  //      block's and told together with it.
+  const bool settings_ok = temperature >= 0.f && temperature < CUDART_INF_F && min_p >= 0.f && top_p == top_p;
+  const bool alone = !cuts && settings_ok && !(min_p > 0.f);
   uint32_t top[1];
   {
     float m = -CUDART_INF_F;
     for (int v = tid; v < n_vec; v += SMP_THREADS) m = max_nan(m, Vec<T>::most(piece + 8 * v));
     top[0] = __float_as_uint(m);
-    reduce(top, [](uint32_t* x, const uint32_t* y) { x[0] = __float_as_uint(max_nan(__uint_as_float(x[0]), __uint_as_float(y[0]))); });
+    auto larger = [](uint32_t* x, const uint32_t* y) { x[0] = __float_as_uint(max_nan(__uint_as_float(x[0]), __uint_as_float(y[0]))); };
+    if (alone) {
+      #pragma unroll
+      for (int d = 16; d > 0; d >>= 1) { const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, top[0], d); larger(top, &o); }
+      if (lane == 0) sh.scan[warp][0] = top[0];
+      __syncthreads();
+      top[0] = sh.scan[lane & (SMP_WARPS - 1)][0];
+      #pragma unroll
+      for (int d = SMP_WARPS / 2; d > 0; d >>= 1) { const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, top[0], d); larger(top, &o); }
+    } else reduce(top, larger);
   }
-  const float zmax = __uint_as_float(top[0]);
-  const bool settings_ok = temperature >= 0.f && temperature < CUDART_INF_F && min_p >= 0.f && top_p == top_p;
-  if (!(zmax < CUDART_INF_F) || zmax == -CUDART_INF_F || !settings_ok) {     // the same in all blocks
+  float zmax = __uint_as_float(top[0]);
+  auto bad_row = [&]() {                              // the same in all blocks, behind a barrier: nothing touches another block any more
+    if (zmax < CUDART_INF_F && zmax > -CUDART_INF_F && settings_ok) return false;
     if (rank == 0 && tid == 0) {
       a.ids[row] = -1; a.logp[row] = 0.f;
       if (!settings_ok || zmax != -CUDART_INF_F) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
     }
-    return;                                    // (the reduction's barrier was the last access to another block)
-  }
+    return true;
+  };
+  if (!alone && bad_row()) return;
   // distance of a token from the largest, in octaves of its weight: (zmax - z) scale, never 0 * inf
   const float scale = greedy ? SMP_LOG2E : fminf(SMP_LOG2E / temperature, 1e30f);
   const float floor_octaves = min_p > 0.f && !greedy ? fmaxf(-log2f(min_p), 0.f) : CUDART_INF_F;     // kept up to here
@@ -215,13 +235,15 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   {
     float s1 = 0.f, sT = 0.f, far = 0.f;
     uint32_t first = 0xFFFFFFFFu;
+    // (a block of -inf, or with a NaN or +inf, has no largest logit to go by: its sums are 0, or the row is bad)
+    const float ref = fabsf(zmax) < CUDART_INF_F ? zmax : 0.f;
     const bool other = !greedy && !cuts && (scale != SMP_LOG2E || floor_octaves < CUDART_INF_F);
     for (int v = tid; v < n_vec; v += SMP_THREADS) {
       float z[8];
       Vec<T>::get(piece + 8 * v, z);
       float p[2] = {0.f, 0.f};
       #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i & 1] += ex2((z[i] - zmax) * SMP_LOG2E);
+      for (int i = 0; i < 8; ++i) p[i & 1] += ex2((z[i] - ref) * SMP_LOG2E);
       s1 += p[0] + p[1];
       if (cuts) {
         #pragma unroll
@@ -232,14 +254,50 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         }
       } else if (other) {
         #pragma unroll
-        for (int i = 0; i < 8; ++i) { const float o = octaves(z[i]); sT += o <= floor_octaves ? ex2(-o) : 0.f; }
+        for (int i = 0; i < 8; ++i) { const float o = (ref - z[i]) * scale; sT += o <= floor_octaves ? ex2(-o) : 0.f; }
       } else if (greedy) {
         #pragma unroll
         for (int i = 7; i >= 0; --i) if (z[i] == zmax) first = min(first, begin + 8 * v + i);
       }
     }
     sums[0] = __float_as_uint(s1); sums[1] = __float_as_uint(other ? sT : s1); sums[2] = first; sums[3] = __float_as_uint(far);
-    reduce(sums, [&](uint32_t* x, const uint32_t* y) { add(x[0], y[0]); add(x[1], y[1]); x[2] = min(x[2], y[2]); add(x[3], y[3]); });
+    if (alone) {
+      // words of a block: its largest logit, its sums against that, its first token with it
+      uint32_t v[4] = {sums[0], sums[1], first, top[0]};
+      #pragma unroll
+      for (int d = 16; d > 0; d >>= 1) {
+        add(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d));
+        if (other) add(v[1], __shfl_xor_sync(0xFFFFFFFFu, v[1], d));
+        if (greedy) v[2] = min(v[2], __shfl_xor_sync(0xFFFFFFFFu, v[2], d));
+      }
+      if (lane == 0)
+        for (int i = 0; i < 3; ++i) sh.warp[turn][warp][i] = v[i];
+      __syncthreads();
+      if (warp == 0) {
+        for (int i = 0; i < 3; ++i) v[i] = sh.warp[turn][lane & (SMP_WARPS - 1)][i];
+        #pragma unroll
+        for (int d = SMP_WARPS / 2; d > 0; d >>= 1) {
+          add(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d));
+          add(v[1], __shfl_xor_sync(0xFFFFFFFFu, v[1], d));
+          v[2] = min(v[2], __shfl_xor_sync(0xFFFFFFFFu, v[2], d));
+        }
+        if (!other) v[1] = v[0];
+      }
+      const uint32_t (*all)[8] = exchange(v, 4);
+      zmax = -CUDART_INF_F;
+      for (uint32_t r = 0; r < C; ++r) zmax = max_nan(zmax, __uint_as_float(all[r][3]));
+      if (bad_row()) return;
+      s1 = 0.f; sT = 0.f; first = 0xFFFFFFFFu;
+      for (uint32_t r = 0; r < C; ++r) {
+        const float less = zmax - __uint_as_float(all[r][3]);
+        s1 += __uint_as_float(all[r][0]) * ex2(-less * SMP_LOG2E);
+        sT += __uint_as_float(all[r][1]) * ex2(-less * scale);
+        if (less == 0.f) first = min(first, all[r][2]);
+      }
+      sums[0] = __float_as_uint(s1); sums[1] = __float_as_uint(sT); sums[2] = first;
+    } else {
+      reduce(sums, [&](uint32_t* x, const uint32_t* y) { add(x[0], y[0]); add(x[1], y[1]); x[2] = min(x[2], y[2]); add(x[3], y[3]); });
+    }
   }
   const float log_sum = logf(__uint_as_float(sums[0]));
   if (greedy) {
@@ -248,7 +306,6 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   }
   float weight = __uint_as_float(sums[1]);       // of the tokens in the race
   // the time at which a token finishes, in 64 bits
-  const double scale64 = fmin(1.0 / (double)temperature, 1e30);
   auto finish = [&](uint32_t token, float z) -> double {
     const uint32_t half = token & 7u, s = 16 * (half & 1u);
     uint32_t bits = 0;
@@ -259,7 +316,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       bits = (bits << 16) | ((w >> s) & 0xFFFFu);
     }
     const double e = -log1p(-((double)bits + 0.5) * 2.3283064365386963e-10);
-    return e * exp(((double)zmax - (double)z) * scale64);
+    return e * exp(((double)zmax - (double)z) * fmin(1.0 / (double)temperature, 1e30));
   };
   // first to finish, the lower index where two finish together; words: time, index, a flag
   auto earlier = [](uint32_t* x, const uint32_t* y) {
@@ -596,17 +653,30 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     }
   }
   __syncthreads();
-  const uint32_t listed = sh.n_list;
+  uint32_t win[4] = {0, 0, 0, 0};
   double best = CUDART_INF;
   uint32_t who = 0xFFFFFFFFu;
-  if (tid < (int)min(listed, (uint32_t)SMP_LIST)) {
-    const uint32_t i = sh.list[tid];
-    best = finish(begin + i, as_float(piece[i]));
-    if (best < CUDART_INF) who = begin + i;
+  if (warp == 0) {                                 // the list is short: one warp works it out
+    const uint32_t listed = sh.n_list;
+    for (uint32_t j = lane; j < min(listed, (uint32_t)SMP_LIST); j += 32) {
+      const uint32_t i = sh.list[j];
+      const double t = finish(begin + i, as_float(piece[i]));
+      if (t < best || (t == best && begin + i < who)) { best = t; who = begin + i; }
+    }
+    words(win, best, who, listed > SMP_LIST ? 1u : 0u);
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      uint32_t o[4];
+      #pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, win[i], d);
+      earlier(win, o);
+    }
   }
-  uint32_t win[4];
-  words(win, best, who, listed > SMP_LIST ? 1u : 0u);
-  reduce(win, earlier);
+  {
+    const uint32_t (*all)[8] = exchange(win, 4);
+    for (int i = 0; i < 4; ++i) win[i] = all[0][i];
+    for (uint32_t r = 1; r < C; ++r) earlier(win, all[r]);
+  }
   if (win[3] || !(__hiloint2double((int)win[1], (int)win[0]) < 0.99 * (double)reach)) {       // the same in all blocks
     best = CUDART_INF; who = 0xFFFFFFFFu;
     #pragma unroll 1
