@@ -24,16 +24,17 @@ namespace sapo {
 namespace cg = cooperative_groups;
 using umma::ex2;
 
-constexpr int SMP_THREADS = 512;
-constexpr int SMP_WARPS = SMP_THREADS / 32;
 constexpr int SMP_MAX_CLUSTER = 8;
+constexpr int SMP_SORT = 512;                 // tokens that are sorted at once, one a thread
 constexpr int SMP_BINS = 2048;
 constexpr float SMP_BINS_PER_OCTAVE = 64.f;   // the last bin takes everything below 2^-32 of the largest weight
 constexpr int SMP_LIST = 256;                 // candidates a block keeps
-constexpr int SMP_SORT = SMP_THREADS;         // tokens that are sorted at once, one a thread
 constexpr float SMP_LEAD = 16.f;              // L: no candidate wins with probability 1e-7
 constexpr float SMP_LOG2E = 1.4426950408889634f;
 constexpr size_t SMP_MAX_PIECE = 180 * 1024;  // bytes of a row a block can hold
+// A call in which no row can have top-k or top-p runs blocks of 256 threads (what a warp does once, whatever its number
+// of tokens, is a quarter of all instructions with 512); the sort of the other calls wants 512.
+template <bool CUTS> constexpr int SMP_THREADS = CUTS ? SMP_SORT : 256;
 
 struct SampleArgs {
   const void* z; int64_t ld; int32_t B, V, piece;      // piece: tokens a block holds, a multiple of 8
@@ -47,16 +48,22 @@ struct Cut { uint32_t bin, before, count, mass_lo, mass_hi, before_lo, before_hi
 struct Last { uint32_t key, index, kept_lo, kept_hi; };                                 // the last token that stays, and the mass up to it
 
 struct SampleShared {
-  uint32_t slots[2][SMP_MAX_CLUSTER][8];    // what the blocks of the cluster tell one another; two sets, taken in turn
-  uint32_t warp[2][SMP_WARPS][4];
-  uint32_t scan[SMP_WARPS][4];
-  Cut cut;
-  Last last;
+  uint32_t slots[2][SMP_MAX_CLUSTER][4];    // what the blocks of the cluster tell one another; two sets, taken in turn
+  uint32_t warp[2][32][4];
+  uint32_t scan[32][4];
   uint32_t n_list, n_sort;
   uint32_t list[SMP_LIST];                  // candidates of the race
-  uint64_t sort[SMP_SORT];                  // tokens to be put in order: key, and the index from above
-  uint32_t count[SMP_BINS], mass_lo[SMP_BINS], mass_hi[SMP_BINS];   // of the tokens in a bin; mass in units of 2^-40
 };
+struct SampleCuts : SampleShared {          // for top-k and top-p
+  Cut cut;
+  Last last;
+  uint64_t sort[SMP_SORT];                  // tokens to be put in order: key, and the index from above
+  // of the tokens in a bin: their number, and their mass: sums of the lower 13 and of the other bits of mass_bits (histogram
+  // of the octaves), or a 64-bit number of units of 2^-40 (histogram of keys)
+  alignas(16) uint32_t count[SMP_BINS];
+  uint32_t mass_lo[SMP_BINS], mass_hi[SMP_BINS];
+};
+template <bool CUTS> constexpr size_t SMP_SHARED = ((CUTS ? sizeof(SampleCuts) : sizeof(SampleShared)) + 15) & ~size_t(15);
 
 // order-preserving map of a float to an unsigned integer (both zeros are equal)
 __device__ __forceinline__ uint32_t order_key(float z) {
@@ -64,11 +71,15 @@ __device__ __forceinline__ uint32_t order_key(float z) {
   return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 __device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
-// w (at most 1) in units of 2^-40, to the nearest
-__device__ __forceinline__ uint64_t fixed_mass(float w) {
-  const float f = w * 1099511627776.f;
-  const uint32_t high = (uint32_t)(f * 9.5367431640625e-7f);          // f 2^-20, truncated
-  return ((uint64_t)high << 20) + __float2uint_rn(f - (float)high * 1048576.f);
+// A weight 2^-o of the octave `oct` (o = oct + a fraction) as an integer of 26 bits, and such integers in units of 2^-40:
+// sums of them do not depend on the order.
+__device__ __forceinline__ uint32_t mass_bits(float o, uint32_t oct) {
+  return __float2uint_rn(__uint_as_float(__float_as_uint(ex2(-o)) + (oct << 23)) * 67108864.f);
+}
+__device__ __forceinline__ uint64_t mass_units(uint64_t bits, uint32_t oct) { return oct <= 14 ? bits << (14 - oct) : bits >> (oct - 14); }
+__device__ __forceinline__ void add_shared_if(bool yes, uint32_t* to, uint32_t x) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}"
+               ::"r"(umma::smem_u32(to)), "r"(x), "r"((uint32_t)yes) : "memory");
 }
 __device__ __forceinline__ uint64_t join64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
 
@@ -101,19 +112,21 @@ template <> struct Vec<__nv_bfloat16> {
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-template <class T>
-__global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs a) {
+template <class T, bool CUTS>
+__global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const SampleArgs a) {
+  constexpr int THREADS = SMP_THREADS<CUTS>, WARPS = THREADS / 32;
+  constexpr uint32_t ALL = 0xFFFFFFFFu;
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  SampleShared& sh = *reinterpret_cast<SampleShared*>(smem_raw);
-  T* piece = reinterpret_cast<T*>(smem_raw + ((sizeof(SampleShared) + 15) & ~size_t(15)));
+  SampleCuts& sh = *reinterpret_cast<SampleCuts*>(smem_raw);       // (without CUTS only its first part is there)
+  T* piece = reinterpret_cast<T*>(smem_raw + SMP_SHARED<CUTS>);
   int turn = 0;
 
   auto barrier = [&]() { if (C > 1) cluster.sync(); else __syncthreads(); };
   // Tell every block of the cluster W words (of the first threads, the same in each) and wait; returns those of all blocks.
-  auto exchange = [&](const uint32_t* v, int W) -> const uint32_t (*)[8] {
+  auto exchange = [&](const uint32_t* v, int W) -> const uint32_t (*)[4] {
     const int t = turn;
     turn ^= 1;
     if (tid < (int)C) {
@@ -123,9 +136,8 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     barrier();
     return sh.slots[t];
   };
-  // Combine the words of every thread of the cluster; op(x, y) folds y into x; all threads get the result.  One warp
-  // combines what the warps of a block have, and tells the blocks.
-  auto reduce = [&](auto& v, auto op) {
+  // Combine the words of every thread of the block in its first warp; op(x, y) folds y into x.
+  auto reduce_block = [&](auto& v, auto op) {
     constexpr int W = sizeof(v) / 4;
     auto fold = [&](int widest) {
       #pragma unroll
@@ -133,7 +145,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         if (d > widest) continue;
         uint32_t o[W];
         #pragma unroll
-        for (int i = 0; i < W; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+        for (int i = 0; i < W; ++i) o[i] = __shfl_xor_sync(ALL, v[i], d);
         op(v, o);
       }
     };
@@ -143,16 +155,21 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       for (int i = 0; i < W; ++i) each[warp][i] = v[i];
     __syncthreads();
     if (warp == 0) {
-      for (int i = 0; i < W; ++i) v[i] = each[lane & (SMP_WARPS - 1)][i];
-      fold(SMP_WARPS / 2);
+      for (int i = 0; i < W; ++i) v[i] = each[lane & (WARPS - 1)][i];
+      fold(WARPS / 2);
     }
-    const uint32_t (*all)[8] = exchange(v, W);
+  };
+  // The same over the cluster: all threads get the result.
+  auto reduce = [&](auto& v, auto op) {
+    constexpr int W = sizeof(v) / 4;
+    reduce_block(v, op);
+    const uint32_t (*all)[4] = exchange(v, W);
     for (int i = 0; i < W; ++i) v[i] = all[0][i];
     for (uint32_t r = 1; r < C; ++r) op(v, all[r]);
   };
   auto add = [](uint32_t& x, uint32_t y) { x = __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); };
+  auto larger = [](uint32_t* x, const uint32_t* y) { x[0] = __float_as_uint(max_nan(__uint_as_float(x[0]), __uint_as_float(y[0]))); };
 
-  cluster.sync();                      // every block's shared memory is there before the first store to it
   wait_for_previous();
   const int row = blockIdx.x / C;
   const uint32_t begin = rank * (uint32_t)a.piece;
@@ -163,7 +180,8 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   {
     const T* from = static_cast<const T*>(a.z) + (int64_t)row * a.ld + begin;
     const bool aligned = (reinterpret_cast<uintptr_t>(from) & 15u) == 0;
-    for (int v = tid; v < n_vec; v += SMP_THREADS) {
+    #pragma unroll 2
+    for (int v = tid; v < n_vec; v += THREADS) {
       if (aligned && 8 * v + 8 <= n) {
         #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h)
@@ -171,6 +189,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
                        ::"r"(umma::smem_u32(reinterpret_cast<uint8_t*>(piece + 8 * v) + 16 * h)),
                          "l"(reinterpret_cast<const uint8_t*>(from + 8 * v) + 16 * h) : "memory");
       } else {
+        #pragma unroll 1
         for (int i = 8 * v; i < 8 * v + 8; ++i) piece[i] = i < n ? from[i] : T(-CUDART_INF_F);   // behind the end: no weight
       }
     }
@@ -179,34 +198,79 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   const float min_p = a.min_p ? a.min_p[row] : a.min_p_all, top_p = a.top_p ? a.top_p[row] : a.top_p_all;
   int32_t top_k = a.top_k ? a.top_k[row] : a.top_k_all;
   if (top_k <= 0 || top_k >= a.V) top_k = 0;
-  const uint32_t k0 = (uint32_t)a.seeds[row], k1 = (uint32_t)((uint64_t)a.seeds[row] >> 32);
+  const uint64_t seed = (uint64_t)a.seeds[row];
+  const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
   const bool greedy = temperature == 0.f || top_k == 1 || top_p <= 0.f;
-  const bool by_mass = top_p < 1.f && !greedy, by_count = top_k > 0 && !greedy, cuts = by_mass || by_count;
-  if (cuts) for (int i = tid; i < SMP_BINS; i += SMP_THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
+  const bool by_mass = CUTS && top_p < 1.f && !greedy, by_count = CUTS && top_k > 0 && !greedy, cuts = by_mass || by_count;
+  if (CUTS && cuts) {
+    uint4* h = reinterpret_cast<uint4*>(sh.count);
+    for (int i = tid; i < 3 * SMP_BINS / 4; i += THREADS) h[i] = make_uint4(0, 0, 0, 0);
+  }
   if (tid == 0) { sh.n_list = 0; sh.n_sort = 0; }
+  if (C > 1) cluster.sync();                    // every block's shared memory is there before the first store to it
   asm volatile("cp.async.wait_all;" ::: "memory");
 
-  // ---- the largest logit: of the block, and of the row.  Without top-k and top-p the sums below are formed against the
-  //      block's and told together with it.
+  // Values of the block's threads in order, largest first: bitonic; partners in other warps meet in shared memory.  Only
+  // the first `many` threads have something else than 0.
+  auto sorted = [&](auto x, uint32_t many) {
+    auto* meet = reinterpret_cast<decltype(x)*>(sh.sort);
+    #pragma unroll 1
+    for (uint32_t size = 2; (size >> 1) < many && size <= (uint32_t)THREADS; size <<= 1)
+      #pragma unroll 1
+      for (uint32_t d = size >> 1; d > 0; d >>= 1) {
+        auto y = x;
+        if (d >= 32) {
+          meet[tid] = x;
+          __syncthreads();
+          y = meet[tid ^ d];
+          __syncthreads();
+        } else y = __shfl_xor_sync(ALL, x, d);
+        const bool want_larger = ((tid & d) == 0) == ((tid & size) == 0);
+        x = (x > y) == want_larger ? x : y;
+      }
+    return x;
+  };
+
+  // ---- the largest logit: of the block, and of the row.  Without cuts and min_p the sums below are formed against the
+  //      block's and told together with it.  With a small top_k: also a logit that at least top_k tokens reach, from the
+  //      threads' largest ones: the larger of any block's k-th, and of the least of the blocks' (k / C)-th.
   const bool settings_ok = temperature >= 0.f && temperature < CUDART_INF_F && min_p >= 0.f && top_p == top_p;
   const bool alone = !cuts && settings_ok && !(min_p > 0.f);
+  const bool few = by_count && top_k <= THREADS / 2;
   uint32_t top[1];
+  float zmax, reached = -CUDART_INF_F;
   {
     float m = -CUDART_INF_F;
-    for (int v = tid; v < n_vec; v += SMP_THREADS) m = max_nan(m, Vec<T>::most(piece + 8 * v));
+    for (int v = tid; v < n_vec; v += THREADS) m = max_nan(m, Vec<T>::most(piece + 8 * v));
     top[0] = __float_as_uint(m);
-    auto larger = [](uint32_t* x, const uint32_t* y) { x[0] = __float_as_uint(max_nan(__uint_as_float(x[0]), __uint_as_float(y[0]))); };
     if (alone) {
-      #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) { const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, top[0], d); larger(top, &o); }
-      if (lane == 0) sh.scan[warp][0] = top[0];
+      reduce_block(top, larger);
+      if (tid == 0) sh.scan[0][0] = top[0];
       __syncthreads();
-      top[0] = sh.scan[lane & (SMP_WARPS - 1)][0];
-      #pragma unroll
-      for (int d = SMP_WARPS / 2; d > 0; d >>= 1) { const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, top[0], d); larger(top, &o); }
-    } else reduce(top, larger);
+      zmax = __uint_as_float(sh.scan[0][0]);
+      top[0] = __float_as_uint(zmax);
+    } else if (CUTS && few) {
+      const bool bad = __syncthreads_or(!(m < CUDART_INF_F));
+      const uint32_t x = sorted(order_key(m), THREADS);
+      if (tid == 0) sh.scan[0][0] = bad ? 0x7FFFFFFFu : __float_as_uint(key_value(x));            // (NaN)
+      if (tid == top_k - 1) sh.scan[0][1] = __float_as_uint(key_value(x));
+      if (tid == (top_k + (int)C - 1) / (int)C - 1) sh.scan[0][2] = __float_as_uint(key_value(x));
+      __syncthreads();
+      const uint32_t v[3] = {sh.scan[0][0], sh.scan[0][1], sh.scan[0][2]};
+      const uint32_t (*all)[4] = exchange(v, 3);
+      zmax = -CUDART_INF_F;
+      float least = CUDART_INF_F;
+      for (uint32_t r = 0; r < C; ++r) {
+        zmax = max_nan(zmax, __uint_as_float(all[r][0]));
+        reached = fmaxf(reached, __uint_as_float(all[r][1]));
+        least = fminf(least, __uint_as_float(all[r][2]));
+      }
+      reached = fmaxf(reached, least);
+    } else {
+      reduce(top, larger);
+      zmax = __uint_as_float(top[0]);
+    }
   }
-  float zmax = __uint_as_float(top[0]);
   auto bad_row = [&]() {                              // the same in all blocks, behind a barrier: nothing touches another block any more
     if (zmax < CUDART_INF_F && zmax > -CUDART_INF_F && settings_ok) return false;
     if (rank == 0 && tid == 0) {
@@ -221,80 +285,103 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   const float floor_octaves = min_p > 0.f && !greedy ? fmaxf(-log2f(min_p), 0.f) : CUDART_INF_F;     // kept up to here
   auto octaves = [&](float z) -> float { return (zmax - z) * scale; };
   auto bin_of = [&](float o) { return (uint32_t)fminf(o * SMP_BINS_PER_OCTAVE, (float)(SMP_BINS - 1)); };
-  auto into_bin = [&](uint32_t bin, float o) {
-    atomicAdd(&sh.count[bin], 1u);
-    if (!by_mass) return;
-    const uint64_t m = fixed_mass(ex2(-o));
-    const uint32_t lo = (uint32_t)m, was = atomicAdd(&sh.mass_lo[bin], lo), hi = (uint32_t)(m >> 32) + (was + lo < was);
-    if (hi) atomicAdd(&sh.mass_hi[bin], hi);
+  // act(index in the piece, logit) for each token of this thread's that `take` picks; the few that are picked are gone through
+  // in a loop, so that the code stays short: it is fetched once a call, which is most of what a single row takes
+  auto for_each = [&](auto take, auto act) {
+    #pragma unroll 1
+    for (int v = tid; v < n_vec; v += THREADS) {
+      float z[8];
+      Vec<T>::get(piece + 8 * v, z);
+      uint32_t picked = 0;
+      #pragma unroll
+      for (int i = 0; i < 8; ++i) picked |= (uint32_t)take(z[i]) << i;
+      if (8 * v + 8 > n) picked &= (1u << (n - 8 * v)) - 1u;
+      #pragma unroll 1
+      for (; picked; picked &= picked - 1) {
+        const int i = 8 * v + __ffs(picked) - 1;
+        act(i, as_float(piece[i]));
+      }
+    }
+  };
+  // the weight of a token in units of 2^-40
+  auto mass_of = [&](float z) -> uint64_t {
+    const float o = octaves(z);
+    const uint32_t oct = min(bin_of(o) >> 6, 31u);
+    return o < 100.f ? mass_units(mass_bits(o, oct), oct) : 0;
+  };
+  // the octaves of the piece's tokens into bins, those of the last bin left out; returns the weight of these
+  auto histogram = [&]() -> float {
+    float far = 0.f;
+    for (int v = tid; v < n_vec; v += THREADS) {
+      float z[8];
+      Vec<T>::get(piece + 8 * v, z);
+      #pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float o = octaves(z[i]);
+        const bool near = o < (SMP_BINS - 1) / SMP_BINS_PER_OCTAVE;      // (behind the row's end it is infinite)
+        const uint32_t bin = bin_of(o);
+        add_shared_if(near, &sh.count[bin], 1u);
+        if (by_mass) {
+          const uint32_t m = mass_bits(o, bin >> 6);
+          add_shared_if(near, &sh.mass_lo[bin], m & 8191u);
+          add_shared_if(near, &sh.mass_hi[bin], m >> 13);
+          far += near ? 0.f : ex2(-o);
+        }
+      }
+    }
+    return far;
   };
 
   // ---- sums of the weights at temperature 1 and at the row's, of the tokens that min_p keeps; the first token with the
   //      largest logit; for top-k and top-p a histogram of the octaves, without the tokens of its last bin
   uint32_t sums[4];
   {
-    float s1 = 0.f, sT = 0.f, far = 0.f;
-    uint32_t first = 0xFFFFFFFFu;
+    float2 s1 = both(0.f), sT = both(0.f);
+    float far = 0.f;
+    uint32_t first = ALL;
     // (a block of -inf, or with a NaN or +inf, has no largest logit to go by: its sums are 0, or the row is bad)
     const float ref = fabsf(zmax) < CUDART_INF_F ? zmax : 0.f;
     const bool other = !greedy && !cuts && (scale != SMP_LOG2E || floor_octaves < CUDART_INF_F);
-    for (int v = tid; v < n_vec; v += SMP_THREADS) {
+    for (int v = tid; v < n_vec; v += THREADS) {
       float z[8];
       Vec<T>::get(piece + 8 * v, z);
-      float p[2] = {0.f, 0.f};
       #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i & 1] += ex2((z[i] - ref) * SMP_LOG2E);
-      s1 += p[0] + p[1];
-      if (cuts) {
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float o = octaves(z[i]);
-          if (o < (SMP_BINS - 1) / SMP_BINS_PER_OCTAVE) into_bin(bin_of(o), o);      // (tokens behind the end are infinitely far)
-          else if (by_mass) far += ex2(-o);
-        }
-      } else if (other) {
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) { const float o = (ref - z[i]) * scale; sT += o <= floor_octaves ? ex2(-o) : 0.f; }
-      } else if (greedy) {
-        #pragma unroll
-        for (int i = 7; i >= 0; --i) if (z[i] == zmax) first = min(first, begin + 8 * v + i);
+      for (int i = 0; i < 4; ++i) {
+        const float2 x = mul2(add2(make_float2(z[2 * i], z[2 * i + 1]), both(-ref)), both(SMP_LOG2E));
+        s1 = add2(s1, make_float2(ex2(x.x), ex2(x.y)));
       }
     }
-    sums[0] = __float_as_uint(s1); sums[1] = __float_as_uint(other ? sT : s1); sums[2] = first; sums[3] = __float_as_uint(far);
-    if (alone) {
-      // words of a block: its largest logit, its sums against that, its first token with it
-      uint32_t v[4] = {sums[0], sums[1], first, top[0]};
-      #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        add(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d));
-        if (other) add(v[1], __shfl_xor_sync(0xFFFFFFFFu, v[1], d));
-        if (greedy) v[2] = min(v[2], __shfl_xor_sync(0xFFFFFFFFu, v[2], d));
-      }
-      if (lane == 0)
-        for (int i = 0; i < 3; ++i) sh.warp[turn][warp][i] = v[i];
-      __syncthreads();
-      if (warp == 0) {
-        for (int i = 0; i < 3; ++i) v[i] = sh.warp[turn][lane & (SMP_WARPS - 1)][i];
+    if (CUTS && cuts) {
+      if (!few) far = histogram();
+    } else if (other) {
+      for (int v = tid; v < n_vec; v += THREADS) {
+        float z[8];
+        Vec<T>::get(piece + 8 * v, z);
         #pragma unroll
-        for (int d = SMP_WARPS / 2; d > 0; d >>= 1) {
-          add(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], d));
-          add(v[1], __shfl_xor_sync(0xFFFFFFFFu, v[1], d));
-          v[2] = min(v[2], __shfl_xor_sync(0xFFFFFFFFu, v[2], d));
-        }
-        if (!other) v[1] = v[0];
+        for (int i = 0; i < 8; ++i) { const float o = (ref - z[i]) * scale; sT.x += o <= floor_octaves ? ex2(-o) : 0.f; }
       }
-      const uint32_t (*all)[8] = exchange(v, 4);
+    } else if (greedy) {
+      for_each([&](float z) { return z == zmax; }, [&](int i, float) { first = min(first, begin + i); });
+    }
+    sums[0] = __float_as_uint(s1.x + s1.y); sums[1] = other ? __float_as_uint(sT.x) : sums[0]; sums[2] = first; sums[3] = __float_as_uint(far);
+    if (alone) {
+      // words of a block: its sums against its largest logit, its first token with it, that logit
+      reduce_block(sums, [&](uint32_t* x, const uint32_t* y) { add(x[0], y[0]); add(x[1], y[1]); x[2] = min(x[2], y[2]); });
+      if (!other) sums[1] = sums[0];
+      sums[3] = top[0];
+      const uint32_t (*all)[4] = exchange(sums, 4);
       zmax = -CUDART_INF_F;
       for (uint32_t r = 0; r < C; ++r) zmax = max_nan(zmax, __uint_as_float(all[r][3]));
       if (bad_row()) return;
-      s1 = 0.f; sT = 0.f; first = 0xFFFFFFFFu;
+      float u1 = 0.f, uT = 0.f;
+      first = ALL;
       for (uint32_t r = 0; r < C; ++r) {
         const float less = zmax - __uint_as_float(all[r][3]);
-        s1 += __uint_as_float(all[r][0]) * ex2(-less * SMP_LOG2E);
-        sT += __uint_as_float(all[r][1]) * ex2(-less * scale);
+        u1 += __uint_as_float(all[r][0]) * ex2(-less * SMP_LOG2E);
+        uT += __uint_as_float(all[r][1]) * ex2(-less * scale);
         if (less == 0.f) first = min(first, all[r][2]);
       }
-      sums[0] = __float_as_uint(s1); sums[1] = __float_as_uint(sT); sums[2] = first;
+      sums[0] = __float_as_uint(u1); sums[1] = __float_as_uint(uT); sums[2] = first;
     } else {
       reduce(sums, [&](uint32_t* x, const uint32_t* y) { add(x[0], y[0]); add(x[1], y[1]); x[2] = min(x[2], y[2]); add(x[3], y[3]); });
     }
@@ -305,8 +392,8 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     return;
   }
   float weight = __uint_as_float(sums[1]);       // of the tokens in the race
-  // the time at which a token finishes, in 64 bits
-  auto finish = [&](uint32_t token, float z) -> double {
+  // the 32 random bits of a token
+  auto random_bits = [&](uint32_t token) -> uint32_t {
     const uint32_t half = token & 7u, s = 16 * (half & 1u);
     uint32_t bits = 0;
     #pragma unroll 1
@@ -315,10 +402,27 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       const uint32_t w = half < 2 ? r.x : half < 4 ? r.y : half < 6 ? r.z : r.w;
       bits = (bits << 16) | ((w >> s) & 0xFFFFu);
     }
-    const double e = -log1p(-((double)bits + 0.5) * 2.3283064365386963e-10);
+    return bits;
+  };
+  // The time at which a token finishes: in 64 bits, and, off by less than 1e-4 of itself, in 32.
+  auto finish = [&](uint32_t token, float z) -> double {
+    const double e = -log1p(-((double)random_bits(token) + 0.5) * 2.3283064365386963e-10);
     return e * exp(((double)zmax - (double)z) * fmin(1.0 / (double)temperature, 1e30));
   };
-  // first to finish, the lower index where two finish together; words: time, index, a flag
+  auto finish32 = [&](uint32_t token, float z) -> float {
+    const uint32_t bits = random_bits(token);
+    const float e = bits < 0x40000000u ? -log1pf(-((float)bits + 0.5f) * 2.3283064e-10f) : -logf(((float)~bits + 0.5f) * 2.3283064e-10f);
+    return e * ex2(octaves(z));
+  };
+  // The first to finish, and how near the second comes: words first time, its token, second time, a flag.
+  auto two_first = [](uint32_t* x, const uint32_t* y) {
+    const float a1 = __uint_as_float(x[0]), b1 = __uint_as_float(y[0]), a2 = __uint_as_float(x[2]), b2 = __uint_as_float(y[2]);
+    x[2] = __float_as_uint(fminf(fmaxf(a1, b1), fminf(a2, b2)));
+    if (b1 < a1) { x[0] = y[0]; x[1] = y[1]; }
+    x[3] |= y[3];
+  };
+  const float TIE = 1.001f;      // times that 32 bits tell apart
+  // the first in 64 bits, the lower index where two finish together; words: time, index, a flag
   auto earlier = [](uint32_t* x, const uint32_t* y) {
     const double p = __longlong_as_double((long long)join64(x[0], x[1])), q = __longlong_as_double((long long)join64(y[0], y[1]));
     x[3] |= y[3];
@@ -330,46 +434,51 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
 
   // ---- where the row, sorted by logit (equal ones by index), is cut: keys above key_cut stay, and of those equal to it
   //      the ones up to index_cut
-  uint32_t key_cut = 0, index_cut = 0xFFFFFFFFu;
-  if (cuts) {
+  uint32_t key_cut = 0, index_cut = ALL;
+  if constexpr (CUTS) if (cuts) {
     // The bin of the histograms in which the search ends: the one with the target-th token, or the one where the mass
-    // reaches `target` (of_total: times the mass of all); beyond the histogram there are far_count tokens of far_mass, in
-    // its last bin.  Each block adds up its share of the bins over the cluster.
-    auto find = [&](bool mass_wanted, double target, bool of_total, uint32_t before, uint64_t before_mass, bool with_far) {
-      const int per_block = SMP_BINS / (int)C, per = max(1, per_block / SMP_THREADS);
-      uint32_t c[4]; uint64_t m[4];
+    // reaches `target` (of_total: times the mass of all); beyond the histogram there are, with_far, the tokens of its last
+    // bin.  Each block adds up its share of the bins over the cluster, in place: no other block reads that part of its own.
+    struct Found { Cut cut; double target; };
+    auto find = [&](bool mass_wanted, double target, bool of_total, uint32_t before, uint64_t before_mass, bool with_far) -> Found {
+      const int per_block = SMP_BINS / (int)C, per = max(1, per_block / THREADS), bin0 = (int)rank * per_block + tid * per;
       uint32_t c_sum = 0; uint64_t m_sum = 0;
-      #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = 0; m[i] = 0;
-        if (i >= per || tid * per >= per_block) continue;
-        const int bin = (int)rank * per_block + tid * per + i;
-        #pragma unroll 4
-        for (uint32_t r = 0; r < C; ++r) {
-          c[i] += *cluster.map_shared_rank(&sh.count[bin], r);
-          if (by_mass) m[i] += join64(*cluster.map_shared_rank(&sh.mass_lo[bin], r), *cluster.map_shared_rank(&sh.mass_hi[bin], r));
+      if (tid * per < per_block)
+        #pragma unroll 1
+        for (int i = bin0; i < bin0 + per; ++i) {
+          uint32_t c = 0; uint64_t m = 0;
+          #pragma unroll
+          for (uint32_t r = 0; r < SMP_MAX_CLUSTER; ++r) {       // (no branches: the loads are all in flight together)
+            const uint32_t from = min(r, C - 1), one = r < C ? 1u : 0u;
+            c += one * *cluster.map_shared_rank(&sh.count[i], from);
+            const uint32_t lo = one * *cluster.map_shared_rank(&sh.mass_lo[i], from), hi = one * *cluster.map_shared_rank(&sh.mass_hi[i], from);
+            m += with_far ? ((uint64_t)hi << 13) + lo : join64(lo, hi);
+          }
+          if (with_far) m = mass_units(m, (uint32_t)i >> 6);
+          sh.count[i] = c; sh.mass_lo[i] = (uint32_t)m; sh.mass_hi[i] = (uint32_t)(m >> 32);
+          c_sum += c; m_sum += m;
         }
-        c_sum += c[i]; m_sum += m[i];
-      }
       uint32_t c_in = c_sum; uint64_t m_in = m_sum;               // inclusive sums over the threads
       #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, c_in, d);
-        const uint64_t y = __shfl_up_sync(0xFFFFFFFFu, m_in, d);
+        const uint32_t x = __shfl_up_sync(ALL, c_in, d);
+        const uint64_t y = __shfl_up_sync(ALL, m_in, d);
         if (lane >= d) { c_in += x; m_in += y; }
       }
       if (lane == 31) { sh.scan[warp][0] = c_in; sh.scan[warp][1] = (uint32_t)m_in; sh.scan[warp][2] = (uint32_t)(m_in >> 32); }
       __syncthreads();
       uint32_t total[3] = {0, 0, 0}, c_base = 0;
       uint64_t m_all = 0, m_base = 0;
-      for (int w = 0; w < SMP_WARPS; ++w) {
+      #pragma unroll 1
+      for (int w = 0; w < WARPS; ++w) {
         if (w == warp) { c_base = total[0]; m_base = m_all; }
         total[0] += sh.scan[w][0]; m_all += join64(sh.scan[w][1], sh.scan[w][2]);
       }
       total[1] = (uint32_t)m_all; total[2] = (uint32_t)(m_all >> 32);
-      const uint32_t (*all)[8] = exchange(total, 3);
+      const uint32_t (*all)[4] = exchange(total, 3);
       uint32_t c_at = before + c_base + c_in - c_sum, c_end = before;
       uint64_t m_at = before_mass + m_base + m_in - m_sum, m_end = before_mass;
+      #pragma unroll 1
       for (uint32_t r = 0; r < C; ++r) {
         if (r == rank) { c_at += c_end - before; m_at += m_end - before_mass; }
         c_end += all[r][0]; m_end += join64(all[r][1], all[r][2]);
@@ -377,118 +486,128 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       const uint32_t far_count = with_far ? (uint32_t)a.V - c_end : 0;
       const uint64_t far_mass = with_far ? (uint64_t)((double)__uint_as_float(sums[3]) * 1099511627776.0) : 0;
       if (of_total) target *= (double)(m_end + far_mass);
-      #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (c[i] > 0) {
-          const bool here = mass_wanted ? (double)m_at < target && (double)(m_at + m[i]) >= target
-                                        : (double)c_at < target && (double)(c_at + c[i]) >= target;
-          if (here) {
-            const Cut cut{(uint32_t)((int)rank * per_block + tid * per + i), c_at, c[i], (uint32_t)m[i], (uint32_t)(m[i] >> 32),
-                          (uint32_t)m_at, (uint32_t)(m_at >> 32)};
-            for (uint32_t r = 0; r < C; ++r) *cluster.map_shared_rank(&sh.cut, r) = cut;
-          }
+      const Cut beyond{SMP_BINS - 1, c_end, far_count, (uint32_t)far_mass, (uint32_t)(far_mass >> 32), (uint32_t)m_end, (uint32_t)(m_end >> 32)};
+      if (mass_wanted ? (double)m_end < target : (double)c_end < target) {       // the same in all blocks
+        barrier();
+        return Found{beyond, target};
+      }
+      // the thread whose bins hold it
+      if (c_sum > 0 && (mass_wanted ? (double)m_at < target && (double)(m_at + m_sum) >= target : (double)c_at < target && (double)(c_at + c_sum) >= target)) {
+        int i = bin0;
+        for (;; ++i) {
+          const uint32_t c = sh.count[i]; const uint64_t m = join64(sh.mass_lo[i], sh.mass_hi[i]);
+          if (i == bin0 + per - 1 || (c > 0 && (mass_wanted ? (double)(m_at + m) >= target : (double)(c_at + c) >= target))) break;
+          c_at += c; m_at += m;
         }
-        c_at += c[i]; m_at += m[i];
+        const Cut cut{(uint32_t)i, c_at, sh.count[i], sh.mass_lo[i], sh.mass_hi[i], (uint32_t)m_at, (uint32_t)(m_at >> 32)};
+        #pragma unroll 1
+        for (uint32_t r = 0; r < C; ++r) *cluster.map_shared_rank(&sh.cut, r) = cut;
       }
       barrier();
-      struct Found { Cut cut; double target; uint64_t total; } f{sh.cut, target, m_end + far_mass};
-      if (mass_wanted ? (double)m_end < target : (double)c_end < target)
-        f.cut = Cut{SMP_BINS - 1, c_end, far_count, (uint32_t)far_mass, (uint32_t)(far_mass >> 32), (uint32_t)m_end, (uint32_t)(m_end >> 32)};
-      return f;
+      return Found{sh.cut, target};
     };
-    // The tokens that `take` picks (at most SMP_SORT in the cluster), in the first block, in order, one a thread (0: none).
-    auto gather_sorted = [&](auto take, uint32_t many) -> uint64_t {
-      SampleShared& first = *cluster.map_shared_rank(&sh, 0);
-      for (int v = tid; v < n_vec; v += SMP_THREADS) {
-        float z[8];
-        Vec<T>::get(piece + 8 * v, z);
-        #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (take(z[i]) && 8 * v + i < n) {
-            const uint32_t at = atomicAdd(&first.n_sort, 1u);
-            if (at < SMP_SORT) first.sort[at] = ((uint64_t)order_key(z[i]) << 32) | (0xFFFFFFFFu - (begin + 8 * v + i));
-          }
-      }
-      barrier();
-      if (rank != 0) return 0;
-      const uint32_t have = min(sh.n_sort, (uint32_t)SMP_SORT);
-      uint64_t x = tid < (int)have ? sh.sort[tid] : 0;
-      __syncthreads();
+    // The tokens that `take` picks, if there are at most SMP_SORT in the cluster: in the first block, in order, one a
+    // thread (0: none).  Returns how many there are.
+    auto gather_sorted = [&](auto take, uint64_t& x) -> uint32_t {
       if (tid == 0) sh.n_sort = 0;
-      // bitonic, largest first; partners in other warps meet in shared memory
-      for (uint32_t size = 2; (size >> 1) < many && size <= SMP_SORT; size <<= 1)
-        for (uint32_t d = size >> 1; d > 0; d >>= 1) {
-          uint64_t y;
-          if (d >= 32) {
-            sh.sort[tid] = x;
-            __syncthreads();
-            y = sh.sort[tid ^ d];
-            __syncthreads();
-          } else y = __shfl_xor_sync(0xFFFFFFFFu, x, d);
-          const bool want_larger = ((tid & d) == 0) == ((tid & size) == 0);
-          x = (x > y) == want_larger ? x : y;
-        }
-      return x;
+      __syncthreads();
+      for_each(take, [&](int i, float z) {
+        const uint32_t at = atomicAdd(&sh.n_sort, 1u);
+        if (at < SMP_SORT) sh.sort[at] = ((uint64_t)order_key(z) << 32) | (ALL - (begin + i));
+      });
+      __syncthreads();
+      const uint32_t mine = sh.n_sort, which = min(mine, (uint32_t)SMP_SORT);
+      const uint64_t own = tid < (int)which ? sh.sort[tid] : 0;
+      const uint32_t (*all)[4] = exchange(&mine, 1);
+      uint32_t before = 0, many = 0;
+      for (uint32_t r = 0; r < C; ++r) { if (r == rank) before = many; many += all[r][0]; }
+      x = 0;
+      if (many > SMP_SORT) return many;                    // the same in all blocks
+      if (tid < (int)which) *cluster.map_shared_rank(&sh.sort[before + tid], 0) = own;
+      barrier();
+      if (rank != 0) return many;
+      if (tid < (int)many) x = sh.sort[tid];
+      __syncthreads();
+      x = sorted(x, many);
+      return many;
     };
     // inclusive sum over the block's threads
     auto scan_mass = [&](uint64_t m) -> uint64_t {
       #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) { const uint64_t y = __shfl_up_sync(0xFFFFFFFFu, m, d); if (lane >= d) m += y; }
+      for (int d = 1; d < 32; d <<= 1) { const uint64_t y = __shfl_up_sync(ALL, m, d); if (lane >= d) m += y; }
       if (lane == 31) { sh.scan[warp][0] = (uint32_t)m; sh.scan[warp][1] = (uint32_t)(m >> 32); }
       __syncthreads();
+      #pragma unroll 1
       for (int w = 0; w < warp; ++w) m += join64(sh.scan[w][0], sh.scan[w][1]);
       __syncthreads();
       return m;
     };
-    auto mass_of = [&](uint64_t x) -> uint64_t { return x ? fixed_mass(ex2(-octaves(key_value((uint32_t)(x >> 32))))) : 0; };
 
-    auto f = by_count ? find(false, (double)top_k, false, 0, 0, true) : find(true, (double)top_p, true, 0, 0, true);
-    if (f.cut.before + f.cut.count <= SMP_SORT) {
-      // ---- few tokens can stay: the first block sorts them, cuts by all three rules and runs the race
-      const uint32_t many = f.cut.before + f.cut.count, bin = f.cut.bin;
-      const uint64_t x = gather_sorted([&](float z) { return bin_of(octaves(z)) <= bin; }, many);
-      if (rank != 0) return;
+    // ---- few tokens can stay: the first block sorts them, cuts by all three rules and runs the race
+    auto among_few = [&](uint64_t x, double mass_target) {
       bool in = x != 0 && (!by_count || tid < top_k);
       const float z = key_value((uint32_t)(x >> 32));
       if (by_mass) {
-        const uint64_t m = in ? mass_of(x) : 0, incl = scan_mass(m);
-        if (tid == SMP_THREADS - 1) { sh.scan[0][2] = (uint32_t)incl; sh.scan[0][3] = (uint32_t)(incl >> 32); }
+        const uint64_t m = in ? mass_of(z) : 0, incl = scan_mass(m);
+        if (tid == THREADS - 1) { sh.scan[0][2] = (uint32_t)incl; sh.scan[0][3] = (uint32_t)(incl >> 32); }
         __syncthreads();
-        const double target = by_count ? (double)top_p * (double)join64(sh.scan[0][2], sh.scan[0][3]) : f.target;
-        in = in && (tid == 0 || (double)(incl - m) < target);
+        if (by_count) mass_target = (double)top_p * (double)join64(sh.scan[0][2], sh.scan[0][3]);
+        in = in && (tid == 0 || (double)(incl - m) < mass_target);
       }
       in = in && octaves(z) <= floor_octaves;
-      uint32_t win[4];
-      const uint32_t token = 0xFFFFFFFFu - (uint32_t)x;
-      words(win, in ? finish(token, z) : CUDART_INF, in ? token : 0xFFFFFFFFu, __float_as_uint(0.f));
-      #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        uint32_t o[4];
-        #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, win[i], d);
-        earlier(win, o);
+      const uint32_t token = ALL - (uint32_t)x;
+      uint32_t win[4] = {__float_as_uint(CUDART_INF_F), ALL, __float_as_uint(CUDART_INF_F), 0u};
+      if (in) { win[0] = __float_as_uint(finish32(token, z)); win[1] = token; }
+      const float mine = __uint_as_float(win[0]);
+      reduce_block(win, two_first);
+      if (tid == 0) { sh.scan[0][0] = win[0]; sh.scan[0][1] = win[1]; sh.scan[0][2] = win[2]; }
+      __syncthreads();
+      uint32_t who = sh.scan[0][1];
+      const float first = __uint_as_float(sh.scan[0][0]);
+      if (__uint_as_float(sh.scan[0][2]) <= first * TIE || !(first < 1e37f)) {       // the same for all threads
+        uint32_t v[4];
+        words(v, CUDART_INF, ALL, 0u);
+        if (in && (mine <= first * TIE || !(first < 1e37f))) words(v, finish(token, z), token, 0u);
+        reduce_block(v, earlier);
+        if (tid == 0) sh.scan[0][0] = v[2];
+        __syncthreads();
+        who = sh.scan[0][0];
       }
-      uint32_t (*each)[4] = sh.warp[turn];
-      __syncthreads();
-      if (lane == 0)
-        for (int i = 0; i < 4; ++i) each[warp][i] = win[i];
-      __syncthreads();
-      for (int w = 0; w < SMP_WARPS; ++w) earlier(win, each[w]);
-      if (in && token == win[2]) { a.ids[row] = (int32_t)token; a.logp[row] = (z - zmax) - log_sum; }
+      if (in && token == who) { a.ids[row] = (int32_t)token; a.logp[row] = (z - zmax) - log_sum; }
+    };
+    if (few) {
+      uint64_t x;
+      const uint32_t many = gather_sorted([&](float z) { return z >= reached; }, x);
+      if (many <= SMP_SORT) {
+        if (rank == 0) among_few(x, 0.0);
+        return;
+      }
+      sums[3] = __float_as_uint(histogram());                  // (too many equal ones): as with a large top_k
+      sums[0] = sums[1] = sums[2] = 0;
+      reduce(sums, [&](uint32_t* p, const uint32_t* q) { add(p[3], q[3]); });
+    }
+    const Found f = find(!by_count, by_count ? (double)top_k : (double)top_p, !by_count, 0, 0, true);
+    if (f.cut.before + f.cut.count <= SMP_SORT) {
+      const uint32_t bin = f.cut.bin;
+      uint64_t x;
+      gather_sorted([&](float z) { return bin_of(octaves(z)) <= bin; }, x);
+      if (rank == 0) among_few(x, f.target);
       return;
     }
     // From a bin to the last token that stays.  Returns the mass of what stays.
-    auto search = [&](const decltype(f)& found, bool mass_wanted) -> uint64_t {
+    auto search = [&](const Found& found, bool mass_wanted) -> uint64_t {
       Cut cut = found.cut;
       const double target = found.target;
       if (cut.count <= SMP_SORT) {
-        const uint64_t x = gather_sorted([&](float z) { return bin_of(octaves(z)) == cut.bin; }, cut.count);
+        uint64_t x;
+        gather_sorted([&](float z) { return bin_of(octaves(z)) == cut.bin; }, x);
         if (rank == 0) {
-          const uint64_t before = join64(cut.before_lo, cut.before_hi), m = by_mass ? mass_of(x) : 0, incl = before + (by_mass ? scan_mass(m) : 0);
+          const uint64_t before = join64(cut.before_lo, cut.before_hi), m = by_mass && x != 0 ? mass_of(key_value((uint32_t)(x >> 32))) : 0;
+          const uint64_t incl = before + (by_mass ? scan_mass(m) : 0);
           const bool stays = x != 0 && (mass_wanted ? tid == 0 || (double)(incl - m) < target : tid < (int)(top_k - cut.before));
           const int last = __syncthreads_count(stays) - 1;
           if (tid == last) {
-            const Last l{(uint32_t)(x >> 32), 0xFFFFFFFFu - (uint32_t)x, (uint32_t)incl, (uint32_t)(incl >> 32)};
+            const Last l{(uint32_t)(x >> 32), ALL - (uint32_t)x, (uint32_t)incl, (uint32_t)(incl >> 32)};
             for (uint32_t r = 0; r < C; ++r) *cluster.map_shared_rank(&sh.last, r) = l;
           }
         }
@@ -498,86 +617,79 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       }
       // Many tokens in one bin: their range of keys is cut into bins again, until a single key is left.
       uint32_t key_low = 0, key_high = 0;
+      #pragma unroll 1
       for (int level = 0; level < 5; ++level) {      // 32 bits of key in steps of 11, and the look that finds one key
-        uint32_t range[2] = {0xFFFFFFFFu, 0};
-        for (int v = tid; v < n_vec; v += SMP_THREADS) {
-          float z[8];
-          Vec<T>::get(piece + 8 * v, z);
-          #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (8 * v + i >= n) break;
-            const uint32_t key = order_key(z[i]);
-            if (level == 0 ? bin_of(octaves(z[i])) == cut.bin : key >= key_low && key <= key_high) { range[0] = min(range[0], key); range[1] = max(range[1], key); }
-          }
-        }
+        auto inside = [&](float z) { return level == 0 ? bin_of(octaves(z)) == cut.bin : order_key(z) >= key_low && order_key(z) <= key_high; };
+        uint32_t range[2] = {ALL, 0};
+        for_each(inside, [&](int, float z) { range[0] = min(range[0], order_key(z)); range[1] = max(range[1], order_key(z)); });
         reduce(range, [](uint32_t* x, const uint32_t* y) { x[0] = min(x[0], y[0]); x[1] = max(x[1], y[1]); });
         key_low = range[0]; key_high = range[1];
         if (key_low >= key_high) break;
         int shift = 0;
         while (((key_high - key_low) >> shift) >= SMP_BINS) ++shift;
-        for (int i = tid; i < SMP_BINS; i += SMP_THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
+        for (int i = tid; i < SMP_BINS; i += THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
         __syncthreads();
-        for (int v = tid; v < n_vec; v += SMP_THREADS) {
-          float z[8];
-          Vec<T>::get(piece + 8 * v, z);
-          #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (8 * v + i >= n) break;
-            const uint32_t key = order_key(z[i]);
-            if (key >= key_low && key <= key_high) into_bin((key_high - key) >> shift, octaves(z[i]));
-          }
-        }
+        for_each([&](float z) { return order_key(z) >= key_low && order_key(z) <= key_high; },
+                 [&](int, float z) {
+                   const uint32_t bin = (key_high - order_key(z)) >> shift;
+                   atomicAdd(&sh.count[bin], 1u);
+                   if (!by_mass) return;
+                   const uint64_t m = mass_of(z);
+                   const uint32_t lo = (uint32_t)m, was = atomicAdd(&sh.mass_lo[bin], lo), hi = (uint32_t)(m >> 32) + (was + lo < was);
+                   if (hi) atomicAdd(&sh.mass_hi[bin], hi);
+                 });
         barrier();
         cut = find(mass_wanted, target, false, cut.before, join64(cut.before_lo, cut.before_hi), false).cut;
         if (cut.count == 0) {                        // the mass falls short of the target by rounding: all of them stay
-          key_cut = key_low; index_cut = 0xFFFFFFFFu;
+          key_cut = key_low; index_cut = ALL;
           return (uint64_t)target;
         }
         key_high -= cut.bin << shift;
         key_low = max(key_low, key_high - ((1u << shift) - 1));
       }
       // how many of the tokens with this key stay, and up to which index
-      const uint64_t before = join64(cut.before_lo, cut.before_hi), mass = by_mass ? fixed_mass(ex2(-octaves(key_value(key_low)))) : 0;
+      const uint64_t before = join64(cut.before_lo, cut.before_hi), mass = by_mass ? mass_of(key_value(key_low)) : 0;
       uint32_t stay = cut.count;
       if (!mass_wanted) stay = (uint32_t)target - cut.before;
       else if (mass > 0) stay = (uint32_t)fmin((double)cut.count, fmax(1.0, ceil((target - (double)before) / (double)mass)));
-      key_cut = key_low; index_cut = 0xFFFFFFFFu;
+      key_cut = key_low; index_cut = ALL;
       if (stay < cut.count) {
         // warps hold runs of eights in index order: tokens of this key a warp, then a block has
-        const int per_warp = (n_vec + SMP_WARPS - 1) / SMP_WARPS, v0 = warp * per_warp, v1 = min(n_vec, v0 + per_warp);
+        const int per_warp = (n_vec + WARPS - 1) / WARPS, v0 = warp * per_warp, v1 = min(n_vec, v0 + per_warp);
+        auto bits_of = [&](int v) -> uint32_t {
+          uint32_t bits = 0;
+          if (v < v1) {
+            float z[8];
+            Vec<T>::get(piece + 8 * v, z);
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) bits |= (uint32_t)(8 * v + i < n && order_key(z[i]) == key_cut) << i;
+          }
+          return bits;
+        };
         uint32_t mine = 0;
-        for (int v = v0 + lane; v < v1; v += 32) {
-          float z[8];
-          Vec<T>::get(piece + 8 * v, z);
-          #pragma unroll
-          for (int i = 0; i < 8; ++i) mine += 8 * v + i < n && order_key(z[i]) == key_cut;
-        }
-        mine = __reduce_add_sync(0xFFFFFFFFu, mine);
+        #pragma unroll 1
+        for (int v = v0 + lane; v < v1; v += 32) mine += __popc(bits_of(v));
+        mine = __reduce_add_sync(ALL, mine);
         __syncthreads();
         if (lane == 0) sh.scan[warp][3] = mine;
         __syncthreads();
         uint32_t all_of_block = 0, at = 0;
-        for (int w = 0; w < SMP_WARPS; ++w) { if (w == warp) at = all_of_block; all_of_block += sh.scan[w][3]; }
-        const uint32_t (*all)[8] = exchange(&all_of_block, 1);
+        for (int w = 0; w < WARPS; ++w) { if (w == warp) at = all_of_block; all_of_block += sh.scan[w][3]; }
+        const uint32_t (*all)[4] = exchange(&all_of_block, 1);
         for (uint32_t r = 0; r < rank; ++r) at += all[r][0];
-        uint32_t who[1] = {0xFFFFFFFFu};
+        uint32_t who[1] = {ALL};
         if (at < stay && at + mine >= stay) {        // the last that stays is one of this warp's
-          for (int v = v0; v < v1 && who[0] == 0xFFFFFFFFu; v += 32) {
-            uint32_t bits = 0;
-            if (v + lane < v1) {
-              float z[8];
-              Vec<T>::get(piece + 8 * (v + lane), z);
-              #pragma unroll
-              for (int i = 0; i < 8; ++i) bits |= (uint32_t)(8 * (v + lane) + i < n && order_key(z[i]) == key_cut) << i;
-            }
+          #pragma unroll 1
+          for (int v = v0; v < v1 && who[0] == ALL; v += 32) {
+            const uint32_t bits = bits_of(v + lane);
             uint32_t in = __popc(bits);
             #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) { const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, in, d); if (lane >= d) in += x; }
-            uint32_t at_lane = at + in - __popc(bits), mine_at = 0xFFFFFFFFu;
+            for (int d = 1; d < 32; d <<= 1) { const uint32_t x = __shfl_up_sync(ALL, in, d); if (lane >= d) in += x; }
+            uint32_t at_lane = at + in - __popc(bits), mine_at = ALL;
             for (int i = 0; i < 8; ++i)
               if ((bits >> i) & 1u) { if (++at_lane == stay) mine_at = begin + 8 * (v + lane) + i; }
-            who[0] = __reduce_min_sync(0xFFFFFFFFu, mine_at);
-            at += __shfl_sync(0xFFFFFFFFu, in, 31);
+            who[0] = __reduce_min_sync(ALL, mine_at);
+            at += __shfl_sync(ALL, in, 31);
           }
         }
         reduce(who, [](uint32_t* x, const uint32_t* y) { x[0] = min(x[0], y[0]); });
@@ -587,34 +699,20 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     };
     uint64_t stays = search(f, !by_count);
     if (by_count && by_mass) {
-      if (f.cut.count > SMP_SORT) {                  // the histogram has been used for keys
-        for (int i = tid; i < SMP_BINS; i += SMP_THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
-        __syncthreads();
-        for (int v = tid; v < n_vec; v += SMP_THREADS) {
-          float z[8];
-          Vec<T>::get(piece + 8 * v, z);
-          #pragma unroll
-          for (int i = 0; i < 8; ++i) { const float o = octaves(z[i]); if (o < (SMP_BINS - 1) / SMP_BINS_PER_OCTAVE) into_bin(bin_of(o), o); }
-        }
-        barrier();
-      }
-      const auto g = find(true, (double)top_p * (double)stays, false, 0, 0, true);
-      stays = search(g, true);
+      if (C > 1) cluster.sync();                     // find() has added the blocks' histograms up in place, search() may have used them
+      for (int i = tid; i < SMP_BINS; i += THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
+      __syncthreads();
+      sums[3] = __float_as_uint(histogram());
+      sums[0] = sums[1] = sums[2] = 0;
+      reduce(sums, [&](uint32_t* p, const uint32_t* q) { add(p[3], q[3]); });
+      stays = search(find(true, (double)top_p * (double)stays, false, 0, 0, true), true);
     }
     weight = (float)((double)stays * 9.094947017729282e-13);      // 2^-40
     if (!by_mass || floor_octaves < CUDART_INF_F) {               // not known from the search, or min_p takes some out
       uint32_t w[1];
       float s = 0.f;
-      for (int v = tid; v < n_vec; v += SMP_THREADS) {
-        float z[8];
-        Vec<T>::get(piece + 8 * v, z);
-        #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t key = order_key(z[i]);
-          const float o = octaves(z[i]);
-          if ((key > key_cut || (key == key_cut && begin + 8 * v + i <= index_cut)) && o <= floor_octaves) s += ex2(-o);
-        }
-      }
+      for_each([&](float z) { return order_key(z) >= key_cut && octaves(z) <= floor_octaves; },
+               [&](int i, float z) { if (order_key(z) > key_cut || begin + i <= index_cut) s += ex2(-octaves(z)); });
       w[0] = __float_as_uint(s);
       reduce(w, [&](uint32_t* x, const uint32_t* y) { add(x[0], y[0]); });
       weight = __uint_as_float(w[0]);
@@ -630,75 +728,82 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   // candidates: upper 16 bits <= 65536 L w / weight (with room for the rounding of w and weight)
   const float reach = SMP_LEAD / weight;
   const float bound = 65536.f * reach * 1.001f;
-  for (int v = tid; v < n_vec; v += SMP_THREADS) {
+  for (int v = tid; v < n_vec; v += THREADS) {
     float z[8];
     Vec<T>::get(piece + 8 * v, z);
     const uint4 r = philox4x32_10((begin >> 3) + v, 0, 0, 0, k0, k1);
     const uint32_t word[4] = {r.x, r.y, r.z, r.w};
-    float lead = -1.f;
+    float lead[2] = {-1.f, -1.f};
     #pragma unroll
-    for (int i = 0; i < 8; ++i) {                   // 2^23 + bound w + 1 against 2^23 + the upper bits
-      const float u = __uint_as_float(__byte_perm(word[i >> 1], 0x4B000000u, (i & 1) ? 0x7632 : 0x7610));
-      lead = fmaxf(lead, fmaf(ex2((z[i] - zmax) * scale), bound, 8388609.f) - u);
+    for (int i = 0; i < 4; ++i) {                 // 2^23 + 1 + bound w against 2^23 + the upper bits
+      const float2 x = mul2(add2(make_float2(z[2 * i], z[2 * i + 1]), both(-zmax)), both(scale));
+      const float2 may = fma2(make_float2(ex2(x.x), ex2(x.y)), both(bound), both(8388609.f));
+      lead[0] = fmaxf(lead[0], may.x - __uint_as_float(__byte_perm(word[i], 0x4B000000u, 0x7610)));
+      lead[1] = fmaxf(lead[1], may.y - __uint_as_float(__byte_perm(word[i], 0x4B000000u, 0x7632)));
     }
-    if (lead >= 0.f) {
+    if (fmaxf(lead[0], lead[1]) >= 0.f) {
       #pragma unroll 1
       for (int i = 0; i < 8; ++i) {
         const uint32_t w = i < 2 ? r.x : i < 4 ? r.y : i < 6 ? r.z : r.w, upper = (i & 1) ? w >> 16 : w & 0xFFFFu;
         const float zi = as_float(piece[8 * v + i]);
-        if (!((float)upper <= fmaf(ex2(-octaves(zi)), bound, 2.f)) || !kept(zi, 8 * v + i)) continue;
+        if (!((float)upper <= fmaf(ex2(-octaves(zi)), bound * 1.001f, 2.f)) || !kept(zi, 8 * v + i)) continue;
         const uint32_t at = atomicAdd(&sh.n_list, 1u);
         if (at < SMP_LIST) sh.list[at] = 8 * v + i;
       }
     }
   }
   __syncthreads();
-  uint32_t win[4] = {0, 0, 0, 0};
-  double best = CUDART_INF;
-  uint32_t who = 0xFFFFFFFFu;
+  uint32_t win[4] = {__float_as_uint(CUDART_INF_F), ALL, __float_as_uint(CUDART_INF_F), 0u};
+  const uint32_t listed = sh.n_list;
   if (warp == 0) {                                 // the list is short: one warp works it out
-    const uint32_t listed = sh.n_list;
+    #pragma unroll 1
     for (uint32_t j = lane; j < min(listed, (uint32_t)SMP_LIST); j += 32) {
-      const uint32_t i = sh.list[j];
-      const double t = finish(begin + i, as_float(piece[i]));
-      if (t < best || (t == best && begin + i < who)) { best = t; who = begin + i; }
+      const uint32_t i = sh.list[j], o[4] = {__float_as_uint(finish32(begin + i, as_float(piece[i]))), begin + i, __float_as_uint(CUDART_INF_F), 0u};
+      two_first(win, o);
     }
-    words(win, best, who, listed > SMP_LIST ? 1u : 0u);
+    win[3] = listed > SMP_LIST ? 1u : 0u;
     #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
       uint32_t o[4];
       #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __shfl_xor_sync(0xFFFFFFFFu, win[i], d);
-      earlier(win, o);
+      for (int i = 0; i < 4; ++i) o[i] = __shfl_xor_sync(ALL, win[i], d);
+      two_first(win, o);
     }
   }
   {
-    const uint32_t (*all)[8] = exchange(win, 4);
+    const uint32_t (*all)[4] = exchange(win, 4);
     for (int i = 0; i < 4; ++i) win[i] = all[0][i];
-    for (uint32_t r = 1; r < C; ++r) earlier(win, all[r]);
+    for (uint32_t r = 1; r < C; ++r) two_first(win, all[r]);
   }
-  if (win[3] || !(__hiloint2double((int)win[1], (int)win[0]) < 0.99 * (double)reach)) {       // the same in all blocks
-    best = CUDART_INF; who = 0xFFFFFFFFu;
-    #pragma unroll 1
-    for (int v = tid; v < n_vec; v += SMP_THREADS)
+  uint32_t winner = win[1];
+  const float first = __uint_as_float(win[0]);
+  const bool sure = !win[3] && first < 0.99f * reach;            // nobody outside the lists is earlier
+  if (!sure || __uint_as_float(win[2]) <= first * TIE) {         // the same in all blocks
+    double best = CUDART_INF;
+    uint32_t who = ALL;
+    auto look = [&](int i) {
+      const double t = finish(begin + i, as_float(piece[i]));
+      if (t < best || (t == best && begin + i < who)) { best = t; who = begin + i; }
+    };
+    if (sure) { if (tid < (int)listed) look((int)sh.list[tid]); }
+    else
       #pragma unroll 1
-      for (int i = 8 * v; i < 8 * v + 8; ++i) {
-        const float z = as_float(piece[i]);
-        if (!kept(z, i)) continue;
-        const double t = finish(begin + i, z);
-        if (t < best) { best = t; who = begin + i; }
-      }
-    words(win, best, who, 0);
-    reduce(win, earlier);
+      for (int v = tid; v < n_vec; v += THREADS)
+        #pragma unroll 1
+        for (int i = 8 * v; i < 8 * v + 8; ++i) if (kept(as_float(piece[i]), i)) look(i);
+    uint32_t v[4];
+    words(v, best, best < CUDART_INF ? who : ALL, 0u);
+    reduce(v, earlier);
+    winner = v[2];
   }
-  const int at = (int)(win[2] - begin);
-  if (tid == 0 && win[2] >= begin && at < n) {             // the winner's block
-    a.ids[row] = (int32_t)win[2];
+  const int at = (int)(winner - begin);
+  if (tid == 0 && winner >= begin && at < n) {             // the winner's block
+    a.ids[row] = (int32_t)winner;
     a.logp[row] = (as_float(piece[at]) - zmax) - log_sum;
   }
 }
 
-template <class T>
+template <class T, bool CUTS>
 static int launch_sample(const SampleArgs& args, int sms, cudaStream_t st) {
   // A row is cut over as many blocks as leave an SM room for two of them (76 KB of logits each); a batch that would not
   // fill the device is cut finer, down to 2048 tokens a block.
@@ -709,17 +814,16 @@ static int launch_sample(const SampleArgs& args, int sms, cudaStream_t st) {
   SampleArgs a = args;
   a.piece = (int32_t)piece_of(C);
   if (a.piece * sizeof(T) > SMP_MAX_PIECE) return SAPO_ERR_UNSUPPORTED_SHAPE;
-  const size_t smem = ((sizeof(SampleShared) + 15) & ~size_t(15)) + a.piece * sizeof(T);
-  static size_t allowed[MAX_DEVICES] = {0};
+  static bool allowed[MAX_DEVICES] = {false};
   const int dev = current_device();
   if (dev < 0) return SAPO_ERR_CUDA;
-  if (allowed[dev] < smem) {
-    const size_t most = ((sizeof(SampleShared) + 15) & ~size_t(15)) + SMP_MAX_PIECE;
-    if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) != cudaSuccess) return SAPO_ERR_CUDA;
-    allowed[dev] = most;
+  if (!allowed[dev]) {
+    if (cudaFuncSetAttribute(sample_kernel<T, CUTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SMP_SHARED<CUTS> + SMP_MAX_PIECE)) != cudaSuccess)
+      return SAPO_ERR_CUDA;
+    allowed[dev] = true;
   }
   KernelScope scope(SAPO_K_SAMPLE, st);
-  return launch_overlapped(sample_kernel<T>, dim3((unsigned)(a.B * C)), SMP_THREADS, smem, C, st, a);
+  return launch_overlapped(sample_kernel<T, CUTS>, dim3((unsigned)(a.B * C)), SMP_THREADS<CUTS>, SMP_SHARED<CUTS> + a.piece * sizeof(T), C, st, a);
 }
 
 }  // namespace sapo
@@ -742,5 +846,7 @@ extern "C" int sapo_sample(const void* logits, int32_t dtype, int32_t B, int32_t
   const SampleArgs a{logits, ld, B, V, 0, seeds, h_cfg->temperature_rows, h_cfg->top_k_rows, h_cfg->top_p_rows, h_cfg->min_p_rows,
                      h_cfg->temperature, h_cfg->top_k, h_cfg->top_p, h_cfg->min_p, ids, logp, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return dtype == SAPO_DTYPE_BF16 ? launch_sample<__nv_bfloat16>(a, sms, st) : launch_sample<float>(a, sms, st);
+  const bool cuts = a.top_k || a.top_p || a.top_k_all > 1 || a.top_p_all < 1.f;      // (top_k 1 is the largest logit)
+  if (dtype == SAPO_DTYPE_BF16) return cuts ? launch_sample<__nv_bfloat16, true>(a, sms, st) : launch_sample<__nv_bfloat16, false>(a, sms, st);
+  return cuts ? launch_sample<float, true>(a, sms, st) : launch_sample<float, false>(a, sms, st);
 }
