@@ -32,9 +32,8 @@ constexpr int SMP_LIST = 256;                 // candidates a block keeps
 constexpr float SMP_LEAD = 16.f;              // L: no candidate wins with probability 1e-7
 constexpr float SMP_LOG2E = 1.4426950408889634f;
 constexpr size_t SMP_MAX_PIECE = 180 * 1024;  // bytes of a row a block can hold
-// A call in which no row can have top-k or top-p runs blocks of 256 threads (what a warp does once, whatever its number
-// of tokens, is a quarter of all instructions with 512); the sort of the other calls wants 512.
-template <bool CUTS> constexpr int SMP_THREADS = CUTS ? SMP_SORT : 256;
+constexpr float SMP_TIE = 1.001f;             // times nearer than this are told apart in 64 bits
+constexpr int SMP_THREADS = SMP_SORT;
 
 struct SampleArgs {
   const void* z; int64_t ld; int32_t B, V, piece;      // piece: tokens a block holds, a multiple of 8
@@ -53,8 +52,6 @@ struct SampleShared {
   uint32_t scan[32][4];
   uint32_t n_list, n_sort;
   uint32_t list[SMP_LIST];                  // candidates of the race
-};
-struct SampleCuts : SampleShared {          // for top-k and top-p
   Cut cut;
   Last last;
   uint64_t sort[SMP_SORT];                  // tokens to be put in order: key, and the index from above
@@ -63,7 +60,7 @@ struct SampleCuts : SampleShared {          // for top-k and top-p
   alignas(16) uint32_t count[SMP_BINS];
   uint32_t mass_lo[SMP_BINS], mass_hi[SMP_BINS];
 };
-template <bool CUTS> constexpr size_t SMP_SHARED = ((CUTS ? sizeof(SampleCuts) : sizeof(SampleShared)) + 15) & ~size_t(15);
+constexpr size_t SMP_SHARED = (sizeof(SampleShared) + 15) & ~size_t(15);
 
 // order-preserving map of a float to an unsigned integer (both zeros are equal)
 __device__ __forceinline__ uint32_t order_key(float z) {
@@ -82,6 +79,24 @@ __device__ __forceinline__ void add_shared_if(bool yes, uint32_t* to, uint32_t x
                ::"r"(umma::smem_u32(to)), "r"(x), "r"((uint32_t)yes) : "memory");
 }
 __device__ __forceinline__ uint64_t join64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
+
+// the 32 random bits of a token: the same 16 of two counters
+__device__ __forceinline__ uint32_t random_bits(uint32_t token, uint32_t k0, uint32_t k1) {
+  const uint32_t half = token & 7u, s = 16 * (half & 1u);
+  uint32_t bits = 0;
+  #pragma unroll 1
+  for (uint32_t part = 0; part < 2; ++part) {
+    const uint4 r = philox4x32_10(token >> 3, part, 0, 0, k0, k1);
+    const uint32_t w = half < 2 ? r.x : half < 4 ? r.y : half < 6 ? r.z : r.w;
+    bits = (bits << 16) | ((w >> s) & 0xFFFFu);
+  }
+  return bits;
+}
+// the time at which a token finishes, off by less than 1e-4 of itself
+__device__ __forceinline__ float finish32(uint32_t bits, float octaves) {
+  const float e = bits < 0x40000000u ? -log1pf(-((float)bits + 0.5f) * 2.3283064e-10f) : -logf(((float)~bits + 0.5f) * 2.3283064e-10f);
+  return e * ex2(octaves);
+}
 
 template <class T> struct Vec;      // eight tokens of a row
 template <> struct Vec<float> {
@@ -112,16 +127,16 @@ template <> struct Vec<__nv_bfloat16> {
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-template <class T, bool CUTS>
-__global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const SampleArgs a) {
-  constexpr int THREADS = SMP_THREADS<CUTS>, WARPS = THREADS / 32;
+template <class T>
+__global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs a) {
+  constexpr int THREADS = SMP_THREADS, WARPS = THREADS / 32;
   constexpr uint32_t ALL = 0xFFFFFFFFu;
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  SampleCuts& sh = *reinterpret_cast<SampleCuts*>(smem_raw);       // (without CUTS only its first part is there)
-  T* piece = reinterpret_cast<T*>(smem_raw + SMP_SHARED<CUTS>);
+  SampleShared& sh = *reinterpret_cast<SampleShared*>(smem_raw);
+  T* piece = reinterpret_cast<T*>(smem_raw + SMP_SHARED);
   int turn = 0;
 
   auto barrier = [&]() { if (C > 1) cluster.sync(); else __syncthreads(); };
@@ -201,8 +216,8 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
   const uint64_t seed = (uint64_t)a.seeds[row];
   const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
   const bool greedy = temperature == 0.f || top_k == 1 || top_p <= 0.f;
-  const bool by_mass = CUTS && top_p < 1.f && !greedy, by_count = CUTS && top_k > 0 && !greedy, cuts = by_mass || by_count;
-  if (CUTS && cuts) {
+  const bool by_mass = top_p < 1.f && !greedy, by_count = top_k > 0 && !greedy, cuts = by_mass || by_count;
+  if (cuts) {
     uint4* h = reinterpret_cast<uint4*>(sh.count);
     for (int i = tid; i < 3 * SMP_BINS / 4; i += THREADS) h[i] = make_uint4(0, 0, 0, 0);
   }
@@ -249,7 +264,7 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
       __syncthreads();
       zmax = __uint_as_float(sh.scan[0][0]);
       top[0] = __float_as_uint(zmax);
-    } else if (CUTS && few) {
+    } else if (few) {
       const bool bad = __syncthreads_or(!(m < CUDART_INF_F));
       const uint32_t x = sorted(order_key(m), THREADS);
       if (tid == 0) sh.scan[0][0] = bad ? 0x7FFFFFFFu : __float_as_uint(key_value(x));            // (NaN)
@@ -351,7 +366,7 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
         s1 = add2(s1, make_float2(ex2(x.x), ex2(x.y)));
       }
     }
-    if (CUTS && cuts) {
+    if (cuts) {
       if (!few) far = histogram();
     } else if (other) {
       for (int v = tid; v < n_vec; v += THREADS) {
@@ -392,28 +407,12 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
     return;
   }
   float weight = __uint_as_float(sums[1]);       // of the tokens in the race
-  // the 32 random bits of a token
-  auto random_bits = [&](uint32_t token) -> uint32_t {
-    const uint32_t half = token & 7u, s = 16 * (half & 1u);
-    uint32_t bits = 0;
-    #pragma unroll 1
-    for (uint32_t part = 0; part < 2; ++part) {
-      const uint4 r = philox4x32_10(token >> 3, part, 0, 0, k0, k1);
-      const uint32_t w = half < 2 ? r.x : half < 4 ? r.y : half < 6 ? r.z : r.w;
-      bits = (bits << 16) | ((w >> s) & 0xFFFFu);
-    }
-    return bits;
-  };
-  // The time at which a token finishes: in 64 bits, and, off by less than 1e-4 of itself, in 32.
+  // The time at which a token finishes: in 64 bits, and in 32.
   auto finish = [&](uint32_t token, float z) -> double {
-    const double e = -log1p(-((double)random_bits(token) + 0.5) * 2.3283064365386963e-10);
+    const double e = -log1p(-((double)random_bits(token, k0, k1) + 0.5) * 2.3283064365386963e-10);
     return e * exp(((double)zmax - (double)z) * fmin(1.0 / (double)temperature, 1e30));
   };
-  auto finish32 = [&](uint32_t token, float z) -> float {
-    const uint32_t bits = random_bits(token);
-    const float e = bits < 0x40000000u ? -log1pf(-((float)bits + 0.5f) * 2.3283064e-10f) : -logf(((float)~bits + 0.5f) * 2.3283064e-10f);
-    return e * ex2(octaves(z));
-  };
+  auto finish_near = [&](uint32_t token, float z) -> float { return finish32(random_bits(token, k0, k1), octaves(z)); };
   // The first to finish, and how near the second comes: words first time, its token, second time, a flag.
   auto two_first = [](uint32_t* x, const uint32_t* y) {
     const float a1 = __uint_as_float(x[0]), b1 = __uint_as_float(y[0]), a2 = __uint_as_float(x[2]), b2 = __uint_as_float(y[2]);
@@ -421,7 +420,6 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
     if (b1 < a1) { x[0] = y[0]; x[1] = y[1]; }
     x[3] |= y[3];
   };
-  const float TIE = 1.001f;      // times that 32 bits tell apart
   // the first in 64 bits, the lower index where two finish together; words: time, index, a flag
   auto earlier = [](uint32_t* x, const uint32_t* y) {
     const double p = __longlong_as_double((long long)join64(x[0], x[1])), q = __longlong_as_double((long long)join64(y[0], y[1]));
@@ -435,7 +433,7 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
   // ---- where the row, sorted by logit (equal ones by index), is cut: keys above key_cut stay, and of those equal to it
   //      the ones up to index_cut
   uint32_t key_cut = 0, index_cut = ALL;
-  if constexpr (CUTS) if (cuts) {
+  if (cuts) {
     // The bin of the histograms in which the search ends: the one with the target-th token, or the one where the mass
     // reaches `target` (of_total: times the mass of all); beyond the histogram there are, with_far, the tokens of its last
     // bin.  Each block adds up its share of the bins over the cluster, in place: no other block reads that part of its own.
@@ -557,17 +555,17 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
       in = in && octaves(z) <= floor_octaves;
       const uint32_t token = ALL - (uint32_t)x;
       uint32_t win[4] = {__float_as_uint(CUDART_INF_F), ALL, __float_as_uint(CUDART_INF_F), 0u};
-      if (in) { win[0] = __float_as_uint(finish32(token, z)); win[1] = token; }
+      if (in) { win[0] = __float_as_uint(finish_near(token, z)); win[1] = token; }
       const float mine = __uint_as_float(win[0]);
       reduce_block(win, two_first);
       if (tid == 0) { sh.scan[0][0] = win[0]; sh.scan[0][1] = win[1]; sh.scan[0][2] = win[2]; }
       __syncthreads();
       uint32_t who = sh.scan[0][1];
       const float first = __uint_as_float(sh.scan[0][0]);
-      if (__uint_as_float(sh.scan[0][2]) <= first * TIE || !(first < 1e37f)) {       // the same for all threads
+      if (__uint_as_float(sh.scan[0][2]) <= first * SMP_TIE || !(first < 1e37f)) {       // the same for all threads
         uint32_t v[4];
         words(v, CUDART_INF, ALL, 0u);
-        if (in && (mine <= first * TIE || !(first < 1e37f))) words(v, finish(token, z), token, 0u);
+        if (in && (mine <= first * SMP_TIE || !(first < 1e37f))) words(v, finish(token, z), token, 0u);
         reduce_block(v, earlier);
         if (tid == 0) sh.scan[0][0] = v[2];
         __syncthreads();
@@ -758,7 +756,7 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
   if (warp == 0) {                                 // the list is short: one warp works it out
     #pragma unroll 1
     for (uint32_t j = lane; j < min(listed, (uint32_t)SMP_LIST); j += 32) {
-      const uint32_t i = sh.list[j], o[4] = {__float_as_uint(finish32(begin + i, as_float(piece[i]))), begin + i, __float_as_uint(CUDART_INF_F), 0u};
+      const uint32_t i = sh.list[j], o[4] = {__float_as_uint(finish_near(begin + i, as_float(piece[i]))), begin + i, __float_as_uint(CUDART_INF_F), 0u};
       two_first(win, o);
     }
     win[3] = listed > SMP_LIST ? 1u : 0u;
@@ -778,7 +776,7 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
   uint32_t winner = win[1];
   const float first = __uint_as_float(win[0]);
   const bool sure = !win[3] && first < 0.99f * reach;            // nobody outside the lists is earlier
-  if (!sure || __uint_as_float(win[2]) <= first * TIE) {         // the same in all blocks
+  if (!sure || __uint_as_float(win[2]) <= first * SMP_TIE) {         // the same in all blocks
     double best = CUDART_INF;
     uint32_t who = ALL;
     auto look = [&](int i) {
@@ -803,27 +801,332 @@ __global__ void __launch_bounds__(SMP_THREADS<CUTS>, 2) sample_kernel(const Samp
   }
 }
 
-template <class T, bool CUTS>
-static int launch_sample(const SampleArgs& args, int sms, cudaStream_t st) {
-  // A row is cut over as many blocks as leave an SM room for two of them (76 KB of logits each); a batch that would not
-  // fill the device is cut finer, down to 2048 tokens a block.
+// ---------------------------------------------------------------------------- rows without top-k and top-p
+// Every block of a row runs the race of its own tokens against its own largest logit and weight, and ends with its first
+// to finish; the first block of the cluster compares the blocks' times.  Until then they do not wait for one another
+// (but for the row's largest logit, with min_p), and the others are gone before it does.
+constexpr int RACE_THREADS = 256, RACE_WARPS = RACE_THREADS / 32;
+constexpr float RACE_LEAD = 6.f;
+
+struct RaceShared {
+  uint32_t slots[SMP_MAX_CLUSTER][4];       // of a block: its largest logit, its sum of weights, its first time, its token
+  float max_of[SMP_MAX_CLUSTER];
+  float warp[2][RACE_WARPS];
+  uint32_t first[RACE_WARPS];
+  double best; uint32_t who, n_list;
+  uint32_t list[SMP_LIST];
+};
+constexpr size_t RACE_SHARED = (sizeof(RaceShared) + 15) & ~size_t(15);
+
+__device__ __forceinline__ void store_weights(float* p, const float2 (&w)[4]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(w[0].x, w[0].y, w[1].x, w[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(w[2].x, w[2].y, w[3].x, w[3].y);
+}
+__device__ __forceinline__ void store_weights(__nv_bfloat16* p, const float2 (&w)[4]) {
+  uint32_t q[4];
+  #pragma unroll
+  for (int i = 0; i < 4; ++i) { const __nv_bfloat162 b = __floats2bfloat162_rn(w[i].x, w[i].y); q[i] = *reinterpret_cast<const uint32_t*>(&b); }
+  *reinterpret_cast<uint4*>(p) = make_uint4(q[0], q[1], q[2], q[3]);
+}
+
+template <class T>
+__global__ void __launch_bounds__(RACE_THREADS, 4) race_kernel(const SampleArgs a) {
+  constexpr uint32_t ALL = 0xFFFFFFFFu;
+  cg::cluster_group cluster = cg::this_cluster();
+  const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  RaceShared& sh = *reinterpret_cast<RaceShared*>(smem_raw);
+  T* piece = reinterpret_cast<T*>(smem_raw + RACE_SHARED);
+  auto arrive = []() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); };
+  auto wait = []() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+
+  arrive();                            // (waited for before the first store to another block's shared memory)
+  wait_for_previous();
+  const int row = blockIdx.x / C;
+  const uint32_t begin = rank * (uint32_t)a.piece;
+  const int n = max(0, min(a.piece, a.V - (int)begin)), n_vec = (n + 7) / 8;      // tokens of this block, and eights of them
+  const T* from = static_cast<const T*>(a.z) + (int64_t)row * a.ld + begin;
+  {
+    const bool aligned = (reinterpret_cast<uintptr_t>(from) & 15u) == 0;
+    #pragma unroll 2
+    for (int v = tid; v < n_vec; v += RACE_THREADS) {
+      if (aligned && 8 * v + 8 <= n) {
+        #pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                       ::"r"(umma::smem_u32(reinterpret_cast<uint8_t*>(piece + 8 * v) + 16 * h)),
+                         "l"(reinterpret_cast<const uint8_t*>(from + 8 * v) + 16 * h) : "memory");
+      } else {
+        #pragma unroll 1
+        for (int i = 8 * v; i < 8 * v + 8; ++i) piece[i] = i < n ? from[i] : T(-CUDART_INF_F);   // behind the end: no weight
+      }
+    }
+  }
+  const float temperature = a.temperature ? a.temperature[row] : a.temperature_all, min_p = a.min_p ? a.min_p[row] : a.min_p_all;
+  const uint64_t seed = (uint64_t)a.seeds[row];
+  const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  const bool greedy = temperature == 0.f || a.top_k_all == 1;
+  const bool settings_ok = temperature >= 0.f && temperature < CUDART_INF_F && min_p >= 0.f;
+  const float scale = greedy ? SMP_LOG2E : fminf(SMP_LOG2E / temperature, 1e30f);
+  if (tid == 0) sh.n_list = 0;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // ---- the largest logit
+  float zmax = -CUDART_INF_F;
+  for (int v = tid; v < n_vec; v += RACE_THREADS) zmax = max_nan(zmax, Vec<T>::most(piece + 8 * v));
+  #pragma unroll
+  for (int d = 16; d > 0; d >>= 1) zmax = max_nan(zmax, __shfl_xor_sync(ALL, zmax, d));
+  if (lane == 0) sh.warp[0][warp] = zmax;
+  __syncthreads();
+  #pragma unroll
+  for (int w = 0; w < RACE_WARPS; ++w) zmax = max_nan(zmax, sh.warp[0][w]);
+  bool waited = false;
+  float floor_octaves = CUDART_INF_F;
+  if (min_p > 0.f && !greedy) {                    // min_p goes by the row's largest
+    wait();
+    waited = true;
+    if (tid < (int)C) *cluster.map_shared_rank(&sh.max_of[rank], tid) = zmax;
+    cluster.sync();
+    for (uint32_t r = 0; r < C; ++r) zmax = max_nan(zmax, sh.max_of[r]);
+    floor_octaves = fmaxf(-log2f(min_p), 0.f);
+  }
+  const bool usable = fabsf(zmax) < CUDART_INF_F;  // (a block of -inf, or with a NaN or +inf, has nothing in the race)
+  const float ref = usable ? zmax : 0.f;
+  uint32_t first = ALL;               // greedy: the first token with the largest logit
+  if (greedy) {
+    #pragma unroll 1
+    for (int v = tid; v < n_vec; v += RACE_THREADS)
+      #pragma unroll 1
+      for (int i = 8 * v; i < 8 * v + 8; ++i) if (as_float(piece[i]) == zmax) first = min(first, begin + i);
+  }
+
+  // ---- the weights: at temperature 1 for the log-prob; at the row's for the race, kept in place of the logits (those of
+  //      bf16 logits as bf16: the race has room for that)
+  float s1 = 0.f, sT = 0.f;
+  const bool other = scale != SMP_LOG2E || floor_octaves < CUDART_INF_F;
+  {
+    float2 sum1 = both(0.f), sum2 = both(0.f);
+    if (!other) {
+      for (int v = tid; v < n_vec; v += RACE_THREADS) {
+        float z[8];
+        Vec<T>::get(piece + 8 * v, z);
+        float2 w[4];
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 x = mul2(add2(make_float2(z[2 * i], z[2 * i + 1]), both(-ref)), both(SMP_LOG2E));
+          w[i] = make_float2(ex2(x.x), ex2(x.y));
+          sum1 = add2(sum1, w[i]);
+        }
+        store_weights(piece + 8 * v, w);
+      }
+    } else {
+      for (int v = tid; v < n_vec; v += RACE_THREADS) {
+        float z[8];
+        Vec<T>::get(piece + 8 * v, z);
+        float2 w[4];
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 d = add2(make_float2(z[2 * i], z[2 * i + 1]), both(-ref)), x = mul2(d, both(SMP_LOG2E)), o = mul2(d, both(scale));
+          sum1 = add2(sum1, make_float2(ex2(x.x), ex2(x.y)));
+          w[i] = make_float2(-o.x <= floor_octaves ? ex2(o.x) : 0.f, -o.y <= floor_octaves ? ex2(o.y) : 0.f);
+          sum2 = add2(sum2, w[i]);
+        }
+        store_weights(piece + 8 * v, w);
+      }
+    }
+    s1 = sum1.x + sum1.y; sT = sum2.x + sum2.y;
+  }
+  #pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    s1 += __shfl_xor_sync(ALL, s1, d);
+    if (other) sT += __shfl_xor_sync(ALL, sT, d);
+  }
+  if (greedy) first = __reduce_min_sync(ALL, first);
+  __syncthreads();
+  if (lane == 0) { sh.warp[0][warp] = s1; sh.warp[1][warp] = sT; sh.first[warp] = first; }
+  __syncthreads();
+  s1 = 0.f; sT = 0.f;
+  #pragma unroll
+  for (int w = 0; w < RACE_WARPS; ++w) { s1 += sh.warp[0][w]; sT += sh.warp[1][w]; }
+  const float weight = other ? sT : s1;
+
+  // ---- the race
+  auto finish = [&](uint32_t token, float z, float top) -> double {          // against the logit `top`, in 64 bits
+    const double e = -log1p(-((double)random_bits(token, k0, k1) + 0.5) * 2.3283064365386963e-10);
+    return e * exp(((double)top - (double)z) * fmin(1.0 / (double)temperature, 1e30));
+  };
+  uint32_t out[4] = {__float_as_uint(zmax), __float_as_uint(s1), __float_as_uint(CUDART_INF_F), ALL};      // what the block has to say
+  if (greedy) {
+    for (int w = 0; w < RACE_WARPS; ++w) out[3] = min(out[3], sh.first[w]);
+  } else if (usable && weight > 0.f) {
+    // A token is worth working out if it may finish before `lead` / weight; the block's first does with probability
+    // 1 - exp(-lead), else the block looks again, further.  The eights with such a token are listed.
+    float t1 = CUDART_INF_F;
+    #pragma unroll 1
+    for (float lead = RACE_LEAD; lead < 1e4f; lead *= 4.f) {
+      const float reach = lead / weight, bound = 65536.f * reach * 1.01f;
+      for (int v = tid; v < n_vec; v += RACE_THREADS) {
+        float w[8];
+        Vec<T>::get(piece + 8 * v, w);
+        const uint4 r = philox4x32_10((begin >> 3) + v, 0, 0, 0, k0, k1);
+        const uint32_t word[4] = {r.x, r.y, r.z, r.w};
+        float ahead[2] = {-1.f, -1.f};
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {               // 2^23 + 1 + bound w against 2^23 + the upper bits
+          const float2 may = fma2(make_float2(w[2 * i], w[2 * i + 1]), both(bound), both(8388609.f));
+          ahead[0] = fmaxf(ahead[0], may.x - __uint_as_float(__byte_perm(word[i], 0x4B000000u, 0x7610)));
+          ahead[1] = fmaxf(ahead[1], may.y - __uint_as_float(__byte_perm(word[i], 0x4B000000u, 0x7632)));
+        }
+        if (fmaxf(ahead[0], ahead[1]) >= 0.f) {
+          const uint32_t at = atomicAdd(&sh.n_list, 1u);
+          if (at < SMP_LIST) sh.list[at] = v;
+        }
+      }
+      __syncthreads();
+      const uint32_t listed = min(sh.n_list, (uint32_t)SMP_LIST), looked = 8 * listed;
+      const bool all_listed = sh.n_list <= SMP_LIST;
+      if (warp == 0) {                             // the list is short: one warp works it out
+        t1 = CUDART_INF_F;
+        float t2 = CUDART_INF_F;
+        uint32_t who = ALL;
+        #pragma unroll 1
+        for (uint32_t j = lane; j < looked; j += 32) {
+          const int i = 8 * (int)sh.list[j >> 3] + (int)(j & 7u);
+          const float o = i < n ? (zmax - as_float(from[i])) * scale : CUDART_INF_F;
+          const float t = o <= floor_octaves ? finish32(random_bits(begin + i, k0, k1), o) : CUDART_INF_F;
+          t2 = fminf(t2, fmaxf(t1, t));
+          if (t < t1) { t1 = t; who = begin + i; }
+        }
+        #pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+          const float u1 = __shfl_xor_sync(ALL, t1, d), u2 = __shfl_xor_sync(ALL, t2, d);
+          const uint32_t x = __shfl_xor_sync(ALL, who, d);
+          t2 = fminf(fmaxf(t1, u1), fminf(t2, u2));
+          if (u1 < t1 || (u1 == t1 && x < who)) { t1 = u1; who = x; }
+        }
+        if (t2 <= t1 * SMP_TIE && t1 < CUDART_INF_F) {       // two come near: in 64 bits
+          double best = CUDART_INF;
+          uint32_t winner = ALL;
+          #pragma unroll 1
+          for (uint32_t j = lane; j < looked; j += 32) {
+            const int i = 8 * (int)sh.list[j >> 3] + (int)(j & 7u);
+            const float z = i < n ? as_float(from[i]) : -CUDART_INF_F;
+            if (!((zmax - z) * scale <= floor_octaves)) continue;
+            const double t = finish(begin + i, z, zmax);
+            if (t < best || (t == best && begin + i < winner)) { best = t; winner = begin + i; }
+          }
+          #pragma unroll 1
+          for (int d = 16; d > 0; d >>= 1) {
+            const double t = __shfl_xor_sync(ALL, best, d);
+            const uint32_t x = __shfl_xor_sync(ALL, winner, d);
+            if (t < best || (t == best && x < winner)) { best = t; winner = x; }
+          }
+          if (winner != ALL) { who = winner; t1 = (float)best; }
+        }
+        if (lane == 0) { sh.warp[0][0] = t1; sh.who = who; sh.n_list = 0; }
+      }
+      __syncthreads();
+      t1 = sh.warp[0][0];
+      out[2] = __float_as_uint(t1); out[3] = sh.who;
+      if (t1 < 0.99f * reach && all_listed) break;
+      t1 = CUDART_INF_F;
+      if (!all_listed) break;
+    }
+    if (t1 == CUDART_INF_F) {                      // too many to list, or none in reach at all: every token
+      double best = CUDART_INF;
+      uint32_t who = ALL;
+      #pragma unroll 1
+      for (int i = tid; i < n; i += RACE_THREADS) {
+        const float z = as_float(from[i]);
+        if (!((zmax - z) * scale <= floor_octaves)) continue;
+        const double t = finish(begin + i, z, zmax);
+        if (t < best) { best = t; who = begin + i; }
+      }
+      __syncthreads();
+      if (tid == 0) { sh.best = CUDART_INF; sh.who = ALL; }
+      #pragma unroll 1
+      for (int turn = 0; turn < RACE_THREADS; ++turn) {
+        __syncthreads();
+        if (tid == turn && (best < sh.best || (best == sh.best && who < sh.who))) { sh.best = best; sh.who = who; }
+      }
+      __syncthreads();
+      out[2] = __float_as_uint((float)sh.best); out[3] = sh.who;
+    }
+  }
+
+  // ---- the first block compares the blocks
+  if (!waited) wait();
+  if (tid == 0) {
+    uint32_t* to = cluster.map_shared_rank(&sh.slots[rank][0], 0);
+    for (int i = 0; i < 4; ++i) to[i] = out[i];
+  }
+  arrive();
+  if (rank != 0) return;
+  wait();
+  if (tid != 0) return;
+  float top = -CUDART_INF_F, total = 0.f, t1 = CUDART_INF_F, t2 = CUDART_INF_F;
+  uint32_t who = ALL;
+  for (uint32_t r = 0; r < C; ++r) top = max_nan(top, __uint_as_float(sh.slots[r][0]));
+  if (!(top < CUDART_INF_F) || top == -CUDART_INF_F || !settings_ok) {
+    a.ids[row] = -1; a.logp[row] = 0.f;
+    if (!settings_ok || top != -CUDART_INF_F) raise_status(a.status, SAPO_ST_NONFINITE_INPUT);
+    return;
+  }
+  auto time_of = [&](uint32_t r) { return __uint_as_float(sh.slots[r][2]) * ex2((top - __uint_as_float(sh.slots[r][0])) * scale); };
+  for (uint32_t r = 0; r < C; ++r) {
+    const float less = top - __uint_as_float(sh.slots[r][0]);
+    total += __uint_as_float(sh.slots[r][1]) * ex2(-less * SMP_LOG2E);
+    if (sh.slots[r][3] == ALL) continue;
+    if (greedy) { if (less == 0.f) who = min(who, sh.slots[r][3]); continue; }
+    const float t = time_of(r);
+    t2 = fminf(t2, fmaxf(t1, t));
+    if (t < t1) { t1 = t; who = sh.slots[r][3]; }
+  }
+  const T* z_row = static_cast<const T*>(a.z) + (int64_t)row * a.ld;
+  if (!greedy && (t2 <= t1 * SMP_TIE || !(t1 < 1e37f))) {                // two blocks' come near: in 64 bits
+    double best = CUDART_INF;
+    for (uint32_t r = 0; r < C; ++r) {
+      const uint32_t token = sh.slots[r][3];
+      if (token == ALL || (t1 < 1e37f && time_of(r) > t1 * SMP_TIE)) continue;
+      const double t = finish(token, as_float(z_row[token]), top);
+      if (t < best || (t == best && token < who)) { best = t; who = token; }
+    }
+  }
+  a.ids[row] = (int32_t)who;
+  a.logp[row] = (as_float(z_row[who]) - top) - logf(total);
+}
+
+// How many blocks share a row: so many that an SM has room for its share of them (`most` bytes of logits each); a batch
+// that would not fill the device is cut finer, down to 2048 tokens a block.
+static int blocks_of_row(const SampleArgs& a, size_t size, int64_t most, int sms, int32_t& piece) {
+  const auto piece_of = [&](int c) { return round_up<int64_t>(ceil_div<int64_t>(a.V, c), 8); };
   int C = 1;
-  const auto piece_of = [&](int c) { return round_up<int64_t>(ceil_div<int64_t>(args.V, c), 8); };
-  while (C < SMP_MAX_CLUSTER && piece_of(C) * (int64_t)sizeof(T) > 76 * 1024) C *= 2;
-  while (C < SMP_MAX_CLUSTER && (int64_t)args.B * C * 2 <= 2 * sms && piece_of(C) > 2048) C *= 2;
-  SampleArgs a = args;
-  a.piece = (int32_t)piece_of(C);
-  if (a.piece * sizeof(T) > SMP_MAX_PIECE) return SAPO_ERR_UNSUPPORTED_SHAPE;
-  static bool allowed[MAX_DEVICES] = {false};
-  const int dev = current_device();
+  while (C < SMP_MAX_CLUSTER && piece_of(C) * (int64_t)size > most) C *= 2;
+  while (C < SMP_MAX_CLUSTER && (int64_t)a.B * C * 2 <= 2 * sms && piece_of(C) > 2048) C *= 2;
+  piece = (int32_t)piece_of(C);
+  return C;
+}
+
+template <class Kernel>
+static int launch_sample(Kernel kernel, bool (&allowed)[MAX_DEVICES], int threads, size_t shared, size_t size, int64_t most, SampleArgs a, int sms,
+                         cudaStream_t st) {
+  const int C = blocks_of_row(a, size, most, sms, a.piece), dev = current_device();
+  if (a.piece * size > SMP_MAX_PIECE) return SAPO_ERR_UNSUPPORTED_SHAPE;
   if (dev < 0) return SAPO_ERR_CUDA;
   if (!allowed[dev]) {
-    if (cudaFuncSetAttribute(sample_kernel<T, CUTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(SMP_SHARED<CUTS> + SMP_MAX_PIECE)) != cudaSuccess)
-      return SAPO_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(shared + SMP_MAX_PIECE)) != cudaSuccess) return SAPO_ERR_CUDA;
     allowed[dev] = true;
   }
   KernelScope scope(SAPO_K_SAMPLE, st);
-  return launch_overlapped(sample_kernel<T, CUTS>, dim3((unsigned)(a.B * C)), SMP_THREADS<CUTS>, SMP_SHARED<CUTS> + a.piece * sizeof(T), C, st, a);
+  return launch_overlapped(kernel, dim3((unsigned)(a.B * C)), threads, shared + a.piece * size, C, st, a);
+}
+template <class T>
+static int launch_sample(const SampleArgs& a, int sms, cudaStream_t st) {
+  static bool allowed[2][MAX_DEVICES] = {{false}, {false}};
+  if (a.top_k || a.top_p || a.top_k_all > 1 || a.top_p_all < 1.f)      // (top_k 1 is the largest logit)
+    return launch_sample(sample_kernel<T>, allowed[0], SMP_THREADS, SMP_SHARED, sizeof(T), 76 * 1024, a, sms, st);
+  return launch_sample(race_kernel<T>, allowed[1], RACE_THREADS, RACE_SHARED, sizeof(T), 40 * 1024, a, sms, st);
 }
 
 }  // namespace sapo
@@ -846,7 +1149,5 @@ extern "C" int sapo_sample(const void* logits, int32_t dtype, int32_t B, int32_t
   const SampleArgs a{logits, ld, B, V, 0, seeds, h_cfg->temperature_rows, h_cfg->top_k_rows, h_cfg->top_p_rows, h_cfg->min_p_rows,
                      h_cfg->temperature, h_cfg->top_k, h_cfg->top_p, h_cfg->min_p, ids, logp, status};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool cuts = a.top_k || a.top_p || a.top_k_all > 1 || a.top_p_all < 1.f;      // (top_k 1 is the largest logit)
-  if (dtype == SAPO_DTYPE_BF16) return cuts ? launch_sample<__nv_bfloat16, true>(a, sms, st) : launch_sample<__nv_bfloat16, false>(a, sms, st);
-  return cuts ? launch_sample<float, true>(a, sms, st) : launch_sample<float, false>(a, sms, st);
+  return dtype == SAPO_DTYPE_BF16 ? launch_sample<__nv_bfloat16>(a, sms, st) : launch_sample<float>(a, sms, st);
 }
