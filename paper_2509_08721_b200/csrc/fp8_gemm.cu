@@ -12,6 +12,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "paired.cuh"
 #include "umma.cuh"
 
 namespace sapo {
@@ -28,6 +29,11 @@ struct Fp8GemmArgs {
   int32_t group_m;          // wide: token blocks that are walked before the next column block
   int32_t tma_store;        // wide: y can be written by TMA
   int32_t split;            // narrow: CTAs that share a tile along K
+  int32_t unit0, units;     // the tiles of this launch
+  int32_t of_wide;          // narrow: four tiles each of the wide tiles from unit0 on, which have this order's num_m, num_n
+  int32_t num_m, num_n;     // wide tiles along tokens and columns
+  int32_t tail_follows;     // another launch of this call takes the last tiles: it may start as soon as this one runs
+  int32_t tail;             // this is that launch
   long long wait_limit;
   int32_t* status;
 };
@@ -44,6 +50,8 @@ __device__ __forceinline__ void mma_f8_pair(uint32_t tmem_d, uint64_t a_desc, ui
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
+// wait until all but the last of this thread's groups of stores have finished reading shared memory
+__device__ __forceinline__ void bulk_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 // named_barrier_sync that also says whether `yes` holds in all its threads
 __device__ __forceinline__ bool named_barrier_and(int id, int n_threads, bool yes) {
   uint32_t all;
@@ -68,19 +76,29 @@ __device__ __forceinline__ void tmem_ld_wait16(float (&v)[16]) {
                  "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
 
+// A grid of one CTA (pair) per SM (pair) leaves most of the device idle while the last, partial round of tiles runs; a
+// second launch takes these tiles and shares each among several CTAs along K.  It does not wait for the first one's results, so
+// the first lets it start (behind its own wait for what comes before the call) and its CTAs fill SMs as they fall idle;
+// what follows the call must wait for both, so the second waits for the first before it ends.
+__device__ __forceinline__ void begin_launch(const Fp8GemmArgs& a) {
+  if (!a.tail) wait_for_previous();
+  if (a.tail_follows) let_next_start();
+}
+__device__ __forceinline__ void end_launch(const Fp8GemmArgs& a) { if (a.tail) wait_for_previous(); }
+
 // ---------------------------------------------------------------------------- wide tiles
-constexpr int F8W_STAGES = 6;
+constexpr int F8W_STAGES = 5;
 constexpr int F8W_THREADS = 320;                           // warp 0: TMA, warp 1: MMA, warps 2-9: scaling and output
 constexpr uint32_t F8W_STAGE = 2 * F8_BOX;                 // this CTA's 128 tokens, and its half of the 256 columns
-constexpr uint32_t F8W_STAGING = 128 * 128;                // output on its way: 128 rows of 128 bytes, one per half of the columns
-constexpr size_t F8W_SMEM = 1024 + F8W_STAGES * F8W_STAGE + 2 * F8W_STAGING + 256;
+constexpr uint32_t F8W_STAGING = 128 * 128;                // output on its way: 128 rows of 128 bytes, two per half of the columns
+constexpr size_t F8W_SMEM = 1024 + F8W_STAGES * F8W_STAGE + 4 * F8W_STAGING + 256;
 static_assert(F8W_SMEM <= 232448, "more shared memory than a CTA can have");
 
 // Tile `unit`: groups of group_m token blocks; inside a group the token block runs fastest, so that a group's tokens stay
 // in L2 while W streams past them once.
-__device__ __forceinline__ void wide_tile(const Fp8GemmArgs& a, int unit, int num_m, int num_n, int& mb, int& nb) {
-  const int per_group = a.group_m * num_n, g = unit / per_group, r = unit - g * per_group;
-  const int rows = min(a.group_m, num_m - g * a.group_m);
+__device__ __forceinline__ void wide_tile(const Fp8GemmArgs& a, int unit, int& mb, int& nb) {
+  const int per_group = a.group_m * a.num_n, g = unit / per_group, r = unit - g * per_group;
+  const int rows = min(a.group_m, a.num_m - g * a.group_m);
   nb = r / rows;
   mb = g * a.group_m + (r - nb * rows);
 }
@@ -91,7 +109,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* staging = smem + F8W_STAGES * F8W_STAGE;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 2 * F8W_STAGING);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 4 * F8W_STAGING);
   uint64_t* full = bars;                          // TMA -> MMA             (even CTA's are used)
   uint64_t* empty = bars + F8W_STAGES;            // MMA -> TMA             (each CTA waits on its own)
   uint64_t* acc_full = bars + 2 * F8W_STAGES;     // [2] MMA -> scaling     (each CTA waits on its own)
@@ -103,7 +121,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_cta_rank();
   const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-  const int num_m = (int)((a.T + 255) / 256), num_n = (a.N + 255) / 256, units = num_m * num_n;
+  const int units = a.units;
   if (threadIdx.x == 0) {
     for (int i = 0; i < F8W_STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 16); }
@@ -116,7 +134,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   fence_before_sync();
   __syncthreads();
   cluster_sync_all();
-  wait_for_previous();
+  begin_launch(a);
   fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   const uint32_t full0 = map_to_cta(smem_u32(full), 0), acc_empty0 = map_to_cta(smem_u32(acc_empty), 0);
@@ -129,7 +147,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     bool ok = true;
     for (int unit = pair; ok && unit < units; unit += num_pairs) {
       int mb, nb;
-      wide_tile(a, unit, num_m, num_n, mb, nb);
+      wide_tile(a, unit, mb, nb);
       for (int kb = 0; kb < a.num_kb; ++kb) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag, a.wait_limit)) { ok = false; break; }
         if (rank == 0) mbar_arrive_expect_tx(&full[stage], 2 * F8W_STAGE);
@@ -175,23 +193,23 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // ------------------------------------------------------------ scaling and output (8 warps, both CTAs)
     // warps 2-5 take the tile's first 128 columns, warps 6-9 the others: one block of W's scales each
     const int quad = warp & 3, half = (warp - 2) >> 2, r = quad * 32 + lane;
-    const uint32_t buf = smem_u32(staging) + half * F8W_STAGING;
+    const uint32_t bufs = smem_u32(staging) + half * 2 * F8W_STAGING;
     const bool elected = quad == 0 && lane == 0;
-    int acc = 0; uint32_t acc_phase = 0;
+    int acc = 0; uint32_t acc_phase = 0, turn = 0;
     bool ok = true;
     for (int unit = pair; ok && unit < units; unit += num_pairs) {
       int mb, nb;
-      wide_tile(a, unit, num_m, num_n, mb, nb);
+      wide_tile(a, unit, mb, nb);
       const int64_t row0 = (int64_t)mb * 256 + rank * 128;
       const int col0 = nb * 256 + half * 128;
       const float* sx = a.sx + min(row0 + r, a.T - 1) * a.ld_sx;                      // rows and columns past the end are
       const float* sw = a.sw + (int64_t)(min(col0, a.N - 1) >> 7) * a.ld_sw;          // not stored
-      float sum[128];
+      float2 sum[64];
       #pragma unroll
-      for (int j = 0; j < 128; ++j) sum[j] = 0.f;
+      for (int j = 0; j < 64; ++j) sum[j] = both(0.f);
       float next = __ldg(sx) * __ldg(sw);
       for (int kb = 0; kb < a.num_kb; ++kb) {
-        const float s = next;
+        const float2 s = both(next);
         if (kb + 1 < a.num_kb) next = __ldg(sx + kb + 1) * __ldg(sw + kb + 1);
         if (!__all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, a.wait_limit))) { ok = false; break; }
         fence_after_sync();
@@ -208,7 +226,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             if (lane == 0) mbar_arrive_cluster(acc_empty0 + acc * 8);
           }
           #pragma unroll
-          for (int j = 0; j < 16; ++j) sum[16 * c + j] = fmaf(s, v[c & 1][j], sum[16 * c + j]);
+          for (int j = 0; j < 8; ++j) sum[8 * c + j] = fma2(s, make_float2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), sum[8 * c + j]);
         }
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       }
@@ -219,7 +237,9 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       #pragma unroll
       for (int p = 0; p < 4; ++p) {
         if (p >= pieces || col0 + p * width >= a.N || row0 >= a.T) break;             // the same for all 128 threads
-        if (a.tma_store && elected) bulk_wait_read_all();
+        const uint32_t buf = bufs + (turn & 1u) * F8W_STAGING;
+        ++turn;
+        if (a.tma_store && elected) bulk_wait_read_but_one();      // the store before the last has left this buffer
         named_barrier_sync(1 + half, 128);
         #pragma unroll
         for (int q = 0; q < 8; ++q) {
@@ -227,13 +247,13 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           if (a.out_bf16) {
             #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int j = (p & 1) * 64 + 8 * q + 2 * i;
-              const __nv_bfloat162 b = __floats2bfloat162_rn(sum[j], sum[j + 1]);
+              const float2 f = sum[(p & 1) * 32 + 4 * q + i];
+              const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
               w[i] = *reinterpret_cast<const uint32_t*>(&b);
             }
           } else {
             #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(sum[p * 32 + 4 * q + i]);
+            for (int i = 0; i < 4; ++i) { const float2 f = sum[p * 16 + 2 * q + (i >> 1)]; w[i] = __float_as_uint((i & 1) ? f.y : f.x); }
           }
           st_shared_v4(buf + r * 128 + ((q ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
         }
@@ -243,7 +263,7 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           if (elected) { tma_store_2d(&map_y, buf, col0 + p * width, (int32_t)row0); bulk_commit_group(); }
         } else {                                    // rows of y on no 16-byte boundary: a warp writes a row's columns
           named_barrier_sync(1 + half, 128);
-          const uint8_t* from = staging + half * F8W_STAGING;
+          const uint8_t* from = staging + (buf - smem_u32(staging));
           for (int i = 0; i < 32; ++i) {
             const int rr = quad * 32 + i;
             if (row0 + rr >= a.T) break;
@@ -272,23 +292,25 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 }
 
 // ---------------------------------------------------------------------------- narrow tiles
-constexpr int F8N_THREADS = 192;                  // warp 0: TMA, warp 1: MMA, warps 2-5: scaling and output
 constexpr int F8N_BUFFERS = 4;                    // partial products in tensor memory
 template <int NT> struct Narrow {
-  static constexpr uint32_t STAGE = F8_BOX + NT * F8_K;
-  static constexpr int STAGES = 200 * 1024 / STAGE < 10 ? 200 * 1024 / STAGE : 10;
-  static constexpr uint32_t COLS = NT * F8N_BUFFERS < 64 ? 64 : NT * F8N_BUFFERS;
-  static constexpr size_t SMEM = 1024 + STAGES * STAGE + 2 * NT * 4 + 256;
-  static_assert((COLS & (COLS - 1)) == 0 && COLS <= 512 && NT * 128 * 4 <= STAGES * STAGE, "tensor memory, or the partial sums");
+  static constexpr int GROUPS = NT >= 64 ? 2 : 1, WARPS = 4 * GROUPS, COLS = NT / GROUPS;      // warps that scale; tokens of a thread
+  static constexpr int THREADS = 64 + 32 * WARPS;                                              // warp 0: TMA, warp 1: MMA
+  static constexpr uint32_t STAGE = F8_BOX + NT * F8_K, OUT = NT * 128 * 4;
+  static constexpr int STAGES = (220 * 1024 - (int)OUT) / (int)STAGE < 10 ? (220 * 1024 - (int)OUT) / (int)STAGE : 10;
+  static constexpr uint32_t TMEM = NT * F8N_BUFFERS < 64 ? 64 : NT * F8N_BUFFERS;
+  static constexpr size_t SMEM = 1024 + STAGES * STAGE + OUT + 2 * NT * 4 + 256;
+  static_assert((TMEM & (TMEM - 1)) == 0 && TMEM <= 512 && SMEM <= 232448 && STAGES >= 4, "tensor or shared memory");
 };
 
 template <int NT>
-__global__ void __launch_bounds__(F8N_THREADS, 1)
+__global__ void __launch_bounds__(Narrow<NT>::THREADS, 1)
 fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const Fp8GemmArgs a) {
   using Z = Narrow<NT>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* scales = reinterpret_cast<float*>(smem + Z::STAGES * Z::STAGE);      // [2][NT]
+  float* out = reinterpret_cast<float*>(smem + Z::STAGES * Z::STAGE);         // [NT][128]: a tile's sums
+  float* scales = out + NT * 128;                                             // [2][NT]
   uint64_t* bars = reinterpret_cast<uint64_t*>(scales + 2 * NT);
   uint64_t* full = bars;
   uint64_t* empty = bars + Z::STAGES;
@@ -302,29 +324,38 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < Z::STAGES; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < F8N_BUFFERS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+    for (int i = 0; i < F8N_BUFFERS; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], Z::WARPS); }
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tensormap(&map_x); prefetch_tensormap(&map_w);
   }
-  if (warp == 1) { tmem_alloc(tmem_slot, Z::COLS); tmem_relinquish(); }
+  if (warp == 1) { tmem_alloc(tmem_slot, Z::TMEM); tmem_relinquish(); }
   fence_before_sync();
   __syncthreads();
   if (a.split > 1) cluster_sync_all();
-  wait_for_previous();
+  begin_launch(a);
   fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   const int rank = blockIdx.x % a.split, first = blockIdx.x / a.split, stride = gridDim.x / a.split;
   const int kb0 = (int)((int64_t)a.num_kb * rank / a.split), kb1 = (int)((int64_t)a.num_kb * (rank + 1) / a.split);
-  const int num_n = (a.N + 127) / 128, num_t = (int)((a.T + NT - 1) / NT), units = num_n * num_t;   // token tiles of a W tile follow one another
+  const int num_t = (int)((a.T + NT - 1) / NT);
+  // tile u: rows of W [128 nb, +128), tokens [NT tb, +NT); the token tiles of a block of W follow one another
+  auto tile = [&](int u, int& nb, int& tb) {
+    if (a.of_wide) {
+      int wm, wn;
+      wide_tile(a, a.unit0 + (u >> 2), wm, wn);
+      nb = 2 * wn + ((u >> 1) & 1); tb = 2 * wm + (u & 1);
+    } else { nb = (a.unit0 + u) / num_t; tb = a.unit0 + u - nb * num_t; }
+  };
 
   if (warp == 0 && lane == 0) {
     // ------------------------------------------------------------ TMA
     int stage = 0; uint32_t phase = 0, in_flight = 0;
     bool ok = true;
-    for (int unit = first; ok && unit < units; unit += stride) {
-      const int nb = unit / num_t, tb = unit - nb * num_t;
+    for (int unit = first; ok && unit < a.units; unit += stride) {
+      int nb, tb;
+      tile(unit, nb, tb);
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag, a.wait_limit)) { ok = false; break; }
         mbar_arrive_expect_tx(&full[stage], Z::STAGE);
@@ -346,7 +377,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     constexpr uint32_t idesc = make_idesc_f8(128, NT);
     int stage = 0, acc = 0; uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
-    for (int unit = first; ok && unit < units; unit += stride)
+    for (int unit = first; ok && unit < a.units; unit += stride)
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1, abort_flag, a.wait_limit) ||
             !mbar_wait(&full[stage], phase, abort_flag, a.wait_limit)) { ok = false; break; }
@@ -365,19 +396,22 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       for (int spin = 0; spin < (1 << 22) && !mbar_try_wait(drain, 0); ++spin) {}
     }
   } else if (warp >= 2) {
-    // ------------------------------------------------------------ scaling and output: a thread has one row of W
-    const int quad = warp & 3, r = quad * 32 + lane, e = threadIdx.x - 64;
+    // ------------------------------------------------------------ scaling and output: a thread has one row of W, COLS tokens
+    constexpr int EPI = 32 * Z::WARPS;
+    const int quad = warp & 3, group = (warp - 2) >> 2, r = quad * 32 + lane, e = threadIdx.x - 64;
     int acc = 0; uint32_t acc_phase = 0, turn = 0;
     bool ok = true;
-    for (int unit = first; unit < units; unit += stride) {
-      const int nb = unit / num_t, tb = unit - nb * num_t;
+    for (int unit = first; unit < a.units; unit += stride) {
+      int nb, tb;
+      tile(unit, nb, tb);
       const int64_t t0 = (int64_t)tb * NT;
-      const float* sw = a.sw + (int64_t)nb * a.ld_sw;
-      const float* sx = a.sx + min(t0 + e, a.T - 1) * a.ld_sx;       // thread e < NT brings the scale of token e
-      float sum[NT];
+      const float* sw = a.sw + (int64_t)min(nb, (a.N - 1) >> 7) * a.ld_sw;      // (tiles past the end are not stored)
+      const float* sx = a.sx + min(t0 + e, a.T - 1) * a.ld_sx;                  // thread e < NT brings the scale of token e
+      float2 sum[Z::COLS / 2];
       #pragma unroll
-      for (int j = 0; j < NT; ++j) sum[j] = 0.f;
+      for (int j = 0; j < Z::COLS / 2; ++j) sum[j] = both(0.f);
       float next = e < NT && kb0 < kb1 ? __ldg(sx + kb0) * __ldg(sw + kb0) : 0.f;
+      #pragma unroll 1
       for (int kb = kb0; kb < kb1; ++kb) {
         float* s = scales + (turn & 1u) * NT;
         ++turn;
@@ -385,62 +419,69 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
           s[e] = next;
           if (kb + 1 < kb1) next = __ldg(sx + kb + 1) * __ldg(sw + kb + 1);
         }
-        named_barrier_sync(1, 128);
+        named_barrier_sync(1, EPI);
         // (after a wait that ran out the warps go on without waiting: the barriers among them stay in step)
         if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, a.wait_limit));
         if (ok) {
           fence_after_sync();
-          const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * NT;
+          const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * NT + group * Z::COLS;
           float v[2][16];
           tmem_ld16(t_addr, v[0]);
           #pragma unroll
-          for (int c = 0; c < NT / 16; ++c) {
+          for (int c = 0; c < Z::COLS / 16; ++c) {
             tmem_ld_wait16(v[c & 1]);
-            if (c + 1 < NT / 16) tmem_ld16(t_addr + 16 * (c + 1), v[(c + 1) & 1]);
+            if (c + 1 < Z::COLS / 16) tmem_ld16(t_addr + 16 * (c + 1), v[(c + 1) & 1]);
             else {
               fence_before_sync();
               __syncwarp();
               if (lane == 0) mbar_arrive(&acc_empty[acc]);
             }
             #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(s + 16 * c + j);
-              sum[16 * c + j] = fmaf(f.x, v[c & 1][j], sum[16 * c + j]);
-              sum[16 * c + j + 1] = fmaf(f.y, v[c & 1][j + 1], sum[16 * c + j + 1]);
-              sum[16 * c + j + 2] = fmaf(f.z, v[c & 1][j + 2], sum[16 * c + j + 2]);
-              sum[16 * c + j + 3] = fmaf(f.w, v[c & 1][j + 3], sum[16 * c + j + 3]);
+            for (int j = 0; j < 8; j += 2) {
+              const float4 f = *reinterpret_cast<const float4*>(s + group * Z::COLS + 16 * c + 2 * j);
+              sum[8 * c + j] = fma2(make_float2(f.x, f.y), make_float2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), sum[8 * c + j]);
+              sum[8 * c + j + 1] = fma2(make_float2(f.z, f.w), make_float2(v[c & 1][2 * j + 2], v[c & 1][2 * j + 3]), sum[8 * c + j + 1]);
             }
           }
         }
         if (++acc == F8N_BUFFERS) { acc = 0; acc_phase ^= 1; }
       }
-      const int n = nb * 128 + r;
+      // through shared memory: the loop over the tokens is short code there, whatever their number
+      named_barrier_sync(1, EPI);
+      #pragma unroll
+      for (int j = 0; j < Z::COLS / 2; ++j) {
+        out[(group * Z::COLS + 2 * j) * 128 + r] = sum[j].x;
+        out[(group * Z::COLS + 2 * j + 1) * 128 + r] = sum[j].y;
+      }
       if (a.split == 1) {
-        #pragma unroll
-        for (int j = 0; j < NT; ++j)
-          if (n < a.N && t0 + j < a.T) {
-            if (a.out_bf16) static_cast<__nv_bfloat16*>(a.y)[(t0 + j) * a.ld_y + n] = __float2bfloat16_rn(sum[j]);
-            else            static_cast<float*>(a.y)[(t0 + j) * a.ld_y + n] = sum[j];
+        named_barrier_sync(1, EPI);
+        const int n = nb * 128 + (e & 127);
+        if (n < a.N) {
+          #pragma unroll 4
+          for (int j = e >> 7; j < NT; j += Z::GROUPS) {
+            if (t0 + j >= a.T) break;
+            if (a.out_bf16) static_cast<__nv_bfloat16*>(a.y)[(t0 + j) * a.ld_y + n] = __float2bfloat16_rn(out[j * 128 + (e & 127)]);
+            else            static_cast<float*>(a.y)[(t0 + j) * a.ld_y + n] = out[j * 128 + (e & 127)];
           }
-      } else {
-        // a cluster has one tile: all its stages have been read, and hold the CTA's sums now
-        float* part = reinterpret_cast<float*>(smem);
-        #pragma unroll
-        for (int j = 0; j < NT; ++j) part[j * 128 + r] = sum[j];
+        }
       }
     }
   }
-  if (a.split > 1) {
+  if (a.split > 1) {                  // a cluster has one tile: its CTAs add up a share of the tokens each
     __syncthreads();
     cluster_sync_all();
-    const int nb = first / num_t, tb = first - nb * num_t, r = threadIdx.x, n = nb * 128 + r;
-    const int j0 = NT * rank / a.split, j1 = NT * (rank + 1) / a.split;       // this CTA adds up these tokens
-    if (r < 128 && n < a.N)
-      for (int j = j0; j < j1 && (int64_t)tb * NT + j < a.T; ++j) {
+    int nb, tb;
+    tile(first, nb, tb);
+    const int r = threadIdx.x & 127, n = nb * 128 + r;
+    const int j0 = NT * rank / a.split, j1 = NT * (rank + 1) / a.split;
+    if (threadIdx.x < 128 * Z::GROUPS && n < a.N)
+      #pragma unroll 1
+      for (int j = j0 + ((int)threadIdx.x >> 7); j < j1 && (int64_t)tb * NT + j < a.T; j += Z::GROUPS) {
         float s = 0.f;
+        #pragma unroll 4
         for (int c = 0; c < a.split; ++c) {
           float p;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(map_to_cta(smem_u32(smem) + (uint32_t)(j * 128 + r) * 4, c)));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(map_to_cta(smem_u32(out) + (uint32_t)(j * 128 + r) * 4, c)));
           s += p;
         }
         const int64_t at = ((int64_t)tb * NT + j) * a.ld_y + n;
@@ -451,8 +492,9 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   }
   fence_before_sync();
   __syncthreads();
-  if (warp == 1) { fence_after_sync(); tmem_dealloc(tmem_base, Z::COLS); }
+  if (warp == 1) { fence_after_sync(); tmem_dealloc(tmem_base, Z::TMEM); }
   if (threadIdx.x == 0 && *abort_flag) raise_status(a.status, SAPO_ST_WAIT_TIMEOUT);
+  end_launch(a);
 }
 
 // ---------------------------------------------------------------------------- host
@@ -487,22 +529,42 @@ static bool allow_smem(Kernel kernel, size_t bytes, bool (&done)[MAX_DEVICES]) {
   return done[dev];
 }
 
+// CTAs that share a tile along K, for `tiles` tiles: as many as the SMs allow, each with at least two blocks of K
+static int split_of(int64_t tiles, int num_kb, int sms) {
+  int split = 1;
+  while (split < 8 && tiles * split * 2 <= sms && num_kb >= 4 * split) split *= 2;
+  return split;
+}
+
 template <int NT>
-static int launch_narrow(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs a, int sms, cudaStream_t st) {
+static int launch_narrow(const CUtensorMap& map_x, const CUtensorMap& map_w, Fp8GemmArgs a, int sms, cudaStream_t st) {
   static bool done[MAX_DEVICES] = {false};
   if (!allow_smem(fp8_narrow_kernel<NT>, Narrow<NT>::SMEM, done)) return SAPO_ERR_CUDA;
+  a.split = split_of(a.units, a.num_kb, sms);
+  const int grid = a.split > 1 ? a.units * a.split : (a.units < sms ? a.units : sms);
+  KernelScope scope(SAPO_K_FP8_MATMUL, st);
+  return launch_overlapped(fp8_narrow_kernel<NT>, dim3((unsigned)grid), Narrow<NT>::THREADS, Narrow<NT>::SMEM, a.split > 1 ? a.split : 0, st, map_x, map_w, a);
+}
+
+template <int NT>
+static int run_narrow(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs a, int sms, cudaStream_t st) {
   CUtensorMap map_x, map_w;
   if (!map_rows(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.data, K, a.T, a.T == 1 ? round_up<int64_t>(K, 16) : x.ld, NT) ||
       !map_rows(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w.data, K, a.N, a.N == 1 ? round_up<int64_t>(K, 16) : w.ld, 128)) return SAPO_ERR_CUDA;
   const int64_t units = ceil_div<int64_t>(a.N, 128) * ceil_div<int64_t>(a.T, NT);
-  a.split = 1;
-  while (a.split < 8 && units * a.split * 2 <= sms && a.num_kb >= 4 * a.split) a.split *= 2;      // at least two blocks of K a CTA
-  const int64_t grid = a.split > 1 ? units * a.split : (units < sms ? units : sms);
-  KernelScope scope(SAPO_K_FP8_MATMUL, st);
-  return launch_overlapped(fp8_narrow_kernel<NT>, dim3((unsigned)grid), F8N_THREADS, Narrow<NT>::SMEM, a.split > 1 ? a.split : 0, st, map_x, map_w, a);
+  if (units > 0x7FFFFFFF / 8) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  const int rest = (int)(units % sms);
+  a.units = (int32_t)units;
+  if (units < sms || rest == 0 || split_of(rest, a.num_kb, sms) == 1) return launch_narrow<NT>(map_x, map_w, a, sms, st);
+  a.units -= rest;
+  a.tail_follows = 1;
+  const int rc = launch_narrow<NT>(map_x, map_w, a, sms, st);
+  if (rc != SAPO_OK) return rc;
+  a.unit0 = a.units; a.units = rest; a.tail_follows = 0; a.tail = 1;
+  return launch_narrow<NT>(map_x, map_w, a, sms, st);
 }
 
-static int launch_wide(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs a, int sms, cudaStream_t st) {
+static int run_wide(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs a, int sms, cudaStream_t st) {
   static bool done[MAX_DEVICES] = {false};
   if (!allow_smem(fp8_wide_kernel, F8W_SMEM, done)) return SAPO_ERR_CUDA;
   const int size = a.out_bf16 ? 2 : 4;
@@ -513,13 +575,24 @@ static int launch_wide(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmA
   map_y = map_x;
   if (a.tma_store && !map_rows(&map_y, a.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, a.y, a.N, a.T,
                                a.ld_y * size, 128)) return SAPO_ERR_CUDA;
-  const int64_t num_m = ceil_div<int64_t>(a.T, 256), units = num_m * ceil_div<int64_t>(a.N, 256);
-  if (units > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  const int64_t num_m = ceil_div<int64_t>(a.T, 256), num_n = ceil_div<int64_t>(a.N, 256), units = num_m * num_n;
+  if (units > 0x7FFFFFFF / 8) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  a.num_m = (int32_t)num_m; a.num_n = (int32_t)num_n;
   const int64_t fit = (32ll << 20) / ((int64_t)256 * K);                    // token blocks that stay in a part of L2
   a.group_m = (int32_t)(fit < 1 ? 1 : (fit < num_m ? fit : num_m));
-  const int pairs = sms / 2;
-  KernelScope scope(SAPO_K_FP8_MATMUL, st);
-  return launch_overlapped(fp8_wide_kernel, dim3((unsigned)(2 * (units < pairs ? units : pairs))), F8W_THREADS, F8W_SMEM, 2, st, map_x, map_w, map_y, a);
+  // a last round that a quarter of the SMs or fewer would work on is left to narrow tiles, four of a wide one
+  const int pairs = sms / 2, rest = (int)(units % pairs);
+  const bool tail = units > pairs && rest > 0 && 4 * rest <= sms;
+  a.units = (int32_t)units - (tail ? rest : 0);
+  a.tail_follows = tail;
+  {
+    KernelScope scope(SAPO_K_FP8_MATMUL, st);
+    const int rc = launch_overlapped(fp8_wide_kernel, dim3((unsigned)(2 * (a.units < pairs ? a.units : pairs))), F8W_THREADS, F8W_SMEM, 2, st,
+                                     map_x, map_w, map_y, a);
+    if (rc != SAPO_OK || !tail) return rc;
+  }
+  a.unit0 = a.units; a.units = 4 * rest; a.of_wide = 1; a.tail_follows = 0; a.tail = 1;
+  return launch_narrow<128>(map_x, map_w, a, sms, st);
 }
 
 static bool usable(const sapo_fp8& m, int64_t rows, int32_t K) {
@@ -544,9 +617,9 @@ extern "C" int sapo_fp8_matmul(const sapo_fp8* h_x, int64_t T, const sapo_fp8* h
   a.y = y; a.ld_y = ld_y; a.T = T; a.N = N; a.num_kb = ceil_div(K, 128); a.out_bf16 = y_dtype == SAPO_DTYPE_BF16;
   a.wait_limit = WAIT_LIMIT_CLOCKS; a.status = status; a.split = 1; a.group_m = 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (T > 128 && ceil_div<int64_t>(T, 256) * ceil_div<int64_t>(N, 256) >= sms / 4) return launch_wide(*h_x, *h_w, K, a, sms, st);
-  if (T <= 16) return launch_narrow<16>(*h_x, *h_w, K, a, sms, st);
-  if (T <= 32) return launch_narrow<32>(*h_x, *h_w, K, a, sms, st);
-  if (T <= 64) return launch_narrow<64>(*h_x, *h_w, K, a, sms, st);
-  return launch_narrow<128>(*h_x, *h_w, K, a, sms, st);
+  if (T > 128 && ceil_div<int64_t>(T, 256) * ceil_div<int64_t>(N, 256) >= sms / 4) return run_wide(*h_x, *h_w, K, a, sms, st);
+  if (T <= 16) return run_narrow<16>(*h_x, *h_w, K, a, sms, st);
+  if (T <= 32) return run_narrow<32>(*h_x, *h_w, K, a, sms, st);
+  if (T <= 64) return run_narrow<64>(*h_x, *h_w, K, a, sms, st);
+  return run_narrow<128>(*h_x, *h_w, K, a, sms, st);
 }
