@@ -29,6 +29,7 @@ struct Fp8GemmArgs {
   int32_t group_m;          // wide: token blocks that are walked before the next column block
   int32_t tma_store;        // wide: y can be written by TMA
   int32_t split;            // narrow: CTAs that share a tile along K
+  int32_t rows, nt;         // narrow: rows of W (at most 128) and tokens (a multiple of 16, at most NT) of a tile
   int32_t unit0, units;     // the tiles of this launch
   int32_t of_wide;          // narrow: four tiles each of the wide tiles from unit0 on, which have this order's num_m, num_n
   int32_t num_m, num_n;     // wide tiles along tokens and columns
@@ -76,8 +77,8 @@ __device__ __forceinline__ void tmem_ld_wait16(float (&v)[16]) {
                  "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
 }
 
-// A grid of one CTA (pair) per SM (pair) leaves most of the device idle while the last, partial round of tiles runs; a
-// second launch takes these tiles and shares each among several CTAs along K.  It does not wait for the first one's results, so
+// A grid of one CTA pair per SM pair leaves most of the device idle while the last, partial round of wide tiles runs; a
+// second launch takes these tiles in narrow ones, and shares each of those among several CTAs along K.  It does not wait for the first one's results, so
 // the first lets it start (behind its own wait for what comes before the call) and its CTAs fill SMs as they fall idle;
 // what follows the call must wait for both, so the second waits for the first before it ends.
 __device__ __forceinline__ void begin_launch(const Fp8GemmArgs& a) {
@@ -293,13 +294,14 @@ fp8_wide_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 
 // ---------------------------------------------------------------------------- narrow tiles
 constexpr int F8N_BUFFERS = 4;                    // partial products in tensor memory
+constexpr int F8N_SCALES = 32;                    // blocks of K whose token scales are in shared memory
 template <int NT> struct Narrow {
   static constexpr int GROUPS = NT >= 64 ? 2 : 1, WARPS = 4 * GROUPS, COLS = NT / GROUPS;      // warps that scale; tokens of a thread
   static constexpr int THREADS = 64 + 32 * WARPS;                                              // warp 0: TMA, warp 1: MMA
   static constexpr uint32_t STAGE = F8_BOX + NT * F8_K, OUT = NT * 128 * 4;
   static constexpr int STAGES = (220 * 1024 - (int)OUT) / (int)STAGE < 10 ? (220 * 1024 - (int)OUT) / (int)STAGE : 10;
   static constexpr uint32_t TMEM = NT * F8N_BUFFERS < 64 ? 64 : NT * F8N_BUFFERS;
-  static constexpr size_t SMEM = 1024 + STAGES * STAGE + OUT + 2 * NT * 4 + 256;
+  static constexpr size_t SMEM = 1024 + STAGES * STAGE + OUT + F8N_SCALES * NT * 4 + 256;
   static_assert((TMEM & (TMEM - 1)) == 0 && TMEM <= 512 && SMEM <= 232448 && STAGES >= 4, "tensor or shared memory");
 };
 
@@ -310,8 +312,8 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* out = reinterpret_cast<float*>(smem + Z::STAGES * Z::STAGE);         // [NT][128]: a tile's sums
-  float* scales = out + NT * 128;                                             // [2][NT]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(scales + 2 * NT);
+  float* scales = out + NT * 128;                                             // [F8N_SCALES][NT]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(scales + F8N_SCALES * NT);
   uint64_t* full = bars;
   uint64_t* empty = bars + Z::STAGES;
   uint64_t* acc_full = bars + 2 * Z::STAGES;
@@ -339,8 +341,8 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
   const uint32_t tmem_base = *tmem_slot;
   const int rank = blockIdx.x % a.split, first = blockIdx.x / a.split, stride = gridDim.x / a.split;
   const int kb0 = (int)((int64_t)a.num_kb * rank / a.split), kb1 = (int)((int64_t)a.num_kb * (rank + 1) / a.split);
-  const int num_t = (int)((a.T + NT - 1) / NT);
-  // tile u: rows of W [128 nb, +128), tokens [NT tb, +NT); the token tiles of a block of W follow one another
+  const int num_t = (int)((a.T + a.nt - 1) / a.nt);
+  // tile u: rows of W [rows nb, + rows), tokens [nt tb, + nt); the token tiles of a block of W follow one another
   auto tile = [&](int u, int& nb, int& tb) {
     if (a.of_wide) {
       int wm, wn;
@@ -348,6 +350,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       nb = 2 * wn + ((u >> 1) & 1); tb = 2 * wm + (u & 1);
     } else { nb = (a.unit0 + u) / num_t; tb = a.unit0 + u - nb * num_t; }
   };
+  const uint32_t stage_bytes = (uint32_t)(a.rows + a.nt) * F8_K;
 
   if (warp == 0 && lane == 0) {
     // ------------------------------------------------------------ TMA
@@ -358,10 +361,10 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       tile(unit, nb, tb);
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(&empty[stage], phase ^ 1, abort_flag, a.wait_limit)) { ok = false; break; }
-        mbar_arrive_expect_tx(&full[stage], Z::STAGE);
-        uint8_t* to = smem + stage * Z::STAGE;
-        tma_load_2d(to, &map_w, &full[stage], kb * F8_K, nb * 128);
-        tma_load_2d(to + F8_BOX, &map_x, &full[stage], kb * F8_K, tb * NT);
+        mbar_arrive_expect_tx(&full[stage], stage_bytes);
+        uint8_t* to = smem + stage * Z::STAGE;             // (what a smaller box leaves of the stage makes sums that are not stored)
+        tma_load_2d(to, &map_w, &full[stage], kb * F8_K, nb * a.rows);
+        tma_load_2d(to + F8_BOX, &map_x, &full[stage], kb * F8_K, tb * a.nt);
         in_flight |= 1u << stage;
         if (++stage == Z::STAGES) { stage = 0; phase ^= 1; }
       }
@@ -374,7 +377,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       }
   } else if (warp == 1 && lane == 0) {
     // ------------------------------------------------------------ MMA
-    constexpr uint32_t idesc = make_idesc_f8(128, NT);
+    const uint32_t idesc = make_idesc_f8(128, a.nt);
     int stage = 0, acc = 0; uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
     for (int unit = first; ok && unit < a.units; unit += stride)
@@ -399,27 +402,33 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     // ------------------------------------------------------------ scaling and output: a thread has one row of W, COLS tokens
     constexpr int EPI = 32 * Z::WARPS;
     const int quad = warp & 3, group = (warp - 2) >> 2, r = quad * 32 + lane, e = threadIdx.x - 64;
-    int acc = 0; uint32_t acc_phase = 0, turn = 0;
+    int acc = 0; uint32_t acc_phase = 0;
     bool ok = true;
+    int held_tb = -1, held_kb = -1;                // token scales in shared memory: of token tile held_tb, from block held_kb on
     for (int unit = first; unit < a.units; unit += stride) {
       int nb, tb;
       tile(unit, nb, tb);
-      const int64_t t0 = (int64_t)tb * NT;
-      const float* sw = a.sw + (int64_t)min(nb, (a.N - 1) >> 7) * a.ld_sw;      // (tiles past the end are not stored)
-      const float* sx = a.sx + min(t0 + e, a.T - 1) * a.ld_sx;                  // thread e < NT brings the scale of token e
+      const int64_t t0 = (int64_t)tb * a.nt;
+      const float* sw = a.sw + (int64_t)(min(nb * a.rows + r, a.N - 1) >> 7) * a.ld_sw;      // (rows past the end are not stored)
       float2 sum[Z::COLS / 2];
       #pragma unroll
       for (int j = 0; j < Z::COLS / 2; ++j) sum[j] = both(0.f);
-      float next = e < NT && kb0 < kb1 ? __ldg(sx + kb0) * __ldg(sw + kb0) : 0.f;
+      float next_w = kb0 < kb1 ? __ldg(sw + kb0) : 0.f;
       #pragma unroll 1
       for (int kb = kb0; kb < kb1; ++kb) {
-        float* s = scales + (turn & 1u) * NT;
-        ++turn;
-        if (e < NT) {
-          s[e] = next;
-          if (kb + 1 < kb1) next = __ldg(sx + kb + 1) * __ldg(sw + kb + 1);
+        const int kb_base = kb0 + ((kb - kb0) / F8N_SCALES) * F8N_SCALES;
+        if (tb != held_tb || kb_base != held_kb) {      // the same for all these warps
+          named_barrier_sync(1, EPI);
+          const int t = e % NT, blocks = min(F8N_SCALES, kb1 - kb_base);
+          const float* from = a.sx + min(t0 + t, a.T - 1) * a.ld_sx + kb_base;
+          #pragma unroll 8
+          for (int k = e / NT; k < blocks; k += EPI / NT) scales[k * NT + t] = __ldg(from + k);
+          held_tb = tb; held_kb = kb_base;
+          named_barrier_sync(1, EPI);
         }
-        named_barrier_sync(1, EPI);
+        const float* s = scales + (kb - kb_base) * NT;
+        const float2 scale_w = both(next_w);
+        if (kb + 1 < kb1) next_w = __ldg(sw + kb + 1);
         // (after a wait that ran out the warps go on without waiting: the barriers among them stay in step)
         if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, a.wait_limit));
         if (ok) {
@@ -439,8 +448,8 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
             #pragma unroll
             for (int j = 0; j < 8; j += 2) {
               const float4 f = *reinterpret_cast<const float4*>(s + group * Z::COLS + 16 * c + 2 * j);
-              sum[8 * c + j] = fma2(make_float2(f.x, f.y), make_float2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), sum[8 * c + j]);
-              sum[8 * c + j + 1] = fma2(make_float2(f.z, f.w), make_float2(v[c & 1][2 * j + 2], v[c & 1][2 * j + 3]), sum[8 * c + j + 1]);
+              sum[8 * c + j] = fma2(mul2(make_float2(f.x, f.y), scale_w), make_float2(v[c & 1][2 * j], v[c & 1][2 * j + 1]), sum[8 * c + j]);
+              sum[8 * c + j + 1] = fma2(mul2(make_float2(f.z, f.w), scale_w), make_float2(v[c & 1][2 * j + 2], v[c & 1][2 * j + 3]), sum[8 * c + j + 1]);
             }
           }
         }
@@ -455,10 +464,10 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       }
       if (a.split == 1) {
         named_barrier_sync(1, EPI);
-        const int n = nb * 128 + (e & 127);
-        if (n < a.N) {
+        const int n = nb * a.rows + (e & 127);
+        if ((e & 127) < a.rows && n < a.N) {
           #pragma unroll 4
-          for (int j = e >> 7; j < NT; j += Z::GROUPS) {
+          for (int j = e >> 7; j < a.nt; j += Z::GROUPS) {
             if (t0 + j >= a.T) break;
             if (a.out_bf16) static_cast<__nv_bfloat16*>(a.y)[(t0 + j) * a.ld_y + n] = __float2bfloat16_rn(out[j * 128 + (e & 127)]);
             else            static_cast<float*>(a.y)[(t0 + j) * a.ld_y + n] = out[j * 128 + (e & 127)];
@@ -472,11 +481,11 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     cluster_sync_all();
     int nb, tb;
     tile(first, nb, tb);
-    const int r = threadIdx.x & 127, n = nb * 128 + r;
-    const int j0 = NT * rank / a.split, j1 = NT * (rank + 1) / a.split;
-    if (threadIdx.x < 128 * Z::GROUPS && n < a.N)
+    const int r = threadIdx.x & 127, n = nb * a.rows + r;
+    const int j0 = a.nt * rank / a.split, j1 = a.nt * (rank + 1) / a.split;
+    if (threadIdx.x < 128 * Z::GROUPS && r < a.rows && n < a.N)
       #pragma unroll 1
-      for (int j = j0 + ((int)threadIdx.x >> 7); j < j1 && (int64_t)tb * NT + j < a.T; j += Z::GROUPS) {
+      for (int j = j0 + ((int)threadIdx.x >> 7); j < j1 && (int64_t)tb * a.nt + j < a.T; j += Z::GROUPS) {
         float s = 0.f;
         #pragma unroll 4
         for (int c = 0; c < a.split; ++c) {
@@ -484,7 +493,7 @@ fp8_narrow_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(map_to_cta(smem_u32(out) + (uint32_t)(j * 128 + r) * 4, c)));
           s += p;
         }
-        const int64_t at = ((int64_t)tb * NT + j) * a.ld_y + n;
+        const int64_t at = ((int64_t)tb * a.nt + j) * a.ld_y + n;
         if (a.out_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(s);
         else            static_cast<float*>(a.y)[at] = s;
       }
@@ -537,10 +546,9 @@ static int split_of(int64_t tiles, int num_kb, int sms) {
 }
 
 template <int NT>
-static int launch_narrow(const CUtensorMap& map_x, const CUtensorMap& map_w, Fp8GemmArgs a, int sms, cudaStream_t st) {
+static int launch_narrow(const CUtensorMap& map_x, const CUtensorMap& map_w, const Fp8GemmArgs& a, int sms, cudaStream_t st) {
   static bool done[MAX_DEVICES] = {false};
   if (!allow_smem(fp8_narrow_kernel<NT>, Narrow<NT>::SMEM, done)) return SAPO_ERR_CUDA;
-  a.split = split_of(a.units, a.num_kb, sms);
   const int grid = a.split > 1 ? a.units * a.split : (a.units < sms ? a.units : sms);
   KernelScope scope(SAPO_K_FP8_MATMUL, st);
   return launch_overlapped(fp8_narrow_kernel<NT>, dim3((unsigned)grid), Narrow<NT>::THREADS, Narrow<NT>::SMEM, a.split > 1 ? a.split : 0, st, map_x, map_w, a);
@@ -548,19 +556,35 @@ static int launch_narrow(const CUtensorMap& map_x, const CUtensorMap& map_w, Fp8
 
 template <int NT>
 static int run_narrow(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs a, int sms, cudaStream_t st) {
+  a.nt = (int32_t)(a.T < NT ? round_up<int64_t>(a.T, 16) : NT);
+  const int64_t num_t = ceil_div<int64_t>(a.T, a.nt), full = ceil_div<int64_t>(a.N, 128) * num_t, rounds = ceil_div<int64_t>(full, sms);
+  if (full > 0x7FFFFFFF / 32) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  // Thin tiles: as few rows of W as make the last round of CTAs full (151936 rows are 9 rounds of 148 tiles of 115, not 8
+  // rounds of 128 and a ninth of 3 tiles).
+  const int64_t along_n = rounds * sms / num_t, least = a.nt > 32 ? a.nt : 32;
+  const int64_t even = along_n < 1 ? 128 : ceil_div<int64_t>(a.N, along_n), thin = even > 128 ? 128 : (even < least ? least : even);
+  // Against them: one round, its tiles shared along K; or, of several rounds, the last one shared so by a second launch.  An
+  // SM takes in about 40 KB a us, and not more than a block of K in 0.3; sharing a tile costs 3 us (a cluster's barriers and
+  // sums), a second launch 3.5.
+  const auto round_us = [&](int64_t rows) { const double us = (double)(rows + a.nt) * 128. / 40e3; return a.num_kb * (us > 0.3 ? us : 0.3); };
+  const double thin_us = rounds * round_us(thin);
+  const int64_t last = full % sms;
+  const int split = split_of(rounds == 1 ? full : last, a.num_kb, sms);
+  double shared_us = 1e30;
+  if (split > 1) shared_us = rounds == 1 ? round_us(128) / split + 3. : (rounds - 1 + 1. / split) * round_us(128) + 3.5;
+  const bool shared = shared_us < thin_us;
+  a.rows = (int32_t)(shared ? 128 : thin);
   CUtensorMap map_x, map_w;
-  if (!map_rows(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.data, K, a.T, a.T == 1 ? round_up<int64_t>(K, 16) : x.ld, NT) ||
-      !map_rows(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w.data, K, a.N, a.N == 1 ? round_up<int64_t>(K, 16) : w.ld, 128)) return SAPO_ERR_CUDA;
-  const int64_t units = ceil_div<int64_t>(a.N, 128) * ceil_div<int64_t>(a.T, NT);
-  if (units > 0x7FFFFFFF / 8) return SAPO_ERR_UNSUPPORTED_SHAPE;
-  const int rest = (int)(units % sms);
-  a.units = (int32_t)units;
-  if (units < sms || rest == 0 || split_of(rest, a.num_kb, sms) == 1) return launch_narrow<NT>(map_x, map_w, a, sms, st);
-  a.units -= rest;
+  if (!map_rows(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.data, K, a.T, a.T == 1 ? round_up<int64_t>(K, 16) : x.ld, a.nt) ||
+      !map_rows(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w.data, K, a.N, a.N == 1 ? round_up<int64_t>(K, 16) : w.ld, a.rows)) return SAPO_ERR_CUDA;
+  a.units = (int32_t)(ceil_div<int64_t>(a.N, a.rows) * num_t);
+  a.split = shared && rounds == 1 ? split : 1;
+  if (!shared || rounds == 1) return launch_narrow<NT>(map_x, map_w, a, sms, st);
+  a.units -= (int32_t)last;
   a.tail_follows = 1;
   const int rc = launch_narrow<NT>(map_x, map_w, a, sms, st);
   if (rc != SAPO_OK) return rc;
-  a.unit0 = a.units; a.units = rest; a.tail_follows = 0; a.tail = 1;
+  a.unit0 = a.units; a.units = (int32_t)last; a.split = split; a.tail_follows = 0; a.tail = 1;
   return launch_narrow<NT>(map_x, map_w, a, sms, st);
 }
 
@@ -580,9 +604,10 @@ static int run_wide(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs
   a.num_m = (int32_t)num_m; a.num_n = (int32_t)num_n;
   const int64_t fit = (32ll << 20) / ((int64_t)256 * K);                    // token blocks that stay in a part of L2
   a.group_m = (int32_t)(fit < 1 ? 1 : (fit < num_m ? fit : num_m));
-  // a last round that a quarter of the SMs or fewer would work on is left to narrow tiles, four of a wide one
+  // a last round of at most half the SM pairs is left to narrow tiles, four of a wide one, unless it is short (a second
+  // launch takes 3 to 4 us; 14 blocks of K take a wide tile 8)
   const int pairs = sms / 2, rest = (int)(units % pairs);
-  const bool tail = units > pairs && rest > 0 && 4 * rest <= sms;
+  const bool tail = units > pairs && rest > 0 && 4 * rest <= sms && a.num_kb >= 14;
   a.units = (int32_t)units - (tail ? rest : 0);
   a.tail_follows = tail;
   {
@@ -591,7 +616,8 @@ static int run_wide(const sapo_fp8& x, const sapo_fp8& w, int32_t K, Fp8GemmArgs
                                      map_x, map_w, map_y, a);
     if (rc != SAPO_OK || !tail) return rc;
   }
-  a.unit0 = a.units; a.units = 4 * rest; a.of_wide = 1; a.tail_follows = 0; a.tail = 1;
+  a.unit0 = a.units; a.units = 4 * rest; a.of_wide = 1; a.rows = 128; a.nt = 128; a.tail_follows = 0; a.tail = 1;
+  a.split = split_of(a.units, a.num_kb, sms);
   return launch_narrow<128>(map_x, map_w, a, sms, st);
 }
 
