@@ -654,7 +654,7 @@ typedef struct sapo_sample_cfg {
  * logp[b] = log softmax(z)[ids[b]], at temperature 1 and over all tokens: old_logp of the loss calls.
  * Logits of -inf rule a token out.  A row of -inf only gets id -1 and logp 0; so does a row with a NaN, with
  * +inf, or with a temperature, top_p or min_p that is NaN or out of range (SAPO_ST_NONFINITE_INPUT).
- * V >= 1, up to 1474048 bytes of logits a row (SAPO_ERR_UNSUPPORTED_SHAPE beyond); B may be 0.  Rows on 16-byte boundaries
+ * V in [1, 524287], up to 1474048 bytes of logits a row (SAPO_ERR_UNSUPPORTED_SHAPE beyond); B may be 0.  Rows on 16-byte boundaries
  * are read faster; ld may be 0 (several draws from one row). */
 int sapo_sample(const void* logits, int32_t dtype, int32_t B, int32_t V, int64_t ld, const int64_t* seeds,
                 const sapo_sample_cfg* h_cfg, int32_t* ids, float* logp, int32_t* status, void* stream);

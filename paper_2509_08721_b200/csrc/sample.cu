@@ -32,6 +32,7 @@ constexpr int SMP_LIST = 256;                 // candidates a block keeps
 constexpr float SMP_LEAD = 16.f;              // L: no candidate wins with probability 1e-7
 constexpr float SMP_LOG2E = 1.4426950408889634f;
 constexpr size_t SMP_MAX_PIECE = 180 * 1024;  // bytes of a row a block can hold
+constexpr int32_t SMP_MAX_TOKENS = (1 << 19) - 1;      // the sums of 13 bits of mass stay below 2^32
 constexpr float SMP_TIE = 1.001f;             // times nearer than this are told apart in 64 bits
 constexpr int SMP_THREADS = SMP_SORT;
 
@@ -47,7 +48,7 @@ struct Cut { uint32_t bin, before, count, mass_lo, mass_hi, before_lo, before_hi
 struct Last { uint32_t key, index, kept_lo, kept_hi; };                                 // the last token that stays, and the mass up to it
 
 struct SampleShared {
-  uint32_t slots[2][SMP_MAX_CLUSTER][4];    // what the blocks of the cluster tell one another; two sets, taken in turn
+  alignas(16) uint32_t slots[2][SMP_MAX_CLUSTER][4];    // what the blocks of the cluster tell one another; two sets, taken in turn
   uint32_t warp[2][32][4];
   uint32_t scan[32][4];
   uint32_t n_list, n_sort;
@@ -55,8 +56,8 @@ struct SampleShared {
   Cut cut;
   Last last;
   uint64_t sort[SMP_SORT];                  // tokens to be put in order: key, and the index from above
-  // of the tokens in a bin: their number, and their mass: sums of the lower 13 and of the other bits of mass_bits (histogram
-  // of the octaves), or a 64-bit number of units of 2^-40 (histogram of keys)
+  // of the tokens in a bin: their number, and the sums of the lower 13 and of the other bits of their mass_bits; once find() has
+  // been over a bin, its mass in units of 2^-40
   alignas(16) uint32_t count[SMP_BINS];
   uint32_t mass_lo[SMP_BINS], mass_hi[SMP_BINS];
 };
@@ -77,6 +78,10 @@ __device__ __forceinline__ uint64_t mass_units(uint64_t bits, uint32_t oct) { re
 __device__ __forceinline__ void add_shared_if(bool yes, uint32_t* to, uint32_t x) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}"
                ::"r"(umma::smem_u32(to)), "r"(x), "r"((uint32_t)yes) : "memory");
+}
+// adds to the same place of another block's shared memory
+__device__ __forceinline__ void add_remote(uint32_t* at, uint32_t block, uint32_t x) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(umma::map_to_cta(umma::smem_u32(at), block)), "r"(x) : "memory");
 }
 __device__ __forceinline__ uint64_t join64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
 
@@ -347,6 +352,25 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     return far;
   };
 
+  // an empty histogram, in all blocks
+  auto clear = [&]() {
+    uint4* h = reinterpret_cast<uint4*>(sh.count);
+    for (int i = tid; i < 3 * SMP_BINS / 4; i += THREADS) h[i] = make_uint4(0, 0, 0, 0);
+    barrier();
+  };
+  // Adds the block's histogram to the blocks that look after its bins (each to an equal share), but for its own share.  Done
+  // once this block's own additions are, and complete at the next barrier of the cluster.
+  auto share_histogram = [&]() {
+    __syncthreads();
+    const int per_block = SMP_BINS / (int)C;
+    for (int i = tid; i < SMP_BINS; i += THREADS) {
+      const uint32_t owner = (uint32_t)(i / per_block), c = sh.count[i];
+      if (owner == rank || c == 0) continue;
+      add_remote(&sh.count[i], owner, c);
+      if (by_mass) { add_remote(&sh.mass_lo[i], owner, sh.mass_lo[i]); add_remote(&sh.mass_hi[i], owner, sh.mass_hi[i]); }
+    }
+  };
+
   // ---- sums of the weights at temperature 1 and at the row's, of the tokens that min_p keeps; the first token with the
   //      largest logit; for top-k and top-p a histogram of the octaves, without the tokens of its last bin
   uint32_t sums[4];
@@ -367,7 +391,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       }
     }
     if (cuts) {
-      if (!few) far = histogram();
+      if (!few) { far = histogram(); share_histogram(); }
     } else if (other) {
       for (int v = tid; v < n_vec; v += THREADS) {
         float z[8];
@@ -434,27 +458,21 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   //      the ones up to index_cut
   uint32_t key_cut = 0, index_cut = ALL;
   if (cuts) {
-    // The bin of the histograms in which the search ends: the one with the target-th token, or the one where the mass
-    // reaches `target` (of_total: times the mass of all); beyond the histogram there are, with_far, the tokens of its last
-    // bin.  Each block adds up its share of the bins over the cluster, in place: no other block reads that part of its own.
+    // The bin of the histogram in which the search ends: the one with the target-th token, or the one where the mass
+    // reaches `target` (of_total: times the mass of all).  octave < 0: a histogram of the octaves, beyond which there are
+    // the tokens of its last bin; else one of keys, of tokens of that octave.  Each block looks through its share of the bins.
     struct Found { Cut cut; double target; };
-    auto find = [&](bool mass_wanted, double target, bool of_total, uint32_t before, uint64_t before_mass, bool with_far) -> Found {
+    auto find = [&](bool mass_wanted, double target, bool of_total, uint32_t before, uint64_t before_mass, int octave) -> Found {
+      const bool with_far = octave < 0;
       const int per_block = SMP_BINS / (int)C, per = max(1, per_block / THREADS), bin0 = (int)rank * per_block + tid * per;
       uint32_t c_sum = 0; uint64_t m_sum = 0;
       if (tid * per < per_block)
         #pragma unroll 1
         for (int i = bin0; i < bin0 + per; ++i) {
-          uint32_t c = 0; uint64_t m = 0;
-          #pragma unroll
-          for (uint32_t r = 0; r < SMP_MAX_CLUSTER; ++r) {       // (no branches: the loads are all in flight together)
-            const uint32_t from = min(r, C - 1), one = r < C ? 1u : 0u;
-            c += one * *cluster.map_shared_rank(&sh.count[i], from);
-            const uint32_t lo = one * *cluster.map_shared_rank(&sh.mass_lo[i], from), hi = one * *cluster.map_shared_rank(&sh.mass_hi[i], from);
-            m += with_far ? ((uint64_t)hi << 13) + lo : join64(lo, hi);
-          }
-          if (with_far) m = mass_units(m, (uint32_t)i >> 6);
-          sh.count[i] = c; sh.mass_lo[i] = (uint32_t)m; sh.mass_hi[i] = (uint32_t)(m >> 32);
-          c_sum += c; m_sum += m;
+          const uint32_t lo = sh.mass_lo[i], hi = sh.mass_hi[i];
+          const uint64_t m = mass_units(((uint64_t)hi << 13) + lo, with_far ? (uint32_t)i >> 6 : (uint32_t)octave);
+          sh.mass_lo[i] = (uint32_t)m; sh.mass_hi[i] = (uint32_t)(m >> 32);
+          c_sum += sh.count[i]; m_sum += m;
         }
       uint32_t c_in = c_sum; uint64_t m_in = m_sum;               // inclusive sums over the threads
       #pragma unroll
@@ -467,19 +485,22 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
       __syncthreads();
       uint32_t total[3] = {0, 0, 0}, c_base = 0;
       uint64_t m_all = 0, m_base = 0;
-      #pragma unroll 1
+      #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
         if (w == warp) { c_base = total[0]; m_base = m_all; }
-        total[0] += sh.scan[w][0]; m_all += join64(sh.scan[w][1], sh.scan[w][2]);
+        const uint4 x = *reinterpret_cast<const uint4*>(sh.scan[w]);
+        total[0] += x.x; m_all += join64(x.y, x.z);
       }
       total[1] = (uint32_t)m_all; total[2] = (uint32_t)(m_all >> 32);
       const uint32_t (*all)[4] = exchange(total, 3);
       uint32_t c_at = before + c_base + c_in - c_sum, c_end = before;
       uint64_t m_at = before_mass + m_base + m_in - m_sum, m_end = before_mass;
-      #pragma unroll 1
-      for (uint32_t r = 0; r < C; ++r) {
+      #pragma unroll
+      for (uint32_t r = 0; r < SMP_MAX_CLUSTER; ++r) {
+        if (r >= C) break;
         if (r == rank) { c_at += c_end - before; m_at += m_end - before_mass; }
-        c_end += all[r][0]; m_end += join64(all[r][1], all[r][2]);
+        const uint4 x = *reinterpret_cast<const uint4*>(all[r]);
+        c_end += x.x; m_end += join64(x.y, x.z);
       }
       const uint32_t far_count = with_far ? (uint32_t)a.V - c_end : 0;
       const uint64_t far_mass = with_far ? (uint64_t)((double)__uint_as_float(sums[3]) * 1099511627776.0) : 0;
@@ -581,10 +602,11 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         return;
       }
       sums[3] = __float_as_uint(histogram());                  // (too many equal ones): as with a large top_k
+      share_histogram();
       sums[0] = sums[1] = sums[2] = 0;
       reduce(sums, [&](uint32_t* p, const uint32_t* q) { add(p[3], q[3]); });
     }
-    const Found f = find(!by_count, by_count ? (double)top_k : (double)top_p, !by_count, 0, 0, true);
+    const Found f = find(!by_count, by_count ? (double)top_k : (double)top_p, !by_count, 0, 0, -1);
     if (f.cut.before + f.cut.count <= SMP_SORT) {
       const uint32_t bin = f.cut.bin;
       uint64_t x;
@@ -614,6 +636,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         return join64(sh.last.kept_lo, sh.last.kept_hi);
       }
       // Many tokens in one bin: their range of keys is cut into bins again, until a single key is left.
+      const uint32_t oct = cut.bin >> 6;
       uint32_t key_low = 0, key_high = 0;
       #pragma unroll 1
       for (int level = 0; level < 5; ++level) {      // 32 bits of key in steps of 11, and the look that finds one key
@@ -625,19 +648,19 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
         if (key_low >= key_high) break;
         int shift = 0;
         while (((key_high - key_low) >> shift) >= SMP_BINS) ++shift;
-        for (int i = tid; i < SMP_BINS; i += THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
-        __syncthreads();
+        clear();
         for_each([&](float z) { return order_key(z) >= key_low && order_key(z) <= key_high; },
                  [&](int, float z) {
                    const uint32_t bin = (key_high - order_key(z)) >> shift;
                    atomicAdd(&sh.count[bin], 1u);
                    if (!by_mass) return;
-                   const uint64_t m = mass_of(z);
-                   const uint32_t lo = (uint32_t)m, was = atomicAdd(&sh.mass_lo[bin], lo), hi = (uint32_t)(m >> 32) + (was + lo < was);
-                   if (hi) atomicAdd(&sh.mass_hi[bin], hi);
+                   const uint32_t m = mass_bits(octaves(z), oct);      // (the tokens of one bin are of one octave)
+                   atomicAdd(&sh.mass_lo[bin], m & 8191u);
+                   atomicAdd(&sh.mass_hi[bin], m >> 13);
                  });
+        share_histogram();
         barrier();
-        cut = find(mass_wanted, target, false, cut.before, join64(cut.before_lo, cut.before_hi), false).cut;
+        cut = find(mass_wanted, target, false, cut.before, join64(cut.before_lo, cut.before_hi), (int)oct).cut;
         if (cut.count == 0) {                        // the mass falls short of the target by rounding: all of them stay
           key_cut = key_low; index_cut = ALL;
           return (uint64_t)target;
@@ -697,13 +720,12 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     };
     uint64_t stays = search(f, !by_count);
     if (by_count && by_mass) {
-      if (C > 1) cluster.sync();                     // find() has added the blocks' histograms up in place, search() may have used them
-      for (int i = tid; i < SMP_BINS; i += THREADS) { sh.count[i] = 0; sh.mass_lo[i] = 0; sh.mass_hi[i] = 0; }
-      __syncthreads();
+      clear();
       sums[3] = __float_as_uint(histogram());
+      share_histogram();
       sums[0] = sums[1] = sums[2] = 0;
       reduce(sums, [&](uint32_t* p, const uint32_t* q) { add(p[3], q[3]); });
-      stays = search(find(true, (double)top_p * (double)stays, false, 0, 0, true), true);
+      stays = search(find(true, (double)top_p * (double)stays, false, 0, 0, -1), true);
     }
     weight = (float)((double)stays * 9.094947017729282e-13);      // 2^-40
     if (!by_mass || floor_octaves < CUDART_INF_F) {               // not known from the search, or min_p takes some out
@@ -1142,7 +1164,7 @@ extern "C" int sapo_sample(const void* logits, int32_t dtype, int32_t B, int32_t
   if (B == 0) return SAPO_OK;
   if (!logits || !seeds || !ids || !logp) return SAPO_ERR_INVALID_ARG;
   const size_t size = dtype == SAPO_DTYPE_BF16 ? 2 : 4;
-  if ((int64_t)V * (int64_t)size > (int64_t)SMP_MAX_CLUSTER * (int64_t)SMP_MAX_PIECE - 64 * SMP_MAX_CLUSTER || B > (1 << 24)) return SAPO_ERR_UNSUPPORTED_SHAPE;
+  if (V > SMP_MAX_TOKENS || (int64_t)V * (int64_t)size > (int64_t)SMP_MAX_CLUSTER * (int64_t)SMP_MAX_PIECE - 64 * SMP_MAX_CLUSTER || B > (1 << 24)) return SAPO_ERR_UNSUPPORTED_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) % size) return SAPO_ERR_INVALID_ARG;
   const int sms = sm_count();
   if (sms <= 0) return SAPO_ERR_CUDA;
