@@ -567,7 +567,8 @@ int sapo_adam_step(float* master, float* m, float* v, const float* grad, void* w
  * the bits of t as fp32 those of weight below 2^20 are cut off after 16 r + 8 has been added, r being 16 random
  * bits; element i of tensor `number` in the list takes half i % 8 (low half of a word first) of
  * philox4x32-10(counter = (i / 8 low, i / 8 high, number, step), key = (seed low, seed high)).  Each product and sum of
- * the state is rounded to fp32 by itself, so that the state is defined to the bit.  Zeroed codes and scales are a fresh state. */
+ * the state is rounded to fp32 by itself, so that the state is defined to the bit (but for a last bit of about one root
+ * in 10^5; the root of a v below the normal numbers is 0).  Zeroed codes and scales are a fresh state. */
 typedef struct sapo_adamw_tensor {
   const float* master;
   float*       master_out;

@@ -9,7 +9,8 @@
 // eps alone.
 //
 // HBM-bound: per weight 4 + 4 (master) + 2 or 4 (gradient) + 2 (bf16 copy) + 16 (32 bits) or 4.13 (8 bits) bytes.  A
-// warp takes 512 consecutive elements, four groups, all loads before the first use.
+// warp takes 512 consecutive elements (256 with 8-bit states, which are as much work as memory: more warps hide it better), all
+// loads before the first use.
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -20,9 +21,10 @@
 namespace sapo {
 
 constexpr int ADW_THREADS = 256;
-constexpr int ADW_GROUPS = 4;                                       // groups of 128 a warp takes at a time
-constexpr int ADW_WARP = ADW_GROUPS * F8_GROUP;
-constexpr int ADW_BLOCK = ADW_WARP * ADW_THREADS / 32;              // elements a block takes
+// groups of 128 a warp takes at a time, and the elements of a warp and of a block
+template <bool BITS8> constexpr int ADW_GROUPS = BITS8 ? 2 : 4;
+template <bool BITS8> constexpr int ADW_WARP = ADW_GROUPS<BITS8> * F8_GROUP;
+template <bool BITS8> constexpr int ADW_BLOCK = ADW_WARP<BITS8> * ADW_THREADS / 32;
 constexpr int ADW_TENSORS = 32;                                     // tensors a launch takes (its parameters hold the list)
 
 struct AdamWEntry {
@@ -122,7 +124,22 @@ __device__ __forceinline__ float2 product(float2 a, float2 b) { return make_floa
 // A root in units of its scale, rounded to one of the two codes around it: bits16 is 16 times a number uniform on [0, 65536).
 __device__ __forceinline__ float round_root(float t, uint32_t bits16) {
   const uint32_t up = (__float_as_uint(fmaxf(t, 0.015625f)) + (bits16 | 8u)) & 0xFFF00000u;
-  return t > 0.f ? fminf(__uint_as_float(up), F8_TOP) : 0.f;
+  return t > 0.f ? __uint_as_float(up) : 0.f;            // (480, one step above the largest code, is stored as that one)
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Square roots of two numbers: an approximation of the inverse root and one step of Newton's method on it, s + (v - s s) / (2 s),
+// with the residual exact.  Rounded correctly but for about one in 10^5 (one unit then); of v below the normal numbers 0.
+__device__ __forceinline__ float2 root2(float2 v) {
+  const float least = 1.17549435e-38f;
+  float2 y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, least)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, least)));
+  const float2 s = mul2(v, y), r = fma2(fma2(make_float2(-s.x, -s.y), s, v), mul2(y, both(0.5f)), s);
+  return make_float2(v.x >= least ? r.x : 0.f, v.y >= least ? r.y : 0.f);
 }
 
 // What a step has in common for the elements of a tensor
@@ -132,14 +149,15 @@ struct AdamWStep { float minus_lr, shrink, grad_scale, inv_bias1, inv_bias2_root
 template <bool BITS8, class G, bool WHOLE>
 __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& t, const AdamWStep& c, int64_t base) {
   constexpr uint32_t ALL = 0xFFFFFFFFu;
+  constexpr int GROUPS = ADW_GROUPS<BITS8>, WARP = ADW_WARP<BITS8>;
   const int lane = threadIdx.x & 31;
   const int64_t at = base + 4 * lane, group = base >> 7, groups = (t.n + F8_GROUP - 1) >> 7;
-  const int left = WHOLE ? ADW_WARP : (int)max((int64_t)-ADW_WARP, min((int64_t)ADW_WARP, t.n - at));      // elements from this lane's first on
-  Four g[ADW_GROUPS], w[ADW_GROUPS], m[ADW_GROUPS], v[ADW_GROUPS];
-  uint32_t qm[ADW_GROUPS], qv[ADW_GROUPS];
-  float sm[ADW_GROUPS], sv[ADW_GROUPS];
+  const int left = WHOLE ? WARP : (int)max((int64_t)-WARP, min((int64_t)WARP, t.n - at));      // elements from this lane's first on
+  Four g[GROUPS], w[GROUPS], m[GROUPS], v[GROUPS];
+  uint32_t qm[GROUPS], qv[GROUPS];
+  float sm[GROUPS], sv[GROUPS];
   #pragma unroll
-  for (int u = 0; u < ADW_GROUPS; ++u) {
+  for (int u = 0; u < GROUPS; ++u) {
     g[u] = load4<WHOLE>(static_cast<const G*>(t.grad) + at + u * F8_GROUP, left - u * F8_GROUP);
     w[u] = load4<WHOLE>(t.master + at + u * F8_GROUP, left - u * F8_GROUP);
     if (BITS8) {
@@ -154,10 +172,10 @@ __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& 
     }
   }
   // random words: the eight elements of a counter belong to two lanes; each of them makes the counters of every other group
-  uint32_t rnd[ADW_GROUPS][2];
+  uint32_t rnd[GROUPS][2];
   if (BITS8) {
     #pragma unroll
-    for (int u = 0; u < ADW_GROUPS; u += 2) {
+    for (int u = 0; u < GROUPS; u += 2) {
       const uint64_t eight = (uint64_t)(base + (u + (lane & 1)) * F8_GROUP + 4 * (lane & ~1)) >> 3;
       const uint4 r = philox4x32_10((uint32_t)eight, (uint32_t)(eight >> 32), (uint32_t)t.number, c.step, a.k0, a.k1);
       const bool odd = lane & 1;
@@ -167,10 +185,10 @@ __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& 
     }
   }
   // moments and weights; afterwards m and v hold the new m and (8 bits) the new root
-  uint32_t most_m[ADW_GROUPS], most_r[ADW_GROUPS];      // of the groups
+  uint32_t most_m[GROUPS], most_r[GROUPS];      // of the groups
   bool bad = false;
   #pragma unroll
-  for (int u = 0; u < ADW_GROUPS; ++u) {
+  for (int u = 0; u < GROUPS; ++u) {
     float big = 0.f, mm = 0.f, mr = 0.f;
     float2 x[2], m0[2], v0[2];
     float root[4];
@@ -202,9 +220,9 @@ __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& 
         m1 = make_float2(fine[0] ? m1.x : m0[h].x, fine[1] ? m1.y : m0[h].y);
         v1 = make_float2(fine[0] ? fminf(v1.x, 3.402823466e38f) : v0[h].x, fine[1] ? fminf(v1.y, 3.402823466e38f) : v0[h].y);
       }
-      const float2 r1 = make_float2(sqrtf(v1.x), sqrtf(v1.y));
+      const float2 r1 = BITS8 ? root2(v1) : make_float2(sqrtf(v1.x), sqrtf(v1.y));
       const float2 above = mul2(m1, both(c.inv_bias1)), below = fma2(r1, both(c.inv_bias2_root), both(a.eps));
-      const float2 now = fma2(both(c.minus_lr), make_float2(__fdividef(above.x, below.x), __fdividef(above.y, below.y)), mul2(was, both(c.shrink)));
+      const float2 now = fma2(both(c.minus_lr), mul2(above, make_float2(rcp_fast(below.x), rcp_fast(below.y))), mul2(was, both(c.shrink)));
       w[u].v[2 * h] = fine[0] ? now.x : was.x; w[u].v[2 * h + 1] = fine[1] ? now.y : was.y;
       m[u].v[2 * h] = m1.x; m[u].v[2 * h + 1] = m1.y;
       v[u].v[2 * h] = BITS8 ? r1.x : v1.x; v[u].v[2 * h + 1] = BITS8 ? r1.y : v1.y;
@@ -221,20 +239,20 @@ __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& 
     }
   }
   if (BITS8) {
-    // the divisions of the eight groups (m and root of four) are done by a lane each
+    // the divisions of the groups (of m, then of the root) are done by a lane each
     uint32_t mine = 0;
     #pragma unroll
-    for (int u = 0; u < ADW_GROUPS; ++u) {
-      if ((lane & 7) == u) mine = most_m[u];
-      if ((lane & 7) == ADW_GROUPS + u) mine = most_r[u];
+    for (int u = 0; u < GROUPS; ++u) {
+      if ((lane & (2 * GROUPS - 1)) == u) mine = most_m[u];
+      if ((lane & (2 * GROUPS - 1)) == GROUPS + u) mine = most_r[u];
     }
     float scale, inv;
     f8_group(__uint_as_float(mine), scale, inv);
-    const int64_t own = group + (lane & (ADW_GROUPS - 1));
-    if (lane < 2 * ADW_GROUPS && (WHOLE || own < groups)) (lane < ADW_GROUPS ? t.m_scale_out : t.v_scale_out)[own] = scale;
+    const int64_t own = group + (lane & (GROUPS - 1));
+    if (lane < 2 * GROUPS && (WHOLE || own < groups)) (lane < GROUPS ? t.m_scale_out : t.v_scale_out)[own] = scale;
     #pragma unroll
-    for (int u = 0; u < ADW_GROUPS; ++u) {
-      const float2 im = both(__shfl_sync(ALL, inv, u)), ir = both(__shfl_sync(ALL, inv, ADW_GROUPS + u));
+    for (int u = 0; u < GROUPS; ++u) {
+      const float2 im = both(__shfl_sync(ALL, inv, u)), ir = both(__shfl_sync(ALL, inv, GROUPS + u));
       const float2 x = mul2(make_float2(m[u].v[0], m[u].v[1]), im), y = mul2(make_float2(m[u].v[2], m[u].v[3]), im);
       store_codes<WHOLE>(static_cast<uint8_t*>(t.m_out) + at + u * F8_GROUP, left - u * F8_GROUP, f8_pack4(x.x, x.y, y.x, y.y));
       const float2 p = mul2(make_float2(v[u].v[0], v[u].v[1]), ir), q = mul2(make_float2(v[u].v[2], v[u].v[3]), ir);
@@ -247,7 +265,7 @@ __device__ __forceinline__ void adamw_run(const AdamWArgs& a, const AdamWEntry& 
 }
 
 template <bool BITS8, class G>
-__global__ void __launch_bounds__(ADW_THREADS, 3) adamw_kernel(const __grid_constant__ AdamWArgs a) {
+__global__ void __launch_bounds__(ADW_THREADS, BITS8 ? 5 : 3) adamw_kernel(const __grid_constant__ AdamWArgs a) {
   wait_for_previous();
   const int warp = threadIdx.x >> 5;
   int lo = 0, hi = a.n_tensors - 1;            // the last tensor whose first block is not behind this one
@@ -265,11 +283,11 @@ __global__ void __launch_bounds__(ADW_THREADS, 3) adamw_kernel(const __grid_cons
     __syncthreads();
     inv_bias1 = bias[0]; inv_bias2_root = bias[1];
   }
-  const int64_t base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK + (int64_t)warp * ADW_WARP;
+  const int64_t base = (int64_t)((int)blockIdx.x - t.first_block) * ADW_BLOCK<BITS8> + (int64_t)warp * ADW_WARP<BITS8>;
   if (base >= t.n) return;
   const double lr = (a.lr_dev != nullptr ? (double)*a.lr_dev : a.lr) * (double)t.lr_factor;
   const AdamWStep c{-(float)lr, (float)(1.0 - lr * (double)t.decay), a.grad_scale != nullptr ? *a.grad_scale : 1.f, inv_bias1, inv_bias2_root, step};
-  if (t.vectors && base + ADW_WARP <= t.n) adamw_run<BITS8, G, true>(a, t, c, base);
+  if (t.vectors && base + ADW_WARP<BITS8> <= t.n) adamw_run<BITS8, G, true>(a, t, c, base);
   else                                     adamw_run<BITS8, G, false>(a, t, c, base);
 }
 
@@ -291,7 +309,7 @@ static int launch_adamw(const sapo_adamw_tensor* list, int32_t n, AdamWArgs& a, 
   for (int32_t i = 0; i < n; ++i) {
     const sapo_adamw_tensor& t = list[i];
     if (t.n == 0 || (t.state_bits == 8) != BITS8 || t.grad_dtype != g_dtype) continue;
-    const int64_t need = ceil_div<int64_t>(t.n, ADW_BLOCK);
+    const int64_t need = ceil_div<int64_t>(t.n, ADW_BLOCK<BITS8>);
     if (a.n_tensors == ADW_TENSORS || blocks + need > 0x7FFFFFFF) {
       const int rc = launch();
       if (rc != SAPO_OK) return rc;
@@ -328,7 +346,7 @@ extern "C" int sapo_adamw_step(const sapo_adamw_tensor* h_tensors, int32_t n_ten
         !multiple_of(t.m_out, s) || !multiple_of(t.v_out, s) || !multiple_of(t.copy_bf16, 2))
       return SAPO_ERR_INVALID_ARG;
     if (!(t.weight_decay - t.weight_decay == 0.f) || !(t.lr_factor - t.lr_factor == 0.f)) return SAPO_ERR_INVALID_ARG;
-    if (ceil_div<int64_t>(t.n, ADW_BLOCK) > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
+    if (ceil_div<int64_t>(t.n, ADW_BLOCK<true>) > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
   }
   if (current_device() < 0) return SAPO_ERR_CUDA;
   AdamWArgs a;
