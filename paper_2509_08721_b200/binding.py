@@ -1016,7 +1016,7 @@ class AdamWTensors:
         self.copies, self.lr_factor, self.weight_decay = each(copies), each(1.0 if lr_factor is None else lr_factor), each(weight_decay)
         if not len(self.states) == len(self.copies) == len(self.lr_factor) == len(self.weight_decay) == n:
             raise SapoError("one state, copy, lr_factor and weight_decay per tensor")
-        self.sizes, self.bits = [], []
+        self.sizes, self.bits, self._kept = [], [], None
         for p, st, copy in zip(self.params, self.states, self.copies):
             k = p.numel()
             self.sizes.append(k)
@@ -1038,6 +1038,22 @@ class AdamWTensors:
         st = self.states[i]
         return self.params[i], st.m, st.v, st.m_scale, st.v_scale
 
+    def _list(self, to: "AdamWTensors"):
+        """The C list of a step into `to`, all but the gradients; kept for the next one as long as no array has moved."""
+        kept = self._kept
+        if kept is not None and kept[0] is to and [f() for f in kept[1]] == kept[2]:
+            return kept[3]
+        n = len(self.params)
+        list_c, asked = (AdamWTensorC * max(n, 1))(), []
+        for i in range(n):
+            (w, m, v, ms, vs), (w2, m2, v2, ms2, vs2) = self.arrays(i), to.arrays(i)
+            list_c[i] = AdamWTensorC(_p(w), _p(w2), None, _p(m), _p(v), _p(m2), _p(v2), _p(ms), _p(vs), _p(ms2), _p(vs2), _p(to.copies[i]),
+                                     self.sizes[i], self.lr_factor[i], self.weight_decay[i] or 0.0, 0, self.bits[i])
+            asked += [t.data_ptr for t in (w, m, v, ms, vs, w2, m2, v2, ms2, vs2, to.copies[i]) if t is not None]
+        asked = list({id(f.__self__): f for f in asked}.values())
+        self._kept = to, asked, [f() for f in asked], list_c
+        return list_c
+
 
 def sapo_adamw_step(tensors: AdamWTensors, grads, step, lr, status: torch.Tensor, beta1: float = 0.9, beta2: float = 0.999,
                     eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0, grad_scale: Optional[torch.Tensor] = None,
@@ -1051,17 +1067,15 @@ def sapo_adamw_step(tensors: AdamWTensors, grads, step, lr, status: torch.Tensor
     if len(grads) != n or to.sizes != tensors.sizes or to.bits != tensors.bits:
         raise SapoError("one gradient per tensor, and outputs of the same sizes and states")
     _here(status, *grads, *tensors.params[:1], *to.params[:1], *(v for v in (step, lr, grad_scale) if isinstance(v, torch.Tensor)))
-    list_c = (AdamWTensorC * max(n, 1))()
-    for i, g in enumerate(grads):
+    kept = tensors._list(to)
+    list_c = type(kept).from_buffer_copy(kept)               # (of this call alone: others may be under way)
+    for c, g, size, decay in zip(list_c, grads, tensors.sizes, tensors.weight_decay):
         code = _DTYPE_CODES.get(g.dtype)
-        if code is None or g.numel() != tensors.sizes[i] or not g.is_contiguous() or not g.is_cuda:
-            raise SapoError(f"gradient {i} must be contiguous bf16 or float32 with {tensors.sizes[i]} elements on the GPU")
-        w, m, v, ms, vs = tensors.arrays(i)
-        w2, m2, v2, ms2, vs2 = to.arrays(i)
-        decay = tensors.weight_decay[i]
-        list_c[i] = AdamWTensorC(w.data_ptr(), w2.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), m2.data_ptr(), v2.data_ptr(),
-                                 _p(ms), _p(vs), _p(ms2), _p(vs2), _p(to.copies[i]), tensors.sizes[i], tensors.lr_factor[i],
-                                 weight_decay if decay is None else decay, code, tensors.bits[i])
+        if code is None or g.numel() != size or not g.is_contiguous() or not g.is_cuda:
+            raise SapoError(f"each gradient must be contiguous bf16 or float32 with as many elements as its weight ({size}), on the GPU")
+        c.grad, c.grad_dtype = g.data_ptr(), code
+        if decay is None:
+            c.weight_decay = weight_decay
     on_device = lambda t, dtype, what: _at_least(t, dtype, 1, what) if isinstance(t, torch.Tensor) else None
     step_dev, lr_dev = on_device(step, torch.int32, "step"), on_device(lr, torch.float32, "lr")
     cfg = AdamWCfgC(0.0 if lr_dev else lr, beta1, beta2, eps, int(seed) & (2**64 - 1), 1 if step_dev else int(step), step_dev, lr_dev,

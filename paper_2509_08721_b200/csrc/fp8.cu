@@ -80,7 +80,8 @@ __device__ __forceinline__ void store8(uint8_t* p, int left, bool vec, const Eig
   }
 }
 
-template <class T>
+// WHOLE: rows of whole pieces on boundaries for vectors, no bounds to look at.
+template <class T, bool WHOLE>
 __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArgs a) {
   wait_for_previous();
   const int lane = threadIdx.x & 31;
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArg
     const int col_first = col;
     #pragma unroll
     for (int u = 0; u < F8S_PIECES; ++u) {
-      load8(e[u], static_cast<const T*>(a.x) + row * a.ld_x + col, first + u < pieces ? a.C - col : 0, a.vec_x);
+      load8(e[u], static_cast<const T*>(a.x) + row * a.ld_x + col, first + u >= pieces ? 0 : (WHOLE ? 8 : a.C - col), WHOLE || a.vec_x);
       if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
     // largest magnitudes of the pieces' groups (16 lanes each); lane j of the 16 works out the scale of piece j
@@ -115,10 +116,9 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_rows_kernel(const Fp8StoreArg
     #pragma unroll
     for (int u = 0; u < F8S_PIECES; ++u) {
       const float inv_u = __shfl_sync(0xFFFFFFFFu, inv, (lane & 16) + u);
-      const int left = first + u < pieces ? a.C - col : 0;
-      if (left > 0) store8(a.q + row * a.ld + col, left, a.vec_q, e[u], inv_u);
-      const int group = col >> 7;
-      if ((lane & 15) == u && first + u < pieces && group * 128 < a.C) a.scale[row * a.ld_scale + group] = scale;
+      const int left = first + u >= pieces ? 0 : (WHOLE ? 8 : a.C - col), group = col >> 7;
+      if (left > 0) store8(a.q + row * a.ld + col, left, WHOLE || a.vec_q, e[u], inv_u);
+      if ((lane & 15) == u && first + u < pieces && (WHOLE || group * 128 < a.C)) a.scale[row * a.ld_scale + group] = scale;
       if ((col += 256) >= (int)per_row * 256) { col -= (int)per_row * 256; ++row; }
     }
   }
@@ -157,6 +157,17 @@ __global__ void __launch_bounds__(F8S_THREADS) fp8_blocks_kernel(const Fp8StoreA
   }
 }
 
+template <class T, bool WHOLE>
+static int launch_fp8_rows(const Fp8StoreArgs& a, int sms, cudaStream_t st) {
+  static int resident[MAX_DEVICES] = {0};
+  const int dev = current_device();
+  if (dev < 0) return SAPO_ERR_CUDA;
+  if (resident[dev] == 0) resident[dev] = resident_blocks_per_sm(fp8_rows_kernel<T, WHOLE>, F8S_THREADS);
+  const int64_t turns = ceil_div<int64_t>(a.R * ceil_div<int64_t>(a.C, 256), F8S_PIECES);
+  const int64_t most = (int64_t)sms * resident[dev], need = ceil_div<int64_t>(turns, F8S_THREADS / 32);
+  return launch_overlapped(fp8_rows_kernel<T, WHOLE>, dim3((unsigned)(need < most ? need : most)), F8S_THREADS, 0, 0, st, a);
+}
+
 template <class T>
 static int launch_fp8_store(const Fp8StoreArgs& a, bool blocks, cudaStream_t st) {
   const int sms = sm_count();
@@ -167,12 +178,7 @@ static int launch_fp8_store(const Fp8StoreArgs& a, bool blocks, cudaStream_t st)
     if (n > 0x7FFFFFFF) return SAPO_ERR_UNSUPPORTED_SHAPE;
     return launch_overlapped(fp8_blocks_kernel<T>, dim3((unsigned)n), F8S_THREADS, 0, 0, st, a);
   }
-  static int resident[MAX_DEVICES] = {0};
-  const int dev = current_device();
-  if (resident[dev] == 0) resident[dev] = resident_blocks_per_sm(fp8_rows_kernel<T>, F8S_THREADS);
-  const int64_t turns = ceil_div<int64_t>(a.R * ceil_div<int64_t>(a.C, 256), F8S_PIECES);
-  const int64_t most = (int64_t)sms * resident[dev], need = ceil_div<int64_t>(turns, F8S_THREADS / 32);
-  return launch_overlapped(fp8_rows_kernel<T>, dim3((unsigned)(need < most ? need : most)), F8S_THREADS, 0, 0, st, a);
+  return a.vec_x && a.vec_q && a.C % 256 == 0 ? launch_fp8_rows<T, true>(a, sms, st) : launch_fp8_rows<T, false>(a, sms, st);
 }
 
 }  // namespace sapo
