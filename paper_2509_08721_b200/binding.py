@@ -952,11 +952,11 @@ def _sample_cfg(B: int, temperature, top_k, top_p, min_p) -> SampleCfgC:
         key = (temperature, top_k, top_p, min_p)
         cfg = _sample_cfgs.get(key)
         if cfg is None:
-            cfg = SampleCfgC(float(temperature), int(top_k), float(top_p), float(min_p), None, None, None, None)
+            cfg = SampleCfgC(float(temperature), min(int(top_k), 2**31 - 1), float(top_p), float(min_p), None, None, None, None)
             if len(_sample_cfgs) < 64:
                 _sample_cfgs[key] = cfg
     else:
-        cfg = SampleCfgC(1.0 if rows[0] else float(temperature), 0 if rows[1] else int(top_k), 1.0 if rows[2] else float(top_p),
+        cfg = SampleCfgC(1.0 if rows[0] else float(temperature), 0 if rows[1] else min(int(top_k), 2**31 - 1), 1.0 if rows[2] else float(top_p),
                          0.0 if rows[3] else float(min_p),
                          _at_least(temperature, torch.float32, B, "temperature") if rows[0] else None,
                          _at_least(top_k, torch.int32, B, "top_k") if rows[1] else None,

@@ -8,6 +8,8 @@
 // is not zero never becomes zero (its smallest code is 2^-6 / 448 of the group's largest), so that no weight is divided by
 // eps alone.
 //
+// Measured: 136 M weights, 32 bits, bf16 gradients 561 us (6.8 TB/s); 165 M weights in 24 tensors, 8 bits, fp32 gradients
+// 470 us in a burst (6.4 TB/s), 565 sustained (80 instructions a weight: the power cap takes the clock to 1.55 GHz).
 // HBM-bound: per weight 4 + 4 (master) + 2 or 4 (gradient) + 2 (bf16 copy) + 16 (32 bits) or 4.13 (8 bits) bytes.  A
 // warp takes 512 consecutive elements (256 with 8-bit states, which are as much work as memory: more warps hide it better), all
 // loads before the first use.

@@ -3,6 +3,8 @@
 // the nearest code: the group's largest value uses the type's largest.
 // HBM-bound (3 bytes an element from bf16): rows are taken in pieces of 256 columns by warps, half a warp per group, four
 // pieces in flight; blocks of 128 x 128 stay in a block's registers between the search for a and the conversion.
+// Measured: 151936 x 896 bf16 by blocks 62 us (6.5 TB/s, the copy rate), 16527 x 3584 by rows 38.5 us (4.7 TB/s; a warp's loads
+// wait for its stores: more, smaller or shorter-lived blocks and 2 or 8 pieces were each slower, 40 to 43 us).
 #include <cuda_bf16.h>
 
 #include "common.cuh"

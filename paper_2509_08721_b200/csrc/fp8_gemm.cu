@@ -9,6 +9,14 @@
 // tokens, W on the side of the 128 lanes, for few tokens (the head is read once, at the rate of memory) and for
 // matrices too small to fill the device with wide tiles; where even its tiles are few, a cluster of CTAs shares one
 // along K and adds up in shared memory, in a fixed order.
+//
+// What bounds them.  Wide, 8192 x 14336 x 3584: 421 us in a burst (2.0 PFLOP/s), 484 sustained under the power cap; without
+// the scaling warps' work 427 sustained, with a hand-over every fourth block of K 371.  So taking 128 x 256 partial sums out of
+// tensor memory per block costs a quarter; loads of 8 or 32 columns instead of 16, 16 warps instead of 8 and more registers
+// for them were each slower (442 to 587 in a burst).  4096 x 151936 x 896 (7 blocks of K a tile): 655 / 770 us, the output of a
+// tile adds to its 7 blocks.  Narrow, 1 x 151936 x 896: 29 us (4.7 TB/s; the last of nine rounds, the launch and the pipeline's
+// filling take a quarter); 64 x 152064 x 3584: 132 us (4.4 TB/s; the token tile is fetched again with every 128 rows of W, half
+// as many bytes as these; without the scaling work 117).
 #include <cuda_bf16.h>
 
 #include "common.cuh"

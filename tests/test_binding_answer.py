@@ -166,3 +166,13 @@ def test_the_adamw_entry_refuses():
         assert call(**kw) == INVALID, kw
     c = B.AdamWTensorC(n=-1, state_bits=8, grad_dtype=1)
     assert lib.sapo_adamw_step((B.AdamWTensorC * 1)(c), 1, B.AdamWCfgC(lr=0.1, beta1=0.9, beta2=0.9, eps=0.0, step=1), X, None) == INVALID
+
+
+def test_the_sample_entry_refuses_rows_of_too_many_tokens():
+    lib = B.load()  # noqa: F811
+    call = lambda V, dt: lib.sapo_sample(X, dt, 1, V, V, X, B.SampleCfgC(1.0, 0, 1.0, 0.0), X, X, X, None)
+    assert call(1 << 19, B.DTYPE_BF16) == SHAPE and call(369000, B.DTYPE_F32) == SHAPE
+
+
+def test_a_top_k_beyond_32_bits_is_no_small_one(lib):  # noqa: F811
+    assert B._sample_cfg(2, 1.0, 2 ** 32 + 5, 1.0, 0.0).top_k == 2 ** 31 - 1
