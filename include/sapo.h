@@ -555,7 +555,7 @@ int sapo_adam_step(float* master, float* m, float* v, const float* grad, void* w
  *   m <- beta1 m + (1-beta1) g;  v <- beta2 v + (1-beta2) g g;
  *   master <- master (1 - lr_i weight_decay) - lr_i (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
  * and copy_bf16 (may be NULL) = master rounded to bf16.  An element whose g is not finite is left as it
- * was (SAPO_ST_NONFINITE_INPUT); v stops at the largest fp32.
+ * was (SAPO_ST_NONFINITE_INPUT; 8-bit moments are rounded anew with their group); v stops at the largest fp32.
  * A tensor has n elements in one run of memory, of any n (0 too) and any alignment of its element type;
  * arrays on 16-byte boundaries are faster.  The _out arrays receive the new values: the same pointers as
  * the old ones for a step in place, or other arrays (the weights of the policy before the step stay).

@@ -17,7 +17,7 @@
 // histogram of 64 bins an octave of weight (counts and masses as integers: the same whatever the order of additions) to the bin
 // in which the row is cut, and a sort of that bin's tokens.
 //
-// What bounds it: 512 x 151936 bf16 118 us (24 at the copy rate): instructions, 200 for eight tokens, of which the
+// What bounds it: 512 x 151936 bf16 109 us (24 at the copy rate): instructions, 200 for eight tokens, of which the
 // generator's 20 wide products occupy the multiplier 80 of 130 issue slots.  One row, top-k and top-p, 14 us: a chain of 6
 // cluster barriers and the code's first fetch.  96 x 152064 fp32 with settings of their own 85 us: the same chain, of
 // 9 barriers where only top-p is set, two blocks an SM.
@@ -837,8 +837,9 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
 // Every block of a row runs the race of its own tokens against its own largest logit and weight, and ends with its first
 // to finish; the first block of the cluster compares the blocks' times.  Until then they do not wait for one another
 // (but for the row's largest logit, with min_p), and the others are gone before it does.
+// (five blocks of 256 an SM, 512 x 151936 bf16: 109 us; four 118; of 128 or 160 threads 107, but a single row 11.6 us instead of 10.5)
 constexpr int RACE_THREADS = 256, RACE_WARPS = RACE_THREADS / 32;
-constexpr float RACE_LEAD = 6.f;
+constexpr float RACE_LEAD = 6.f;      // (16: three times as many candidates, 125 us instead of 118; 4: 120)
 
 struct RaceShared {
   uint32_t slots[SMP_MAX_CLUSTER][4];       // of a block: its largest logit, its sum of weights, its first time, its token
@@ -862,7 +863,7 @@ __device__ __forceinline__ void store_weights(__nv_bfloat16* p, const float2 (&w
 }
 
 template <class T>
-__global__ void __launch_bounds__(RACE_THREADS, 4) race_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(RACE_THREADS, 5) race_kernel(const SampleArgs a) {
   constexpr uint32_t ALL = 0xFFFFFFFFu;
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t C = cluster.num_blocks(), rank = cluster.block_rank();
