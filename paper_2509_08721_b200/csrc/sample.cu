@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
   T* piece = reinterpret_cast<T*>(smem_raw + SMP_SHARED);
   int turn = 0;
 
-  auto barrier = [&]() { if (C > 1) cluster.sync(); else __syncthreads(); };
+  auto barrier = [&]() { if (C > 1) { __syncwarp(); umma::cluster_sync_all(); } else __syncthreads(); };
   // Tell every block of the cluster W words (of the first threads, the same in each) and wait; returns those of all blocks.
   auto exchange = [&](const uint32_t* v, int W) -> const uint32_t (*)[4] {
     const int t = turn;
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(SMP_THREADS, 2) sample_kernel(const SampleArgs
     for (int i = tid; i < 3 * SMP_BINS / 4; i += THREADS) h[i] = make_uint4(0, 0, 0, 0);
   }
   if (tid == 0) { sh.n_list = 0; sh.n_sort = 0; }
-  if (C > 1) cluster.sync();                    // every block's shared memory is there before the first store to it
+  barrier();                                    // every block's shared memory is there before the first store to it
   asm volatile("cp.async.wait_all;" ::: "memory");
 
   // Values of the block's threads in order, largest first: bitonic; partners in other warps meet in shared memory.  Only
@@ -917,10 +917,12 @@ __global__ void __launch_bounds__(RACE_THREADS, 5) race_kernel(const SampleArgs 
   bool waited = false;
   float floor_octaves = CUDART_INF_F;
   if (min_p > 0.f && !greedy) {                    // min_p goes by the row's largest
+    __syncwarp();
     wait();
     waited = true;
     if (tid < (int)C) *cluster.map_shared_rank(&sh.max_of[rank], tid) = zmax;
-    cluster.sync();
+    __syncwarp();
+    umma::cluster_sync_all();
     for (uint32_t r = 0; r < C; ++r) zmax = max_nan(zmax, sh.max_of[r]);
     floor_octaves = fmaxf(-log2f(min_p), 0.f);
   }
@@ -1089,11 +1091,13 @@ __global__ void __launch_bounds__(RACE_THREADS, 5) race_kernel(const SampleArgs 
   }
 
   // ---- the first block compares the blocks
+  __syncwarp();
   if (!waited) wait();
   if (tid == 0) {
     uint32_t* to = cluster.map_shared_rank(&sh.slots[rank][0], 0);
     for (int i = 0; i < 4; ++i) to[i] = out[i];
   }
+  __syncwarp();
   arrive();
   if (rank != 0) return;
   wait();
